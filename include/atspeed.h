@@ -307,6 +307,125 @@ atspeed_status atspeed_op_attention(atspeed_stream stream, const void *d_q, cons
                                     const int32_t *h_vis, const int32_t *h_path_rows, const int32_t *h_n_path,
                                     void *d_out, void *d_part);
 
+/* ----------------------------------------------------------------------------------------------
+ * Stateless operators of a serving step over a batch of requests (drafted trees, single tokens or
+ * pieces of prompts) with a paged K/V cache: plan -> rope_append -> tree_attention (the last two
+ * once per layer) -> adjust_logits.  All lengths, tables and masks live on the device, so that no
+ * call copies to or waits for the host and a step can be captured into a CUDA graph.  (Sec. 3.3 and
+ * App. A.3.1's tree attention for a batch; the paper has no counterpart of the rest.)
+ *
+ * Requests b < n_req own the tokens cu_q[b] .. cu_q[b+1]-1 of the step's T tokens, in order.
+ * Cache position p of request b is row p % page_size of page block_table[b][p / page_size].
+ * ---------------------------------------------------------------------------------------------- */
+
+typedef enum { ATSPEED_F32 = 0, ATSPEED_BF16 = 1, ATSPEED_F16 = 2 } atspeed_dtype;
+
+/* One layer's paged cache.  Element (page, token, kv head, c) of K is at
+ * page * k_stride[0] + token * k_stride[1] + head * k_stride[2] + c elements (V likewise; 64-bit offsets).
+ * Types (k, v): (BF16, BF16), (F16, F16), or (BF16, F16), the layout of this library's own caches. */
+typedef struct {
+  void *d_k, *d_v;
+  atspeed_dtype k_type, v_type;
+  int n_pages, page_size, n_kv_heads, head_dim;
+  int64_t k_stride[3], v_stride[3];
+} atspeed_kv_pages;
+
+/* What became of a request of a batch plan. */
+typedef enum {
+  ATSPEED_PLAN_OK = 0,
+  ATSPEED_PLAN_NO_PAGES = 1, /* the free pages did not reach to it */
+  ATSPEED_PLAN_LIMIT = 2     /* negative length, more pages than its table row, tokens past max_tokens or past
+                              * the mask's 32 * mask_words bits */
+} atspeed_plan_state;
+
+/* Block tables and slot maps of a step from the requests' lengths.
+ *   d_q_len, d_kv_len [n_req]: new and cached tokens;  d_parent [max_tokens] or NULL: each new token's parent among its
+ *     request's (an index below its request's q_len; anything else: none), NULL for chains;
+ *   d_block_table [n_req][table_width]: the ceil(kv_len / page_size) pages of the cached tokens are read, the entries of the
+ *     pages that the new tokens need beyond those are written;
+ *   d_free [*d_n_free]: free pages, taken from the front, request after request.  A request is served, with all the pages
+ *     it needs, if its need and those of the requests before it fit the free pages together, or if it needs none.
+ * Outputs: d_cu_q [n_req+1] offsets of the requests' tokens;  d_ctx_len [n_req] kv_len, or -1 for a request that was not
+ * served (the attention skips it);  d_state [n_req] an atspeed_plan_state;  d_pages [2]: pages taken from the front of
+ * d_free, and pages that the requests up to the last served one ask for (with those of the requests passed over, so it
+ * may exceed the free pages);  for each of max_tokens rows d_req its request, d_pos its position (kv_len + its depth in the tree), d_slot
+ * (64 bits) page * page_size + row of its cache row, -1 if not served;  d_mask [max_tokens][mask_words] (with d_parent;
+ * else NULL): bit a of a row's words, lowest first, is set if token a of its request is the token itself or an
+ * ancestor of it.  Rows past the last token: request and slot -1, position and mask 0.
+ * Outputs overlap no input, except that the table is both.  Idempotent: the free list is not changed (advance it by d_pages[0]).
+ * n_req <= 16384, mask_words <= 128 (ATSPEED_E_SHAPE). */
+atspeed_status atspeed_op_batch_plan(atspeed_stream stream, int n_req, const int32_t *d_q_len, const int32_t *d_kv_len,
+                                     const int32_t *d_parent, int page_size, int32_t *d_block_table, int table_width,
+                                     const int32_t *d_free, const int32_t *d_n_free, int max_tokens, int mask_words,
+                                     int32_t *d_cu_q, int32_t *d_ctx_len, int32_t *d_state, int32_t *d_pages, int32_t *d_req,
+                                     int32_t *d_pos, int64_t *d_slot, uint32_t *d_mask);
+
+/* Rotary embedding of T new tokens and their entry into the cache, from the rows of a fused QKV projection:
+ * d_qkv [T][qkv_stride] of src_type (F32, the GEMM operator's output, or the cache's k_type), each row n_heads q heads,
+ * then n_kv_heads k heads, then as many v heads.  q and k heads are rotated (dimension i against i + head_dim / 2, by
+ * d_pos[t] * theta^(-2 i / head_dim); d_pos NULL: not at all), every value is rounded once to the type it is stored in;
+ * q goes to d_q [T][q_stride] (k_type; NULL when n_heads = 0), k and v to cache row d_slot[t] = page * page_size + row
+ * (rows with a slot outside the cache are not stored, their q is).  Two rows with one slot: either is stored.
+ * Rows, strides and pointers 16-byte aligned (ATSPEED_E_ARG); head_dim a multiple of 16 up to 256 (ATSPEED_E_SHAPE). */
+atspeed_status atspeed_op_rope_append(atspeed_stream stream, const void *d_qkv, atspeed_dtype src_type, int64_t qkv_stride,
+                                      int T, int n_heads, const atspeed_kv_pages *cache, const int64_t *d_slot,
+                                      const int32_t *d_pos, float theta, void *d_q, int64_t q_stride);
+
+/* Attention of a step's tokens over their requests' caches: token i of request b attends to the cache positions
+ * p < ctx_len[b] and to the positions ctx_len[b] + a of those new tokens a of its request whose bit is set in its row of
+ * d_mask [T][mask_words] (d_mask NULL: a <= i, causal), scores scale * q.k, softmax in 32 bits (weights rounded to the
+ * type of V for the product with V).  Query head h reads key head h / (n_heads / n_kv_heads).  Keys and values that a
+ * token does not attend to never reach its result, whatever they hold (a cache row that was never written, an infinity, a
+ * NaN); a token that attends to nothing gets zeros (and a log-sum-exp of -infinity).  Requests with ctx_len < 0 get zeros.
+ *   d_q [T] rows of n_heads * head_dim, q_stride elements apart, of the cache's k_type; d_out the same with out_stride;
+ *   d_lse NULL or [T][n_heads]: natural log of the sum of exp(score);
+ *   d_cu_q [n_req+1], d_ctx_len [n_req], d_block_table [n_req][table_width] (entries past the last page of a request are not
+ *   read; positions past the table are not attended to).
+ * head_dim 32, 64 or 128; page_size 16, 32, 64, 128 or 256; n_heads a multiple of n_kv_heads, at most 128 times it;
+ * n_req <= 16384 (ATSPEED_E_SHAPE); scale > 0; rows and strides 16-byte aligned (ATSPEED_E_ARG).
+ * d_ws: atspeed_op_tree_attention_workspace() bytes, 256-byte aligned, zero-filled before its first use, of one stream at a
+ * time (every call leaves its counters zeroed).  Long key ranges are divided by the lengths of the whole call, in an
+ * order that the lengths alone fix: the same call gives the same bits, a request's last bits may differ in another batch.
+ * Device-side timeouts surface through atspeed_op_status(stream, NULL); after one, zero the workspace again. */
+size_t atspeed_op_tree_attention_workspace(void);
+atspeed_status atspeed_op_tree_attention(atspeed_stream stream, const atspeed_kv_pages *cache, const void *d_q,
+                                         int64_t q_stride, int n_heads, int n_req, int T, const int32_t *d_cu_q,
+                                         const int32_t *d_ctx_len, const int32_t *d_block_table, int table_width,
+                                         const uint32_t *d_mask, int mask_words, float scale, void *d_out, int64_t out_stride,
+                                         float *d_lse, void *d_ws);
+
+/* Rules on the next-token logits of a step's rows; NULL leaves a rule out.  Per request b:
+ *   its history d_hist[hist_off[b] .. hist_off[b+1]), of which the first prompt_len[b] tokens (NULL: none) are the prompt and
+ *   the rest its output so far; with d_mask (of adjust_logits) the tokens d_tree_tok[cu_q[b] + a] of the bits a of a row's
+ *   mask are output too, for that row;
+ *   seen in prompt or output: x > 0 ? x / repetition : x * repetition;  then x -= frequency * count + presence for a token
+ *   that occurs count > 0 times in the output;
+ *   x += bias_val[k] for the entries k in [bias_off[b], bias_off[b+1]) of token bias_tok[k] (a token listed twice: the
+ *   later entry alone);
+ *   row r of grammar state s = d_state[r] (a negative one: no grammar): tokens whose bit is not set in
+ *   d_grammar[s * grammar_stride ..], lowest bit first, become -infinity, whatever their logit;
+ *   x /= temperature (a temperature that is not above 0: not divided).
+ * Tokens outside [0, vocab) are ignored.  Arithmetic in 32 bits, one rounding to the output's type. */
+typedef struct {
+  int n_req;
+  const int32_t *d_hist, *d_hist_off, *d_prompt_len;
+  const float *d_repetition, *d_frequency, *d_presence, *d_temperature;
+  const int32_t *d_bias_off, *d_bias_tok;
+  const float *d_bias_val;
+  const uint32_t *d_grammar;
+  int64_t grammar_stride; /* words */
+  int n_states;
+  const int32_t *d_tree_tok, *d_cu_q;
+} atspeed_logit_rules;
+
+/* out[r] = rules(logits[r]) for rows r < R of `vocab` logits (F32, BF16 or F16; ld_in, ld_out elements between rows); out
+ * of the same type or F32.  In place if d_out = d_logits with the same type and stride; no other overlap.  d_req [R]: each
+ * row's request (outside [0, n_req): no rule but the grammar). */
+atspeed_status atspeed_op_adjust_logits(atspeed_stream stream, const void *d_logits, atspeed_dtype in_type, int64_t ld_in,
+                                        int R, int vocab, const int32_t *d_req, const atspeed_logit_rules *rules,
+                                        const uint32_t *d_mask, int mask_words, const int32_t *d_state, void *d_out,
+                                        atspeed_dtype out_type, int64_t ld_out);
+
 #ifdef __cplusplus
 }
 #endif

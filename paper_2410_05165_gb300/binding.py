@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Dict, List, Optional, Sequence, Tuple
+from typing import Dict, List, NamedTuple, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -20,6 +20,8 @@ OK, E_ARG, E_SHAPE, E_OOM, E_CUDA, E_TIMEOUT, E_STATE, E_UNSUPPORTED = 0, -1, -2
 STRICT, RELAXED = 0, 1
 NORM_MASKED, NORM_FULL = 0, 1
 PLAIN_TOPK, PLAIN_SAMPLE, SD_STRICT, SD_RELAXED = 0, 1, 2, 3
+PLAN_OK, PLAN_NO_PAGES, PLAN_LIMIT = 0, 1, 2
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 EXPORTS = [
     "atspeed_create", "atspeed_destroy", "atspeed_last_error", "atspeed_prefill", "atspeed_begin_step",
@@ -27,6 +29,8 @@ EXPORTS = [
     "atspeed_beam_search", "atspeed_set_early_reject", "atspeed_profile", "atspeed_profile_read", "atspeed_tree_shape", "atspeed_debug_tree",
     "atspeed_debug_node_logits", "atspeed_debug_node_lse", "atspeed_debug_buffer", "atspeed_set_tree", "atspeed_op_workspace_bytes", "atspeed_op_gemm",
     "atspeed_op_gemm_noalloc", "atspeed_op_status", "atspeed_op_gemm_swiglu", "atspeed_op_rmsnorm", "atspeed_op_attention_scratch", "atspeed_op_attention",
+    "atspeed_op_batch_plan", "atspeed_op_rope_append", "atspeed_op_tree_attention_workspace", "atspeed_op_tree_attention",
+    "atspeed_op_adjust_logits",
 ]
 
 
@@ -59,6 +63,19 @@ class Limits(ctypes.Structure):
 class DecodeOpts(ctypes.Structure):
     _fields_ = [("K", ctypes.c_int), ("N", ctypes.c_int), ("gamma", ctypes.c_int), ("norm", ctypes.c_int),
                 ("philox_seed", ctypes.c_uint64)]
+
+
+class KvPages(ctypes.Structure):
+    _fields_ = [("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("k_type", ctypes.c_int), ("v_type", ctypes.c_int),
+                ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3)]
+
+
+class LogitRulesDesc(ctypes.Structure):
+    _fields_ = [("n_req", ctypes.c_int)] + [(f, ctypes.c_void_p) for f in (
+        "d_hist", "d_hist_off", "d_prompt_len", "d_repetition", "d_frequency", "d_presence", "d_temperature", "d_bias_off",
+        "d_bias_tok", "d_bias_val", "d_grammar")] + [("grammar_stride", ctypes.c_int64), ("n_states", ctypes.c_int),
+                                                     ("d_tree_tok", ctypes.c_void_p), ("d_cu_q", ctypes.c_void_p)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -105,6 +122,15 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "atspeed_op_attention_scratch": (ctypes.c_size_t, [c_int, c_int, c_int, c_int]),
         "atspeed_op_attention": (c_int, [vp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int, i32p, i32p, i32p, i32p,
                                          vp, vp]),
+        "atspeed_op_batch_plan": (c_int, [vp, c_int, vp, vp, vp, c_int, vp, c_int, vp, vp, c_int, c_int, vp, vp, vp, vp,
+                                          vp, vp, vp, vp]),
+        "atspeed_op_rope_append": (c_int, [vp, vp, c_int, ctypes.c_int64, c_int, c_int, ctypes.POINTER(KvPages), vp, vp,
+                                           ctypes.c_float, vp, ctypes.c_int64]),
+        "atspeed_op_tree_attention_workspace": (ctypes.c_size_t, []),
+        "atspeed_op_tree_attention": (c_int, [vp, ctypes.POINTER(KvPages), vp, ctypes.c_int64, c_int, c_int, c_int, vp, vp,
+                                              vp, c_int, vp, c_int, ctypes.c_float, vp, ctypes.c_int64, vp, vp]),
+        "atspeed_op_adjust_logits": (c_int, [vp, vp, c_int, ctypes.c_int64, c_int, c_int, vp,
+                                             ctypes.POINTER(LogitRulesDesc), vp, c_int, vp, vp, c_int, ctypes.c_int64]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -397,4 +423,191 @@ def op_attention(q: torch.Tensor, kc: torch.Tensor, vc: torch.Tensor, n_heads: i
         npth, npp = _i32(n_path)
     _check(lib.atspeed_op_attention(_stream(stream), q.data_ptr(), kc.data_ptr(), vc.data_ptr(), kc.shape[0], T,
                                     n_heads, head_dim, P, pgp, vvp, prp, npp, out.data_ptr(), scratch.data_ptr()))
+    return out
+
+
+# ---------------------------------------------------------------------------------------------------
+# a serving step over a batch of requests: plan, cache append, tree attention, logit rules
+# ---------------------------------------------------------------------------------------------------
+def _need(ok: bool, what: str):
+    """Arguments that the C ABI cannot see (types, shapes, devices) are refused as it refuses its own."""
+    if not ok:
+        raise AtSpeedError(E_ARG, what)
+
+
+def _tensor(t: Optional[torch.Tensor], dtype, n: Optional[int], what: str, optional=False):
+    """A contiguous device tensor of the given type with at least n elements (n = None: any number)."""
+    if t is None:
+        _need(optional, f"{what}: missing")
+        return
+    _need(t.is_cuda and t.dtype == dtype and t.is_contiguous() and (n is None or t.numel() >= n),
+          f"{what}: {dtype} on the device, contiguous, {n} elements or more, not {tuple(t.shape)} {t.dtype}")
+
+
+def _new(shape, dtype, device, stream) -> torch.Tensor:
+    """An output of a call on `stream`: its memory is not given to others before the stream is done with it."""
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _kv_pages(kc: torch.Tensor, vc: torch.Tensor) -> KvPages:
+    """Caches [pages][page_size][kv heads][head_dim], any strides but the last (a head-by-head cache: transpose(1, 2))."""
+    _need(kc.is_cuda and vc.is_cuda and kc.dim() == 4 and kc.shape == vc.shape and kc.stride(3) == 1 and vc.stride(3) == 1,
+          f"caches: two of one shape [pages][page_size][heads][head_dim], not {tuple(kc.shape)} and {tuple(vc.shape)}")
+    _need(kc.dtype in _DTYPES and vc.dtype in _DTYPES, f"caches of {kc.dtype} and {vc.dtype}")
+    n, page, heads, hd = kc.shape
+    return KvPages(kc.data_ptr(), vc.data_ptr(), _DTYPES[kc.dtype], _DTYPES[vc.dtype], n, page, heads, hd,
+                   (ctypes.c_int64 * 3)(*kc.stride()[:3]), (ctypes.c_int64 * 3)(*vc.stride()[:3]))
+
+
+class BatchPlan(NamedTuple):
+    """Outputs of op_batch_plan (see atspeed_op_batch_plan)."""
+    cu_q: torch.Tensor      # [n + 1] int32
+    ctx_len: torch.Tensor   # [n] int32, -1: not served
+    state: torch.Tensor     # [n] int32, PLAN_*
+    used: torch.Tensor      # [] int32, pages taken from the front of the free list
+    taken: torch.Tensor     # [] int32, pages that the requests up to the last served one ask for, passed-over ones included
+    req: torch.Tensor       # [T] int32
+    pos: torch.Tensor       # [T] int32
+    slot: torch.Tensor      # [T] int64, -1: not served
+    mask: Optional[torch.Tensor]   # [T][words] int32 bit patterns (trees)
+
+
+def op_batch_plan(q_len: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, free: torch.Tensor,
+                  n_free: torch.Tensor, page_size: int, max_tokens: int, parent: Optional[torch.Tensor] = None,
+                  mask_words: int = 0, stream=None) -> BatchPlan:
+    """Pages, slots, positions and tree masks of a step from the requests' lengths; block_table is extended in place."""
+    n, dev = q_len.numel(), q_len.device
+    _tensor(q_len, torch.int32, 1, "q_len")
+    _tensor(kv_len, torch.int32, n, "kv_len")
+    _tensor(block_table, torch.int32, n, "block_table")
+    _need(block_table.dim() == 2 and block_table.shape[0] == n, f"block_table: [{n}][width], not {tuple(block_table.shape)}")
+    _tensor(free, torch.int32, 1, "free")
+    _tensor(n_free, torch.int32, 1, "n_free")
+    _tensor(parent, torch.int32, max_tokens, "parent", optional=True)
+    i32 = lambda *shape: _new(shape, torch.int32, dev, stream)
+    T = max(0, max_tokens)
+    words = max(0, mask_words)
+    pages = i32(2)
+    p = BatchPlan(i32(n + 1), i32(n), i32(n), pages[0], pages[1], i32(T), i32(T), _new((T,), torch.int64, dev, stream),
+                  i32(T, words) if parent is not None else None)
+    _check(load().atspeed_op_batch_plan(_stream(stream), n, q_len.data_ptr(), kv_len.data_ptr(), _ptr(parent), page_size,
+                                        block_table.data_ptr(), block_table.shape[1], free.data_ptr(), n_free.data_ptr(),
+                                        max_tokens, mask_words, p.cu_q.data_ptr(), p.ctx_len.data_ptr(), p.state.data_ptr(),
+                                        pages.data_ptr(), p.req.data_ptr(), p.pos.data_ptr(), p.slot.data_ptr(),
+                                        _ptr(p.mask)))
+    return p
+
+
+def op_rope_append(qkv: torch.Tensor, n_heads: int, kc: torch.Tensor, vc: torch.Tensor, slot: torch.Tensor,
+                   pos: Optional[torch.Tensor] = None, theta: float = 10000.0, stream=None) -> torch.Tensor:
+    """Rotates q and k of fused QKV rows [T][(heads + 2 kv heads) * head_dim], stores k and v by slot, returns q
+    [T][heads][head_dim]."""
+    pages = _kv_pages(kc, vc)
+    hd, T = pages.head_dim, qkv.shape[0]
+    _need(qkv.is_cuda and qkv.dim() == 2 and qkv.dtype in _DTYPES and (qkv.stride(1) == 1 or qkv.shape[1] == 1) and
+          qkv.shape[1] == (n_heads + 2 * pages.n_kv_heads) * hd, f"qkv: [T][heads * {hd}], not {tuple(qkv.shape)}")
+    _tensor(slot, torch.int64, T, "slot")
+    _tensor(pos, torch.int32, T, "pos", optional=True)
+    q = _new((T, n_heads, hd), kc.dtype, qkv.device, stream)
+    _check(load().atspeed_op_rope_append(_stream(stream), qkv.data_ptr(), _DTYPES[qkv.dtype], qkv.stride(0), T, n_heads,
+                                         ctypes.byref(pages), slot.data_ptr(), _ptr(pos), theta,
+                                         q.data_ptr() if n_heads else None, n_heads * hd))
+    return q
+
+
+_tree_ws: Dict[Tuple[int, int], torch.Tensor] = {}
+
+
+def op_tree_attention_workspace(device, stream: int) -> torch.Tensor:
+    """The attention's workspace of one stream (calls on one stream follow each other; two streams' would not)."""
+    key = (device.index or 0, stream)
+    if key not in _tree_ws:
+        _tree_ws[key] = torch.zeros(load().atspeed_op_tree_attention_workspace(), dtype=torch.uint8, device=device)
+        torch.cuda.current_stream(device).synchronize()   # (the zeros come before a call on whatever stream)
+    return _tree_ws[key]
+
+
+def op_tree_attention(q: torch.Tensor, kc: torch.Tensor, vc: torch.Tensor, cu_q: torch.Tensor, ctx_len: torch.Tensor,
+                      block_table: torch.Tensor, mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                      out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of q [T][heads][head_dim] (rows any stride apart) over the batch's paged caches and, by the mask's bits
+    (None: causal), the step's own tokens.  scale: 1 / sqrt(head_dim) by default."""
+    pages = _kv_pages(kc, vc)
+    n = ctx_len.numel()
+
+    def rows(t, what):
+        _need(t.is_cuda and t.dim() == 3 and t.dtype == kc.dtype and t.shape == q.shape and t.shape[2] == pages.head_dim and
+              t.stride(2) == 1 and t.stride(1) == pages.head_dim,
+              f"{what}: [T][heads][{pages.head_dim}] of {kc.dtype}, each row contiguous, not {tuple(t.shape)} {t.dtype}")
+
+    rows(q, "q")
+    T, H, hd = q.shape
+    if out is None:
+        out = _new((T, H, hd), q.dtype, q.device, stream)
+    rows(out, "out")
+    _tensor(cu_q, torch.int32, n + 1, "cu_q")
+    _tensor(ctx_len, torch.int32, 1, "ctx_len")
+    _tensor(block_table, torch.int32, n, "block_table")
+    _need(block_table.dim() == 2 and block_table.shape[0] >= n, f"block_table: [{n}][width], not {tuple(block_table.shape)}")
+    _tensor(mask, torch.int32, T, "mask", optional=True)
+    _need(mask is None or (mask.dim() == 2 and mask.shape[0] >= T), "mask: [T][words]")
+    _tensor(lse, torch.float32, T * H, "lse", optional=True)
+    st = _stream(stream)
+    _check(load().atspeed_op_tree_attention(st, ctypes.byref(pages), q.data_ptr(), q.stride(0), H, n, T, cu_q.data_ptr(),
+                                            ctx_len.data_ptr(), block_table.data_ptr(), block_table.shape[1], _ptr(mask),
+                                            mask.shape[1] if mask is not None else 0, hd ** -0.5 if scale is None else scale,
+                                            out.data_ptr(), out.stride(0), _ptr(lse),
+                                            op_tree_attention_workspace(q.device, st).data_ptr()))
+    return out
+
+
+class LogitRules:
+    """The per-request rules of op_adjust_logits (see atspeed_logit_rules); None leaves a rule out.  Keeps the tensors alive."""
+
+    def __init__(self, n_req: Optional[int] = None, hist=None, hist_off=None, prompt_len=None, repetition=None, frequency=None,
+                 presence=None, temperature=None, bias_off=None, bias_tok=None, bias_val=None, grammar=None, tree_tok=None,
+                 cu_q=None):
+        per = {"prompt_len": prompt_len, "repetition": repetition, "frequency": frequency, "presence": presence,
+               "temperature": temperature}
+        if n_req is None:
+            n_req = next((t.numel() for t in per.values() if t is not None),
+                         next((t.numel() - 1 for t in (hist_off, bias_off, cu_q) if t is not None), 0))
+        for k, t in per.items():
+            _tensor(t, torch.int32 if k == "prompt_len" else torch.float32, n_req, k, optional=True)
+        for k, t in (("hist_off", hist_off), ("bias_off", bias_off), ("cu_q", cu_q)):
+            _tensor(t, torch.int32, n_req + 1, k, optional=True)
+        for k, t in (("hist", hist), ("bias_tok", bias_tok), ("tree_tok", tree_tok), ("grammar", grammar)):
+            _tensor(t, torch.int32, None, k, optional=True)
+        _tensor(bias_val, torch.float32, bias_tok.numel() if bias_tok is not None else None, "bias_val", optional=True)
+        _need(grammar is None or grammar.dim() == 2, "grammar: [states][words]")
+        self._keep = [hist, hist_off, prompt_len, repetition, frequency, presence, temperature, bias_off, bias_tok, bias_val,
+                      grammar, tree_tok, cu_q]
+        self.n_req = n_req
+        p = [_ptr(t) for t in self._keep]
+        self.desc = LogitRulesDesc(n_req, *p[:11], grammar.shape[1] if grammar is not None else 0,
+                                   grammar.shape[0] if grammar is not None else 0, *p[11:])
+
+
+def op_adjust_logits(logits: torch.Tensor, req: torch.Tensor, rules: LogitRules, mask: Optional[torch.Tensor] = None,
+                     state: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype=None,
+                     stream=None) -> torch.Tensor:
+    """Rules on logits [R][vocab] (rows any stride apart) of requests req [R]; out may be logits itself."""
+    _need(logits.is_cuda and logits.dim() == 2 and logits.dtype in _DTYPES and (logits.stride(1) == 1 or logits.shape[1] == 1),
+          f"logits: [R][vocab], not {tuple(logits.shape)} {logits.dtype}")
+    R, V = logits.shape
+    if out is None:
+        out = _new((R, V), out_dtype or logits.dtype, logits.device, stream)
+    _need(out.is_cuda and out.shape == logits.shape and out.dtype in _DTYPES and (out.stride(1) == 1 or V == 1),
+          f"out: [{R}][{V}], not {tuple(out.shape)} {out.dtype}")
+    _tensor(req, torch.int32, R, "req")
+    _tensor(mask, torch.int32, R, "mask", optional=True)
+    _need(mask is None or (mask.dim() == 2 and mask.shape[0] >= R), "mask: [R][words]")
+    _tensor(state, torch.int32, R, "state", optional=True)
+    _check(load().atspeed_op_adjust_logits(_stream(stream), logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0), R, V,
+                                           req.data_ptr(), ctypes.byref(rules.desc), _ptr(mask),
+                                           mask.shape[1] if mask is not None else 0, _ptr(state), out.data_ptr(),
+                                           _DTYPES[out.dtype], out.stride(0)))
     return out
