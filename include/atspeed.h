@@ -271,10 +271,10 @@ atspeed_status atspeed_op_gemm_noalloc(atspeed_stream stream, const void *d_W, c
                                        int x_rows, float *d_Y, int ldy, int accumulate);
 
 /* Device-side failures of the op GEMMs (atspeed_op_gemm, atspeed_op_gemm_swiglu,
- * atspeed_op_gemm_noalloc) and of atspeed_op_attention.  Their launches return ATSPEED_OK once
+ * atspeed_op_gemm_noalloc), of atspeed_op_attention and of atspeed_op_tree_attention.  Their launches return ATSPEED_OK once
  * enqueued; a bounded wait inside the kernel that gives up (a copy or a peer CTA that never arrives)
  * does not trap but sets an error word in the call's workspace (for the allocation-free entry point
- * and the attention: a word of this library on the device), which stays set (sticky) across later calls
+ * and the attentions: a word of this library on the device), which stays set (sticky) across later calls
  * until this function reads it.  Synchronises `stream`, reads and clears the word of the workspace d_ws
  * (or, with d_ws = NULL, the library's words on the current device) and returns ATSPEED_OK,
  * ATSPEED_E_TIMEOUT (a bounded wait gave up: the outputs of the calls since the last check are not

@@ -15,6 +15,7 @@
 #include "gemm.cuh"
 #include "common.cuh"
 #include "kernels.cuh"
+#include "step_ops.cuh"
 
 using namespace atspeed;
 
@@ -280,13 +281,14 @@ atspeed_status atspeed_op_gemm_noalloc(atspeed_stream stream, const void* d_W, c
 
 /* See include/atspeed.h.  Reads (and clears) the error words that the operators' bounded waits set. */
 atspeed_status atspeed_op_status(atspeed_stream stream, void* d_ws) {
-  unsigned int* words[2] = {nullptr, nullptr};
+  unsigned int* words[3] = {nullptr, nullptr, nullptr};
   if (d_ws) {
     words[0] = scratch_from(d_ws, current_grid()).err;
   } else {
     void* base = noalloc_base();
     words[1] = attn_err_word();
-    if (!base || !words[1]) return ATSPEED_E_CUDA;
+    words[2] = tree_attn_err_word();
+    if (!base || !words[1] || !words[2]) return ATSPEED_E_CUDA;
     words[0] = noalloc_err_word(base);
   }
   cudaStream_t st = (cudaStream_t)stream;

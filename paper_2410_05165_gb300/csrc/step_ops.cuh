@@ -26,6 +26,9 @@ inline atspeed_status check_pages(const atspeed_kv_pages* c) {
   return ATSPEED_OK;
 }
 
+// The tree attention's error word on the current device (ATSPEED_DEV_ERR_* bits); null if it cannot be found.
+unsigned int* tree_attn_err_word();
+
 inline atspeed_status launch_status() { return cudaGetLastError() == cudaSuccess ? ATSPEED_OK : ATSPEED_E_CUDA; }
 
 // Two values rounded to a pair of 16-bit ones.
