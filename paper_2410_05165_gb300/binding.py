@@ -429,19 +429,25 @@ def op_attention(q: torch.Tensor, kc: torch.Tensor, vc: torch.Tensor, n_heads: i
 # ---------------------------------------------------------------------------------------------------
 # a serving step over a batch of requests: plan, cache append, tree attention, logit rules
 # ---------------------------------------------------------------------------------------------------
-def _need(ok: bool, what: str):
+def _refuse(what: str):
     """Arguments that the C ABI cannot see (types, shapes, devices) are refused as it refuses its own."""
-    if not ok:
-        raise AtSpeedError(E_ARG, what)
+    raise AtSpeedError(E_ARG, what)
 
 
-def _tensor(t: Optional[torch.Tensor], dtype, n: Optional[int], what: str, optional=False):
-    """A contiguous device tensor of the given type with at least n elements (n = None: any number)."""
+def _tensor(t: Optional[torch.Tensor], dtype, n: int, what: str) -> Optional[int]:
+    """The address of a contiguous device tensor of the given type with n elements or more; None for None."""
     if t is None:
-        _need(optional, f"{what}: missing")
-        return
-    _need(t.is_cuda and t.dtype == dtype and t.is_contiguous() and (n is None or t.numel() >= n),
-          f"{what}: {dtype} on the device, contiguous, {n} elements or more, not {tuple(t.shape)} {t.dtype}")
+        return None
+    if t.dtype is not dtype or t.numel() < n or not t.is_cuda or not t.is_contiguous():
+        _refuse(f"{what}: {dtype} on the device, contiguous, {n} elements or more, not {tuple(t.shape)} {t.dtype} {t.device}")
+    return t.data_ptr()
+
+
+def _given(t: Optional[torch.Tensor], dtype, n: int, what: str) -> int:
+    """The same for an argument that has to be there."""
+    if t is None:
+        _refuse(f"{what}: missing")
+    return _tensor(t, dtype, n, what)
 
 
 def _new(shape, dtype, device, stream) -> torch.Tensor:
@@ -452,14 +458,19 @@ def _new(shape, dtype, device, stream) -> torch.Tensor:
     return t
 
 
+def _raw_stream(stream: Optional[torch.cuda.Stream], device) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+
+
 def _kv_pages(kc: torch.Tensor, vc: torch.Tensor) -> KvPages:
     """Caches [pages][page_size][kv heads][head_dim], any strides but the last (a head-by-head cache: transpose(1, 2))."""
-    _need(kc.is_cuda and vc.is_cuda and kc.dim() == 4 and kc.shape == vc.shape and kc.stride(3) == 1 and vc.stride(3) == 1,
-          f"caches: two of one shape [pages][page_size][heads][head_dim], not {tuple(kc.shape)} and {tuple(vc.shape)}")
-    _need(kc.dtype in _DTYPES and vc.dtype in _DTYPES, f"caches of {kc.dtype} and {vc.dtype}")
-    n, page, heads, hd = kc.shape
-    return KvPages(kc.data_ptr(), vc.data_ptr(), _DTYPES[kc.dtype], _DTYPES[vc.dtype], n, page, heads, hd,
-                   (ctypes.c_int64 * 3)(*kc.stride()[:3]), (ctypes.c_int64 * 3)(*vc.stride()[:3]))
+    shape, ks, vs = kc.shape, kc.stride(), vc.stride()
+    kt, vt = _DTYPES.get(kc.dtype), _DTYPES.get(vc.dtype)
+    if len(shape) != 4 or shape != vc.shape or ks[3] != 1 or vs[3] != 1 or kt is None or vt is None or not (kc.is_cuda and
+                                                                                                            vc.is_cuda):
+        _refuse(f"caches: two [pages][page_size][heads][head_dim] on the device, not {tuple(shape)} {kc.dtype} and "
+                f"{tuple(vc.shape)} {vc.dtype}")
+    return KvPages(kc.data_ptr(), vc.data_ptr(), kt, vt, shape[0], shape[1], shape[2], shape[3], ks[:3], vs[:3])
 
 
 class BatchPlan(NamedTuple):
@@ -479,26 +490,25 @@ def op_batch_plan(q_len: torch.Tensor, kv_len: torch.Tensor, block_table: torch.
                   n_free: torch.Tensor, page_size: int, max_tokens: int, parent: Optional[torch.Tensor] = None,
                   mask_words: int = 0, stream=None) -> BatchPlan:
     """Pages, slots, positions and tree masks of a step from the requests' lengths; block_table is extended in place."""
-    n, dev = q_len.numel(), q_len.device
-    _tensor(q_len, torch.int32, 1, "q_len")
-    _tensor(kv_len, torch.int32, n, "kv_len")
-    _tensor(block_table, torch.int32, n, "block_table")
-    _need(block_table.dim() == 2 and block_table.shape[0] == n, f"block_table: [{n}][width], not {tuple(block_table.shape)}")
-    _tensor(free, torch.int32, 1, "free")
-    _tensor(n_free, torch.int32, 1, "n_free")
-    _tensor(parent, torch.int32, max_tokens, "parent", optional=True)
-    i32 = lambda *shape: _new(shape, torch.int32, dev, stream)
-    T = max(0, max_tokens)
-    words = max(0, mask_words)
-    pages = i32(2)
-    p = BatchPlan(i32(n + 1), i32(n), i32(n), pages[0], pages[1], i32(T), i32(T), _new((T,), torch.int64, dev, stream),
-                  i32(T, words) if parent is not None else None)
-    _check(load().atspeed_op_batch_plan(_stream(stream), n, q_len.data_ptr(), kv_len.data_ptr(), _ptr(parent), page_size,
-                                        block_table.data_ptr(), block_table.shape[1], free.data_ptr(), n_free.data_ptr(),
-                                        max_tokens, mask_words, p.cu_q.data_ptr(), p.ctx_len.data_ptr(), p.state.data_ptr(),
-                                        pages.data_ptr(), p.req.data_ptr(), p.pos.data_ptr(), p.slot.data_ptr(),
-                                        _ptr(p.mask)))
-    return p
+    n, T = q_len.numel(), max_tokens
+    if block_table.dim() != 2 or block_table.shape[0] != n or T <= 0 or n == 0 or (parent is not None and mask_words <= 0):
+        _refuse(f"{n} requests, {T} tokens, block_table {tuple(block_table.shape)}, {mask_words} mask words")
+    args = (_given(q_len, torch.int32, n, "q_len"), _given(kv_len, torch.int32, n, "kv_len"),
+            _tensor(parent, torch.int32, T, "parent"), page_size, _given(block_table, torch.int32, n, "block_table"),
+            block_table.shape[1], _given(free, torch.int32, 1, "free"), _given(n_free, torch.int32, 1, "n_free"), T, mask_words)
+    # one block of memory: slots (64 bits) first, then the 32-bit outputs
+    words = mask_words if parent is not None else 0
+    sizes = (2 * T, n + 1, n, n, 2, T, T, T * words)
+    whole = _new(sum(sizes), torch.int32, q_len.device, stream)
+    slot, cu_q, ctx_len, state, pages, req, pos, mask = whole.split_with_sizes(sizes)
+    at, out = whole.data_ptr(), []
+    for k in sizes:
+        out.append(at)
+        at += 4 * k
+    _check(load().atspeed_op_batch_plan(_raw_stream(stream, q_len.device), n, *args, *out[1:7], out[0],
+                                        out[7] if words else None))
+    return BatchPlan(cu_q, ctx_len, state, pages[0], pages[1], req, pos, slot.view(torch.int64),
+                     mask.view(T, words) if words else None)
 
 
 def op_rope_append(qkv: torch.Tensor, n_heads: int, kc: torch.Tensor, vc: torch.Tensor, slot: torch.Tensor,
@@ -506,14 +516,13 @@ def op_rope_append(qkv: torch.Tensor, n_heads: int, kc: torch.Tensor, vc: torch.
     """Rotates q and k of fused QKV rows [T][(heads + 2 kv heads) * head_dim], stores k and v by slot, returns q
     [T][heads][head_dim]."""
     pages = _kv_pages(kc, vc)
-    hd, T = pages.head_dim, qkv.shape[0]
-    _need(qkv.is_cuda and qkv.dim() == 2 and qkv.dtype in _DTYPES and (qkv.stride(1) == 1 or qkv.shape[1] == 1) and
-          qkv.shape[1] == (n_heads + 2 * pages.n_kv_heads) * hd, f"qkv: [T][heads * {hd}], not {tuple(qkv.shape)}")
-    _tensor(slot, torch.int64, T, "slot")
-    _tensor(pos, torch.int32, T, "pos", optional=True)
+    hd, src = pages.head_dim, _DTYPES.get(qkv.dtype)
+    if qkv.dim() != 2 or src is None or not qkv.is_cuda or qkv.stride(1) != 1 or qkv.shape[1] != (n_heads + 2 * pages.n_kv_heads) * hd:
+        _refuse(f"qkv: [T][({n_heads} + 2 * {pages.n_kv_heads}) * {hd}] on the device, not {tuple(qkv.shape)} {qkv.dtype}")
+    T = qkv.shape[0]
     q = _new((T, n_heads, hd), kc.dtype, qkv.device, stream)
-    _check(load().atspeed_op_rope_append(_stream(stream), qkv.data_ptr(), _DTYPES[qkv.dtype], qkv.stride(0), T, n_heads,
-                                         ctypes.byref(pages), slot.data_ptr(), _ptr(pos), theta,
+    _check(load().atspeed_op_rope_append(_raw_stream(stream, qkv.device), qkv.data_ptr(), src, qkv.stride(0), T, n_heads, pages,
+                                         _given(slot, torch.int64, T, "slot"), _tensor(pos, torch.int32, T, "pos"), theta,
                                          q.data_ptr() if n_heads else None, n_heads * hd))
     return q
 
@@ -536,30 +545,24 @@ def op_tree_attention(q: torch.Tensor, kc: torch.Tensor, vc: torch.Tensor, cu_q:
     """Attention of q [T][heads][head_dim] (rows any stride apart) over the batch's paged caches and, by the mask's bits
     (None: causal), the step's own tokens.  scale: 1 / sqrt(head_dim) by default."""
     pages = _kv_pages(kc, vc)
-    n = ctx_len.numel()
-
-    def rows(t, what):
-        _need(t.is_cuda and t.dim() == 3 and t.dtype == kc.dtype and t.shape == q.shape and t.shape[2] == pages.head_dim and
-              t.stride(2) == 1 and t.stride(1) == pages.head_dim,
-              f"{what}: [T][heads][{pages.head_dim}] of {kc.dtype}, each row contiguous, not {tuple(t.shape)} {t.dtype}")
-
-    rows(q, "q")
-    T, H, hd = q.shape
+    n, hd = ctx_len.numel(), pages.head_dim
+    if q.dim() != 3 or q.dtype is not kc.dtype or q.shape[2] != hd or q.stride(2) != 1 or q.stride(1) != hd or not q.is_cuda:
+        _refuse(f"q: [T][heads][{hd}] of {kc.dtype} on the device, each row contiguous, not {tuple(q.shape)} {q.dtype}")
+    T, H, _ = q.shape
     if out is None:
-        out = _new((T, H, hd), q.dtype, q.device, stream)
-    rows(out, "out")
-    _tensor(cu_q, torch.int32, n + 1, "cu_q")
-    _tensor(ctx_len, torch.int32, 1, "ctx_len")
-    _tensor(block_table, torch.int32, n, "block_table")
-    _need(block_table.dim() == 2 and block_table.shape[0] >= n, f"block_table: [{n}][width], not {tuple(block_table.shape)}")
-    _tensor(mask, torch.int32, T, "mask", optional=True)
-    _need(mask is None or (mask.dim() == 2 and mask.shape[0] >= T), "mask: [T][words]")
-    _tensor(lse, torch.float32, T * H, "lse", optional=True)
-    st = _stream(stream)
-    _check(load().atspeed_op_tree_attention(st, ctypes.byref(pages), q.data_ptr(), q.stride(0), H, n, T, cu_q.data_ptr(),
-                                            ctx_len.data_ptr(), block_table.data_ptr(), block_table.shape[1], _ptr(mask),
-                                            mask.shape[1] if mask is not None else 0, hd ** -0.5 if scale is None else scale,
-                                            out.data_ptr(), out.stride(0), _ptr(lse),
+        out = _new(q.shape, q.dtype, q.device, stream)
+    elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1 or out.stride(1) != hd or not out.is_cuda:
+        _refuse(f"out: as q {tuple(q.shape)} {q.dtype}, each row contiguous, not {tuple(out.shape)} {out.dtype}")
+    if block_table.dim() != 2 or block_table.shape[0] < n or (mask is not None and (mask.dim() != 2 or mask.shape[0] < T)):
+        _refuse(f"block_table: [{n}][width] and mask: [{T}][words], not {tuple(block_table.shape)} and "
+                f"{None if mask is None else tuple(mask.shape)}")
+    st = _raw_stream(stream, q.device)
+    _check(load().atspeed_op_tree_attention(st, pages, q.data_ptr(), q.stride(0), H, n, T,
+                                            _given(cu_q, torch.int32, n + 1, "cu_q"), _given(ctx_len, torch.int32, 1, "ctx_len"),
+                                            _given(block_table, torch.int32, n, "block_table"), block_table.shape[1],
+                                            _tensor(mask, torch.int32, T, "mask"), mask.shape[1] if mask is not None else 0,
+                                            hd ** -0.5 if scale is None else scale, out.data_ptr(), out.stride(0),
+                                            _tensor(lse, torch.float32, T * H, "lse"),
                                             op_tree_attention_workspace(q.device, st).data_ptr()))
     return out
 
@@ -570,44 +573,43 @@ class LogitRules:
     def __init__(self, n_req: Optional[int] = None, hist=None, hist_off=None, prompt_len=None, repetition=None, frequency=None,
                  presence=None, temperature=None, bias_off=None, bias_tok=None, bias_val=None, grammar=None, tree_tok=None,
                  cu_q=None):
-        per = {"prompt_len": prompt_len, "repetition": repetition, "frequency": frequency, "presence": presence,
-               "temperature": temperature}
         if n_req is None:
-            n_req = next((t.numel() for t in per.values() if t is not None),
+            n_req = next((t.numel() for t in (repetition, frequency, presence, temperature, prompt_len) if t is not None),
                          next((t.numel() - 1 for t in (hist_off, bias_off, cu_q) if t is not None), 0))
-        for k, t in per.items():
-            _tensor(t, torch.int32 if k == "prompt_len" else torch.float32, n_req, k, optional=True)
-        for k, t in (("hist_off", hist_off), ("bias_off", bias_off), ("cu_q", cu_q)):
-            _tensor(t, torch.int32, n_req + 1, k, optional=True)
-        for k, t in (("hist", hist), ("bias_tok", bias_tok), ("tree_tok", tree_tok), ("grammar", grammar)):
-            _tensor(t, torch.int32, None, k, optional=True)
-        _tensor(bias_val, torch.float32, bias_tok.numel() if bias_tok is not None else None, "bias_val", optional=True)
-        _need(grammar is None or grammar.dim() == 2, "grammar: [states][words]")
-        self._keep = [hist, hist_off, prompt_len, repetition, frequency, presence, temperature, bias_off, bias_tok, bias_val,
-                      grammar, tree_tok, cu_q]
+        if grammar is not None and grammar.dim() != 2:
+            _refuse(f"grammar: [states][words], not {tuple(grammar.shape)}")
+        f32, i32 = torch.float32, torch.int32
+        self._keep = (hist, hist_off, prompt_len, repetition, frequency, presence, temperature, bias_off, bias_tok, bias_val,
+                      grammar, tree_tok, cu_q)
         self.n_req = n_req
-        p = [_ptr(t) for t in self._keep]
-        self.desc = LogitRulesDesc(n_req, *p[:11], grammar.shape[1] if grammar is not None else 0,
-                                   grammar.shape[0] if grammar is not None else 0, *p[11:])
+        self.desc = LogitRulesDesc(
+            n_req, _tensor(hist, i32, 0, "hist"), _tensor(hist_off, i32, n_req + 1, "hist_off"),
+            _tensor(prompt_len, i32, n_req, "prompt_len"), _tensor(repetition, f32, n_req, "repetition"),
+            _tensor(frequency, f32, n_req, "frequency"), _tensor(presence, f32, n_req, "presence"),
+            _tensor(temperature, f32, n_req, "temperature"), _tensor(bias_off, i32, n_req + 1, "bias_off"),
+            _tensor(bias_tok, i32, 0, "bias_tok"),
+            _tensor(bias_val, f32, 0 if bias_tok is None else bias_tok.numel(), "bias_val"), _tensor(grammar, i32, 0, "grammar"),
+            0 if grammar is None else grammar.shape[1], 0 if grammar is None else grammar.shape[0],
+            _tensor(tree_tok, i32, 0, "tree_tok"), _tensor(cu_q, i32, n_req + 1, "cu_q"))
 
 
 def op_adjust_logits(logits: torch.Tensor, req: torch.Tensor, rules: LogitRules, mask: Optional[torch.Tensor] = None,
                      state: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype=None,
                      stream=None) -> torch.Tensor:
     """Rules on logits [R][vocab] (rows any stride apart) of requests req [R]; out may be logits itself."""
-    _need(logits.is_cuda and logits.dim() == 2 and logits.dtype in _DTYPES and (logits.stride(1) == 1 or logits.shape[1] == 1),
-          f"logits: [R][vocab], not {tuple(logits.shape)} {logits.dtype}")
+    it = _DTYPES.get(logits.dtype)
+    if logits.dim() != 2 or it is None or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] != 1):
+        _refuse(f"logits: [R][vocab] on the device, not {tuple(logits.shape)} {logits.dtype}")
     R, V = logits.shape
     if out is None:
         out = _new((R, V), out_dtype or logits.dtype, logits.device, stream)
-    _need(out.is_cuda and out.shape == logits.shape and out.dtype in _DTYPES and (out.stride(1) == 1 or V == 1),
-          f"out: [{R}][{V}], not {tuple(out.shape)} {out.dtype}")
-    _tensor(req, torch.int32, R, "req")
-    _tensor(mask, torch.int32, R, "mask", optional=True)
-    _need(mask is None or (mask.dim() == 2 and mask.shape[0] >= R), "mask: [R][words]")
-    _tensor(state, torch.int32, R, "state", optional=True)
-    _check(load().atspeed_op_adjust_logits(_stream(stream), logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0), R, V,
-                                           req.data_ptr(), ctypes.byref(rules.desc), _ptr(mask),
-                                           mask.shape[1] if mask is not None else 0, _ptr(state), out.data_ptr(),
-                                           _DTYPES[out.dtype], out.stride(0)))
+    ot = _DTYPES.get(out.dtype)
+    if out.shape != logits.shape or ot is None or not out.is_cuda or (out.stride(1) != 1 and V != 1):
+        _refuse(f"out: [{R}][{V}] on the device, not {tuple(out.shape)} {out.dtype}")
+    if mask is not None and (mask.dim() != 2 or mask.shape[0] < R):
+        _refuse(f"mask: [{R}][words], not {tuple(mask.shape)}")
+    _check(load().atspeed_op_adjust_logits(_raw_stream(stream, logits.device), logits.data_ptr(), it, logits.stride(0), R, V,
+                                           _given(req, torch.int32, R, "req"), rules.desc,
+                                           _tensor(mask, torch.int32, R, "mask"), mask.shape[1] if mask is not None else 0,
+                                           _tensor(state, torch.int32, R, "state"), out.data_ptr(), ot, out.stride(0)))
     return out
