@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Dict, List, NamedTuple, Optional, Sequence, Tuple
+from typing import Dict, List, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -473,42 +473,50 @@ def _kv_pages(kc: torch.Tensor, vc: torch.Tensor) -> KvPages:
     return KvPages(kc.data_ptr(), vc.data_ptr(), kt, vt, shape[0], shape[1], shape[2], shape[3], ks[:3], vs[:3])
 
 
-class BatchPlan(NamedTuple):
+class BatchPlan:
     """Outputs of op_batch_plan (see atspeed_op_batch_plan)."""
-    cu_q: torch.Tensor      # [n + 1] int32
-    ctx_len: torch.Tensor   # [n] int32, -1: not served
-    state: torch.Tensor     # [n] int32, PLAN_*
-    used: torch.Tensor      # [] int32, pages taken from the front of the free list
-    taken: torch.Tensor     # [] int32, pages that the requests up to the last served one ask for, passed-over ones included
-    req: torch.Tensor       # [T] int32
-    pos: torch.Tensor       # [T] int32
-    slot: torch.Tensor      # [T] int64, -1: not served
-    mask: Optional[torch.Tensor]   # [T][words] int32 bit patterns (trees)
+    __slots__ = ("cu_q", "ctx_len", "state", "pages", "req", "pos", "slot", "mask")
+
+    def __init__(self, cu_q, ctx_len, state, pages, req, pos, slot, mask):
+        self.cu_q = cu_q          # [n + 1] int32
+        self.ctx_len = ctx_len    # [n] int32, -1: not served
+        self.state = state        # [n] int32, PLAN_*
+        self.pages = pages        # [2] int32: used, taken
+        self.req = req            # [T] int32
+        self.pos = pos            # [T] int32
+        self.slot = slot          # [T] int64, -1: not served
+        self.mask = mask          # [T][words] int32 bit patterns (trees), or None
+
+    @property
+    def used(self) -> torch.Tensor:
+        """[] int32, pages taken from the front of the free list."""
+        return self.pages[0]
+
+    @property
+    def taken(self) -> torch.Tensor:
+        """[] int32, pages that the requests up to the last served one ask for, those of the passed-over ones included."""
+        return self.pages[1]
 
 
 def op_batch_plan(q_len: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, free: torch.Tensor,
                   n_free: torch.Tensor, page_size: int, max_tokens: int, parent: Optional[torch.Tensor] = None,
                   mask_words: int = 0, stream=None) -> BatchPlan:
     """Pages, slots, positions and tree masks of a step from the requests' lengths; block_table is extended in place."""
-    n, T = q_len.numel(), max_tokens
+    n, T, i32, dev = q_len.numel(), max_tokens, torch.int32, q_len.device
     if block_table.dim() != 2 or block_table.shape[0] != n or T <= 0 or n == 0 or (parent is not None and mask_words <= 0):
         _refuse(f"{n} requests, {T} tokens, block_table {tuple(block_table.shape)}, {mask_words} mask words")
-    args = (_given(q_len, torch.int32, n, "q_len"), _given(kv_len, torch.int32, n, "kv_len"),
-            _tensor(parent, torch.int32, T, "parent"), page_size, _given(block_table, torch.int32, n, "block_table"),
-            block_table.shape[1], _given(free, torch.int32, 1, "free"), _given(n_free, torch.int32, 1, "n_free"), T, mask_words)
-    # one block of memory: slots (64 bits) first, then the 32-bit outputs
-    words = mask_words if parent is not None else 0
-    sizes = (2 * T, n + 1, n, n, 2, T, T, T * words)
-    whole = _new(sum(sizes), torch.int32, q_len.device, stream)
-    slot, cu_q, ctx_len, state, pages, req, pos, mask = whole.split_with_sizes(sizes)
-    at, out = whole.data_ptr(), []
-    for k in sizes:
-        out.append(at)
-        at += 4 * k
-    _check(load().atspeed_op_batch_plan(_raw_stream(stream, q_len.device), n, *args, *out[1:7], out[0],
-                                        out[7] if words else None))
-    return BatchPlan(cu_q, ctx_len, state, pages[0], pages[1], req, pos, slot.view(torch.int64),
-                     mask.view(T, words) if words else None)
+    q_ptr, kv_ptr, up_ptr = _given(q_len, i32, n, "q_len"), _given(kv_len, i32, n, "kv_len"), _tensor(parent, i32, T, "parent")
+    table_ptr = _given(block_table, i32, n, "block_table")
+    free_ptr, n_free_ptr = _given(free, i32, 1, "free"), _given(n_free, i32, 1, "n_free")
+    cu_q, ctx_len, state = _new((n + 1,), i32, dev, stream), _new((n,), i32, dev, stream), _new((n,), i32, dev, stream)
+    pages, req, pos = _new((2,), i32, dev, stream), _new((T,), i32, dev, stream), _new((T,), i32, dev, stream)
+    slot = _new((T,), torch.int64, dev, stream)
+    mask = _new((T, mask_words), i32, dev, stream) if parent is not None else None
+    _check(load().atspeed_op_batch_plan(_raw_stream(stream, dev), n, q_ptr, kv_ptr, up_ptr, page_size, table_ptr,
+                                        block_table.shape[1], free_ptr, n_free_ptr, T, mask_words, cu_q.data_ptr(),
+                                        ctx_len.data_ptr(), state.data_ptr(), pages.data_ptr(), req.data_ptr(), pos.data_ptr(),
+                                        slot.data_ptr(), _ptr(mask)))
+    return BatchPlan(cu_q, ctx_len, state, pages, req, pos, slot, mask)
 
 
 def op_rope_append(qkv: torch.Tensor, n_heads: int, kc: torch.Tensor, vc: torch.Tensor, slot: torch.Tensor,

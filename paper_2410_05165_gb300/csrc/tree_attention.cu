@@ -2,23 +2,29 @@
 //   o = sum_j w_j v_j / sum_j w_j, w_j = exp(scale q.k_j), over the positions j < ctx and those of the token's ancestors
 //
 // The rows of a (request, key head) are its new tokens times the G query heads that share the key head: they read the same
-// K and V, so a block of up to 256 rows reads each K / V tile of 128 keys once.  A tile is two products on tcgen05 with M =
+// K and V, so a block of up to 256 rows (two tiles of 128, or of the largest multiple of G below) reads each K / V tile of
+// 128 keys once.  A tile is two products on tcgen05 with M =
 // 128 rows: S = Q K^T (both K-major in shared memory) into TMEM, and O += P V with P (16 bits) as TMEM operand over S's
 // columns and V in place, MN-major.  One thread a row runs the softmax from TMEM: no shuffles, no shared memory; O is scaled
 // only where the running maximum rises by more than 2^8 (all weights are relative to the maximum in use, so the quotient
 // is the same).
 //
-// Two streams of (S, P, O) alternate on the tensor core, each with a warpgroup of its own: one's softmax runs under the
-// other's products.  Blocks of more than 128 rows: a stream is 128 of the rows, each sees every tile.  Fewer: both hold the
-// same rows and take alternate tiles; they are joined at the end.  (Padding a single token's G rows to 128 costs tensor
-// time that the tile's 64 KB of K and V, 2800 clocks of an SM's share of the HBM, leave free: 1024 clocks.)
+// Two streams of (S, P, O) share the tensor core, each with a warp that issues its products and a warpgroup that runs its
+// softmax.  Blocks of more than 128 rows: a stream is 128 of the rows, each sees every tile.  Fewer: both hold the same rows
+// and take alternate tiles; they are joined at the end.  (Padding a single token's G rows to 128 costs tensor time that the
+// tile's 64 KB of K and V, 2800 clocks of an SM's share of the HBM, leave free.)
+//
+// P goes out in two halves of 64 keys, so that the first half's product runs under the second half's exponentials.  (Tiles of
+// 64 keys with two S a stream, so that a softmax never waits for its S, lose more than they gain: a product of N = 64 takes the
+// tensor core the 64 clocks of one of N = 128.  Two threads a row made the softmax no faster.)
 //
 // Work is the concatenation of all blocks' tiles, cut into one equal range a CTA (every CTA finds its own range from the
 // lengths); a block cut by a range's end is summed from partial results in device memory, each of its CTAs taking a share
 // of the rows, in range order.  Waits for partial results come after all own results are out and the grid is launched
 // cooperatively, so that they end; they are bounded all the same.
 //
-// Roles (384 threads): warp 0 copies (TMA), warp 1 issues the products, warps 2-3 load Q, warps 4-7 and 8-11 are the streams.
+// Roles (384 threads): warp 0 copies (TMA), warps 1 and 2 issue the products of a stream each, warp 3 loads Q, warps 4-7 and
+// 8-11 run the streams' softmax.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -33,11 +39,11 @@ namespace {
 
 __device__ unsigned int g_tree_attn_err;
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 384, kStreamThreads = 256;
 constexpr int kTile = 128;       // keys of a tile
-constexpr int kBlock = 256;      // rows of a block
+constexpr int kBlock = 256;      // rows of a block, at most
 constexpr int kRoleRegs = 80, kStreamRegs = 208;
-static_assert(128 * kRoleRegs + 256 * kStreamRegs <= kThreads * 168, "registers at launch");
+static_assert(128 * kRoleRegs + kStreamThreads * kStreamRegs <= kThreads * 168, "registers at launch");
 constexpr float kSlack = 8.f;    // rise of the running maximum (log2) below which O keeps its scale
 constexpr int kMaxCtas = 512;    // counters in the workspace
 
@@ -45,13 +51,13 @@ template <int HD>
 struct Cfg {
   static constexpr int SW = HD >= 64 ? 128 : 64;       // bytes of a panel's row, and its swizzle
   static constexpr int PANELS = HD * 2 / SW;
-  static constexpr int PANEL = kTile * SW;
-  static constexpr int TILE = PANELS * PANEL;          // K or V tile, or 128 rows of Q
+  static constexpr int PANEL = kTile * SW, Q_PANEL = 128 * SW;
+  static constexpr int TILE = PANELS * PANEL, Q_TILE = PANELS * Q_PANEL;   // K or V tile; 128 rows of Q
   static constexpr int STAGES = HD == 128 ? 5 : 8;
   static constexpr int Q_OFF = STAGES * TILE;
-  static constexpr int X_OFF = Q_OFF + 2 * TILE;       // (m, l) of both streams
-  static constexpr int BAR_OFF = X_OFF + 2 * 128 * 8;
-  static constexpr int SMEM = BAR_OFF + 512;
+  static constexpr int X_OFF = Q_OFF + 2 * Q_TILE;       // (m, l) of both streams' rows
+  static constexpr int BAR_OFF = X_OFF + kStreamThreads * 8;
+  static constexpr int SMEM = BAR_OFF + 640;
   static constexpr int S_COL = 128, O_COL = 256;       // TMEM columns: S / P of stream s at s * 128, O at 256 + s * HD
   static constexpr int O_STEP = HD;
   static constexpr size_t PART = (size_t)kBlock * (HD + 2) * 4;   // bytes of a partial result: O [256][HD], (m, l) [256]
@@ -59,15 +65,17 @@ struct Cfg {
 static_assert(Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448, "shared memory of a CTA");
 
 struct TreeAttnArgs {
-  const uint16_t *q, *v;
-  long long vs[3], q_stride, out_stride;
-  int H, Hkv, G, n, T, page, width, words, cap;   // cap: positions that a table row covers
+  const uint16_t* v;
+  long long vs[3], out_stride;
+  int H, Hkv, G, n, T, page, page_log, n_pages, width, words;
+  int cap;                                        // positions that a table row covers
+  int rt;                                         // rows of a stream's tile: the multiple of G up to 128
   const int *cu_q, *ctx, *table;
   const uint32_t* mask;
   float c;                                        // scale * log2(e)
   uint16_t* out;
   float* lse;
-  bool k_f16, v_f16;
+  bool k_f16, v_f16, out32;                       // out32: rows of the output begin at multiples of 32 bytes
   unsigned char* parts;
   int* arrived;                                   // [kMaxCtas] partial results of the block that starts in a CTA
   int* done;                                      // [kMaxCtas] shares of it that are merged
@@ -88,11 +96,11 @@ __device__ __forceinline__ Request request(const TreeAttnArgs& a, int b) {
   // (offsets outside the call's rows: nothing of the request is read or written)
   if (r.t0 < 0 || r.q < 0 || r.t0 > a.T - r.q) r.q = 0;
   r.rows = r.q * a.G;
-  r.blocks = r.ctx < 0 ? 0 : (r.rows + kBlock - 1) / kBlock;
+  r.blocks = r.ctx < 0 ? 0 : (r.rows + 2 * a.rt - 1) / (2 * a.rt);
   return r;
 }
 __device__ __forceinline__ int block_keys(const TreeAttnArgs& a, const Request& r, int blk) {
-  const int last = a.mask ? r.q : (min(r.rows, (blk + 1) * kBlock) - 1) / a.G + 1;
+  const int last = a.mask ? r.q : min(r.q, (blk + 1) * 2 * a.rt / a.G);
   return (int)min((long long)r.ctx + last, (long long)a.cap);
 }
 __device__ __forceinline__ int tiles_of(int keys) { return (keys + kTile - 1) / kTile; }
@@ -142,32 +150,40 @@ struct Walk {
     }
     block(0);
   }
-  __device__ int rows() const { return min(kBlock, r.rows - blk * kBlock); }
-  __device__ bool dual() const { return rows() > 128; }
+  __device__ int rows() const { return min(2 * a.rt, r.rows - blk * 2 * a.rt); }
+  __device__ bool dual() const { return rows() > a.rt; }
 };
 
 // ---------------------------------------------------------------------------------------------
 // instructions
 // ---------------------------------------------------------------------------------------------
-__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z, int w) {
+// (by the thread with `lead`: issued by several lanes at once, a copy's operands are moved to uniform registers lane by lane)
+__device__ __forceinline__ void tma_load_4d(uint32_t lead, uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z,
+                                            int w) {
   asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-          smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+      "{\n .reg .pred e;\n setp.ne.b32 e, %7, 0;\n @e cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::"
+      "complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n}" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "r"(lead)
       : "memory");
 }
-__device__ __forceinline__ void mma_ss(uint32_t lead, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+// One product of 16 along K, by the thread with `lead`.  Descriptors come as their low words (address, lead offset) and the
+// high word that all operands of a kernel share.  A in shared memory, or in TMEM.
+__device__ __forceinline__ void mma_ss(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t idesc,
+                                       uint32_t add) {
   asm volatile(
-      "{\n .reg .pred e, p;\n setp.ne.b32 e, %5, 0;\n setp.ne.b32 p, %4, 0;\n"
-      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(add), "r"(lead)
+      "{\n .reg .pred e, p;\n .reg .b64 da, db;\n setp.ne.b32 e, %6, 0;\n setp.ne.b32 p, %5, 0;\n"
+      " mov.b64 da, {%1, %3};\n mov.b64 db, {%2, %3};\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(hi), "r"(idesc), "r"(add), "r"(lead)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t lead, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+__device__ __forceinline__ void mma_ts(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t idesc,
+                                       uint32_t add) {
   asm volatile(
-      "{\n .reg .pred e, p;\n setp.ne.b32 e, %5, 0;\n setp.ne.b32 p, %4, 0;\n"
-      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(add), "r"(lead)
+      "{\n .reg .pred e, p;\n .reg .b64 db;\n setp.ne.b32 e, %6, 0;\n setp.ne.b32 p, %5, 0;\n"
+      " mov.b64 db, {%2, %3};\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(hi), "r"(idesc), "r"(add), "r"(lead)
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_32x32b_x32(uint32_t taddr, const uint32_t* v) {
@@ -180,54 +196,159 @@ __device__ __forceinline__ void tmem_st_32x32b_x32(uint32_t taddr, const uint32_
       "r"(v[31])
       : "memory");
 }
+// wait::ld with the registers it is about, so that nothing that uses them moves ahead of it
+__device__ __forceinline__ void tmem_ld_wait128(uint32_t (&x)[128]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < 128; j += 16)
+    asm volatile(""
+                 : "+r"(x[j]), "+r"(x[j + 1]), "+r"(x[j + 2]), "+r"(x[j + 3]), "+r"(x[j + 4]), "+r"(x[j + 5]), "+r"(x[j + 6]),
+                   "+r"(x[j + 7]), "+r"(x[j + 8]), "+r"(x[j + 9]), "+r"(x[j + 10]), "+r"(x[j + 11]), "+r"(x[j + 12]),
+                   "+r"(x[j + 13]), "+r"(x[j + 14]), "+r"(x[j + 15]));
+}
+__device__ __forceinline__ void tmem_ld_wait16(uint32_t (&x)[16], uint32_t (&y)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < 16; j += 8)
+    asm volatile(""
+                 : "+r"(x[j]), "+r"(x[j + 1]), "+r"(x[j + 2]), "+r"(x[j + 3]), "+r"(x[j + 4]), "+r"(x[j + 5]), "+r"(x[j + 6]),
+                   "+r"(x[j + 7]), "+r"(y[j]), "+r"(y[j + 1]), "+r"(y[j + 2]), "+r"(y[j + 3]), "+r"(y[j + 4]), "+r"(y[j + 5]),
+                   "+r"(y[j + 6]), "+r"(y[j + 7]));
+}
+// 32 bytes, a whole sector, by one thread
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+__device__ __forceinline__ void hold64(uint32_t* x) {
+#pragma unroll
+  for (int j = 0; j < 64; j += 16)
+    asm volatile(""
+                 : "+r"(x[j]), "+r"(x[j + 1]), "+r"(x[j + 2]), "+r"(x[j + 3]), "+r"(x[j + 4]), "+r"(x[j + 5]), "+r"(x[j + 6]),
+                   "+r"(x[j + 7]), "+r"(x[j + 8]), "+r"(x[j + 9]), "+r"(x[j + 10]), "+r"(x[j + 11]), "+r"(x[j + 12]),
+                   "+r"(x[j + 13]), "+r"(x[j + 14]), "+r"(x[j + 15]));
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
-// Shared-memory descriptors (fields: common.cuh, smem_desc_sw128).  stride: between groups of eight rows of a panel; lead:
-// between panels of an MN-major operand wider than one.  Layout 2 is the 128-byte swizzle, 4 the 64-byte one.
-template <int SW>
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t lead) {
-  return (uint64_t)((addr >> 4) & 0x3FFFu) | (uint64_t)((lead >> 4) & 0x3FFFu) << 16 | (uint64_t)((8u * SW) >> 4) << 32 |
-         (uint64_t)1u << 46 | (uint64_t)(SW == 128 ? 2u : 4u) << 61;
+// Two values at once: x * m + a, and x + y (in 32 bits each).
+__device__ __forceinline__ float2 fma2(float2 x, float2 m, float2 a) {
+  float2 y;
+  asm("{\n .reg .b64 r, s, t;\n mov.b64 r, {%2, %3};\n mov.b64 s, {%4, %5};\n mov.b64 t, {%6, %7};\n"
+      " fma.rn.f32x2 r, r, s, t;\n mov.b64 {%0, %1}, r;\n}"
+      : "=f"(y.x), "=f"(y.y)
+      : "f"(x.x), "f"(x.y), "f"(m.x), "f"(m.y), "f"(a.x), "f"(a.y));
+  return y;
 }
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  float2 z;
+  asm("{\n .reg .b64 r, s;\n mov.b64 r, {%2, %3};\n mov.b64 s, {%4, %5};\n add.rn.f32x2 r, r, s;\n mov.b64 {%0, %1}, r;\n}"
+      : "=f"(z.x), "=f"(z.y)
+      : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+  return z;
+}
+__device__ __forceinline__ int warp_uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+
+// Shared-memory descriptors (fields: common.cuh, smem_desc_sw128): the low word holds the address and `lead`, the bytes
+// between panels of an MN-major operand wider than one; the high word the bytes between groups of eight rows of a panel,
+// the version and the swizzle (2: 128 bytes, 4: 64).
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lead) {
+  return ((addr >> 4) & 0x3FFFu) | ((lead >> 4) & 0x3FFFu) << 16;
+}
+template <int SW>
+constexpr uint32_t kDescHi = ((8u * SW) >> 4) | 1u << 14 | (SW == 128 ? 2u : 4u) << 29;
 // Instruction descriptor (fields: idesc_bf16_f32); bit 16: B is MN-major
 __device__ __forceinline__ uint32_t instr_desc(int n, bool f16, bool b_mn) {
   const uint32_t t = f16 ? 0u : 1u;
   return (1u << 4) | (t << 7) | (t << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
-// Place of a K or V tile in the order of the copies: blocks on both streams' rows read K, V, K, V, ..; blocks that
-// alternate tiles read K one ahead (K0, K1, V0, K2, V1, ..), as the products do.
-__device__ __forceinline__ int seq_k(bool dual, int i) { return dual ? 2 * i : max(0, 2 * i - 1); }
-__device__ __forceinline__ int seq_v(bool dual, int i, int n) { return dual ? 2 * i + 1 : min(2 * i + 2, 2 * n - 1); }
+// Place of a K or V tile in the order of the copies, of a range of n tiles: K runs ahead of V by the S that are under way (one
+// tile where both streams see every tile, two where they alternate), then V and K take turns: K0 .. K(L-1), V0, K(L), V1, ..
+__device__ __forceinline__ int k_lead(bool dual) { return dual ? 1 : 2; }
+__device__ __forceinline__ int seq_k(int lead, int i) { return i < lead ? i : 2 * i - lead + 1; }
+__device__ __forceinline__ int seq_v(int lead, int i, int n) { return min(lead, n) + i + min(i, max(0, n - lead)); }
 
-__device__ __forceinline__ bool finite16(uint32_t two, bool f16, uint32_t& clean) {
-  const uint32_t e = f16 ? 0x7c00u : 0x7f80u;
-  clean = two;
-  if ((two & e) == e) clean &= 0xffff0000u;
-  if ((two >> 16 & e) == e) clean &= 0x0000ffffu;
-  return clean == two;
-}
-
-// 32 bits of a row's mask from bit j0 on (bits outside [0, q) are 0)
-__device__ __forceinline__ uint32_t mask_window(const uint32_t* row, int words, int j0, int q) {
-  const auto word = [&](int i) { return i >= 0 && i < words ? __ldg(row + i) : 0u; };
-  const int w = j0 >> 5, sh = j0 & 31;   // (arithmetic: j0 may be negative)
-  const uint32_t x = __funnelshift_r(word(w), word(w + 1), sh);
-  const int up = q - j0;
-  return up >= 32 ? x : up <= 0 ? 0u : x & ((1u << up) - 1u);
-}
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// The 32 keys from `key` on that row token i of request r sees.
-__device__ __forceinline__ uint32_t seen_word(const TreeAttnArgs& a, const Request& r, int i, int key) {
-  const int j0 = key - r.ctx;
-  uint32_t x = a.mask ? mask_window(a.mask + (long long)(r.t0 + i) * a.words, a.words, j0, r.q) : low_bits(i + 1 - j0);
-  x |= low_bits(-j0);                    // cached positions
-  return x & low_bits(a.cap - key);
+// The 32 NW keys from `key` on that token i of request r sees, lowest bit first.
+template <int NW>
+__device__ __forceinline__ void seen_keys(const TreeAttnArgs& a, const Request& r, int i, int key, uint32_t (&x)[NW]) {
+  const int j0 = key - r.ctx;   // first of them among the new tokens; below 0 there are cached positions
+  if (a.mask) {
+    const uint32_t* row = a.mask + (long long)(r.t0 + i) * a.words;
+    const int w = j0 >> 5, sh = j0 & 31;   // (arithmetic: j0 may be negative)
+    uint32_t m[NW + 1];
+#pragma unroll
+    for (int k = 0; k <= NW; ++k) m[k] = w + k >= 0 && w + k < a.words ? __ldg(row + w + k) : 0u;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) x[k] = __funnelshift_r(m[k], m[k + 1], sh) & low_bits(r.q - j0 - 32 * k);
+  } else {
+#pragma unroll
+    for (int k = 0; k < NW; ++k) x[k] = low_bits(i + 1 - j0 - 32 * k);
+  }
+#pragma unroll
+  for (int k = 0; k < NW; ++k) x[k] = (x[k] | low_bits(-j0 - 32 * k)) & low_bits(a.cap - key - 32 * k);
+}
+
+// Of a V tile's keys those from `first` on: NaN and infinities become 0, in every key; *odd is set if one was found before
+// key `last`.  By 128 threads.  (Two 16-bit values are tested at once: with its sign off, a value that is not finite plus
+// `step` reaches the sign's place.)
+template <int HD>
+__device__ __forceinline__ void clean_v(uint8_t* v0, int r, int first, int last, bool f16, volatile int* odd) {
+  using C = Cfg<HD>;
+  constexpr int RC = C::SW / 16;   // 16-byte chunks of a panel's row
+  const uint32_t step = f16 ? 0x04000400u : 0x00800080u;
+  const auto beyond = [&](uint32_t two) { return (two & 0x7fff7fffu) + step & 0x80008000u; };
+  uint4* chunk = reinterpret_cast<uint4*>(v0) + r % RC;
+  uint32_t any = 0;
+#pragma unroll
+  for (int panel = 0; panel < C::PANELS; ++panel)
+#pragma unroll 4
+    for (int row = first + r / RC; row < kTile; row += 128 / RC) {
+      const uint4 v = chunk[(panel * C::PANEL + row * C::SW) / 16];
+      any |= beyond(v.x) | beyond(v.y) | beyond(v.z) | beyond(v.w);
+    }
+  if (!any) return;
+  for (int panel = 0; panel < C::PANELS; ++panel)
+    for (int row = first + r / RC; row < kTile; row += 128 / RC) {
+      uint16_t* v = reinterpret_cast<uint16_t*>(chunk + (panel * C::PANEL + row * C::SW) / 16);
+      for (int j = 0; j < 8; ++j) {
+        if (!beyond(v[j])) continue;
+        if (row < last) {
+          *odd = 1;
+          __threadfence_block();
+        }
+        v[j] = 0;
+      }
+    }
+  fence_proxy_async_shared();
+}
+
+// The NaN and infinities of V that a row sees among keys [p0, p1) and that were 0 in its tiles, added to columns [c0, c1) of
+// its result in device memory (the call's output, or a partial result in 32 bits).
+template <int HD>
+__device__ __noinline__ void add_odd_v(const TreeAttnArgs& a, int b, int kh, int tok, int p0, int p1, int c0, int c1, uint16_t* out,
+                                       float* part) {
+  const Request r = request(a, b);
+  for (int p = p0; p < p1; ++p) {
+    uint32_t see[1];
+    seen_keys(a, r, tok, p, see);
+    if (!(see[0] & 1)) continue;
+    const int id = a.table[(long long)b * a.width + (p >> a.page_log)];
+    if (id < 0 || id >= a.n_pages) continue;
+    const uint16_t* v = a.v + id * a.vs[0] + (p & (a.page - 1)) * a.vs[1] + kh * a.vs[2];
+    for (int c = c0; c < c1; ++c) {
+      const float x = unpack2(v[c], a.v_f16).x;
+      if (isfinite(x)) continue;
+      if (part) part[c] += x;
+      else out[c] = (uint16_t)pack2(unpack2(out[c], a.k_f16).x + x, 0.f, a.k_f16);
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -245,9 +366,9 @@ template <int HD>
 __device__ __forceinline__ void merge_share(const TreeAttnArgs& a, const Request& r, int kh, int blk, int first, int parts,
                                             int share, int tid) {
   constexpr int V4 = HD / 4;
-  const int rows = min(kBlock, r.rows - blk * kBlock), total = rows * V4;
+  const int rows = min(2 * a.rt, r.rows - blk * 2 * a.rt), total = rows * V4;
   const int i0 = (int)((long long)total * share / parts), i1 = (int)((long long)total * (share + 1) / parts);
-  for (int i = i0 + tid; i < i1; i += 256) {
+  for (int i = i0 + tid; i < i1; i += kStreamThreads) {
     const int row = i / V4, c4 = i % V4;
     const auto ml = [&](int p) {
       return __ldcg(reinterpret_cast<const float2*>(part_of<HD>(a, first + p, p == 0) + kBlock * HD) + row);
@@ -266,7 +387,7 @@ __device__ __forceinline__ void merge_share(const TreeAttnArgs& a, const Request
       o.x += w * y.x, o.y += w * y.y, o.z += w * y.z, o.w += w * y.w;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int rg = blk * kBlock + row, t = r.t0 + rg / a.G, h = kh * a.G + rg % a.G;
+    const int rg = blk * 2 * a.rt + row, t = r.t0 + rg / a.G, h = kh * a.G + rg % a.G;
     uint2 u = make_uint2(pack2(o.x * inv, o.y * inv, a.k_f16), pack2(o.z * inv, o.w * inv, a.k_f16));
     *reinterpret_cast<uint2*>(a.out + (long long)t * a.out_stride + (long long)h * HD + c4 * 4) = u;
     if (a.lse && c4 == 0) a.lse[(long long)t * a.H + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
@@ -286,31 +407,40 @@ __device__ __forceinline__ bool wait_count(const int* p, int want, unsigned int*
   }
 }
 
+// Whether a phase of a barrier of this CTA is complete.
+__device__ __forceinline__ bool bar_done(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok)
+               : "r"(smem_u32(bar)), "r"(parity)
+               : "memory");
+  return ok != 0;
+}
 // A wait of a whole warp, which goes on together; after the first that gave up the rest are not waited for (the loops run
 // to their ends without the work, so that every barrier meets its threads).
 __device__ __forceinline__ bool warp_wait(bool ok, uint64_t* bar, uint32_t parity, unsigned int* err) {
-  if (ok) ok = mbar_wait(bar, parity, err);
-  return __all_sync(0xffffffffu, ok);
+  if (__builtin_expect(__all_sync(0xffffffffu, bar_done(bar, parity)), 1) || !ok) return ok;
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, err));
 }
 
-template <int HD>
+template <int HD, bool KF16, bool VF16>
 __global__ void __launch_bounds__(kThreads, 1)
-    tree_attention_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv,
-                          const __grid_constant__ TreeAttnArgs a) {
+    tree_attention_kernel(const __grid_constant__ CUtensorMap tmq, const __grid_constant__ CUtensorMap tmk,
+                          const __grid_constant__ CUtensorMap tmv, const __grid_constant__ TreeAttnArgs a) {
   using C = Cfg<HD>;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::BAR_OFF);
   uint64_t* empty = full + C::STAGES;
-  uint64_t* s_full = empty + C::STAGES;   // [2] S of a stream is in TMEM
-  uint64_t* p_ready = s_full + 2;         // [2] P of a stream is in TMEM
-  uint64_t* q_full = p_ready + 2;
+  uint64_t* s_full = empty + C::STAGES;   // [2] S of a stream is in TMEM (and the P V before it complete)
+  uint64_t* p_ready = s_full + 2;         // [2][2] the halves of its P are
+  uint64_t* q_full = p_ready + 4;
   uint64_t* q_free = q_full + 1;
   uint64_t* o_done = q_free + 1;          // the block's products are complete
   uint64_t* o_free = o_done + 1;          // its O is read
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_free + 1);
   volatile int* odd_v = reinterpret_cast<int*>(tmem_slot + 1);   // a NaN or infinity was found in a new token's V
-  Start* start = reinterpret_cast<Start*>(smem + C::BAR_OFF + 256);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  Start* start = reinterpret_cast<Start*>(smem + C::BAR_OFF + 512);
+  const int tid = threadIdx.x, warp = warp_uniform(tid >> 5), lane = tid & 31;
   unsigned int* err = a.err;
 
   // ---- this CTA's range of the call's units ----
@@ -326,19 +456,20 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane >= o) sum += x;
     }
     if (lane == 31) sums[warp] = sum;
-    if (warp == 2) tmem_alloc(tmem_slot, 512);
+    if (warp == 3) tmem_alloc(tmem_slot, 512);
     if (tid == 0) {
-      for (int i = 0; i < C::STAGES; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 1);
-      for (int i = 0; i < 2; ++i) mbar_init(s_full + i, 1), mbar_init(p_ready + i, 4);
-      mbar_init(q_full, 2);
-      mbar_init(q_free, 1);
-      mbar_init(o_done, 1);
-      mbar_init(o_free, 8);
+      for (int i = 0; i < C::STAGES; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 2);
+      for (int i = 0; i < 2; ++i) mbar_init(s_full + i, 1);
+      for (int i = 0; i < 4; ++i) mbar_init(p_ready + i, 4);
+      mbar_init(q_full, 1);
+      mbar_init(q_free, 2);
+      mbar_init(o_done, 2);
+      mbar_init(o_free, kStreamThreads / 32);
       fence_mbar_init();
       *odd_v = 0;
       start->u0 = start->u1 = 0;
     }
-    if (tid == 32) tma_prefetch_desc(&tmk), tma_prefetch_desc(&tmv);
+    if (tid == 32) tma_prefetch_desc(&tmq), tma_prefetch_desc(&tmk), tma_prefetch_desc(&tmv);
     __syncthreads();
     long long total = 0, before = sum - own;
     for (int w = 0; w < kThreads / 32; ++w) {
@@ -386,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncthreads();
     tc_fence_after();
   }
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = warp_uniform(*tmem_slot);
   const Start st = *start;
   bool ok = true;
 
@@ -394,138 +525,155 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRoleRegs));
     if (warp == 0) {
       // ---- copies ----
-      const int box = min(a.page, kTile), n_box = kTile / box;   // pages (or the half page) of a tile
-      const int lp = lane / C::PANELS, panel = lane % C::PANELS;
+      // A tile is copied page by page (or half a page of 256), a panel of 64 dimensions at a time.  The page numbers of 32
+      // boxes are read at once, one a lane, the next 32 ahead of time.
+      const uint32_t lead = elect_one(), ring = smem_u32(smem), bars = smem_u32(full);
+      const int box_log = min(a.page_log, 7), n_box = kTile >> box_log;
       unsigned seq = 0;
+      struct Pages {
+        int now, next, base;   // of the 32 boxes from `base` on, and of the 32 after
+      };
       for (Walk w(a, st); w.more(); w.next()) {
-        const bool dual = w.dual();
-        const int n = w.tiles;
+        const int n = warp_uniform(w.tiles), ahead = k_lead(warp_uniform(w.dual()));
+        const int tile0 = warp_uniform(w.tile0), keys = warp_uniform(w.keys), kh = warp_uniform(w.kh);
         const int* table = a.table + (long long)w.b * a.width;
-        const auto pages = [&](int i) {   // this lane's page of tile i (its keys' first position / page)
-          const int key = (w.tile0 + i) * kTile + lp * box;
-          return i < n && lp < n_box && key < w.keys ? __ldg(table + key / a.page) : 0;
+        const auto read = [&](int box) {   // this lane's of the 32 boxes from `box` on
+          const int key = (box + lane) << box_log;
+          return key < keys ? __ldg(table + (key >> a.page_log)) : 0;
         };
-        const auto copy = [&](const CUtensorMap* map, int i, int id) {
-          const int slot = seq % C::STAGES;
+        const auto copy = [&](const CUtensorMap* map, int i, Pages& p) {
+          const unsigned slot = seq % C::STAGES;
+          const int key0 = (tile0 + i) * kTile, box0 = key0 >> box_log;
+          const int boxes = min(n_box, (keys - key0 + (1 << box_log) - 1) >> box_log);
+          if (box0 - p.base >= 32) p.now = p.next, p.base += 32, p.next = read(p.base + 32);
           ok = warp_wait(ok, empty + slot, (seq / C::STAGES & 1) ^ 1, err);
           ++seq;
           if (!ok) return;
-          const int key0 = (w.tile0 + i) * kTile, boxes = min(n_box, (w.keys - key0 + box - 1) / box);
-          if (lane == 0) mbar_arrive_expect_tx(full + slot, boxes * box * HD * 2);
-          __syncwarp();
-          if (lp < boxes)
-            tma_load_4d(smem + slot * C::TILE + panel * C::PANEL + lp * box * C::SW, map, full + slot, panel * (C::SW / 2),
-                        (key0 + lp * box) % a.page, w.kh, id);
+          mbar_expect_tx_lead(lead, full + slot, (boxes << box_log) * HD * 2);
+#pragma unroll 1
+          for (int b = 0; b < boxes; ++b) {
+            const int id = __shfl_sync(0xffffffffu, p.now, box0 + b - p.base);
+#pragma unroll
+            for (int panel = 0; panel < C::PANELS; ++panel)
+              tma_load_4d(lead, ring + slot * C::TILE + panel * C::PANEL + (b << box_log) * C::SW, map, bars + slot * 8,
+                          panel * (C::SW / 2), (key0 + (b << box_log)) & (a.page - 1), kh, id);
+          }
         };
-        int ids = pages(0), next = pages(1);
-        if (dual) {
-          for (int i = 0; i < n; ++i) {
-            copy(&tmk, i, ids);
-            copy(&tmv, i, ids);
-            ids = next;
-            next = pages(i + 2);
-          }
-        } else {
-          int last = 0;
-          for (int i = 0; i <= n; ++i) {
-            if (i < n) copy(&tmk, i, ids);
-            if (i > 0) copy(&tmv, i - 1, last);
-            last = ids;
-            ids = next;
-            next = pages(i + 2);
-          }
+        Pages pk, pv;
+        pk.base = pv.base = tile0 * n_box;
+        pk.now = pv.now = read(pk.base);
+        pk.next = pv.next = read(pk.base + 32);
+#pragma unroll 1
+        for (int i = -ahead; i < n; ++i) {   // V of tile i, K of tile i + ahead
+          if (i >= 0) copy(&tmv, i, pv);
+          if (i + ahead < n) copy(&tmk, i + ahead, pk);
         }
       }
-    } else if (warp == 1) {
-      // ---- products ----
+    } else if (warp < 3) {
+      // ---- products of a stream ----
+      // (all that the products' operands are made of is the same in every lane, and said to be so: an operand that may
+      // differ is moved to a uniform register anew for each product)
       const uint32_t lead = elect_one();
-      const uint32_t id_s = instr_desc(kTile, a.k_f16, false), id_o = instr_desc(HD, a.v_f16, true);
-      unsigned seq0 = 0, item = 0, used[2] = {0, 0};   // used: P's consumed on a stream
-      const uint32_t ring = smem_u32(smem), qs = smem_u32(smem + C::Q_OFF);
-      for (Walk w(a, st); w.more(); w.next(), ++item) {
-        const bool dual = w.dual();
-        const int n = w.tiles, steps = dual ? 2 * n : n;
-        ok = warp_wait(ok, q_full, item & 1, err);
-        const auto scores = [&](int t) {
-          const int s = t & 1, i = dual ? t >> 1 : t;
-          const unsigned seq = seq0 + seq_k(dual, i), slot = seq % C::STAGES;
-          ok = warp_wait(ok, full + slot, seq / C::STAGES & 1, err);
-          if (!ok) return;
-          tc_fence_after();
-          const uint64_t qd = operand_desc<C::SW>(qs + (dual ? s * C::TILE : 0), 16);
-          const uint64_t kd = operand_desc<C::SW>(ring + slot * C::TILE, 16);
-#pragma unroll
-          for (int k = 0; k < HD / 16; ++k) {
-            const uint64_t step = (uint64_t)((k * 32 / C::SW) * C::PANEL + k * 32 % C::SW) >> 4;
-            mma_ss(lead, tmem + s * C::S_COL, qd + step, kd + step, id_s, k > 0);
-          }
-          tc_commit_lead(lead, s_full + s);
-          if (!dual || s) tc_commit_lead(lead, empty + slot);
-          if (t == steps - 1) tc_commit_lead(lead, q_free);
-        };
-        scores(0);
-        if (steps > 1) scores(1);
-        ok = warp_wait(ok, o_free, (item & 1) ^ 1, err);
-        for (int t = 0; t < steps; ++t) {
-          const int s = t & 1, i = dual ? t >> 1 : t;
-          const unsigned seq = seq0 + seq_v(dual, i, n), slot = seq % C::STAGES;
-          ok = warp_wait(ok, full + slot, seq / C::STAGES & 1, err);
-          ok = warp_wait(ok, p_ready + s, used[s] & 1, err);
-          ++used[s];
-          if (ok) {
-            tc_fence_after();
-            const uint64_t vd = operand_desc<C::SW>(ring + slot * C::TILE, C::PANEL);
-#pragma unroll
-            for (int k = 0; k < kTile / 16; ++k)
-              mma_ts(lead, tmem + C::O_COL + s * C::O_STEP, tmem + s * C::S_COL + k * 8, vd + (k * 16 * C::SW >> 4), id_o,
-                     t > 1 || k > 0);
-            if (!dual || s) tc_commit_lead(lead, empty + slot);
-            if (t == steps - 1) tc_commit_lead(lead, o_done);
-          }
-          if (t + 2 < steps) scores(t + 2);
+      const int s = warp - 1;
+      const uint32_t id_s = instr_desc(kTile, KF16, false), id_o = instr_desc(HD, VF16, true), hi = kDescHi<C::SW>;
+      const uint32_t ring = desc_lo(smem_u32(smem), C::PANEL), qs = desc_lo(smem_u32(smem + C::Q_OFF), C::Q_PANEL);
+      const uint32_t t_s = tmem + s * C::S_COL, t_o = tmem + C::O_COL + s * C::O_STEP;
+      unsigned seq0 = 0, item = 0, turn = 0, pos = 0;   // turn: tiles this stream has been through; pos: places
+      // Every place of the ring up to `seq` is gone through in order.  Of the other stream's tiles that is all: their copy is
+      // waited for and the place given back.  (A wait tells a phase from the next one only, by its parity: a place that is
+      // filled again before this stream has seen it would be taken for the wrong copy.)
+      const auto pass = [&](unsigned seq) {
+        for (; pos < seq; ++pos) {
+          ok = warp_wait(ok, full + pos % C::STAGES, pos / C::STAGES & 1, err);
+          if (lane == 0 && ok) mbar_arrive(empty + pos % C::STAGES);
         }
+      };
+      for (Walk w(a, st); w.more(); w.next(), ++item) {
+        const bool dual = warp_uniform(w.dual());
+        const int n = warp_uniform(w.tiles), tiles = dual ? n : (n - s + 1) / 2, ahead = k_lead(dual);
+        const uint32_t qd = qs + (dual ? s * (C::Q_TILE >> 4) : 0);
+        const auto copied = [&](unsigned seq) {
+          if (pos > seq) return;
+          pass(seq);
+          ok = warp_wait(ok, full + seq % C::STAGES, seq / C::STAGES & 1, err);
+          pos = seq + 1;
+        };
+        // The same as far as it takes no waiting.
+        const auto copied_by_now = [&](unsigned seq) {
+          for (; pos <= seq; ++pos) {
+            if (!__all_sync(0xffffffffu, bar_done(full + pos % C::STAGES, pos / C::STAGES & 1))) return;
+            if (pos < seq && lane == 0) mbar_arrive(empty + pos % C::STAGES);
+          }
+        };
+        // (a stream without tiles waits too: no stream may be a block ahead on these barriers)
+        ok = warp_wait(ok, q_full, item & 1, err);
+        if (tiles == 0 && ok) tc_commit_lead(lead, q_free);
+        // S of the stream's first tile, then P V of tile k and S of tile k + 1 in turn
+#pragma unroll 1
+        for (int k = -1; k < tiles; ++k) {
+          const unsigned v_seq = seq0 + seq_v(ahead, dual ? k : 2 * k + s, n), v_slot = v_seq % C::STAGES;
+          const unsigned k_seq = seq0 + seq_k(ahead, dual ? k + 1 : 2 * k + 2 + s), k_slot = k_seq % C::STAGES;
+          if (k >= 0) {
+            if (k == 0) ok = warp_wait(ok, o_free, (item & 1) ^ 1, err);
+            copied(v_seq);
+            if (k + 1 < tiles && ok) copied_by_now(k_seq);
+            const uint32_t vd = ring + v_slot * (C::TILE >> 4);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              ok = warp_wait(ok, p_ready + 2 * s + h, (turn + k) & 1, err);
+              if (!ok) continue;
+              tc_fence_after();
+#pragma unroll
+              for (int j = 4 * h; j < 4 * h + 4; ++j)
+                mma_ts(lead, t_o, t_s + j * 8, vd + (j * 16 * C::SW >> 4), hi, id_o, k > 0 || j > 0);
+            }
+          }
+          if (k + 1 < tiles) {
+            copied(k_seq);
+            if (ok) {
+              tc_fence_after();
+              const uint32_t kd = ring + k_slot * (C::TILE >> 4);
+#pragma unroll
+              for (int j = 0; j < HD / 16; ++j) {
+                const uint32_t step = ((j * 32 / C::SW) * C::PANEL + j * 32 % C::SW) >> 4;
+                mma_ss(lead, t_s, qd + step, kd + step, hi, id_s, j > 0);
+              }
+              tc_commit_lead(lead, s_full + s);   // (the stream's threads give K's place back when they see it)
+              if (k + 1 == tiles - 1) tc_commit_lead(lead, q_free);
+            }
+          }
+          if (k >= 0 && ok) tc_commit_lead(lead, empty + v_slot);
+        }
+        if (tiles == 0) ok = warp_wait(ok, o_free, (item & 1) ^ 1, err);
+        if (ok) tc_commit_lead(lead, o_done);
+        turn += tiles;
         seq0 += 2 * n;
+        pass(seq0);
       }
     } else {
-      // ---- Q ----
-      const int l64 = tid - 64;
+      // ---- Q: a tile's tokens x G heads of one key head ----
+      const uint32_t lead = elect_one();
       unsigned item = 0;
       for (Walk w(a, st); w.more(); w.next(), ++item) {
         ok = warp_wait(ok, q_free, (item & 1) ^ 1, err);
-        constexpr int CH = HD / 8, U = 8;   // 16-byte chunks of a row, loads in flight
-        const int total = w.rows() * CH;
-        for (int c0 = l64; c0 < total; c0 += 64 * U) {
-          uint4 v[U];
+        if (!ok) continue;
+        const int both = w.dual() ? 2 : 1;
+        mbar_expect_tx_lead(lead, q_full, both * a.rt * HD * 2);
+        for (int x = 0; x < both; ++x)
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int ch = c0 + 64 * u;
-            if (ch >= total) break;
-            const int rg = w.blk * kBlock + ch / CH, t = w.r.t0 + rg / a.G, h = w.kh * a.G + rg % a.G;
-            v[u] = __ldg(reinterpret_cast<const uint4*>(a.q + (long long)t * a.q_stride + (long long)h * HD) + ch % CH);
-          }
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int ch = c0 + 64 * u;
-            if (ch >= total) break;
-            const int row = ch / CH, r = row & 127, x = ch % CH, pc = C::SW / 16;   // (pc: chunks of a panel's row)
-            const int sw = C::SW == 128 ? r & 7 : (r >> 1) & 3;
-            *reinterpret_cast<uint4*>(smem + C::Q_OFF + (row >> 7) * C::TILE + (x / pc) * C::PANEL + r * C::SW +
-                                      ((x % pc ^ sw) << 4)) = v[u];
-          }
-        }
-        fence_proxy_async_shared();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(q_full);
+          for (int panel = 0; panel < C::PANELS; ++panel)
+            tma_load_4d(lead, smem_u32(smem + C::Q_OFF) + x * C::Q_TILE + panel * C::Q_PANEL, &tmq, smem_u32(q_full),
+                        panel * (C::SW / 2), 0, w.kh, w.r.t0 + (2 * w.blk + x) * (a.rt / a.G));
       }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kStreamRegs));
-    // ---- a stream: softmax, and the block's results ----
+    // ---- a stream: softmax, and the block's results; a thread a row ----
     const int s = (warp - 4) >> 2, r = tid & 127;
     const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);   // this warp's 32 TMEM lanes
     const uint32_t t_s = lanes + s * C::S_COL, t_o = lanes + C::O_COL + s * C::O_STEP;
     float2* xchg = reinterpret_cast<float2*>(smem + C::X_OFF);
-    unsigned item = 0, steps_done = 0, seq0 = 0;
+    unsigned item = 0, turn = 0, seq0 = 0;
     struct Shared {   // a block that other CTAs have a part of
       int b, kh, blk, first, parts;
     } cut[2];
@@ -533,160 +681,155 @@ __global__ void __launch_bounds__(kThreads, 1)
     long long unit = st.u0;
     for (Walk w(a, st); w.more(); w.next(), ++item) {
       const bool dual = w.dual();
-      const int n = w.tiles, rows = w.rows(), row = dual ? s * 128 + r : r;
-      const bool mine = row < rows;                              // this thread's row exists
-      const bool active = (row & ~31) < rows;                    // .. one of the warp's does
-      const int tok = min(w.blk * kBlock + row, w.r.rows - 1) / a.G;
+      const int n = w.tiles, row = dual ? s * a.rt + r : r, here = min(a.rt, w.rows() - (row - r));
+      const bool mine = r < here;                                // this thread's row exists
+      const bool active = (r & ~31) < here;                      // .. one of the warp's does
+      const int tok = min(w.blk * 2 * a.rt + row, w.r.rows - 1) / a.G;
       const int seen_all = min(w.r.ctx, a.cap);                  // keys before this one are seen by every row
       float m = -INFINITY, l = 0.f;
-      bool first_step = true;
-      for (int i = dual ? 0 : s; i < n; i += dual ? 1 : 2) {
-        ok = warp_wait(ok, s_full + s, steps_done & 1, err);
-        ++steps_done;
-        tc_fence_after();
-        const int key0 = (w.tile0 + i) * kTile;
+      const int tiles = dual ? n : (n - s + 1) / 2, ahead = k_lead(dual);
+#pragma unroll 1
+      for (int k = 0; k < tiles; ++k) {
+        const int i = dual ? k : 2 * k + s, key0 = (w.tile0 + i) * kTile;
         const bool masked = key0 + kTile > seen_all;
-        if (active && ok) {
+        uint32_t see[4];
+        if (__builtin_expect(masked && active, 0)) seen_keys(a, w.r, tok, key0, see);   // (under the product)
+        ok = warp_wait(ok, s_full + s, (turn + k) & 1, err);
+        tc_fence_after();
+        if (r == 0 && ok) mbar_arrive(empty + (seq0 + seq_k(ahead, i)) % C::STAGES);
+        if (active) {
           uint32_t x[128];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) tmem_ld_32x32b_x32(t_s + 32 * k, *reinterpret_cast<uint32_t(*)[32]>(x + 32 * k));
-          tmem_ld_wait();
-          if (masked) {
+          for (int j = 0; j < 4; ++j) tmem_ld_32x32b_x32(t_s + 32 * j, *reinterpret_cast<uint32_t(*)[32]>(x + 32 * j));
+          tmem_ld_wait128(x);
+          if (__builtin_expect(masked, 0)) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t see = mine ? seen_word(a, w.r, tok, key0 + 32 * k) : 0u;
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (!(see >> j & 1)) x[32 * k + j] = 0xff800000u;   // -infinity
-            }
+              for (int e = 0; e < 32; ++e)
+                if (!(see[j] >> e & 1)) x[32 * j + e] = 0xff800000u;   // -infinity
           }
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int j = 0; j < 128; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(x[j]));
+          for (int j = 0; j < 64; ++j)
+            mx[j & 3] = fmaxf(mx[j & 3], fmaxf(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])));
           const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.c);
           const bool rise = mine && (m == -INFINITY ? m_new > m : m_new > m + kSlack);
-          if (__any_sync(0xffffffffu, rise)) {
+          if (__builtin_expect(__any_sync(0xffffffffu, rise), 0)) {
             const float f = !rise ? 1.f : m == -INFINITY ? 0.f : exp2_fast(m - m_new);
-            if (!first_step) {
+            if (k > 0) {   // (O is at rest: S is complete, which was issued after the P V before)
 #pragma unroll 1
-              for (int k = 0; k < HD; k += 16) {
+              for (int c = 0; c < HD; c += 16) {
                 uint32_t o[16];
-                tmem_ld_32x32b_x16(t_o + k, o);
+                tmem_ld_32x32b_x16(t_o + c, o);
                 tmem_ld_wait();
-                float y[16];
+                float z[16];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) y[j] = __uint_as_float(o[j]) * f;
-                tmem_st_32x32b_x16(t_o + k, y);
+                for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(o[j]) * f;
+                tmem_st_32x32b_x16(t_o + c, z);
               }
             }
             l *= f;
             if (rise) m = m_new;
           }
-          const float base = m == -INFINITY ? 0.f : m;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          const float base = m == -INFINITY ? 0.f : -m;
+          const float2 c2 = make_float2(a.c, a.c), b2 = make_float2(base, base);
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            uint32_t p[32];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const float y0 = exp2_fast(fmaf(__uint_as_float(x[64 * h + 2 * j]), a.c, -base));
-              const float y1 = exp2_fast(fmaf(__uint_as_float(x[64 * h + 2 * j + 1]), a.c, -base));
-              sum[j & 3] += y0 + y1;
-              p[j] = pack2(y0, y1, a.v_f16);
+            for (int j = 32 * h; j < 32 * h + 32; ++j) {
+              float2 z = fma2(make_float2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), c2, b2);
+              z.x = exp2_fast(z.x), z.y = exp2_fast(z.y);
+              sum[j & 1] = add2(sum[j & 1], z);
+              x[j] = pack2(z.x, z.y, VF16);
             }
-            tmem_st_32x32b_x32(t_s + 32 * h, p);
+            tmem_st_32x32b_x32(t_s + 32 * h, x + 32 * h);
+            if (h == 0 && !masked) {   // (masked: once the tile's V is seen to, below)
+              tmem_st_wait();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(p_ready + 2 * s);
+            }
+            // (the second half's exponentials stay behind the first half's store)
+            if (h == 0) hold64(x + 64);
           }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          sum[0] = add2(sum[0], sum[1]);
+          l += sum[0].x + sum[0].y;
           tmem_st_wait();
         }
-        first_step = false;
-        if (masked) {
+        if (__builtin_expect(masked, 0)) {
           // V rows that some row of the block does not see: a NaN or infinity there would reach it as 0 x NaN.  They
           // become 0 in the tile (every one of them), and the rows that do see one get it back at the end.
-          const unsigned seq = seq0 + seq_v(dual, i, n), slot = seq % C::STAGES;
-          ok = warp_wait(ok, full + slot, seq / C::STAGES & 1, err);
-          const int first = max(0, seen_all - key0), last = w.keys - key0;
-          constexpr int RC = C::SW / 16;
-          if (ok)
-            for (int k = r; k < (kTile - first) * RC * C::PANELS; k += 128) {
-              const int panel = k / ((kTile - first) * RC), at = k % ((kTile - first) * RC);
-              uint4* p = reinterpret_cast<uint4*>(smem + slot * C::TILE + panel * C::PANEL + first * C::SW) + at;
-              const uint4 v = *p;
-              uint4 c;
-              const bool f0 = finite16(v.x, a.v_f16, c.x), f1 = finite16(v.y, a.v_f16, c.y);
-              const bool f2 = finite16(v.z, a.v_f16, c.z), f3 = finite16(v.w, a.v_f16, c.w);
-              if (!(f0 && f1 && f2 && f3)) {
-                if (first + at / RC < last) {
-                  *odd_v = 1;
-                  __threadfence_block();
-                }
-                *p = c;
-              }
-            }
-          fence_proxy_async_shared();
+          const unsigned seq = seq0 + seq_v(ahead, i, n), slot = seq % C::STAGES;
+          ok = warp_wait(ok, full + slot, seq / C::STAGES & 1, err);   // (the place's copy before was seen with K's)
+          clean_v<HD>(smem + slot * C::TILE, r, max(0, seen_all - key0), w.keys - key0, VF16, odd_v);
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_ready + s);
+        if (lane == 0) {
+          if (masked || !active) mbar_arrive(p_ready + 2 * s);
+          mbar_arrive(p_ready + 2 * s + 1);
+        }
       }
+      turn += tiles;
       // ---- the block's (or this part's) result ----
-      ok = warp_wait(ok, o_done, item & 1, err);
-      tc_fence_after();
-      float f0 = 1.f, f1 = 0.f, m_all = m, l_all = l;   // weights of the own rows' O, or of both streams' O
+      float f0 = 1.f, f1 = 0.f, m_all = m, l_all = l;   // weights of the own stream's O, or of both streams' O
       if (!dual) {
         xchg[s * 128 + r] = make_float2(m, l);
-        named_bar_sync(1, 256);
+        named_bar_sync(1, kStreamThreads);
         const float2 e0 = xchg[r], e1 = xchg[128 + r];
-        named_bar_sync(1, 256);
+        named_bar_sync(1, kStreamThreads);
         m_all = fmaxf(e0.x, e1.x);
         f0 = e0.x == -INFINITY ? e0.y : exp2_fast(e0.x - m_all);   // (nothing seen: 0, or a NaN)
         f1 = e1.x == -INFINITY ? e1.y : exp2_fast(e1.x - m_all);
         l_all = (e0.x == -INFINITY ? e0.y : f0 * e0.y) + (e1.x == -INFINITY ? e1.y : f1 * e1.y);
       }
+      ok = warp_wait(ok, o_done, item & 1, err);
+      tc_fence_after();
       const bool whole = w.tile0 == 0 && n == w.all;
       const int slot = w.tile0 > 0 ? 0 : 1;
       float* part = part_of<HD>(a, blockIdx.x, slot);
       const float inv = whole ? (l_all == 0.f ? 0.f : 1.f / l_all) : 1.f;
-      const int rg = w.blk * kBlock + row, t = w.r.t0 + tok, head = w.kh * a.G + (mine ? rg % a.G : 0);
-      const int c0 = dual || s == 0 ? 0 : HD / 2, c1 = dual || s == 1 ? HD : HD / 2;
+      const int rg = w.blk * 2 * a.rt + row, t = w.r.t0 + tok, head = w.kh * a.G + (mine ? rg % a.G : 0);
+      const int width = dual ? HD : HD / 2, c0 = dual ? 0 : s * width;   // this thread's columns
       if (active && ok) {
         const uint32_t o0 = lanes + C::O_COL + (dual ? s * C::O_STEP : 0), o1 = lanes + C::O_COL + C::O_STEP;
-#pragma unroll 1
-        for (int c = c0; c < c1; c += 16) {
+        uint16_t* out = a.out + (long long)t * a.out_stride + (long long)head * HD;
+        float* prow = whole ? nullptr : part + row * HD;
+        const float g0 = f0 * inv, g1 = f1 * inv;
+#pragma unroll 2
+        for (int c = c0; c < c0 + width; c += 16) {
           uint32_t y0[16], y1[16];
-          float y[16];
           tmem_ld_32x32b_x16(o0 + c, y0);
           if (!dual) tmem_ld_32x32b_x16(o1 + c, y1);
-          tmem_ld_wait();
+          tmem_ld_wait16(y0, y1);
+          float y[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            y[j] = f0 == 0.f ? 0.f : __uint_as_float(y0[j]) * f0;   // (a stream without tiles leaves its O as it was)
-            if (!dual && f1 != 0.f) y[j] += __uint_as_float(y1[j]) * f1;
+            y[j] = f0 == 0.f ? 0.f : __uint_as_float(y0[j]) * g0;   // (a stream without tiles leaves its O as it was)
+            if (!dual && f1 != 0.f) y[j] += __uint_as_float(y1[j]) * g1;
           }
-          if (mine && *odd_v)
-            for (int p = max(w.tile0 * kTile, seen_all); p < min(w.keys, (w.tile0 + n) * kTile); ++p) {
-              if (!(seen_word(a, w.r, tok, p) & 1)) continue;
-              const int id = a.table[(long long)w.b * a.width + p / a.page];
-              const uint16_t* v = a.v + id * a.vs[0] + (p % a.page) * a.vs[1] + w.kh * a.vs[2] + c;
-              for (int j = 0; j < 16; ++j) {
-                uint32_t clean;
-                if (!finite16(v[j], a.v_f16, clean)) y[j] += unpack2(v[j], a.v_f16).x;
-              }
-            }
           if (!mine) continue;
           if (whole) {
-            uint4* d = reinterpret_cast<uint4*>(a.out + (long long)t * a.out_stride + (long long)head * HD + c);
+            uint32_t u[8];
 #pragma unroll
-            for (int j = 0; j < 16; j += 8)
-              d[j / 8] = make_uint4(pack2(y[j] * inv, y[j + 1] * inv, a.k_f16), pack2(y[j + 2] * inv, y[j + 3] * inv, a.k_f16),
-                                    pack2(y[j + 4] * inv, y[j + 5] * inv, a.k_f16), pack2(y[j + 6] * inv, y[j + 7] * inv, a.k_f16));
+            for (int j = 0; j < 8; ++j) u[j] = KF16 ? pack2(y[2 * j], y[2 * j + 1], true) : pack2(y[2 * j], y[2 * j + 1], false);
+            if (a.out32) {
+              st_global_32(out + c, u);
+            } else {
+              reinterpret_cast<uint4*>(out + c)[0] = make_uint4(u[0], u[1], u[2], u[3]);
+              reinterpret_cast<uint4*>(out + c)[1] = make_uint4(u[4], u[5], u[6], u[7]);
+            }
           } else {
-            float4* d = reinterpret_cast<float4*>(part + row * HD + c);
-#pragma unroll
-            for (int j = 0; j < 16; j += 4) d[j / 4] = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
+            st_global_32(prow + c, reinterpret_cast<const uint32_t(&)[8]>(y[0]));
+            st_global_32(prow + c + 8, reinterpret_cast<const uint32_t(&)[8]>(y[8]));
           }
         }
-        if (mine && (dual || s == 0)) {
+        if (mine && *odd_v)
+          add_odd_v<HD>(a, w.b, w.kh, tok, max(w.tile0 * kTile, seen_all), min(w.keys, (w.tile0 + n) * kTile), c0, c0 + width, out,
+                        prow);
+        if (mine && c0 == 0) {
           if (!whole) reinterpret_cast<float2*>(part + kBlock * HD)[row] = make_float2(m_all, l_all);
           else if (a.lse)
             a.lse[(long long)t * a.H + head] = l_all == 0.f ? -INFINITY : (m_all + log2f(l_all)) * 0.6931471805599453f;
@@ -712,9 +855,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Shared x = cut[k];
       if (ok) ok = wait_count(a.arrived + x.first, 2 * x.parts, err);
       ok = named_bar_and(2 + s, 128, ok);
-      if (ok) merge_share<HD>(a, request(a, x.b), x.kh, x.blk, x.first, x.parts, blockIdx.x - x.first, s * 128 + r);
+      if (ok)
+        merge_share<HD>(a, request(a, x.b), x.kh, x.blk, x.first, x.parts, blockIdx.x - x.first, tid - 128);
       named_bar_sync(2 + s, 128);
-      if (r == 0 && ok && atomicAdd(a.done + x.first, 1) == 2 * x.parts - 1) {   // the last share: counters back to zero
+      if (r == 0 && ok && atomicAdd(a.done + x.first, 1) == 2 * x.parts - 1) {   // the last share: back to zero
         a.arrived[x.first] = 0;
         a.done[x.first] = 0;
       }
@@ -727,7 +871,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   tc_fence_after();
-  if (warp == 2) {
+  if (warp == 3) {
     tmem_relinquish();
     tmem_dealloc(tmem, 512);
   }
@@ -745,27 +889,35 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-// [page][token][head][dimension] with any strides: boxes of up to 64 dimensions of the tokens of a page (or half of one).
-atspeed_status page_map(CUtensorMap* m, const void* base, int type, const atspeed_kv_pages& c, const int64_t* stride) {
+// A map of four dimensions, of 16-bit values, in boxes of up to 64 of the first.  Strides in elements.
+atspeed_status map4(CUtensorMap* m, const void* base, int type, const int (&n)[4], const int64_t (&stride)[3],
+                    const int (&box)[3]) {
   auto fn = encode_fn();
   if (!fn) return ATSPEED_E_CUDA;
-  const int w = c.head_dim < 64 ? c.head_dim : 64, rows = c.page_size < kTile ? c.page_size : kTile;
-  const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.n_kv_heads, (cuuint64_t)c.n_pages};
+  const int w = n[0] < 64 ? n[0] : 64;
+  cuuint64_t dims[4], strides[3];
+  cuuint32_t boxes[4] = {(cuuint32_t)w, (cuuint32_t)box[0], (cuuint32_t)box[1], (cuuint32_t)box[2]}, es[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 4; ++i) dims[i] = (cuuint64_t)n[i];
   // (the stride of a dimension of one entry is never used; the encoder wants a valid one)
-  const auto bytes = [&](int i, int n) { return (cuuint64_t)(n == 1 && stride[i] == 0 ? c.head_dim : stride[i]) * 2; };
-  const cuuint64_t strides[3] = {bytes(1, c.page_size), bytes(2, c.n_kv_heads), bytes(0, c.n_pages)};
-  const cuuint32_t box[4] = {(cuuint32_t)w, (cuuint32_t)rows, 1, 1}, es[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 3; ++i) strides[i] = (cuuint64_t)(n[i + 1] == 1 && stride[i] == 0 ? n[0] : stride[i]) * 2;
   const CUresult r = fn(m, type == ATSPEED_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
-                        const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        w * 2 == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        const_cast<void*>(base), dims, strides, boxes, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        w == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? ATSPEED_OK : ATSPEED_E_ARG;
 }
+// [page][token][head][dimension] of a cache: boxes of the tokens of a page, or of half a page
+atspeed_status page_map(CUtensorMap* m, const void* base, int type, const atspeed_kv_pages& c, const int64_t* stride) {
+  return map4(m, base, type, {c.head_dim, c.page_size, c.n_kv_heads, c.n_pages}, {stride[1], stride[2], stride[0]},
+              {c.page_size < kTile ? c.page_size : kTile, 1, 1});
+}
 
-template <int HD>
-atspeed_status launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeAttnArgs& a, int grid, cudaStream_t st) {
+template <int HD, bool KF16, bool VF16>
+atspeed_status launch(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const TreeAttnArgs& a, int grid,
+                      cudaStream_t st) {
+  const auto kernel = tree_attention_kernel<HD, KF16, VF16>;
   static std::atomic<unsigned long long> done{0};
-  if (smem_attr_once(done, tree_attention_kernel<HD>, Cfg<HD>::SMEM) != cudaSuccess) return ATSPEED_E_CUDA;
+  if (smem_attr_once(done, kernel, Cfg<HD>::SMEM) != cudaSuccess) return ATSPEED_E_CUDA;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeCooperative;
   at[0].val.cooperative = 1;
@@ -776,7 +928,13 @@ atspeed_status launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeAt
   cfg.stream = st;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, tree_attention_kernel<HD>, mk, mv, a) == cudaSuccess ? ATSPEED_OK : ATSPEED_E_CUDA;
+  return cudaLaunchKernelEx(&cfg, kernel, mq, mk, mv, a) == cudaSuccess ? ATSPEED_OK : ATSPEED_E_CUDA;
+}
+template <int HD>
+atspeed_status launch(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const TreeAttnArgs& a, int grid,
+                      cudaStream_t st) {
+  if (a.k_f16) return launch<HD, true, true>(mq, mk, mv, a, grid, st);
+  return a.v_f16 ? launch<HD, false, true>(mq, mk, mv, a, grid, st) : launch<HD, false, false>(mq, mk, mv, a, grid, st);
 }
 
 int sm_count() {
@@ -823,29 +981,32 @@ atspeed_status atspeed_op_tree_attention(atspeed_stream stream, const atspeed_kv
   if (q_stride < (int64_t)n_heads * hd || out_stride < (int64_t)n_heads * hd || q_stride % 8 || out_stride % 8 ||
       !aligned16(d_q) || !aligned16(d_out) || (reinterpret_cast<uintptr_t>(d_ws) & 255))
     return ATSPEED_E_ARG;
-  CUtensorMap mk, mv;
-  atspeed_status st = page_map(&mk, c.d_k, c.k_type, c, c.k_stride);
+  const int G = n_heads / c.n_kv_heads;
+  CUtensorMap mq, mk, mv;
+  atspeed_status st = map4(&mq, d_q, c.k_type, {hd, G, c.n_kv_heads, T}, {hd, (int64_t)G * hd, q_stride}, {G, 1, 128 / G});
+  if (st == ATSPEED_OK) st = page_map(&mk, c.d_k, c.k_type, c, c.k_stride);
   if (st == ATSPEED_OK) st = page_map(&mv, c.d_v, c.v_type, c, c.v_stride);
   if (st != ATSPEED_OK) return st;
   TreeAttnArgs a = {};
-  a.q = static_cast<const uint16_t*>(d_q), a.v = static_cast<const uint16_t*>(c.d_v);
+  a.v = static_cast<const uint16_t*>(c.d_v);
   for (int i = 0; i < 3; ++i) a.vs[i] = c.v_stride[i];
-  a.q_stride = q_stride, a.out_stride = out_stride;
-  a.H = n_heads, a.Hkv = c.n_kv_heads, a.G = n_heads / c.n_kv_heads, a.n = n_req, a.T = T, a.page = ps;
+  a.out_stride = out_stride, a.rt = 128 / G * G;
+  a.H = n_heads, a.Hkv = c.n_kv_heads, a.G = G, a.n = n_req, a.T = T, a.page_log = ps == 16 ? 4 : ps == 32 ? 5 : ps == 64 ? 6 : ps == 128 ? 7 : 8, a.page = ps, a.n_pages = c.n_pages;
   a.width = table_width, a.words = mask_words, a.cu_q = d_cu_q, a.ctx = d_ctx_len, a.table = d_block_table, a.mask = d_mask;
   const long long cap = (long long)table_width * ps;
   a.cap = (int)(cap < (1LL << 30) ? cap : 1LL << 30);
   a.c = scale * 1.4426950408889634f;
   a.out = static_cast<uint16_t*>(d_out), a.lse = d_lse;
   a.k_f16 = c.k_type == ATSPEED_F16, a.v_f16 = c.v_type == ATSPEED_F16;
+  a.out32 = ((reinterpret_cast<uintptr_t>(d_out) | (uintptr_t)out_stride * 2) & 31) == 0;
   a.arrived = static_cast<int*>(d_ws), a.done = a.arrived + kMaxCtas;
   a.parts = static_cast<unsigned char*>(d_ws) + kCounterBytes;
   a.err = tree_attn_err_word();
   const int grid = sm_count();
   if (!a.err || grid <= 0 || grid > kMaxCtas) return ATSPEED_E_CUDA;
-  if (hd == 32) return launch<32>(mk, mv, a, grid, (cudaStream_t)stream);
-  if (hd == 64) return launch<64>(mk, mv, a, grid, (cudaStream_t)stream);
-  return launch<128>(mk, mv, a, grid, (cudaStream_t)stream);
+  if (hd == 32) return launch<32>(mq, mk, mv, a, grid, (cudaStream_t)stream);
+  if (hd == 64) return launch<64>(mq, mk, mv, a, grid, (cudaStream_t)stream);
+  return launch<128>(mq, mk, mv, a, grid, (cudaStream_t)stream);
 }
 
 }  // extern "C"

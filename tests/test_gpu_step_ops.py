@@ -312,6 +312,15 @@ def test_tree_attention_lengths(ats, q_len, ctx, tree):
     _attention_case(ats, q_len, ctx, 4, 2, 64, 16, "bf16", "token", tree, seed=len(q_len) + q_len[0])
 
 
+@pytest.mark.parametrize("q_len,ctx,H,hd,page", [([1] * 12, [11000 + 37 * i for i in range(12)], 4, 128, 64),
+                                                  ([1] * 19, [9000 - 100 * i for i in range(19)], 8, 64, 16),
+                                                  ([150] * 12, [4000 + 64 * i for i in range(12)], 4, 128, 32)])
+def test_tree_attention_long_ranges(ats, q_len, ctx, H, hd, page):
+    """Some ten key tiles in a row for every CTA, under the memory traffic of all of them: the copies' ring goes round many
+    times, on few rows (alternate tiles to two streams) and on many (every tile to both)."""
+    _attention_case(ats, q_len, ctx, H, H, hd, page, "bf16", tree=_drafted, poison=False, seed=hd + page)
+
+
 @pytest.mark.parametrize("G", [1, 2, 3, 5, 16, 127, 128])
 def test_tree_attention_groups(ats, G):
     _attention_case(ats, [3, 1, 9], [200, 77, 513], 2 * G if G < 100 else G, 2 if G < 100 else 1, 32, 16, "f16", tree=_drafted, seed=G)
