@@ -3,30 +3,35 @@
 //   x <- seen ? (x > 0 ? x / rep : x * rep) : x;  x <- x - freq c - pres [c > 0] + bias(v);  forbidden: -inf;  x <- x / temp
 // Bound: HBM (each logit read and written once).
 //
-// A warp owns 1024 tokens of the vocabulary and one word of shared memory for each (its count and whether the prompt has
-// it).  A CTA counts a request's history into its warps' words once and walks several rows of that request; a row's path
-// is added by each warp to its own words and taken away after, so that rows cost no barrier, and the history is scanned
-// once per CTA, not once per row.  Rows are read and written by 16 bytes at addresses that are multiples of 16, whatever the
-// row's start is: a warp's 1024 tokens begin up to 7 tokens early, and the words of 16 tokens at a border are held by both.
+// The penalties and biases touch some hundred tokens of a vocabulary of tens of thousands.  So a warp streams its 512 tokens of
+// a row (temperature and the grammar's bits: a few instructions a logit) and then does the touched ones among them again,
+// each from its own logit: they stand in a list, made once per request for several of its rows, with the counts in a table
+// of one word a token.  A row's path in its tree joins the counts and the list for that row.  The table is the warp's own, so
+// that a row takes no barrier of the CTA (one a row: 3840 rows of 33024 took 270 us); counts looked up for every logit cost
+// 160 instructions per 128 logits (403 us).
+// Rows are read and written at multiples of 16 bytes whatever their start: a warp's tokens of a row begin up to 7 early, and the
+// words of 16 tokens at a border are held by both warps.
 #include <algorithm>
 
 #include "common.cuh"
-#include "gemm.cuh"
 #include "step_ops.cuh"
 
 namespace atspeed {
 namespace {
 
-constexpr int kWarps = 8;               // of a CTA, at most
-constexpr int kSub = 1024;              // tokens of a warp
-constexpr int kRegion = kSub + 16;      // .. and its words
-constexpr uint32_t kPrompt = 1u << 31;  // the token occurs in the prompt; below it the count in the output
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kSub = 512;               // tokens of a warp
+constexpr int kRegion = kSub + 16;      // .. and its words: from 8 tokens before the first
+constexpr int kChunk = kSub * kWarps;   // tokens of a CTA
+constexpr uint32_t kPrompt = 1u << 31, kListed = 1u << 30;   // flags of a token's word; below them its count in the output
 
 struct RulesArgs {
   const void* in;
   void* out;
   long long ld_in, ld_out;
-  int R, V, n, rows, words, subs;   // rows: consecutive rows a CTA takes; subs: warps of a CTA
+  int R, V, n, rows, words;   // rows: consecutive rows a CTA takes
+  unsigned groups, chunks;    // of rows, of the vocabulary
+  bool in_place, by_row;      // by_row: neighbouring CTAs take other rows, not other pieces
   const int* req;
   const uint32_t* mask;
   const int* state;
@@ -41,10 +46,6 @@ struct Logit {   // values of one 16-byte access
     const uint32_t w = (&v.x)[TYPE == ATSPEED_F32 ? j : j / 2];
     if constexpr (TYPE == ATSPEED_F32) return __uint_as_float(w);
     else return j & 1 ? unpack2(w, TYPE == ATSPEED_F16).y : unpack2(w, TYPE == ATSPEED_F16).x;
-  }
-  static __device__ __forceinline__ uint32_t load1(const char* p) {   // one value's bits
-    if constexpr (TYPE == ATSPEED_F32) return *reinterpret_cast<const uint32_t*>(p);
-    else return *reinterpret_cast<const uint16_t*>(p);
   }
   static __device__ __forceinline__ void store1(char* p, float x) {
     if constexpr (TYPE == ATSPEED_F32) *reinterpret_cast<float*>(p) = x;
@@ -62,196 +63,232 @@ struct Factors {
 __device__ __forceinline__ bool usual(float x) { return x > 0x1p-100f && x < 0x1p100f; }
 
 template <int IN, int OUT>
-__global__ void __launch_bounds__(32 * kWarps) adjust_logits_kernel(const __grid_constant__ RulesArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) adjust_logits_kernel(const __grid_constant__ RulesArgs a) {
   using I = Logit<IN>;
   using O = Logit<OUT>;
   constexpr int N = I::N, U = kSub / (32 * N);
   extern __shared__ __align__(16) uint32_t sm[];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
+  __shared__ int s_n[kWarps];   // tokens in a warp's list
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool biased = a.r.d_bias_off != nullptr;
-  uint32_t* cnt = sm + warp * kRegion;                  // this warp's words
-  uint32_t* all_bias = sm + a.subs * kRegion;           // index + 1 of a token's bias entry (with biases)
-  uint32_t* bias = all_bias + warp * kRegion;
-  const int v0 = blockIdx.x * a.subs * kSub, s0 = v0 + warp * kSub;
-  const int r0 = blockIdx.y * a.rows, r1 = min(a.R, r0 + a.rows);
-  int held = -2, held_shift = 0;   // the request whose counts the words hold, and the tokens they begin early
-  Factors f = {1.f, 1.f, 0.f, 0.f, 1.f, 1.f, false};
-  for (int row = r0; row < r1; ++row) {
-    const char* in = static_cast<const char*>(a.in) + row * a.ld_in * I::SIZE;
-    char* out = static_cast<char*>(a.out) + row * a.ld_out * O::SIZE;
-    // the warp's first token in this row: the last one not past s0 whose address is a multiple of 16
-    const int shift = (int)((reinterpret_cast<uintptr_t>(in) / I::SIZE + s0) & (N - 1));
-    const int t0 = s0 - shift;
-    uint4 raw[U];
+  // a warp's words: counts, its list (16 bits an entry), with biases the number + 1 of a token's entry, in place the listed
+  // tokens' logits
+  const int words = kRegion + kRegion / 2 + (biased ? kRegion : 0) + (a.in_place ? kRegion : 0);
+  uint32_t* cnt = sm + warp * words;
+  uint16_t* list = reinterpret_cast<uint16_t*>(cnt + kRegion);
+  uint32_t* bias = cnt + kRegion + kRegion / 2;
+  uint32_t* raw = bias + (biased ? kRegion : 0);
+  const int v0 = (int)(a.by_row ? blockIdx.x / a.groups : blockIdx.x % a.chunks) * kChunk, s0 = v0 + warp * kSub;
+  const int r0 = (int)(a.by_row ? blockIdx.x % a.groups : blockIdx.x / a.chunks) * a.rows, r1 = min(a.R, r0 + a.rows);
+  const auto in_row = [&](int row) { return static_cast<const char*>(a.in) + (long long)row * a.ld_in * I::SIZE; };
+  // the warp's first token in a row: the last one not past s0 whose address is a multiple of 16
+  const auto begin = [&](const char* in) { return s0 - (int)((reinterpret_cast<uintptr_t>(in) / I::SIZE + s0) & (N - 1)); };
+  const auto one = [&](const char* in, int t) {   // a logit's bits
+    if constexpr (I::SIZE == 4) return reinterpret_cast<const uint32_t*>(in)[t];
+    else return (uint32_t)reinterpret_cast<const uint16_t*>(in)[t];
+  };
+  const auto value = [](uint32_t bits) {
+    if constexpr (IN == ATSPEED_F32) return __uint_as_float(bits);
+    else return unpack2(bits, IN == ATSPEED_F16).x;
+  };
+  uint4 x[U];
+  const auto load = [&](int row) {
+    const char* in = in_row(row);
+    const int w0 = begin(in), t0 = w0 + lane * N;
+    if (w0 >= 0 && w0 + kSub <= a.V) {
+      const uint4* v = reinterpret_cast<const uint4*>(in + (long long)t0 * I::SIZE);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int t = t0 + (lane + 32 * u) * N;
-      raw[u] = make_uint4(0, 0, 0, 0);
-      if (t >= 0 && t + N <= a.V) {
-        raw[u] = __ldcs(reinterpret_cast<const uint4*>(in + (long long)t * I::SIZE));
-      } else if (t + N > 0 && t < a.V) {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (t + j >= 0 && t + j < a.V) {
-            const uint32_t b = I::load1(in + (long long)(t + j) * I::SIZE);
-            (&raw[u].x)[j * I::SIZE / 4] |= I::SIZE == 4 ? b : b << (j % 2 * 16);
-          }
-      }
+      for (int u = 0; u < U; ++u) x[u] = __ldcs(v + 32 * u);
     }
-    int b = a.req[row];
-    if (b < 0 || b >= a.n) b = -1;
+  };
+  const auto request_of = [&](int row) {
+    const int b = row < r1 ? __ldg(a.req + row) : -1;
+    return b < a.n ? b : -1;
+  };
+  const auto state_of = [&](int row) { return a.state && a.r.d_grammar && row < r1 ? __ldg(a.state + row) : -1; };
+  load(r0);
+  for (int i = lane; i < kRegion / 4; i += 32) reinterpret_cast<uint4*>(cnt)[i] = make_uint4(0, 0, 0, 0);
+  if (biased)
+    for (int i = lane; i < kRegion / 4; i += 32) reinterpret_cast<uint4*>(bias)[i] = make_uint4(0, 0, 0, 0);
+  if (lane == 0) s_n[warp] = 0;
+  // the request whose counts the table holds, the tokens it lists, its first bias entry, its tree's first token and length
+  int held = -2, base = 0, k0 = 0, q0 = 0, q_len = 0;
+  Factors f = {1.f, 1.f, 0.f, 0.f, 1.f, 1.f, false};
+  // (a row's request and state are read a row ahead: what they lead to takes long enough)
+  const auto bits_of = [&](int row) {   // a lane's word of a row's mask
+    return a.mask && row < r1 && lane < a.words ? __ldg(a.mask + (long long)row * a.words + lane) : 0u;
+  };
+  int b = request_of(r0), st = state_of(r0);
+  uint32_t mask_bits = bits_of(r0);
+  for (int row = r0; row < r1; ++row) {
+    const int b_next = request_of(row + 1), st_next = state_of(row + 1);
+    const uint32_t bits_next = bits_of(row + 1);
     if (b != held) {
-      // the words begin with this row's first token, so that its reads of them are aligned
       held = b;
-      held_shift = (int)((reinterpret_cast<uintptr_t>(in) / I::SIZE + v0) & (N - 1));
       f = {1.f, 1.f, 0.f, 0.f, 1.f, 1.f, false};
-      __syncthreads();
-      const uint4 zero = make_uint4(0, 0, 0, 0);
-      for (int i = tid; i < a.subs * kRegion / 4 * (biased ? 2 : 1); i += threads) reinterpret_cast<uint4*>(sm)[i] = zero;
-      int h0 = 0, h1 = 0, p = 0, k0 = 0, k1 = 0;
+      int h0 = 0, h1 = 0, p = 0, k1 = 0;
+      k0 = 0, q_len = 0;
       if (b >= 0) {
-        if (a.r.d_repetition) f.rep = a.r.d_repetition[b];
-        if (a.r.d_frequency) f.freq = a.r.d_frequency[b];
-        if (a.r.d_presence) f.pres = a.r.d_presence[b];
-        if (a.r.d_temperature) f.temp = a.r.d_temperature[b];
+        if (a.mask && a.r.d_tree_tok) q0 = __ldg(a.r.d_cu_q + b), q_len = __ldg(a.r.d_cu_q + b + 1) - q0;
+        if (a.r.d_hist) {
+          h0 = __ldg(a.r.d_hist_off + b), h1 = __ldg(a.r.d_hist_off + b + 1);
+          p = h0 + (a.r.d_prompt_len ? __ldg(a.r.d_prompt_len + b) : 0);
+        }
+        if (biased) k0 = __ldg(a.r.d_bias_off + b), k1 = __ldg(a.r.d_bias_off + b + 1);
+        if (a.r.d_repetition) f.rep = __ldg(a.r.d_repetition + b);
+        if (a.r.d_frequency) f.freq = __ldg(a.r.d_frequency + b);
+        if (a.r.d_presence) f.pres = __ldg(a.r.d_presence + b);
+        if (a.r.d_temperature) f.temp = __ldg(a.r.d_temperature + b);
         if (!(f.temp > 0.f)) f.temp = 1.f;
         f.rep_inv = 1.f / f.rep;
         f.temp_inv = 1.f / f.temp;
         f.divide = !usual(f.rep) || !usual(f.temp);
-        if (a.r.d_hist) {
-          h0 = a.r.d_hist_off[b], h1 = a.r.d_hist_off[b + 1];
-          p = h0 + (a.r.d_prompt_len ? a.r.d_prompt_len[b] : 0);
-        }
-        if (biased) k0 = a.r.d_bias_off[b], k1 = a.r.d_bias_off[b + 1];
       }
+      for (int e = lane; e < base; e += 32) {   // the words of the request before
+        const int i = list[e];
+        cnt[i] = 0;
+        if (biased) bias[i] = 0;
+      }
+      if (lane == 0) s_n[warp] = 0;
       __syncthreads();
-      // a token's word, and its second one if it lies at a border
+      // a token's words, with the warp's number, and the second ones if it lies at a border
       const auto each = [&](int v, auto&& go) {
-        if ((unsigned)v >= (unsigned)a.V) return;
-        const int rel = v - v0 + held_shift + 8;
-        if (rel < 0 || rel >= a.subs * kSub + 16) return;
+        const int rel = v - v0 + 8;
+        if ((unsigned)v >= (unsigned)a.V || (unsigned)rel >= (unsigned)(kChunk + 16)) return;
         const int w = rel / kSub, i = rel % kSub;
-        if (w < a.subs) go(w * kRegion + i);
-        if (w > 0 && i < 16) go((w - 1) * kRegion + kSub + i);
+        if (w < kWarps) go(w, i);
+        if (w > 0 && i < 16) go(w - 1, kSub + i);
+      };
+      const auto enlist = [&](int w, int i) {
+        uint32_t* c = sm + w * words;
+        if (!(atomicOr(c + i, kListed) & kListed)) reinterpret_cast<uint16_t*>(c + kRegion)[atomicAdd(&s_n[w], 1)] = (uint16_t)i;
       };
 #pragma unroll 4
-      for (int k = h0 + tid; k < h1; k += threads)
-        each(__ldg(a.r.d_hist + k), [&](int i) {
-          if (k < p) atomicOr(sm + i, kPrompt);
-          else atomicAdd(sm + i, 1u);
+      for (int k = h0 + tid; k < h1; k += kThreads)
+        each(__ldg(a.r.d_hist + k), [&](int w, int i) {
+          if (k < p) atomicOr(sm + w * words + i, kPrompt);
+          else atomicAdd(sm + w * words + i, 1u);
+          enlist(w, i);
         });
-      for (int k = k0 + tid; k < k1; k += threads)
-        each(a.r.d_bias_tok[k], [&](int i) { atomicMax(all_bias + i, (uint32_t)(k - k0) + 1u); });   // (the later entry)
+      for (int k = k0 + tid; k < k1; k += kThreads)
+        each(__ldg(a.r.d_bias_tok + k), [&](int w, int i) {   // (the later entry)
+          atomicMax(sm + w * words + kRegion + kRegion / 2 + i, (uint32_t)(k - k0) + 1u);
+          enlist(w, i);
+        });
       __syncthreads();
+      base = s_n[warp];
     }
-    const int first = 8 + held_shift - shift;   // word of token t0
-    const float* bias_val = biased && b >= 0 ? a.r.d_bias_val + a.r.d_bias_off[b] : nullptr;
-    const bool path = a.mask && b >= 0 && a.r.d_tree_tok;
-    // the row's path: `by` added to the words of its tokens among the warp's
-    const auto walk = [&](uint32_t by) {
-      const int q0 = __ldg(a.r.d_cu_q + b), len = __ldg(a.r.d_cu_q + b + 1) - q0;
-      for (int w = lane; w < a.words && 32 * w < len; w += 32) {
-        uint32_t bits = __ldg(a.mask + (long long)row * a.words + w);
+    const char* in = in_row(row);
+    char* out = static_cast<char*>(a.out) + (long long)row * a.ld_out * O::SIZE;
+    const int t0 = begin(in);
+    const uint32_t* allowed = st >= 0 && st < a.r.n_states ? a.r.d_grammar + st * a.r.grammar_stride : nullptr;
+    const auto forbidden = [&](int t) { return allowed && !(__ldg(allowed + (t >> 5)) >> (t & 31) & 1); };
+    // the row's path: its tokens among the warp's, counted and listed for this row
+    int listed = base;
+    const auto walk = [&](auto&& go) {
+      for (int w = lane; w < a.words && 32 * w < q_len; w += 32) {
+        uint32_t bits = w < 32 ? mask_bits : __ldg(a.mask + (long long)row * a.words + w);
         while (bits) {
           const int j = 32 * w + __ffs(bits) - 1;
           bits &= bits - 1;
-          if (j >= len) break;
-          const int v = __ldg(a.r.d_tree_tok + q0 + j), i = v - t0;
-          if (i >= 0 && i < kSub && v >= 0 && v < a.V) atomicAdd(cnt + first + i, by);
+          if (j >= q_len) break;
+          const int v = __ldg(a.r.d_tree_tok + q0 + j);
+          if (v >= max(t0, 0) && v < min(t0 + kSub, a.V)) go(v - s0 + 8);
         }
+      }
+    };
+    bool path = q_len > 0;
+    if (path) {
+      bool hit = false;
+      walk([&](int i) {
+        hit = true;
+        atomicAdd(cnt + i, 1u);
+        if (!(atomicOr(cnt + i, kListed) & kListed)) list[atomicAdd(&s_n[warp], 1)] = (uint16_t)i;
+      });
+      path = __any_sync(0xffffffffu, hit);
+      __syncwarp();
+      if (path) listed = *reinterpret_cast<volatile int*>(&s_n[warp]);
+    }
+    // the listed tokens' logits, before they are overwritten; a lane's first one stays in a register
+    const auto token = [&](int e) {   // a listed token, -1: not the warp's in this row
+      const int t = s0 - 8 + list[e];
+      return t >= t0 && t < t0 + kSub ? t : -1;
+    };
+    const int my_t = lane < listed ? token(lane) : -1;
+    uint32_t my_raw = 0;
+    bool my_forbidden = false;
+    if (my_t >= 0) {
+      my_raw = one(in, my_t);
+      my_forbidden = forbidden(my_t);
+    }
+    if (a.in_place) {
+      for (int e = 32 + lane; e < listed; e += 32) {
+        const int t = token(e);
+        if (t >= 0) raw[e] = one(in, t);
       }
       __syncwarp();
-    };
-    if (path) walk(1u);
-    const int s = a.state && a.r.d_grammar ? __ldg(a.state + row) : -1;
-    const uint32_t* allowed = s >= 0 && s < a.r.n_states ? a.r.d_grammar + s * a.r.grammar_stride : nullptr;
-    const bool straight = (first & 3) == 0;
-    const bool wide = (reinterpret_cast<uintptr_t>(out + (long long)t0 * O::SIZE) & 15) == 0;
+    }
+    // every logit by temperature and grammar
+    char* to = out + (long long)(t0 + lane * N) * O::SIZE;
+    const bool wide = ((reinterpret_cast<uintptr_t>(out) + (long long)t0 * O::SIZE) & 15) == 0;
+    if (t0 >= 0 && t0 + kSub <= a.V && wide && !f.divide) {
+      // (the bits of a vector begin at the same place of a word in all of the lane's vectors)
+      const int t = t0 + lane * N, sh = t & 31;
+      const uint32_t* g_at = allowed + (t >> 5);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = (lane + 32 * u) * N, t = t0 + i;
-      if (t + N <= 0 || t >= a.V) continue;
-      float x[N];
-      uint32_t w[N];
-      if (straight) {
+      for (int u = 0; u < U; ++u) {
+        float y[N];
 #pragma unroll
-        for (int j = 0; j < N; j += 4) {
-          const uint4 c = *reinterpret_cast<const uint4*>(cnt + first + i + j);
-          w[j] = c.x, w[j + 1] = c.y, w[j + 2] = c.z, w[j + 3] = c.w;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) w[j] = cnt[first + i + j];
-      }
-      uint32_t any = 0;
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        x[j] = I::at(raw[u], j);
-        any |= w[j];
-      }
-      if (any) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          if (!w[j]) continue;
-          const uint32_t c = w[j] & ~kPrompt;
-          x[j] = x[j] > 0.f ? (f.divide ? x[j] / f.rep : x[j] * f.rep_inv) : x[j] * f.rep;
-          if (c) x[j] = x[j] - f.freq * (float)c - f.pres;
-        }
-      }
-      if (bias_val) {
-        uint32_t e[N], any_bias = 0;
-        if (straight) {
-#pragma unroll
-          for (int j = 0; j < N; j += 4) {
-            const uint4 c = *reinterpret_cast<const uint4*>(bias + first + i + j);
-            e[j] = c.x, e[j + 1] = c.y, e[j + 2] = c.z, e[j + 3] = c.w;
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < N; ++j) e[j] = bias[first + i + j];
-        }
-#pragma unroll
-        for (int j = 0; j < N; ++j) any_bias |= e[j];
-        if (any_bias) {
+        for (int j = 0; j < N; ++j) y[j] = I::at(x[u], j) * f.temp_inv;
+        if (allowed) {
+          uint32_t g = __ldg(g_at + u * N) >> sh;
+          if (sh + N > 32) g |= __ldg(g_at + u * N + 1) << (32 - sh);
 #pragma unroll
           for (int j = 0; j < N; ++j)
-            if (e[j]) x[j] += __ldg(bias_val + e[j] - 1);
+            if (!(g >> j & 1)) y[j] = -INFINITY;
         }
-      }
-      if (f.divide) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) x[j] = x[j] / f.temp;
-      } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) x[j] *= f.temp_inv;
-      }
-      if (allowed) {
-        const int tw = max(t, 0), last = (a.V - 1) >> 5;
-        const uint32_t g = __funnelshift_r(__ldg(allowed + (tw >> 5)), __ldg(allowed + min((tw >> 5) + 1, last)), tw & 31);
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (!(g >> (t + j - tw & 31) & 1)) x[j] = -INFINITY;   // (a token before the row is not stored)
-      }
-      if (t >= 0 && t + N <= a.V && wide) {
         if constexpr (OUT == ATSPEED_F32) {
 #pragma unroll
           for (int j = 0; j < N; j += 4)
-            __stcs(reinterpret_cast<float4*>(out + ((long long)t + j) * 4), make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]));
+            *reinterpret_cast<float4*>(to + (u * 32 * N + j) * 4) = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
         } else {
           constexpr bool H = OUT == ATSPEED_F16;
-          *reinterpret_cast<uint4*>(out + (long long)t * O::SIZE) =
-              make_uint4(pack2(x[0], x[1], H), pack2(x[2], x[3], H), pack2(x[4], x[5], H), pack2(x[6], x[7], H));
+          *reinterpret_cast<uint4*>(to + u * 32 * N * 2) =
+              make_uint4(pack2(y[0], y[1], H), pack2(y[2], y[3], H), pack2(y[4], y[5], H), pack2(y[6], y[7], H));
         }
-      } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (t + j >= 0 && t + j < a.V) O::store1(out + (long long)(t + j) * O::SIZE, x[j]);
+      }
+    } else {   // a row's ends, an output out of line with its input, an unusual temperature
+      for (int t = max(t0, 0) + lane; t < min(t0 + kSub, a.V); t += 32) {
+        const float y = value(one(in, t));
+        O::store1(out + (long long)t * O::SIZE, forbidden(t) ? -INFINITY : f.divide ? y / f.temp : y * f.temp_inv);
       }
     }
-    if (path) {
-      __syncwarp();
-      walk(~0u);
+    if (row + 1 < r1) load(row + 1);
+    __syncwarp();
+    // the listed ones with all rules
+    const auto finish = [&](int e, int t, uint32_t logit, bool forbid) {
+      const int i = list[e];
+      const uint32_t w = cnt[i], c = w & (kListed - 1);
+      float y = value(logit);
+      if (c || w & kPrompt) y = y > 0.f ? (f.divide ? y / f.rep : y * f.rep_inv) : y * f.rep;
+      if (c) y = y - f.freq * (float)c - f.pres;
+      if (biased && bias[i]) y += __ldg(a.r.d_bias_val + k0 + bias[i] - 1);
+      y = f.divide ? y / f.temp : y * f.temp_inv;
+      O::store1(out + (long long)t * O::SIZE, forbid ? -INFINITY : y);
+    };
+    if (my_t >= 0) finish(lane, my_t, my_raw, my_forbidden);
+    for (int e = 32 + lane; e < listed; e += 32) {
+      const int t = token(e);
+      if (t >= 0) finish(e, t, a.in_place ? raw[e] : one(in, t), forbidden(t));
     }
+    __syncwarp();
+    if (path) {   // the path's tokens leave again
+      walk([&](int i) { atomicAdd(cnt + i, ~0u); });
+      for (int e = base + lane; e < listed; e += 32) atomicAnd(cnt + list[e], ~kListed);
+      if (lane == 0) s_n[warp] = base;
+      __syncwarp();
+    }
+    b = b_next, st = st_next, mask_bits = bits_next;
   }
 }
 
@@ -280,21 +317,22 @@ extern "C" atspeed_status atspeed_op_adjust_logits(atspeed_stream stream, const 
   a.in = d_logits, a.out = d_out, a.ld_in = ld_in, a.ld_out = ld_out;
   a.R = R, a.V = vocab, a.n = r.n_req, a.words = mask_words, a.req = d_req, a.mask = d_mask, a.state = d_state;
   a.r = r;
-  // Warps of 1024 tokens (7 more for rows that begin between 16-byte addresses), as evenly over CTAs as they go; rows a CTA:
-  // a request's history is counted once for all of them, as long as every SM keeps a few CTAs.
-  const int subs = (vocab + 7 + kSub - 1) / kSub, chunks = (subs + kWarps - 1) / kWarps;
-  a.subs = (subs + chunks - 1) / chunks;
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return ATSPEED_E_CUDA;
-  const long long room = 12LL * gemm_grid_size(dev);
-  a.rows = (int)std::min(16LL, std::max(1LL, (long long)R * chunks / room));
-  const long long groups = (R + a.rows - 1LL) / a.rows;
-  if (groups > 65535) return ATSPEED_E_SHAPE;
-  const int smem = a.subs * kRegion * 4 * (r.d_bias_off ? 2 : 1);
-  const dim3 grid(chunks, (unsigned)groups);
+  a.in_place = d_out == d_logits;
+  // Pieces of 4096 tokens (7 more for rows that begin between 16-byte addresses).  Rows a CTA: a request's list is made once for
+  // those that follow each other, and more CTAs than run at once even out their ends.  us for 1 / 2 / 4 / 8 / 16 rows: 3840 rows of
+  // 33024, 240 a request, 316 / 265 / 244 / 246 / 265; 509 rows of 100003, one a request, 144 / 144 / 156 / 179 / 179.
+  // Neighbouring CTAs take a row's pieces one after the other (3840 rows: 244, row after row 259), except where every row has
+  // a history of its own, whose long ones then spread (509 rows: 144 and 128).
+  a.chunks = (unsigned)((vocab + 7LL + kChunk - 1) / kChunk);
+  a.rows = std::min(4, std::max(1, R / std::max(1, r.n_req)));
+  a.groups = (unsigned)((R + a.rows - 1LL) / a.rows);
+  a.by_row = a.rows == 1;
+  if ((long long)a.chunks * a.groups > 0x7fffffffLL) return ATSPEED_E_SHAPE;
+  const unsigned grid = a.chunks * a.groups;
+  const int smem = kWarps * 2 * (kRegion * 3 + (r.d_bias_off ? kRegion * 2 : 0) + (a.in_place ? kRegion * 2 : 0));
   auto go = [&](auto kernel, std::atomic<unsigned long long>& done) {
-    if (smem_attr_once(done, kernel, kWarps * kRegion * 8) != cudaSuccess) return ATSPEED_E_CUDA;
-    kernel<<<grid, 32 * a.subs, smem, (cudaStream_t)stream>>>(a);
+    if (smem_attr_once(done, kernel, kWarps * kRegion * 14) != cudaSuccess) return ATSPEED_E_CUDA;
+    kernel<<<grid, kThreads, smem, (cudaStream_t)stream>>>(a);
     return launch_status();
   };
   static std::atomic<unsigned long long> done[5];

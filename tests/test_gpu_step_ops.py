@@ -518,7 +518,7 @@ def _logits_case(ats, V, q_len, hist_max, inp, out_dtype, seed, leave=(), tree=T
     n, R = len(q_len), int(np.sum(q_len))
     hist_len = rng.integers(0, hist_max + 1, size=n)
     d = dict(n_req=n, hist_off=np.concatenate([[0], np.cumsum(hist_len)]).astype(np.int32),
-             hist=rng.integers(-2, min(V, 60) + 2, size=max(1, hist_len.sum())).astype(np.int32),
+             hist=rng.integers(-2, (V if hist_max > 4000 else min(V, 60)) + 2, size=max(1, hist_len.sum())).astype(np.int32),
              prompt_len=(hist_len * rng.random(n)).astype(np.int32), repetition=rng.uniform(0.8, 1.6, n).astype(np.float32),
              frequency=rng.uniform(-0.5, 1.0, n).astype(np.float32), presence=rng.uniform(-0.5, 1.0, n).astype(np.float32),
              temperature=np.where(rng.random(n) < 0.3, 0.0, rng.uniform(0.5, 2.0, n)).astype(np.float32))
@@ -581,6 +581,14 @@ def test_adjust_logits_rules_left_out(ats, leave):
 def test_adjust_logits_strides_and_in_place(ats, stride, inplace):
     _logits_case(ats, 9000, [4, 9], 300, torch.bfloat16, torch.bfloat16, 18, stride=stride, inplace=inplace)
     _logits_case(ats, 9001, [4, 9], 300, torch.float32, torch.float32, 19, stride=stride, inplace=inplace, tree=False)
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+def test_adjust_logits_long_lists_and_paths(ats, inplace):
+    """Histories that touch most of the vocabulary (lists longer than a CTA), paths of hundreds of tokens, rows of one
+    request and of others in turn."""
+    _logits_case(ats, 5003, [300, 1, 17], 9000, torch.float32, torch.float32, 23, inplace=inplace)
+    _logits_case(ats, 60, [520, 2], 100, torch.float16, torch.float16, 24, inplace=inplace)
 
 
 def test_adjust_logits_forbids_nan_and_keeps_the_rest(ats):
