@@ -42,7 +42,7 @@ __device__ unsigned int g_tree_attn_err;
 constexpr int kThreads = 384, kStreamThreads = 256;
 constexpr int kTile = 128;       // keys of a tile
 constexpr int kBlock = 256;      // rows of a block, at most
-constexpr int kRoleRegs = 80, kStreamRegs = 208;
+constexpr int kRoleRegs = 56, kStreamRegs = 216;
 static_assert(128 * kRoleRegs + kStreamThreads * kStreamRegs <= kThreads * 168, "registers at launch");
 constexpr float kSlack = 8.f;    // rise of the running maximum (log2) below which O keeps its scale
 constexpr int kMaxCtas = 512;    // counters in the workspace
@@ -69,7 +69,7 @@ struct TreeAttnArgs {
   long long vs[3], out_stride;
   int H, Hkv, G, n, T, page, page_log, n_pages, width, words;
   int cap;                                        // positions that a table row covers
-  int rt;                                         // rows of a stream's tile: the multiple of G up to 128
+  int rt, block_tokens;                           // rows of a stream's tile: the multiple of G up to 128; tokens of a block
   const int *cu_q, *ctx, *table;
   const uint32_t* mask;
   float c;                                        // scale * log2(e)
@@ -96,11 +96,11 @@ __device__ __forceinline__ Request request(const TreeAttnArgs& a, int b) {
   // (offsets outside the call's rows: nothing of the request is read or written)
   if (r.t0 < 0 || r.q < 0 || r.t0 > a.T - r.q) r.q = 0;
   r.rows = r.q * a.G;
-  r.blocks = r.ctx < 0 ? 0 : (r.rows + 2 * a.rt - 1) / (2 * a.rt);
+  r.blocks = r.ctx < 0 ? 0 : (r.q + a.block_tokens - 1) / a.block_tokens;
   return r;
 }
 __device__ __forceinline__ int block_keys(const TreeAttnArgs& a, const Request& r, int blk) {
-  const int last = a.mask ? r.q : min(r.q, (blk + 1) * 2 * a.rt / a.G);
+  const int last = a.mask ? r.q : min(r.q, (blk + 1) * a.block_tokens);
   return (int)min((long long)r.ctx + last, (long long)a.cap);
 }
 __device__ __forceinline__ int tiles_of(int keys) { return (keys + kTile - 1) / kTile; }
@@ -251,6 +251,9 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
       : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
   return z;
 }
+__device__ __forceinline__ void named_bar_arrive(int id, int nthreads) {
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
+}
 __device__ __forceinline__ int warp_uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 // Shared-memory descriptors (fields: common.cuh, smem_desc_sw128): the low word holds the address and `lead`, the bytes
@@ -361,36 +364,70 @@ __device__ __forceinline__ float* part_of(const TreeAttnArgs& a, int cta, int sl
   return reinterpret_cast<float*>(a.parts + (size_t)(2 * cta + slot) * Cfg<HD>::PART);
 }
 
-// Four columns of a row: sum over a block's partial results in their order.
+// A CTA's share of a cut block's rows: the sum of the partial results in their order, by both streams' threads.  First every
+// part's weight in every row of the share, into shared memory (rows x parts is 256 and a little, however many of each);
+// then four columns a thread, several threads' worth of loads under way.
 template <int HD>
 __device__ __forceinline__ void merge_share(const TreeAttnArgs& a, const Request& r, int kh, int blk, int first, int parts,
-                                            int share, int tid) {
-  constexpr int V4 = HD / 4;
-  const int rows = min(2 * a.rt, r.rows - blk * 2 * a.rt), total = rows * V4;
-  const int i0 = (int)((long long)total * share / parts), i1 = (int)((long long)total * (share + 1) / parts);
-  for (int i = i0 + tid; i < i1; i += kStreamThreads) {
-    const int row = i / V4, c4 = i % V4;
+                                            int share, int tid, float* w) {
+  constexpr int V4 = HD / 4, U = 4;
+  const int rows = min(2 * a.rt, r.rows - blk * 2 * a.rt);
+  const int row0 = rows * share / parts, n = rows * (share + 1) / parts - row0;
+  const auto place = [&](int row, int& t, int& h) {
+    const int rg = blk * 2 * a.rt + row;
+    t = r.t0 + rg / a.G, h = kh * a.G + rg % a.G;
+  };
+  for (int i = tid; i < n; i += kStreamThreads) {
     const auto ml = [&](int p) {
-      return __ldcg(reinterpret_cast<const float2*>(part_of<HD>(a, first + p, p == 0) + kBlock * HD) + row);
+      return __ldcg(reinterpret_cast<const float2*>(part_of<HD>(a, first + p, p == 0) + kBlock * HD) + row0 + i);
     };
-    float m = -INFINITY;
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 4
     for (int p = 0; p < parts; ++p) m = fmaxf(m, ml(p).x);
-    float l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
     for (int p = 0; p < parts; ++p) {
-      const float2 x = ml(p);
-      const float4 y = __ldcg(reinterpret_cast<const float4*>(part_of<HD>(a, first + p, p == 0) + row * HD) + c4);
       // (a part that saw none of the row's keys has l = 0 and no scale; a NaN in l stays one)
-      const float w = x.x == -INFINITY ? x.y : exp2_fast(x.x - m);
-      l += x.x == -INFINITY ? x.y : w * x.y;
-      o.x += w * y.x, o.y += w * y.y, o.z += w * y.z, o.w += w * y.w;
+      const float2 x = ml(p);
+      const float f = x.x == -INFINITY ? x.y : exp2_fast(x.x - m);
+      l += x.x == -INFINITY ? x.y : f * x.y;
+      w[i * parts + p] = f;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int rg = blk * 2 * a.rt + row, t = r.t0 + rg / a.G, h = kh * a.G + rg % a.G;
-    uint2 u = make_uint2(pack2(o.x * inv, o.y * inv, a.k_f16), pack2(o.z * inv, o.w * inv, a.k_f16));
-    *reinterpret_cast<uint2*>(a.out + (long long)t * a.out_stride + (long long)h * HD + c4 * 4) = u;
-    if (a.lse && c4 == 0) a.lse[(long long)t * a.H + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    for (int p = 0; p < parts; ++p) w[i * parts + p] *= inv;
+    if (a.lse) {
+      int t, h;
+      place(row0 + i, t, h);
+      a.lse[(long long)t * a.H + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    }
+  }
+  named_bar_sync(1, kStreamThreads);
+  for (int i0 = tid; i0 < n * V4; i0 += U * kStreamThreads) {
+    float4 o[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+    for (int p = 0; p < parts; ++p) {
+      const float* part = part_of<HD>(a, first + p, p == 0) + row0 * HD;
+      float4 y[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i0 + u * kStreamThreads < n * V4) y[u] = __ldcg(reinterpret_cast<const float4*>(part) + i0 + u * kStreamThreads);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (i0 + u * kStreamThreads >= n * V4) continue;
+        const float f = w[(i0 + u * kStreamThreads) / V4 * parts + p];
+        o[u].x += f * y[u].x, o[u].y += f * y[u].y, o[u].z += f * y[u].z, o[u].w += f * y[u].w;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kStreamThreads;
+      if (i >= n * V4) continue;
+      int t, h;
+      place(row0 + i / V4, t, h);
+      *reinterpret_cast<uint2*>(a.out + (long long)t * a.out_stride + (long long)h * HD + i % V4 * 4) =
+          make_uint2(pack2(o[u].x, o[u].y, a.k_f16), pack2(o[u].z, o[u].w, a.k_f16));
+    }
   }
 }
 
@@ -663,7 +700,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int panel = 0; panel < C::PANELS; ++panel)
             tma_load_4d(lead, smem_u32(smem + C::Q_OFF) + x * C::Q_TILE + panel * C::Q_PANEL, &tmq, smem_u32(q_full),
-                        panel * (C::SW / 2), 0, w.kh, w.r.t0 + (2 * w.blk + x) * (a.rt / a.G));
+                        panel * (C::SW / 2), 0, w.kh, w.r.t0 + (2 * w.blk + x) * (a.block_tokens / 2));
       }
     }
   } else {
@@ -697,8 +734,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = warp_wait(ok, s_full + s, (turn + k) & 1, err);
         tc_fence_after();
         if (r == 0 && ok) mbar_arrive(empty + (seq0 + seq_k(ahead, i)) % C::STAGES);
+        uint32_t x[128];
         if (active) {
-          uint32_t x[128];
 #pragma unroll
           for (int j = 0; j < 4; ++j) tmem_ld_32x32b_x32(t_s + 32 * j, *reinterpret_cast<uint32_t(*)[32]>(x + 32 * j));
           tmem_ld_wait128(x);
@@ -732,6 +769,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             l *= f;
             if (rise) m = m_new;
           }
+        }
+        // The streams' exponentials take turns, scheduler by scheduler (a warp of each): both at once would share one special
+        // function unit and leave the tensor core to both streams' products at once after.
+        if (dual && (s == 1 || k > 0)) named_bar_sync(4 + 4 * s + (warp & 3), 64);
+        if (active) {
           const float base = m == -INFINITY ? 0.f : -m;
           const float2 c2 = make_float2(a.c, a.c), b2 = make_float2(base, base);
           float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -756,8 +798,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           sum[0] = add2(sum[0], sum[1]);
           l += sum[0].x + sum[0].y;
-          tmem_st_wait();
         }
+        if (dual && (s == 0 || k + 1 < n)) named_bar_arrive(8 - 4 * s + (warp & 3), 64);
+        if (active) tmem_st_wait();
         if (__builtin_expect(masked, 0)) {
           // V rows that some row of the block does not see: a NaN or infinity there would reach it as 0 x NaN.  They
           // become 0 in the tile (every one of them), and the rows that do see one get it back at the end.
@@ -854,11 +897,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int k = 0; k < cuts; ++k) {
       const Shared x = cut[k];
       if (ok) ok = wait_count(a.arrived + x.first, 2 * x.parts, err);
-      ok = named_bar_and(2 + s, 128, ok);
+      ok = named_bar_and(1, kStreamThreads, ok);
       if (ok)
-        merge_share<HD>(a, request(a, x.b), x.kh, x.blk, x.first, x.parts, blockIdx.x - x.first, tid - 128);
-      named_bar_sync(2 + s, 128);
-      if (r == 0 && ok && atomicAdd(a.done + x.first, 1) == 2 * x.parts - 1) {   // the last share: back to zero
+        merge_share<HD>(a, request(a, x.b), x.kh, x.blk, x.first, x.parts, blockIdx.x - x.first, tid - 128,
+                        reinterpret_cast<float*>(smem + C::X_OFF));
+      named_bar_sync(1, kStreamThreads);
+      if (tid == 128 && ok && atomicAdd(a.done + x.first, 1) == x.parts - 1) {   // the last share: counters back to zero
         a.arrived[x.first] = 0;
         a.done[x.first] = 0;
       }
@@ -990,7 +1034,7 @@ atspeed_status atspeed_op_tree_attention(atspeed_stream stream, const atspeed_kv
   TreeAttnArgs a = {};
   a.v = static_cast<const uint16_t*>(c.d_v);
   for (int i = 0; i < 3; ++i) a.vs[i] = c.v_stride[i];
-  a.out_stride = out_stride, a.rt = 128 / G * G;
+  a.out_stride = out_stride, a.rt = 128 / G * G, a.block_tokens = 2 * (128 / G);
   a.H = n_heads, a.Hkv = c.n_kv_heads, a.G = G, a.n = n_req, a.T = T, a.page_log = ps == 16 ? 4 : ps == 32 ? 5 : ps == 64 ? 6 : ps == 128 ? 7 : 8, a.page = ps, a.n_pages = c.n_pages;
   a.width = table_width, a.words = mask_words, a.cu_q = d_cu_q, a.ctx = d_ctx_len, a.table = d_block_table, a.mask = d_mask;
   const long long cap = (long long)table_width * ps;
