@@ -18,13 +18,14 @@
 // 64 keys with two S a stream, so that a softmax never waits for its S, lose more than they gain: a product of N = 64 takes the
 // tensor core the 64 clocks of one of N = 128.  Two threads a row made the softmax no faster.)
 //
-// Work is the concatenation of all blocks' tiles, cut into one equal range a CTA (every CTA finds its own range from the
-// lengths); a block cut by a range's end is summed from partial results in device memory, each of its CTAs taking a share
+// Work is the concatenation of all blocks' tiles, each block's with a cost in front, cut into one equal range a CTA (every CTA
+// finds its own range from the lengths); a block cut by a range's end is summed from partial results in device memory, each of its CTAs taking a share
 // of the rows, in range order.  Waits for partial results come after all own results are out and the grid is launched
 // cooperatively, so that they end; they are bounded all the same.
 //
 // Roles (384 threads): warp 0 copies (TMA), warps 1 and 2 issue the products of a stream each, warp 3 loads Q, warps 4-7 and
-// 8-11 run the streams' softmax.
+// 8-11 run the streams' softmax.  A stream's warps keep their place in the walk over the blocks in shared memory: beside a
+// row of S it does not fit the registers, and spilled it cost 20 to 75% of the time where the HBM is the bound.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -42,9 +43,10 @@ __device__ unsigned int g_tree_attn_err;
 constexpr int kThreads = 384, kStreamThreads = 256;
 constexpr int kTile = 128;       // keys of a tile
 constexpr int kBlock = 256;      // rows of a block, at most
-constexpr int kRoleRegs = 56, kStreamRegs = 216;
+constexpr int kRoleRegs = 88, kStreamRegs = 208;
 static_assert(128 * kRoleRegs + kStreamThreads * kStreamRegs <= kThreads * 168, "registers at launch");
 constexpr float kSlack = 8.f;    // rise of the running maximum (log2) below which O keeps its scale
+constexpr int kWalkBytes = 72;   // of a warp's place in the walk
 constexpr int kMaxCtas = 512;    // counters in the workspace
 
 template <int HD>
@@ -57,7 +59,8 @@ struct Cfg {
   static constexpr int Q_OFF = STAGES * TILE;
   static constexpr int X_OFF = Q_OFF + 2 * Q_TILE;       // (m, l) of both streams' rows
   static constexpr int BAR_OFF = X_OFF + kStreamThreads * 8;
-  static constexpr int SMEM = BAR_OFF + 640;
+  static constexpr int WALK_OFF = BAR_OFF + 256, START_OFF = WALK_OFF + 8 * kWalkBytes;
+  static constexpr int SMEM = START_OFF + 64;
   static constexpr int S_COL = 128, O_COL = 256;       // TMEM columns: S / P of stream s at s * 128, O at 256 + s * HD
   static constexpr int O_STEP = HD;
   static constexpr size_t PART = (size_t)kBlock * (HD + 2) * 4;   // bytes of a partial result: O [256][HD], (m, l) [256]
@@ -104,41 +107,60 @@ __device__ __forceinline__ int block_keys(const TreeAttnArgs& a, const Request& 
   return (int)min((long long)r.ctx + last, (long long)a.cap);
 }
 __device__ __forceinline__ int tiles_of(int keys) { return (keys + kTile - 1) / kTile; }
+__device__ __forceinline__ int block_rows(const TreeAttnArgs& a, const Request& r, int blk) {
+  return min(2 * a.rt, r.rows - blk * 2 * a.rt);
+}
+// What a block costs beside its tiles (its Q, its pipeline's start, its masks and its result), in tiles, so that ranges of equal
+// units take equal times.  Measured at heads of 128, against no cost at all: 61 single tokens 208 -> 188 us with 1 (a CTA has
+// up to three blocks, another one long one); 16 trees of 61 tokens 107 -> 99 us with 2 to 6; a causal prompt of 4001 tokens
+// loses instead, 390 -> 403 us (its blocks are all of one kind and long).
+__device__ __forceinline__ int block_cost(const TreeAttnArgs& a, const Request& r, int blk) {
+  return block_rows(a, r, blk) <= a.rt ? 1 : a.mask ? 4 : 0;
+}
+__device__ __forceinline__ int block_units(const TreeAttnArgs& a, const Request& r, int blk) {
+  return block_cost(a, r, blk) + tiles_of(block_keys(a, r, blk));
+}
 __device__ __forceinline__ long long request_units(const TreeAttnArgs& a, const Request& r) {
   if (r.blocks == 0) return 0;
-  long long u = 0;
-  if (a.mask) u = (long long)r.blocks * tiles_of(block_keys(a, r, 0));
+  long long u = block_units(a, r, r.blocks - 1);
+  if (a.mask) u += (r.blocks - 1LL) * block_units(a, r, 0);
   else
-    for (int i = 0; i < r.blocks; ++i) u += tiles_of(block_keys(a, r, i));
+    for (int i = 0; i < r.blocks - 1; ++i) u += block_units(a, r, i);
   return u * a.Hkv;
 }
 
 struct Start {      // a CTA's range: where it begins
   long long u0, u1, units;
-  int b, kh, blk, tile, ctas;
+  int b, kh, blk, off, ctas;   // (off: units into the block)
 };
 
 struct Walk {
-  const TreeAttnArgs& a;
   Request r;
   long long left;     // units of the range from this block on
   int b, kh, blk;
   int tile0, tiles;   // this CTA's tiles of the block
   int all, keys;      // tiles and keys of the whole block
-  __device__ Walk(const TreeAttnArgs& args, const Start& s) : a(args), left(s.u1 - s.u0), b(s.b), kh(s.kh), blk(s.blk) {
+  int rows;           // rows of the block
+  int cost, units;    // its cost, and the range's units in it
+  __device__ __forceinline__ void start(const TreeAttnArgs& a, const Start& s) {
+    left = s.u1 - s.u0, b = s.b, kh = s.kh, blk = s.blk, tiles = 0;
     if (left <= 0) return;
     r = request(a, b);
-    block(s.tile);
+    block(a, s.off);
   }
-  __device__ void block(int first) {
+  // A block's units are its cost's, which are no work, and its tiles' after them.
+  __device__ __forceinline__ void block(const TreeAttnArgs& a, int off) {
     keys = block_keys(a, r, blk);
     all = tiles_of(keys);
-    tile0 = first;
-    tiles = (int)min((long long)(all - first), left);
+    rows = block_rows(a, r, blk);
+    cost = block_cost(a, r, blk);
+    units = (int)min((long long)(cost + all - off), left);
+    tile0 = max(0, off - cost);
+    tiles = max(0, off + units - cost) - tile0;
   }
-  __device__ bool more() const { return left > 0; }
-  __device__ void next() {
-    left -= tiles;
+  __device__ bool more() const { return left > 0 && tiles > 0; }
+  __device__ __forceinline__ void next(const TreeAttnArgs& a) {
+    left -= units;
     if (left <= 0) return;
     if (++blk == r.blocks) {
       blk = 0;
@@ -148,11 +170,11 @@ struct Walk {
         while (r.blocks == 0 && b < a.n - 1);
       }
     }
-    block(0);
+    block(a, 0);
   }
-  __device__ int rows() const { return min(2 * a.rt, r.rows - blk * 2 * a.rt); }
-  __device__ bool dual() const { return rows() > a.rt; }
+  __device__ bool dual(const TreeAttnArgs& a) const { return rows > a.rt; }
 };
+static_assert(sizeof(Walk) <= kWalkBytes, "a warp's place in shared memory");
 
 // ---------------------------------------------------------------------------------------------
 // instructions
@@ -309,17 +331,20 @@ __device__ __forceinline__ void clean_v(uint8_t* v0, int r, int first, int last,
   const auto beyond = [&](uint32_t two) { return (two & 0x7fff7fffu) + step & 0x80008000u; };
   uint4* chunk = reinterpret_cast<uint4*>(v0) + r % RC;
   uint32_t any = 0;
-#pragma unroll
-  for (int panel = 0; panel < C::PANELS; ++panel)
 #pragma unroll 4
-    for (int row = first + r / RC; row < kTile; row += 128 / RC) {
+  for (int row = first + r / RC; row < kTile; row += 128 / RC)
+#pragma unroll
+    for (int panel = 0; panel < C::PANELS; ++panel) {
       const uint4 v = chunk[(panel * C::PANEL + row * C::SW) / 16];
       any |= beyond(v.x) | beyond(v.y) | beyond(v.z) | beyond(v.w);
     }
   if (!any) return;
+#pragma unroll 1
   for (int panel = 0; panel < C::PANELS; ++panel)
+#pragma unroll 1
     for (int row = first + r / RC; row < kTile; row += 128 / RC) {
       uint16_t* v = reinterpret_cast<uint16_t*>(chunk + (panel * C::PANEL + row * C::SW) / 16);
+#pragma unroll 1
       for (int j = 0; j < 8; ++j) {
         if (!beyond(v[j])) continue;
         if (row < last) {
@@ -437,6 +462,7 @@ __device__ __forceinline__ bool wait_count(const int* p, int want, unsigned int*
     int v;
     asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     if (v >= want) return true;
+    __nanosleep(100);   // (a CTA that is early must not take the memory system's time from those that are not)
     if ((it & 255u) == 0u && globaltimer_ns() - t0 > kWaitBudgetNs) {
       set_error(err, ATSPEED_DEV_ERR_TIMEOUT);
       return false;
@@ -476,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* o_free = o_done + 1;          // its O is read
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_free + 1);
   volatile int* odd_v = reinterpret_cast<int*>(tmem_slot + 1);   // a NaN or infinity was found in a new token's V
-  Start* start = reinterpret_cast<Start*>(smem + C::BAR_OFF + 512);
+  Start* start = reinterpret_cast<Start*>(smem + C::START_OFF);
   const int tid = threadIdx.x, warp = warp_uniform(tid >> 5), lane = tid & 31;
   unsigned int* err = a.err;
 
@@ -527,14 +553,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             int blk = 0;
             start->kh = (int)(off / head);
             off %= head;
-            for (int k; off >= (k = tiles_of(block_keys(a, r, blk))); ++blk) off -= k;
+            for (int k; off >= (k = block_units(a, r, blk)); ++blk) off -= k;
             start->blk = blk;
             break;
           }
           off -= u;
         }
         start->b = b;
-        start->tile = (int)off;
+        start->off = (int)off;
         start->u0 = u0, start->u1 = u1, start->units = total, start->ctas = ctas;
       }
     }
@@ -570,8 +596,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       struct Pages {
         int now, next, base;   // of the 32 boxes from `base` on, and of the 32 after
       };
-      for (Walk w(a, st); w.more(); w.next()) {
-        const int n = warp_uniform(w.tiles), ahead = k_lead(warp_uniform(w.dual()));
+      Walk w;
+      for (w.start(a, st); w.more(); w.next(a)) {
+        const int n = warp_uniform(w.tiles), ahead = k_lead(warp_uniform(w.dual(a)));
         const int tile0 = warp_uniform(w.tile0), keys = warp_uniform(w.keys), kh = warp_uniform(w.kh);
         const int* table = a.table + (long long)w.b * a.width;
         const auto read = [&](int box) {   // this lane's of the 32 boxes from `box` on
@@ -625,8 +652,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (lane == 0 && ok) mbar_arrive(empty + pos % C::STAGES);
         }
       };
-      for (Walk w(a, st); w.more(); w.next(), ++item) {
-        const bool dual = warp_uniform(w.dual());
+      Walk w;
+      for (w.start(a, st); w.more(); w.next(a), ++item) {
+        const bool dual = warp_uniform(w.dual(a));
         const int n = warp_uniform(w.tiles), tiles = dual ? n : (n - s + 1) / 2, ahead = k_lead(dual);
         const uint32_t qd = qs + (dual ? s * (C::Q_TILE >> 4) : 0);
         const auto copied = [&](unsigned seq) {
@@ -691,10 +719,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       // ---- Q: a tile's tokens x G heads of one key head ----
       const uint32_t lead = elect_one();
       unsigned item = 0;
-      for (Walk w(a, st); w.more(); w.next(), ++item) {
+      Walk w;
+      for (w.start(a, st); w.more(); w.next(a), ++item) {
         ok = warp_wait(ok, q_free, (item & 1) ^ 1, err);
         if (!ok) continue;
-        const int both = w.dual() ? 2 : 1;
+        const int both = w.dual(a) ? 2 : 1;
         mbar_expect_tx_lead(lead, q_full, both * a.rt * HD * 2);
         for (int x = 0; x < both; ++x)
 #pragma unroll
@@ -715,10 +744,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       int b, kh, blk, first, parts;
     } cut[2];
     int cuts = 0;
-    long long unit = st.u0;
-    for (Walk w(a, st); w.more(); w.next(), ++item) {
-      const bool dual = w.dual();
-      const int n = w.tiles, row = dual ? s * a.rt + r : r, here = min(a.rt, w.rows() - (row - r));
+    long long unit = st.u0 - st.off;   // where the block at hand begins
+    Walk& w = reinterpret_cast<Walk*>(smem + C::WALK_OFF)[warp - 4];   // (the warp's; in registers it would not stay)
+    if (lane == 0) w.start(a, st);
+    __syncwarp();
+    for (; w.more(); ++item) {
+      const bool dual = w.dual(a);
+      const int n = w.tiles, row = dual ? s * a.rt + r : r, here = min(a.rt, w.rows - (row - r));
       const bool mine = r < here;                                // this thread's row exists
       const bool active = (r & ~31) < here;                      // .. one of the warp's does
       const int tok = min(w.blk * 2 * a.rt + row, w.r.rows - 1) / a.G;
@@ -841,23 +873,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint16_t* out = a.out + (long long)t * a.out_stride + (long long)head * HD;
         float* prow = whole ? nullptr : part + row * HD;
         const float g0 = f0 * inv, g1 = f1 * inv;
-#pragma unroll 2
+#pragma unroll 1
         for (int c = c0; c < c0 + width; c += 16) {
           uint32_t y0[16], y1[16];
           tmem_ld_32x32b_x16(o0 + c, y0);
-          if (!dual) tmem_ld_32x32b_x16(o1 + c, y1);
+          tmem_ld_32x32b_x16(o1 + c, y1);   // (dual: with weight 0)
           tmem_ld_wait16(y0, y1);
           float y[16];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            y[j] = f0 == 0.f ? 0.f : __uint_as_float(y0[j]) * g0;   // (a stream without tiles leaves its O as it was)
-            if (!dual && f1 != 0.f) y[j] += __uint_as_float(y1[j]) * g1;
-          }
+          for (int j = 0; j < 16; ++j)   // (a stream without tiles leaves its O as it was: a weight of 0 takes nothing from it)
+            y[j] = (f0 == 0.f ? 0.f : __uint_as_float(y0[j]) * g0) + (f1 == 0.f ? 0.f : __uint_as_float(y1[j]) * g1);
           if (!mine) continue;
           if (whole) {
             uint32_t u[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = KF16 ? pack2(y[2 * j], y[2 * j + 1], true) : pack2(y[2 * j], y[2 * j + 1], false);
+            for (int j = 0; j < 8; ++j) u[j] = pack2(y[2 * j], y[2 * j + 1], KF16);
             if (a.out32) {
               st_global_32(out + c, u);
             } else {
@@ -882,7 +912,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(o_free);
       if (!whole) {
-        const long long begin = unit - w.tile0;   // the block's first unit
+        const long long begin = unit + w.cost;   // the block's first tile
         Shared& x = cut[cuts++];
         x.b = w.b, x.kh = w.kh, x.blk = w.blk, x.first = cta_of(begin, st);
         x.parts = cta_of(begin + w.all - 1, st) - x.first + 1;
@@ -891,12 +921,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (r == 0 && ok) asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(a.arrived + x.first) : "memory");
       }
       seq0 += 2 * n;
-      unit += n;
+      unit += w.cost + w.all;
+      __syncwarp();
+      if (lane == 0) w.next(a);
+      __syncwarp();
     }
     // ---- shares of the blocks that were cut ----
     for (int k = 0; k < cuts; ++k) {
       const Shared x = cut[k];
-      if (ok) ok = wait_count(a.arrived + x.first, 2 * x.parts, err);
+      if (tid == 128 && ok) ok = wait_count(a.arrived + x.first, 2 * x.parts, err);   // (one thread asks)
       ok = named_bar_and(1, kStreamThreads, ok);
       if (ok)
         merge_share<HD>(a, request(a, x.b), x.kh, x.blk, x.first, x.parts, blockIdx.x - x.first, tid - 128,
