@@ -389,7 +389,11 @@ def op_status(noalloc: bool = False, stream=None) -> int:
     workspace (noalloc: those of the allocation-free scratch and of the attention); returns the status
     code (0 = no device error)."""
     ws = None if noalloc else op_workspace().data_ptr()
-    return int(load().atspeed_op_status(_stream(stream), ws))
+    status = int(load().atspeed_op_status(_stream(stream), ws))
+    if noalloc and status != 0:   # a call that gave up leaves its counters as they are
+        for w in _tree_ws.values():
+            w.zero_()
+    return status
 
 
 def op_gemm_swiglu(W: torch.Tensor, X: torch.Tensor, T: int, stream=None) -> torch.Tensor:

@@ -1,7 +1,10 @@
 // Penalties, biases, grammar masks and temperature on next-token logits (atspeed_op_adjust_logits).
 //   c(v) = occurrences of v in the request's output and on the row's path in its tree, seen(v) = c(v) > 0 or v in the prompt
 //   x <- seen ? (x > 0 ? x / rep : x * rep) : x;  x <- x - freq c - pres [c > 0] + bias(v);  forbidden: -inf;  x <- x / temp
-// Bound: HBM (each logit read and written once).
+// Bound: HBM (each logit read and written once).  3840 rows of 33024 (32 bits) take 237 us, 4.3 TB/s; with the temperature alone
+// 172, a plain copy 152.  509 rows of 100003 (bf16) with histories of up to 8000 tokens take 114 us, 1.8 TB/s: there each piece
+// of a row goes through the whole history, whose loads wait for the request's, and a CTA has too few bytes under way meanwhile
+// (without histories 85 us, a copy 40).  Pieces twice as long leave two CTAs an SM for the table's sake and take 154 us.
 //
 // The penalties and biases touch some hundred tokens of a vocabulary of tens of thousands.  So a warp streams its 512 tokens of
 // a row (temperature and the grammar's bits: a few instructions a logit) and then does the touched ones among them again,
@@ -23,6 +26,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kSub = 512;               // tokens of a warp
 constexpr int kRegion = kSub + 16;      // .. and its words: from 8 tokens before the first
 constexpr int kChunk = kSub * kWarps;   // tokens of a CTA
+constexpr int kBatch = 8;               // entries of a history that a thread has under way
 constexpr uint32_t kPrompt = 1u << 31, kListed = 1u << 30;   // flags of a token's word; below them its count in the output
 
 struct RulesArgs {
@@ -163,13 +167,24 @@ __global__ void __launch_bounds__(kThreads, 4) adjust_logits_kernel(const __grid
         uint32_t* c = sm + w * words;
         if (!(atomicOr(c + i, kListed) & kListed)) reinterpret_cast<uint16_t*>(c + kRegion)[atomicAdd(&s_n[w], 1)] = (uint16_t)i;
       };
-#pragma unroll 4
-      for (int k = h0 + tid; k < h1; k += kThreads)
-        each(__ldg(a.r.d_hist + k), [&](int w, int i) {
-          if (k < p) atomicOr(sm + w * words + i, kPrompt);
-          else atomicAdd(sm + w * words + i, 1u);
-          enlist(w, i);
-        });
+      // (kBatch entries a thread at once; few are among the CTA's tokens, and those are read again)
+      for (int k_at = h0 + tid; k_at < h1; k_at += kBatch * kThreads) {
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          const int k = k_at + j * kThreads, v = k < h1 ? __ldg(a.r.d_hist + k) : -1;
+          if ((unsigned)v < (unsigned)a.V && (unsigned)(v - v0 + 8) < (unsigned)(kChunk + 16)) hits |= 1u << j;
+        }
+#pragma unroll 1
+        for (; hits; hits &= hits - 1) {
+          const int k = k_at + (__ffs(hits) - 1) * kThreads;
+          each(__ldg(a.r.d_hist + k), [&](int w, int i) {
+            if (k < p) atomicOr(sm + w * words + i, kPrompt);
+            else atomicAdd(sm + w * words + i, 1u);
+            enlist(w, i);
+          });
+        }
+      }
       for (int k = k0 + tid; k < k1; k += kThreads)
         each(__ldg(a.r.d_bias_tok + k), [&](int w, int i) {   // (the later entry)
           atomicMax(sm + w * words + kRegion + kRegion / 2 + i, (uint32_t)(k - k0) + 1u);
@@ -215,11 +230,14 @@ __global__ void __launch_bounds__(kThreads, 4) adjust_logits_kernel(const __grid
       return t >= t0 && t < t0 + kSub ? t : -1;
     };
     const int my_t = lane < listed ? token(lane) : -1;
-    uint32_t my_raw = 0;
+    uint32_t my_raw = 0, my_w = 0;
+    float my_bias = 0.f;
     bool my_forbidden = false;
     if (my_t >= 0) {
       my_raw = one(in, my_t);
       my_forbidden = forbidden(my_t);
+      my_w = cnt[list[lane]];
+      if (const uint32_t k = biased ? bias[list[lane]] : 0u) my_bias = __ldg(a.r.d_bias_val + k0 + k - 1);
     }
     if (a.in_place) {
       for (int e = 32 + lane; e < listed; e += 32) {
@@ -266,20 +284,22 @@ __global__ void __launch_bounds__(kThreads, 4) adjust_logits_kernel(const __grid
     if (row + 1 < r1) load(row + 1);
     __syncwarp();
     // the listed ones with all rules
-    const auto finish = [&](int e, int t, uint32_t logit, bool forbid) {
-      const int i = list[e];
-      const uint32_t w = cnt[i], c = w & (kListed - 1);
+    const auto finish = [&](int t, uint32_t logit, uint32_t w, float add, bool forbid) {
+      const uint32_t c = w & (kListed - 1);
       float y = value(logit);
       if (c || w & kPrompt) y = y > 0.f ? (f.divide ? y / f.rep : y * f.rep_inv) : y * f.rep;
       if (c) y = y - f.freq * (float)c - f.pres;
-      if (biased && bias[i]) y += __ldg(a.r.d_bias_val + k0 + bias[i] - 1);
+      y += add;
       y = f.divide ? y / f.temp : y * f.temp_inv;
       O::store1(out + (long long)t * O::SIZE, forbid ? -INFINITY : y);
     };
-    if (my_t >= 0) finish(lane, my_t, my_raw, my_forbidden);
+    if (my_t >= 0) finish(my_t, my_raw, my_w, my_bias, my_forbidden);
     for (int e = 32 + lane; e < listed; e += 32) {
       const int t = token(e);
-      if (t >= 0) finish(e, t, a.in_place ? raw[e] : one(in, t), forbidden(t));
+      if (t < 0) continue;
+      const int i = list[e];
+      const uint32_t k = biased ? bias[i] : 0u;
+      finish(t, a.in_place ? raw[e] : one(in, t), cnt[i], k ? __ldg(a.r.d_bias_val + k0 + k - 1) : 0.f, forbidden(t));
     }
     __syncwarp();
     if (path) {   // the path's tokens leave again
@@ -320,9 +340,9 @@ extern "C" atspeed_status atspeed_op_adjust_logits(atspeed_stream stream, const 
   a.in_place = d_out == d_logits;
   // Pieces of 4096 tokens (7 more for rows that begin between 16-byte addresses).  Rows a CTA: a request's list is made once for
   // those that follow each other, and more CTAs than run at once even out their ends.  us for 1 / 2 / 4 / 8 / 16 rows: 3840 rows of
-  // 33024, 240 a request, 316 / 265 / 244 / 246 / 265; 509 rows of 100003, one a request, 144 / 144 / 156 / 179 / 179.
-  // Neighbouring CTAs take a row's pieces one after the other (3840 rows: 244, row after row 259), except where every row has
-  // a history of its own, whose long ones then spread (509 rows: 144 and 128).
+  // 33024, 240 a request, 335 / 261 / 237 / 237 / 254; 509 rows of 100003, one a request, 114 / 131 / 144 / 160 / 212.
+  // Neighbouring CTAs take a row's pieces one after the other (3840 rows: 237, row after row 254), except where every row has
+  // a history of its own, whose long ones then spread (509 rows: 120 and 114).
   a.chunks = (unsigned)((vocab + 7LL + kChunk - 1) / kChunk);
   a.rows = std::min(4, std::max(1, R / std::max(1, r.n_req)));
   a.groups = (unsigned)((R + a.rows - 1LL) / a.rows);
