@@ -380,11 +380,11 @@ atspeed_status atspeed_op_rope_append(atspeed_stream stream, const void *d_qkv, 
  *   d_q [T] rows of n_heads * head_dim, q_stride elements apart, of the cache's k_type; d_out the same with out_stride;
  *   d_lse NULL or [T][n_heads]: natural log of the sum of exp(score);
  *   d_cu_q [n_req+1], d_ctx_len [n_req], d_block_table [n_req][table_width] (entries past the last page of a request are not
- *   read; positions past the table are not attended to).
+ *   read; positions past the table are not attended to; an entry outside the cache stands for a page of zeros).
  * head_dim 32, 64 or 128; page_size 16, 32, 64, 128 or 256; n_heads a multiple of n_kv_heads, at most 128 times it;
  * n_req <= 16384 (ATSPEED_E_SHAPE); scale > 0; rows and strides 16-byte aligned (ATSPEED_E_ARG).
  * d_ws: atspeed_op_tree_attention_workspace() bytes, 256-byte aligned, zero-filled before its first use, of one stream at a
- * time (every call leaves its counters zeroed).  Long key ranges are divided by the lengths of the whole call, in an
+ * time (every call leaves its counters zeroed).  The first call on a device is made outside stream capture.  Long key ranges are divided by the lengths of the whole call, in an
  * order that the lengths alone fix: the same call gives the same bits, a request's last bits may differ in another batch.
  * Device-side timeouts surface through atspeed_op_status(stream, NULL); after one, zero the workspace again. */
 size_t atspeed_op_tree_attention_workspace(void);
