@@ -19,9 +19,10 @@
 // tensor core the 64 clocks of one of N = 128.  Two threads a row made the softmax no faster.)
 //
 // Work is the concatenation of all blocks' tiles, each block's with a cost in front, cut into one equal range a CTA (every CTA
-// finds its own range from the lengths); a block cut by a range's end is summed from partial results in device memory, each of its CTAs taking a share
-// of the rows, in range order.  Waits for partial results come after all own results are out and the grid is launched
-// cooperatively, so that they end; they are bounded all the same.
+// finds its own range from the lengths; an end next to a block's border is moved there).  A block that an end cuts is summed
+// from partial results in device memory, each of its CTAs taking a share of the rows, in range order.  Waits for partial
+// results come after all own results are out and the grid is launched cooperatively, so that they end; they are bounded all
+// the same.
 //
 // Roles (384 threads): warp 0 copies (TMA), warps 1 and 2 issue the products of a stream each, warp 3 loads Q, warps 4-7 and
 // 8-11 run the streams' softmax.  A stream's warps keep their place in the walk over the blocks in shared memory: beside a
@@ -46,7 +47,7 @@ constexpr int kBlock = 256;      // rows of a block, at most
 constexpr int kRoleRegs = 88, kStreamRegs = 208;
 static_assert(128 * kRoleRegs + kStreamThreads * kStreamRegs <= kThreads * 168, "registers at launch");
 constexpr float kSlack = 8.f;    // rise of the running maximum (log2) below which O keeps its scale
-constexpr int kWalkBytes = 72;   // of a warp's place in the walk
+constexpr int kWalkBytes = 80;   // of a warp's place in the walk
 constexpr int kMaxCtas = 512;    // counters in the workspace
 
 template <int HD>
@@ -129,14 +130,28 @@ __device__ __forceinline__ long long request_units(const TreeAttnArgs& a, const 
   return u * a.Hkv;
 }
 
+// x / d, of numbers that are small as a rule
+__device__ __forceinline__ long long quotient(long long x, long long d) {
+  return (unsigned long long)(x | d) >> 32 ? x / d : (long long)((unsigned)x / (unsigned)d);
+}
+// How far a range's end may be moved to a block's border, so that the block is not cut for it (a cut block of 256 rows costs each
+// of its CTAs some 5 us: 132 KB out, a wait, its share back in); `most`: a sixth of the range.  Measured, heads of 128, against
+// no move: 512 blocks of 16 trees 97 -> 82 us; heads of 64: a prompt 317 -> 309; looking for both of a range's ends costs a
+// call of one token 1.2 us (13.4 -> 14.6).
+__device__ __forceinline__ int block_slack(const TreeAttnArgs& a, int rows, int most) {
+  return min(rows > a.rt ? 6 : 1, most);
+}
+
 struct Start {      // a CTA's range: where it begins
   long long u0, u1, units;
   int b, kh, blk, off, ctas;   // (off: units into the block)
+  int most;                    // of block_slack
 };
 
 struct Walk {
   Request r;
   long long left;     // units of the range from this block on
+  long long begin;    // the block's first unit
   int b, kh, blk;
   int tile0, tiles;   // this CTA's tiles of the block
   int all, keys;      // tiles and keys of the whole block
@@ -146,7 +161,9 @@ struct Walk {
     left = s.u1 - s.u0, b = s.b, kh = s.kh, blk = s.blk, tiles = 0;
     if (left <= 0) return;
     r = request(a, b);
+    begin = s.u0 - s.off;
     block(a, s.off);
+    if (units == 0) next(a);
   }
   // A block's units are its cost's, which are no work, and its tiles' after them.
   __device__ __forceinline__ void block(const TreeAttnArgs& a, int off) {
@@ -161,6 +178,7 @@ struct Walk {
   __device__ bool more() const { return left > 0 && tiles > 0; }
   __device__ __forceinline__ void next(const TreeAttnArgs& a) {
     left -= units;
+    begin += cost + all;
     if (left <= 0) return;
     if (++blk == r.blocks) {
       blk = 0;
@@ -382,7 +400,7 @@ __device__ __noinline__ void add_odd_v(const TreeAttnArgs& a, int b, int kh, int
 // ---------------------------------------------------------------------------------------------
 // a partial result's place, and the block's CTAs
 // ---------------------------------------------------------------------------------------------
-__device__ __forceinline__ int cta_of(long long u, const Start& s) { return (int)(((u + 1) * s.ctas - 1) / s.units); }
+__device__ __forceinline__ int cta_of(long long u, const Start& s) { return (int)quotient((u + 1) * s.ctas - 1, s.units); }
 
 template <int HD>
 __device__ __forceinline__ float* part_of(const TreeAttnArgs& a, int cta, int slot) {
@@ -519,6 +537,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane >= o) sum += x;
     }
     if (lane == 31) sums[warp] = sum;
+    sums[kThreads / 32 + tid] = sum - own, sums[kThreads / 32 + kThreads + tid] = own;
     if (warp == 3) tmem_alloc(tmem_slot, 512);
     if (tid == 0) {
       for (int i = 0; i < C::STAGES; ++i) mbar_init(full + i, 1), mbar_init(empty + i, 2);
@@ -534,34 +553,46 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (tid == 32) tma_prefetch_desc(&tmq), tma_prefetch_desc(&tmk), tma_prefetch_desc(&tmv);
     __syncthreads();
-    long long total = 0, before = sum - own;
+    // (another thread looks for the range's end among the requests of this one)
+    const int other = tid < kThreads / 2 ? tid + kThreads / 2 : tid - kThreads / 2;
+    long long total = 0, before = sum - own, before1 = sums[kThreads / 32 + other];
+    const long long own1 = sums[kThreads / 32 + kThreads + other];
     for (int w = 0; w < kThreads / 32; ++w) {
       if (w < warp) before += sums[w];
+      if (w < other >> 5) before1 += sums[w];
       total += sums[w];
     }
     const int ctas = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
     if (cta < ctas) {
-      const long long u0 = cta * total / ctas, u1 = (cta + 1LL) * total / ctas;
-      if (u0 >= before && u0 < before + own) {
-        int b = b0;
-        long long off = u0 - before;
-        for (;; ++b) {
-          const Request r = request(a, b);
-          const long long u = request_units(a, r);
-          if (off < u) {
-            const long long head = u / a.Hkv;
-            int blk = 0;
-            start->kh = (int)(off / head);
-            off %= head;
-            for (int k; off >= (k = block_units(a, r, blk)); ++blk) off -= k;
-            start->blk = blk;
+      const long long u0 = quotient(cta * total, ctas), u1 = quotient((cta + 1LL) * total, ctas);
+      const int most = (int)min(quotient(total, ctas * 6), 1LL << 20);
+      // The block that holds a unit, and how far into it the border at that unit is, moved where that saves a cut.
+      const auto find = [&](long long off, int first, int& b, int& kh, int& blk) {
+        Request r;
+        for (b = first;; ++b) {
+          r = request(a, b);
+          const long long x = request_units(a, r);
+          if (off < x) {
+            const long long head = quotient(x, a.Hkv);
+            kh = (int)quotient(off, head), off -= kh * head, blk = 0;
             break;
           }
-          off -= u;
+          off -= x;
         }
-        start->b = b;
-        start->off = (int)off;
-        start->u0 = u0, start->u1 = u1, start->units = total, start->ctas = ctas;
+        int units;
+        for (; off >= (units = block_units(a, r, blk)); ++blk) off -= units;
+        const int slack = block_slack(a, block_rows(a, r, blk), most);
+        return off <= slack ? make_int2((int)off, 0) : make_int2((int)off, units - off <= slack ? units : (int)off);
+      };
+      if (u0 >= before && u0 < before + own) {
+        const int2 x = find(u0 - before, b0, start->b, start->kh, start->blk);
+        start->off = x.y;
+        start->u0 = u0 - x.x + x.y, start->units = total, start->ctas = ctas, start->most = most;
+      }
+      if (u1 == total ? tid == 0 : u1 >= before1 && u1 < before1 + own1) {
+        int b, kh, blk;
+        const int2 x = u1 == total ? make_int2(0, 0) : find(u1 - before1, min(a.n, other * per), b, kh, blk);
+        start->u1 = u1 - x.x + x.y;
       }
     }
     // requests that were not served: zeros
@@ -744,7 +775,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       int b, kh, blk, first, parts;
     } cut[2];
     int cuts = 0;
-    long long unit = st.u0 - st.off;   // where the block at hand begins
     Walk& w = reinterpret_cast<Walk*>(smem + C::WALK_OFF)[warp - 4];   // (the warp's; in registers it would not stay)
     if (lane == 0) w.start(a, st);
     __syncwarp();
@@ -754,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool mine = r < here;                                // this thread's row exists
       const bool active = (r & ~31) < here;                      // .. one of the warp's does
       const int tok = min(w.blk * 2 * a.rt + row, w.r.rows - 1) / a.G;
-      const int seen_all = min(w.r.ctx, a.cap);                  // keys before this one are seen by every row
+      const int seen_all = (int)min((long long)w.r.ctx + (a.mask ? 0 : w.blk * a.block_tokens + 1), (long long)a.cap);
       float m = -INFINITY, l = 0.f;
       const int tiles = dual ? n : (n - s + 1) / 2, ahead = k_lead(dual);
 #pragma unroll 1
@@ -912,16 +942,20 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(o_free);
       if (!whole) {
-        const long long begin = unit + w.cost;   // the block's first tile
+        const int slack = block_slack(a, w.rows, st.most);
+        const long long end = w.begin + w.cost + w.all;
+        const auto border = [&](int cta) { return quotient(cta * st.units, st.ctas); };   // (before it is moved)
         Shared& x = cut[cuts++];
-        x.b = w.b, x.kh = w.kh, x.blk = w.blk, x.first = cta_of(begin, st);
-        x.parts = cta_of(begin + w.all - 1, st) - x.first + 1;
+        int last = cta_of(end - 1, st);
+        x.b = w.b, x.kh = w.kh, x.blk = w.blk, x.first = cta_of(w.begin + w.cost, st);
+        if (const long long u = border(x.first + 1); x.first + 1 < st.ctas && u < end && u - w.begin <= slack) ++x.first;
+        if (const long long u = border(last); u - w.begin > slack && end - u <= slack) --last;
+        x.parts = last - x.first + 1;
         __threadfence();
         named_bar_sync(2 + s, 128);
         if (r == 0 && ok) asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(a.arrived + x.first) : "memory");
       }
       seq0 += 2 * n;
-      unit += w.cost + w.all;
       __syncwarp();
       if (lane == 0) w.next(a);
       __syncwarp();

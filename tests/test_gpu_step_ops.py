@@ -321,6 +321,17 @@ def test_tree_attention_long_ranges(ats, q_len, ctx, H, hd, page):
     _attention_case(ats, q_len, ctx, H, H, hd, page, "bf16", tree=_drafted, poison=False, seed=hd + page)
 
 
+@pytest.mark.parametrize("q_len,ctx,H,hd,tree", [([65] * 45, [500 + 23 * i for i in range(45)], 8, 64, _drafted),
+                                                  ([130, 3] * 20, [40 * i for i in range(40)], 8, 128, _drafted),
+                                                  ([1] * 300, [10 * i for i in range(300)], 8, 32, None),
+                                                  ([700, 900], [100, 0], 24, 64, None)])
+def test_tree_attention_many_blocks(ats, q_len, ctx, H, hd, tree):
+    """Several blocks a CTA, of one kind or mixed, so that ranges end at blocks' borders or next to them as well as inside; a
+    causal prompt, whose blocks see their own tokens' keys in part."""
+    _attention_case(ats, q_len, ctx, H, H // 4, hd, 16, "bf16", tree=tree, seed=len(q_len) + H)
+    _attention_case(ats, q_len, ctx, H, H, hd, 64, "f16", tree=tree, seed=len(q_len) + hd)
+
+
 @pytest.mark.parametrize("G", [1, 2, 3, 5, 16, 127, 128])
 def test_tree_attention_groups(ats, G):
     _attention_case(ats, [3, 1, 9], [200, 77, 513], 2 * G if G < 100 else G, 2 if G < 100 else 1, 32, 16, "f16", tree=_drafted, seed=G)
