@@ -378,6 +378,27 @@ def test_tree_attention_attended_infinity_and_nan(ats):
     assert torch.equal(got[:, keep], ref[:, keep])
 
 
+@pytest.mark.parametrize("G,hd", [(2, 64), (8, 128), (1, 32)])
+def test_causal_attention_of_infinity_and_nan(ats, G, hd):
+    """The same in a causal call of several blocks: from the token on whose value it is, and not before."""
+    H, page, ctx, L = 2 * G, 16, 70, 300
+    kc, vc = _cache("bf16", 24, page, 2, hd, seed=12)
+    clean = vc.clone()
+    bad = {0: (0, float("inf")), 3: (1, float("nan")), 127: (2, NEG), 128: (3, float("nan")), 150: (4, float("inf")),
+           299: (5, float("nan"))}
+    for a, (c, x) in bad.items():
+        vc[(ctx + a) // page, (ctx + a) % page, 1, c] = x
+    q = torch.randn(L, H, hd, device="cuda").to(torch.bfloat16)
+    args = (_dev([0, L]), _dev([ctx]), _dev(np.arange(24, dtype=np.int32)[None]))
+    got = ats.op_tree_attention(q, kc, vc, *args)
+    ref = ats.op_tree_attention(q, kc, clean, *args)
+    for a, (c, x) in bad.items():
+        assert torch.equal(got[:a, G:, c], ref[:a, G:, c])
+        after = got[a:, G:, c].float()
+        assert bool(torch.isnan(after).all()) if np.isnan(x) else bool((after == x).all())
+    assert torch.equal(got[:, :G], ref[:, :G]) and torch.equal(got[:, G:, 6:], ref[:, G:, 6:])
+
+
 def test_tree_attention_strides_streams_and_shared_pages(ats):
     """q and out as slices of wider rows, two requests over the same prefix pages, a stream of the caller's."""
     H, Hkv, hd, page = 8, 2, 64, 32
