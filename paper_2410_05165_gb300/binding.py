@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Dict, List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -69,6 +70,10 @@ class KvPages(ctypes.Structure):
     _fields_ = [("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("k_type", ctypes.c_int), ("v_type", ctypes.c_int),
                 ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
                 ("head_dim", ctypes.c_int), ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3)]
+
+
+_KV_PACK = struct.Struct("@PPiiiiiiqqqqqq").pack
+assert struct.calcsize("@PPiiiiiiqqqqqq") == ctypes.sizeof(KvPages)
 
 
 class LogitRulesDesc(ctypes.Structure):
@@ -474,7 +479,8 @@ def _kv_pages(kc: torch.Tensor, vc: torch.Tensor) -> KvPages:
                                                                                                             vc.is_cuda):
         _refuse(f"caches: two [pages][page_size][heads][head_dim] on the device, not {tuple(shape)} {kc.dtype} and "
                 f"{tuple(vc.shape)} {vc.dtype}")
-    return KvPages(kc.data_ptr(), vc.data_ptr(), kt, vt, shape[0], shape[1], shape[2], shape[3], ks[:3], vs[:3])
+    return KvPages.from_buffer_copy(_KV_PACK(kc.data_ptr(), vc.data_ptr(), kt, vt, shape[0], shape[1], shape[2], shape[3],
+                                             ks[0], ks[1], ks[2], vs[0], vs[1], vs[2]))   # (0.5 us; field by field 1.3)
 
 
 class BatchPlan:
