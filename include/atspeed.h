@@ -383,10 +383,11 @@ atspeed_status atspeed_op_rope_append(atspeed_stream stream, const void *d_qkv, 
  *   read; positions past the table are not attended to; an entry outside the cache stands for a page of zeros).
  * head_dim 32, 64 or 128; page_size 16, 32, 64, 128 or 256; n_heads a multiple of n_kv_heads, at most 128 times it;
  * n_req <= 16384 (ATSPEED_E_SHAPE); scale > 0; rows and strides 16-byte aligned (ATSPEED_E_ARG).
- * d_ws: atspeed_op_tree_attention_workspace() bytes, 256-byte aligned, zero-filled before its first use, of one stream at a
- * time (every call leaves its counters zeroed).  The first call on a device is made outside stream capture.  Long key ranges are divided by the lengths of the whole call, in an
+ * d_ws: atspeed_op_tree_attention_workspace() bytes, 256-byte aligned, the first ATSPEED_TREE_ATTENTION_COUNTER_BYTES of them
+ * zero-filled before its first use, of one stream (or graph) at a time (every call leaves its counters zeroed).  The first call on a device is made outside stream capture.  Long key ranges are divided by the lengths of the whole call, in an
  * order that the lengths alone fix: the same call gives the same bits, a request's last bits may differ in another batch.
- * Device-side timeouts surface through atspeed_op_status(stream, NULL); after one, zero the workspace again. */
+ * Device-side timeouts surface through atspeed_op_status(stream, NULL); after one, zero those bytes again. */
+#define ATSPEED_TREE_ATTENTION_COUNTER_BYTES 4096
 size_t atspeed_op_tree_attention_workspace(void);
 atspeed_status atspeed_op_tree_attention(atspeed_stream stream, const atspeed_kv_pages *cache, const void *d_q,
                                          int64_t q_stride, int n_heads, int n_req, int T, const int32_t *d_cu_q,

@@ -396,8 +396,9 @@ def op_status(noalloc: bool = False, stream=None) -> int:
     ws = None if noalloc else op_workspace().data_ptr()
     status = int(load().atspeed_op_status(_stream(stream), ws))
     if noalloc and status != 0:   # a call that gave up leaves its counters as they are
-        for w in _tree_ws.values():
-            w.zero_()
+        for (device, st), w in _tree_ws.items():
+            with torch.cuda.stream(torch.cuda.ExternalStream(st, device=device)):
+                w[:TREE_ATTENTION_COUNTER_BYTES].zero_()
     return status
 
 
@@ -546,12 +547,18 @@ def op_rope_append(qkv: torch.Tensor, n_heads: int, kc: torch.Tensor, vc: torch.
 
 
 _tree_ws: Dict[Tuple[int, int], torch.Tensor] = {}
+TREE_ATTENTION_COUNTER_BYTES = 4096
 
 
 def op_tree_attention_workspace(device, stream: int) -> torch.Tensor:
-    """The attention's workspace of one stream (calls on one stream follow each other; two streams' would not)."""
+    """The attention's workspace of one stream (calls on one stream follow each other; two streams' would not).  While a stream
+    is captured that has none, one of the graph's own memory, whose counters the graph itself clears."""
     key = (device.index or 0, stream)
     if key not in _tree_ws:
+        if torch.cuda.is_current_stream_capturing():
+            w = torch.empty(load().atspeed_op_tree_attention_workspace(), dtype=torch.uint8, device=device)
+            w[:TREE_ATTENTION_COUNTER_BYTES].zero_()
+            return w
         _tree_ws[key] = torch.zeros(load().atspeed_op_tree_attention_workspace(), dtype=torch.uint8, device=device)
         torch.cuda.current_stream(device).synchronize()   # (the zeros come before a call on whatever stream)
     return _tree_ws[key]

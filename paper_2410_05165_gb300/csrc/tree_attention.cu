@@ -1060,6 +1060,7 @@ int sm_count() {
 }
 
 constexpr size_t kCounterBytes = 2 * kMaxCtas * sizeof(int);
+static_assert(kCounterBytes == ATSPEED_TREE_ATTENTION_COUNTER_BYTES, "the workspace's counters");
 
 }  // namespace
 

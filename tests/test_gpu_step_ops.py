@@ -473,6 +473,48 @@ def test_tree_attention_in_a_graph(ats):
         assert torch.equal(out, want)
 
 
+def test_tree_attention_in_a_graph_of_another_stream(ats):
+    """Captured on a stream that the attention was never called on, and replayed on the caller's, twice."""
+    kc, vc = _cache("bf16", 40, 16, 2, 64, seed=31)
+    q = torch.randn(9, 4, 64, device="cuda").to(torch.bfloat16)
+    args = (_dev([0, 1, 9]), _dev([300, 100]), _dev(np.arange(40).reshape(2, 20)))
+    want = ats.op_tree_attention(q, kc, vc, *args)
+    out = torch.zeros_like(q)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+        for _ in range(3):
+            ats.op_tree_attention(q, kc, vc, *args, out=out)
+    for _ in range(2):
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    assert ats.op_status(noalloc=True) == 0
+
+
+def test_a_timeout_once_read_clears_the_workspaces(ats, monkeypatch):
+    """(The status is a fake's: nothing waits in vain here.)  Counters that a call left behind are cleared, on every stream."""
+    from paper_2410_05165_gb300 import binding
+    streams = [torch.cuda.current_stream(), torch.cuda.Stream()]
+    spaces = [binding.op_tree_attention_workspace(torch.device("cuda", 0), s.cuda_stream) for s in streams]
+    torch.cuda.synchronize()
+    for w in spaces:
+        w[:64] = 1
+    torch.cuda.synchronize()
+
+    class Failed:
+        @staticmethod
+        def atspeed_op_status(stream, ws):
+            return binding.E_TIMEOUT
+
+    with monkeypatch.context() as m:
+        m.setattr(binding, "load", lambda: Failed)
+        assert binding.op_status(noalloc=True) == binding.E_TIMEOUT
+    torch.cuda.synchronize()
+    assert all(int(w[:binding.TREE_ATTENTION_COUNTER_BYTES].sum()) == 0 for w in spaces)
+
+
 def test_step_ops_refuse_wrong_tensors(ats):
     kc, vc = _cache("bf16", 4, 16, 2, 64)
     q = torch.zeros(3, 4, 64, device="cuda", dtype=torch.bfloat16)
