@@ -26,8 +26,8 @@
 //
 // Bound and measured: few rows over long caches by HBM (61 single tokens over 500 to 16 000 keys, 32 heads on 8 of 128: 188 us,
 // 6.2 TB/s); many rows by the streams' chain S, maximum, exponentials (1000 of 2900 clocks a tile), P, O, not by the tensor
-// pipe (29 to 43% busy): 16 trees of 240 tokens 82 us, 515 TFLOP/s; a prompt of 2 x 4001 tokens, heads of 64, 309 us, 787 TFLOP/s.
-// A single token over 512 keys takes 14.6 us, all latency.
+// pipe (29 to 43% busy): 16 trees of 240 tokens 82 us, 515 TFLOP/s; a prompt of 2 x 4001 tokens, heads of 64, 312 us, 780 TFLOP/s.
+// A single token over 512 keys takes 13.7 us, all latency.
 //
 // Roles (384 threads): warp 0 copies (TMA), warps 1 and 2 issue the products of a stream each, warp 3 loads Q, warps 4-7 and
 // 8-11 run the streams' softmax.  A stream's warps keep their place in the walk over the blocks in shared memory: beside a
@@ -53,6 +53,7 @@ constexpr int kRoleRegs = 88, kStreamRegs = 208;
 static_assert(128 * kRoleRegs + kStreamThreads * kStreamRegs <= kThreads * 168, "registers at launch");
 constexpr float kSlack = 8.f;    // rise of the running maximum (log2) below which O keeps its scale
 constexpr int kWalkBytes = 80;   // of a warp's place in the walk
+constexpr int kLeastUnits = 2;   // of a CTA's range (1: 2 to 14% slower over ten small calls, 3: 10 to 30% on most)
 constexpr int kMaxCtas = 512;    // counters in the workspace
 
 template <int HD>
@@ -412,60 +413,32 @@ __device__ __forceinline__ float* part_of(const TreeAttnArgs& a, int cta, int sl
   return reinterpret_cast<float*>(a.parts + (size_t)(2 * cta + slot) * Cfg<HD>::PART);
 }
 
-// A CTA's share of a cut block's rows: the sum of the partial results in their order, by both streams' threads.  First every
-// part's weight in every row of the share, into shared memory (rows x parts is 256 and a little, however many of each);
-// then four columns a thread, several threads' worth of loads under way.
-template <int HD>
-__device__ __forceinline__ void merge_share(const TreeAttnArgs& a, const Request& r, int kh, int blk, int first, int parts,
-                                            int share, int tid, float* w) {
-  constexpr int V4 = HD / 4, U = 4;
-  const int rows = min(2 * a.rt, r.rows - blk * 2 * a.rt);
-  const int row0 = rows * share / parts, n = rows * (share + 1) / parts - row0;
-  const auto place = [&](int row, int& t, int& h) {
-    const int rg = blk * 2 * a.rt + row;
-    t = r.t0 + rg / a.G, h = kh * a.G + rg % a.G;
-  };
-  for (int i = tid; i < n; i += kStreamThreads) {
-    const auto ml = [&](int p) {
-      return __ldcg(reinterpret_cast<const float2*>(part_of<HD>(a, first + p, p == 0) + kBlock * HD) + row0 + i);
-    };
-    float m = -INFINITY, l = 0.f;
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, ml(p).x);
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
-      // (a part that saw none of the row's keys has l = 0 and no scale; a NaN in l stays one)
-      const float2 x = ml(p);
-      const float f = x.x == -INFINITY ? x.y : exp2_fast(x.x - m);
-      l += x.x == -INFINITY ? x.y : f * x.y;
-      w[i * parts + p] = f;
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    for (int p = 0; p < parts; ++p) w[i * parts + p] *= inv;
-    if (a.lse) {
-      int t, h;
-      place(row0 + i, t, h);
-      a.lse[(long long)t * a.H + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-    }
-  }
-  named_bar_sync(1, kStreamThreads);
+// Rows [row0, row0 + n) of a cut block, four columns a thread at a time: U of them side by side and the parts in steps of P, so
+// that U P loads are under way; the parts are added in their order either way.
+template <int HD, int U, int P, typename Place>
+__device__ __forceinline__ void sum_parts(const TreeAttnArgs& a, int first, int parts, int n, int row0, int tid, const float* w,
+                                          const Place& place) {
+  constexpr int V4 = HD / 4;
   for (int i0 = tid; i0 < n * V4; i0 += U * kStreamThreads) {
     float4 o[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-    for (int p = 0; p < parts; ++p) {
-      const float* part = part_of<HD>(a, first + p, p == 0) + row0 * HD;
-      float4 y[U];
+    for (int q = 0; q < parts; q += P) {
+      float4 y[P][U];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (i0 + u * kStreamThreads < n * V4) y[u] = __ldcg(reinterpret_cast<const float4*>(part) + i0 + u * kStreamThreads);
+      for (int p = 0; p < P; ++p)
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (i0 + u * kStreamThreads >= n * V4) continue;
-        const float f = w[(i0 + u * kStreamThreads) / V4 * parts + p];
-        o[u].x += f * y[u].x, o[u].y += f * y[u].y, o[u].z += f * y[u].z, o[u].w += f * y[u].w;
-      }
+        for (int u = 0; u < U; ++u)
+          if (q + p < parts && i0 + u * kStreamThreads < n * V4)
+            y[p][u] = __ldcg(reinterpret_cast<const float4*>(part_of<HD>(a, first + q + p, q + p == 0) + row0 * HD) + i0 + u * kStreamThreads);
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (q + p >= parts || i0 + u * kStreamThreads >= n * V4) continue;
+          const float f = w[(i0 + u * kStreamThreads) / V4 * parts + q + p];
+          o[u].x += f * y[p][u].x, o[u].y += f * y[p][u].y, o[u].z += f * y[p][u].z, o[u].w += f * y[p][u].w;
+        }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -477,6 +450,55 @@ __device__ __forceinline__ void merge_share(const TreeAttnArgs& a, const Request
           make_uint2(pack2(o[u].x, o[u].y, a.k_f16), pack2(o[u].z, o[u].w, a.k_f16));
     }
   }
+}
+
+// A CTA's share of a cut block's rows: the sum of the partial results in their order, by both streams' threads.  First every
+// part's weight in every row of the share, into shared memory (rows x parts is 256 and a little, however many of each);
+// then four columns a thread, several loads under way.  (8 query heads over 16 000 keys of one key head, 63 parts: 61 us with a
+// thread a row and two loads under way and ranges of one unit, 21 like this.)
+template <int HD>
+__device__ __forceinline__ void merge_share(const TreeAttnArgs& a, const Request& r, int kh, int blk, int first, int parts,
+                                            int share, int tid, float* w) {
+  constexpr int V4 = HD / 4;
+  const int rows = min(2 * a.rt, r.rows - blk * 2 * a.rt);
+  const int row0 = rows * share / parts, n = rows * (share + 1) / parts - row0;
+  const auto place = [&](int row, int& t, int& h) {
+    const int rg = blk * 2 * a.rt + row;
+    t = r.t0 + rg / a.G, h = kh * a.G + rg % a.G;
+  };
+  // Weights: a thread a row, or, of many parts (and so few rows), a warp a row.
+  const bool wide = parts >= 16;
+  const int lane = tid & 31, p0 = wide ? lane : 0, step = wide ? 32 : 1;
+  for (int i = wide ? tid >> 5 : tid; i < n; i += wide ? kStreamThreads / 32 : kStreamThreads) {
+    const auto ml = [&](int p) {
+      return __ldcg(reinterpret_cast<const float2*>(part_of<HD>(a, first + p, p == 0) + kBlock * HD) + row0 + i);
+    };
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+    for (int p = p0; p < parts; p += step) m = fmaxf(m, ml(p).x);
+    if (wide)
+      for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll 4
+    for (int p = p0; p < parts; p += step) {
+      // (a part that saw none of the row's keys has l = 0 and no scale; a NaN in l stays one)
+      const float2 x = ml(p);
+      const float f = x.x == -INFINITY ? x.y : exp2_fast(x.x - m);
+      l += x.x == -INFINITY ? x.y : f * x.y;
+      w[i * parts + p] = f;
+    }
+    if (wide)
+      for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    for (int p = p0; p < parts; p += step) w[i * parts + p] *= inv;
+    if (a.lse && p0 == 0) {
+      int t, h;
+      place(row0 + i, t, h);
+      a.lse[(long long)t * a.H + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    }
+  }
+  named_bar_sync(1, kStreamThreads);
+  if (n * V4 <= kStreamThreads) sum_parts<HD, 1, 8>(a, first, parts, n, row0, tid, w, place);
+  else sum_parts<HD, 4, 2>(a, first, parts, n, row0, tid, w, place);
 }
 
 __device__ __forceinline__ bool wait_count(const int* p, int want, unsigned int* err) {
@@ -567,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (w < other >> 5) before1 += sums[w];
       total += sums[w];
     }
-    const int ctas = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
+    const int ctas = (int)min((long long)gridDim.x, (total + kLeastUnits - 1) / kLeastUnits), cta = blockIdx.x;
     if (cta < ctas) {
       const long long u0 = quotient(cta * total, ctas), u1 = quotient((cta + 1LL) * total, ctas);
       const int most = (int)min(quotient(total, ctas * 6), 1LL << 20);
