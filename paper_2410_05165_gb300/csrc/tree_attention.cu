@@ -26,7 +26,7 @@
 //
 // Bound and measured: few rows over long caches by HBM (61 single tokens over 500 to 16 000 keys, 32 heads on 8 of 128: 188 us,
 // 6.2 TB/s); many rows by the streams' chain S, maximum, exponentials (1000 of 2900 clocks a tile), P, O, not by the tensor
-// pipe (29 to 43% busy): 16 trees of 240 tokens 82 us, 515 TFLOP/s; a prompt of 2 x 4001 tokens, heads of 64, 312 us, 780 TFLOP/s.
+// pipe (29 to 43% busy): 16 trees of 240 tokens 82 us, 515 TFLOP/s; a prompt of 2 x 4001 tokens, heads of 64, 315 us, 772 TFLOP/s.
 // A single token over 512 keys takes 13.7 us, all latency.
 //
 // Roles (384 threads): warp 0 copies (TMA), warps 1 and 2 issue the products of a stream each, warp 3 loads Q, warps 4-7 and
