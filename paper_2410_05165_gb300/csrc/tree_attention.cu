@@ -6,8 +6,8 @@
 // 128 keys once.  A tile is two products on tcgen05 with M =
 // 128 rows: S = Q K^T (both K-major in shared memory) into TMEM, and O += P V with P (16 bits) as TMEM operand over S's
 // columns and V in place, MN-major.  One thread a row runs the softmax from TMEM: no shuffles, no shared memory; O is scaled
-// only where the running maximum rises by more than 2^8 (all weights are relative to the maximum in use, so the quotient
-// is the same).
+// only where the running maximum rises by more than 2^8 (all weights are relative to the maximum in use, or to 2^-7 of it where
+// they are rounded to fp16, so the quotient is the same).
 //
 // Two streams of (S, P, O) share the tensor core, each with a warp that issues its products and a warpgroup that runs its
 // softmax.  Blocks of more than 128 rows: a stream is 128 of the rows, each sees every tile.  Fewer: both hold the same rows
@@ -52,6 +52,11 @@ constexpr int kBlock = 256;      // rows of a block, at most
 constexpr int kRoleRegs = 88, kStreamRegs = 208;
 static_assert(128 * kRoleRegs + kStreamThreads * kStreamRegs <= kThreads * 168, "registers at launch");
 constexpr float kSlack = 8.f;    // rise of the running maximum (log2) below which O keeps its scale
+// Where V and so P are fp16, weights are relative to 2^-7 of the maximum in use: fp16 ends at 2^-24 and the largest P would be
+// 2^kSlack of its 2^16, so that weights below 2^-25 of a large one would be 0 in P V, however many they are (20 000 keys 17.4 nats
+// below one whose V is 0: 100% off; with this below 1%, down to the 2^-32 of the maximum where a weight has no bits).
+constexpr float kRaise = 7.f;
+static_assert(kSlack + kRaise <= 15.f, "P in fp16");
 constexpr int kWalkBytes = 80;   // of a warp's place in the walk
 constexpr int kLeastUnits = 2;   // of a CTA's range (1: 2 to 14% slower over ten small calls, 3: 10 to 30% on most)
 constexpr int kMaxCtas = 512;    // counters in the workspace
@@ -839,7 +844,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int j = 0; j < 64; ++j)
             mx[j & 3] = fmaxf(mx[j & 3], fmaxf(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])));
-          const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.c);
+          const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.c - (VF16 ? kRaise : 0.f));
           const bool rise = mine && (m == -INFINITY ? m_new > m : m_new > m + kSlack);
           if (__builtin_expect(__any_sync(0xffffffffu, rise), 0)) {
             const float f = !rise ? 1.f : m == -INFINITY ? 0.f : exp2_fast(m - m_new);

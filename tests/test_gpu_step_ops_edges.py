@@ -1,0 +1,50 @@
+"""The batched serving step's operators where lengths, weights, states and streams are unusual."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+NEG = float("-inf")
+UNIT = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}   # unit roundoff
+TYPES = {"bf16": (torch.bfloat16, torch.bfloat16), "f16": (torch.float16, torch.float16), "mixed": (torch.bfloat16, torch.float16)}
+
+
+@pytest.fixture(scope="module")
+def ats():
+    import __graft_entry__
+    __graft_entry__.build()
+    import paper_2410_05165_gb300 as m
+    return m
+
+
+def _dev(a, dtype=torch.int32):
+    return torch.from_numpy(np.ascontiguousarray(a)).to("cuda", dtype)
+
+
+# ---------------------------------------------------------------------------------------------------
+# small weights beside a large one
+# ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("types", ["f16", "mixed", "bf16"])
+@pytest.mark.parametrize("L,heads", [(1, 320), (200, 160)])   # one row a block, and blocks of more than 128; whole blocks a CTA
+@pytest.mark.parametrize("score", [15.5, 17.0, 17.375, 20.0])
+def test_small_weights_add_up(ats, types, L, heads, score):
+    """One key with a value of 0 that is `score` nats above 20 000 others with a value of 1: the others' sum is the result."""
+    kt, vt = TYPES[types]
+    hd, page, ctx = 32, 256, 20000
+    pages = -(-(ctx + L) // page)
+    kc = torch.zeros(pages, page, heads, hd, dtype=kt, device="cuda")
+    vc = torch.ones(pages, page, heads, hd, dtype=vt, device="cuda")
+    kc[0, 0, :, 3], vc[0, 0] = score, 0
+    q = torch.zeros(L, heads, hd, dtype=kt, device="cuda")
+    q[:, :, 3] = 1
+    lse = torch.zeros(L, heads, device="cuda")
+    out = ats.op_tree_attention(q, kc, vc, _dev([0, L]), _dev([ctx]), _dev(np.arange(pages)[None]), scale=1.0, lse=lse)
+    assert ats.op_status(noalloc=True) == 0
+    n = (ctx + np.arange(L))[:, None, None].astype(np.float64)   # keys with a score of 0
+    ref, log_sum = n / (n + np.exp(score)), np.log(n + np.exp(score))
+    # weights rounded to V's type: UNIT of each, and in fp16 at least the 2^-32 of the largest below which a weight has no
+    # bits; exponentials and sums in 32 bits; the result rounded to q's type
+    tol = UNIT[kt] * ref + (UNIT[vt] + 1e-4) * ref + n * 2.0 ** -32
+    err = np.abs(out.double().cpu().numpy() - ref)
+    assert np.all(err <= tol), (err.max(), ref.max(), tol.min())
+    assert np.all(np.abs(lse.double().cpu().numpy() - log_sum[..., 0]) <= 1e-4 * (1 + log_sum[..., 0]))
