@@ -192,6 +192,7 @@ __global__ void __launch_bounds__(kThreads, 4) adjust_logits_kernel(const __grid
         });
       __syncthreads();
       base = s_n[warp];
+      __syncwarp();   // (every lane has it before a row's path adds to the list)
     }
     const char* in = in_row(row);
     char* out = static_cast<char*>(a.out) + (long long)row * a.ld_out * O::SIZE;

@@ -48,3 +48,42 @@ def test_small_weights_add_up(ats, types, L, heads, score):
     err = np.abs(out.double().cpu().numpy() - ref)
     assert np.all(err <= tol), (err.max(), ref.max(), tol.min())
     assert np.all(np.abs(lse.double().cpu().numpy() - log_sum[..., 0]) <= 1e-4 * (1 + log_sum[..., 0]))
+
+
+# ---------------------------------------------------------------------------------------------------
+# requests that change from row to row, each with a list and a path
+# ---------------------------------------------------------------------------------------------------
+def test_lists_of_requests_in_turn(ats):
+    """A few rows a request, so that a CTA's rows are of several: the path of a request's first row joins the list that was
+    made just before, and leaves it whole to the next row."""
+    rng = np.random.default_rng(41)
+    n, V = 300, 700
+    q_len = rng.integers(1, 6, size=n)
+    cu = np.concatenate([[0], np.cumsum(q_len)]).astype(np.int32)
+    R = int(cu[-1])
+    hist = rng.integers(0, 40, size=(n, 12)).astype(np.int32) + (np.arange(n)[:, None] % 600)
+    tok = rng.integers(0, V, size=R).astype(np.int32)
+    req = np.repeat(np.arange(n), q_len).astype(np.int32)
+    at = np.arange(R) - cu[req]
+    mask = np.array([(2 << i) - 1 for i in at], np.int32)[:, None]   # a chain: a token and all before it
+    x = torch.randn(R, V, device="cuda")
+    want = x.double().cpu().numpy()
+    for r in range(R):
+        b = req[r]
+        count, seen = np.zeros(V), np.zeros(V, bool)
+        path = tok[cu[b]:cu[b] + at[r] + 1]
+        np.add.at(count, np.concatenate([hist[b, 5:], path]), 1)
+        seen[hist[b, :5]] = True
+        y = want[r]
+        y = np.where(seen | (count > 0), np.where(y > 0, y / 1.25, y * 1.25), y)
+        want[r] = y - 0.5 * count - 3.0 * (count > 0)
+    full = lambda v: torch.full((n,), v, device="cuda")   # noqa: E731
+    rules = ats.LogitRules(hist=_dev(hist.ravel()), hist_off=_dev(12 * np.arange(n + 1)), prompt_len=_dev(np.full(n, 5)),
+                           repetition=full(1.25), frequency=full(0.5), presence=full(3.0), tree_tok=_dev(tok), cu_q=_dev(cu))
+    first = None
+    for _ in range(20):
+        got = ats.op_adjust_logits(x, _dev(req), rules, mask=_dev(mask))
+        first = got if first is None else first
+        assert torch.equal(got, first)
+    # four operations in 32 bits on terms of up to |x| + 12
+    assert np.all(np.abs(first.double().cpu().numpy() - want) <= 2.0 ** -21 * (np.abs(want) + 20))
