@@ -404,7 +404,8 @@ atspeed_status atspeed_op_tree_attention(atspeed_stream stream, const atspeed_kv
  *   x += bias_val[k] for the entries k in [bias_off[b], bias_off[b+1]) of token bias_tok[k] (a token listed twice: the
  *   later entry alone);
  *   row r of grammar state s = d_state[r] (a negative one: no grammar): tokens whose bit is not set in
- *   d_grammar[s * grammar_stride ..], lowest bit first, become -infinity, whatever their logit;
+ *   d_grammar[s * grammar_stride ..], lowest bit first, become -infinity, whatever their logit (a state of
+ *   n_states or above allows no token);
  *   x /= temperature (a temperature that is not above 0: not divided).
  * Tokens outside [0, vocab) are ignored.  Arithmetic in 32 bits, one rounding to the output's type. */
 typedef struct {

@@ -87,3 +87,20 @@ def test_lists_of_requests_in_turn(ats):
         assert torch.equal(got, first)
     # four operations in 32 bits on terms of up to |x| + 12
     assert np.all(np.abs(first.double().cpu().numpy() - want) <= 2.0 ** -21 * (np.abs(want) + 20))
+
+
+# ---------------------------------------------------------------------------------------------------
+# grammar states past the table
+# ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("inp", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [70, 9001])
+def test_a_grammar_state_past_the_table_allows_nothing(ats, V, inp):
+    x = torch.randn(5, V, device="cuda").to(inp)
+    words = -(-V // 32)
+    rules = ats.LogitRules(n_req=1, grammar=torch.full((2, words), -1, dtype=torch.int32, device="cuda"),
+                           bias_off=_dev([0, 1]), bias_tok=_dev([5]), bias_val=torch.full((1,), 3.0, device="cuda"))
+    got = ats.op_adjust_logits(x, _dev([0, 0, 0, -1, 0]), rules, state=_dev([1, 2, 2 ** 31 - 1, 5, -1]))
+    assert bool((got[1:4] == NEG).all())
+    want = x.float()
+    want[:, 5] += 3
+    assert torch.equal(got[[0, 4]], want.to(inp)[[0, 4]])
