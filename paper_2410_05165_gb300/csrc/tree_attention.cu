@@ -59,7 +59,7 @@ constexpr float kRaise = 7.f;
 static_assert(kSlack + kRaise <= 15.f, "P in fp16");
 constexpr int kWalkBytes = 80;   // of a warp's place in the walk
 constexpr int kLeastUnits = 2;   // of a CTA's range (1: 2 to 14% slower over ten small calls, 3: 10 to 30% on most)
-constexpr int kMaxCtas = 512;    // counters in the workspace
+constexpr int kMaxCtas = 256;    // of a grid: counters in the workspace, and a share's weights in shared memory (below)
 
 template <int HD>
 struct Cfg {
@@ -70,7 +70,10 @@ struct Cfg {
   static constexpr int STAGES = HD == 128 ? 5 : 8;
   static constexpr int Q_OFF = STAGES * TILE;
   static constexpr int X_OFF = Q_OFF + 2 * Q_TILE;       // (m, l) of both streams' rows
-  static constexpr int BAR_OFF = X_OFF + kStreamThreads * 8;
+  static constexpr int X_BYTES = kStreamThreads * 8;     // .. and, when they are done, the weights of a share of a cut block
+  // (a share of 1 / parts of a block's rows, rounded up, by parts: at most rows + parts - 1 weights)
+  static_assert((kBlock + kMaxCtas - 1) * (int)sizeof(float) <= X_BYTES, "weights of a share");
+  static constexpr int BAR_OFF = X_OFF + X_BYTES;
   static constexpr int WALK_OFF = BAR_OFF + 256, START_OFF = WALK_OFF + 8 * kWalkBytes;
   static constexpr int SMEM = START_OFF + 64;
   static constexpr int S_COL = 128, O_COL = 256;       // TMEM columns: S / P of stream s at s * 128, O at 256 + s * HD
@@ -458,7 +461,7 @@ __device__ __forceinline__ void sum_parts(const TreeAttnArgs& a, int first, int 
 }
 
 // A CTA's share of a cut block's rows: the sum of the partial results in their order, by both streams' threads.  First every
-// part's weight in every row of the share, into shared memory (rows x parts is 256 and a little, however many of each);
+// part's weight in every row of the share, into shared memory (at most 256 + parts - 1 of them, however many of each);
 // then four columns a thread, several loads under way.  (8 query heads over 16 000 keys of one key head, 63 parts: 61 us with a
 // thread a row and two loads under way and ranges of one unit, 21 like this.)
 template <int HD>
@@ -1086,8 +1089,8 @@ int sm_count() {
   return gemm_grid_size(dev);
 }
 
-constexpr size_t kCounterBytes = 2 * kMaxCtas * sizeof(int);
-static_assert(kCounterBytes == ATSPEED_TREE_ATTENTION_COUNTER_BYTES, "the workspace's counters");
+constexpr size_t kCounterBytes = ATSPEED_TREE_ATTENTION_COUNTER_BYTES;
+static_assert(2 * kMaxCtas * sizeof(int) <= kCounterBytes, "the workspace's counters");
 
 }  // namespace
 
