@@ -104,3 +104,26 @@ def test_a_grammar_state_past_the_table_allows_nothing(ats, V, inp):
     want = x.float()
     want[:, 5] += 3
     assert torch.equal(got[[0, 4]], want.to(inp)[[0, 4]])
+
+
+# ---------------------------------------------------------------------------------------------------
+# a wait that gives up
+# ---------------------------------------------------------------------------------------------------
+def test_a_wait_that_gives_up_is_reported(ats):
+    """Counters of partial results that start far below zero: the CTAs that wait for them give up after the kernel's own limit
+    and return, the status says so once, and with the counters zeroed the same call is right."""
+    from paper_2410_05165_gb300 import binding
+    kc, vc = (torch.randn(300, 16, 1, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(1, 4, 64, device="cuda").to(torch.bfloat16)
+    args = (q, kc, vc, _dev([0, 1]), _dev([4700]), _dev(np.arange(300)[None]))
+    want = ats.op_tree_attention(*args)   # (one block of 37 tiles: cut for many CTAs)
+    assert ats.op_status(noalloc=True) == ats.OK
+    w = binding.op_tree_attention_workspace(q.device, torch.cuda.current_stream().cuda_stream)
+    counters = w[:binding.TREE_ATTENTION_COUNTER_BYTES].view(torch.int32)
+    counters[:torch.cuda.get_device_properties(0).multi_processor_count] = -100000   # (the arrivals come first)
+    ats.op_tree_attention(*args)
+    assert ats.op_status(noalloc=True) == ats.E_TIMEOUT
+    assert ats.op_status(noalloc=True) == ats.OK
+    assert int(counters.abs().max()) == 0
+    assert torch.equal(ats.op_tree_attention(*args), want)
+    assert ats.op_status(noalloc=True) == ats.OK
