@@ -460,12 +460,17 @@ def _given(t: Optional[torch.Tensor], dtype, n: int, what: str) -> int:
     return _tensor(t, dtype, n, what)
 
 
-def _new(shape, dtype, device, stream) -> torch.Tensor:
-    """An output of a call on `stream`: its memory is not given to others before the stream is done with it."""
-    t = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None:
-        t.record_stream(stream)
-    return t
+def _outputs(device, stream, *specs) -> List[torch.Tensor]:
+    """Tensors (shape, dtype) for a call on `stream` to write.  They are of that stream's memory: what was given back on the
+    current one may still be read there.  The current stream, which uses them next, is recorded."""
+    if stream is None:
+        return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in specs]
+    here = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        out = [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in specs]
+    for t in out:
+        t.record_stream(here)
+    return out
 
 
 def _raw_stream(stream: Optional[torch.cuda.Stream], device) -> int:
@@ -519,10 +524,10 @@ def op_batch_plan(q_len: torch.Tensor, kv_len: torch.Tensor, block_table: torch.
     q_ptr, kv_ptr, up_ptr = _given(q_len, i32, n, "q_len"), _given(kv_len, i32, n, "kv_len"), _tensor(parent, i32, T, "parent")
     table_ptr = _given(block_table, i32, n, "block_table")
     free_ptr, n_free_ptr = _given(free, i32, 1, "free"), _given(n_free, i32, 1, "n_free")
-    cu_q, ctx_len, state = _new((n + 1,), i32, dev, stream), _new((n,), i32, dev, stream), _new((n,), i32, dev, stream)
-    pages, req, pos = _new((2,), i32, dev, stream), _new((T,), i32, dev, stream), _new((T,), i32, dev, stream)
-    slot = _new((T,), torch.int64, dev, stream)
-    mask = _new((T, mask_words), i32, dev, stream) if parent is not None else None
+    cu_q, ctx_len, state, pages, req, pos, slot, *trees = _outputs(
+        dev, stream, (n + 1, i32), (n, i32), (n, i32), (2, i32), (T, i32), (T, i32), (T, torch.int64),
+        *([((T, mask_words), i32)] if parent is not None else []))
+    mask = trees[0] if trees else None
     _check(load().atspeed_op_batch_plan(_raw_stream(stream, dev), n, q_ptr, kv_ptr, up_ptr, page_size, table_ptr,
                                         block_table.shape[1], free_ptr, n_free_ptr, T, mask_words, cu_q.data_ptr(),
                                         ctx_len.data_ptr(), state.data_ptr(), pages.data_ptr(), req.data_ptr(), pos.data_ptr(),
@@ -539,7 +544,7 @@ def op_rope_append(qkv: torch.Tensor, n_heads: int, kc: torch.Tensor, vc: torch.
     if qkv.dim() != 2 or src is None or not qkv.is_cuda or qkv.stride(1) != 1 or qkv.shape[1] != (n_heads + 2 * pages.n_kv_heads) * hd:
         _refuse(f"qkv: [T][({n_heads} + 2 * {pages.n_kv_heads}) * {hd}] on the device, not {tuple(qkv.shape)} {qkv.dtype}")
     T = qkv.shape[0]
-    q = _new((T, n_heads, hd), kc.dtype, qkv.device, stream)
+    q, = _outputs(qkv.device, stream, ((T, n_heads, hd), kc.dtype))
     _check(load().atspeed_op_rope_append(_raw_stream(stream, qkv.device), qkv.data_ptr(), src, qkv.stride(0), T, n_heads, pages,
                                          _given(slot, torch.int64, T, "slot"), _tensor(pos, torch.int32, T, "pos"), theta,
                                          q.data_ptr() if n_heads else None, n_heads * hd))
@@ -575,7 +580,7 @@ def op_tree_attention(q: torch.Tensor, kc: torch.Tensor, vc: torch.Tensor, cu_q:
         _refuse(f"q: [T][heads][{hd}] of {kc.dtype} on the device, each row contiguous, not {tuple(q.shape)} {q.dtype}")
     T, H, _ = q.shape
     if out is None:
-        out = _new(q.shape, q.dtype, q.device, stream)
+        out, = _outputs(q.device, stream, (q.shape, q.dtype))
     elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1 or out.stride(1) != hd or not out.is_cuda:
         _refuse(f"out: as q {tuple(q.shape)} {q.dtype}, each row contiguous, not {tuple(out.shape)} {out.dtype}")
     if block_table.dim() != 2 or block_table.shape[0] < n or (mask is not None and (mask.dim() != 2 or mask.shape[0] < T)):
@@ -627,7 +632,7 @@ def op_adjust_logits(logits: torch.Tensor, req: torch.Tensor, rules: LogitRules,
         _refuse(f"logits: [R][vocab] on the device, not {tuple(logits.shape)} {logits.dtype}")
     R, V = logits.shape
     if out is None:
-        out = _new((R, V), out_dtype or logits.dtype, logits.device, stream)
+        out, = _outputs(logits.device, stream, ((R, V), out_dtype or logits.dtype))
     ot = _DTYPES.get(out.dtype)
     if out.shape != logits.shape or ot is None or not out.is_cuda or (out.stride(1) != 1 and V != 1):
         _refuse(f"out: [{R}][{V}] on the device, not {tuple(out.shape)} {out.dtype}")

@@ -127,3 +127,59 @@ def test_a_wait_that_gives_up_is_reported(ats):
     assert int(counters.abs().max()) == 0
     assert torch.equal(ats.op_tree_attention(*args), want)
     assert ats.op_status(noalloc=True) == ats.OK
+
+
+# ---------------------------------------------------------------------------------------------------
+# streams
+# ---------------------------------------------------------------------------------------------------
+def _calls(ats):
+    """Each operator's call on a stream: the output that is looked at, as a function of the stream."""
+    kc, vc = (torch.randn(60, 16, 2, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(9, 4, 64, device="cuda").to(torch.bfloat16)
+    cu, ctx, table = _dev([0, 1, 9]), _dev([300, 100]), _dev(np.arange(60).reshape(2, 30))
+    qkv, slot = torch.randn(9, 8 * 64, device="cuda"), torch.arange(900, 909, device="cuda")
+    x, req = torch.randn(9, 1003, device="cuda"), _dev([0] + [1] * 8)
+    rules = ats.LogitRules(n_req=2, temperature=torch.full((2,), 0.5, device="cuda"))
+    q_len, kv_len, n_free = _dev([1, 8]), _dev([300, 100]), _dev([5])
+    return {"plan": lambda s: ats.op_batch_plan(q_len, kv_len, table, table.flatten(), n_free, 16, 9, stream=s).slot,
+            "append": lambda s: ats.op_rope_append(qkv, 4, kc, vc, slot, stream=s),
+            "attention": lambda s: ats.op_tree_attention(q, kc, vc, cu, ctx, table, stream=s),
+            "logits": lambda s: ats.op_adjust_logits(x, req, rules, stream=s)}
+
+
+@pytest.mark.parametrize("op", ["plan", "append", "attention", "logits"])
+def test_outputs_on_a_stream_take_no_memory_that_the_current_one_reads(ats, op):
+    """Memory given back on the current stream, with a read of it still to come there, is not what a call on another stream
+    writes its output into."""
+    call, s = _calls(ats)[op], torch.cuda.Stream()
+    want = call(None).clone()
+    torch.cuda.synchronize()
+    old = torch.full_like(want, 5)
+    kept, at = torch.empty_like(old), old.data_ptr()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)   # (some 50 ms)
+    kept.copy_(old)
+    del old
+    out = call(s)
+    assert out.data_ptr() != at
+    torch.cuda.synchronize()
+    assert bool((kept == 5).all()) and torch.equal(out, want)
+
+
+@pytest.mark.parametrize("op", ["plan", "append", "attention", "logits"])
+def test_outputs_on_a_stream_stay_until_the_current_one_has_read_them(ats, op):
+    """Given back with a read of it still to come on the current stream, an output is not the next tensor of its own stream."""
+    call, s = _calls(ats)[op], torch.cuda.Stream()
+    want = call(None).clone()
+    torch.cuda.synchronize()
+    out = call(s)
+    s.synchronize()
+    kept, at = torch.empty_like(out), out.data_ptr()
+    torch.cuda._sleep(100_000_000)
+    kept.copy_(out)
+    del out
+    with torch.cuda.stream(s):
+        other = torch.full_like(want, 5)
+    assert other.data_ptr() != at
+    torch.cuda.synchronize()
+    assert torch.equal(kept, want)
