@@ -388,6 +388,9 @@ atspeed_status atspeed_op_rope_append(atspeed_stream stream, const void *d_qkv, 
  * order that the lengths alone fix: the same call gives the same bits, a request's last bits may differ in another batch.
  * Device-side timeouts surface through atspeed_op_status(stream, NULL); after one, zero those bytes again. */
 #define ATSPEED_TREE_ATTENTION_COUNTER_BYTES 4096
+/* The id of the capture (into a CUDA graph) that `stream` is part of, 0 for a stream that is not captured: a workspace used by
+ * captured calls belongs to their graph, which zeroes its counters itself.  Not part of the paper. */
+uint64_t atspeed_op_capture_id(atspeed_stream stream);
 size_t atspeed_op_tree_attention_workspace(void);
 atspeed_status atspeed_op_tree_attention(atspeed_stream stream, const atspeed_kv_pages *cache, const void *d_q,
                                          int64_t q_stride, int n_heads, int n_req, int T, const int32_t *d_cu_q,

@@ -31,7 +31,7 @@ EXPORTS = [
     "atspeed_debug_node_logits", "atspeed_debug_node_lse", "atspeed_debug_buffer", "atspeed_set_tree", "atspeed_op_workspace_bytes", "atspeed_op_gemm",
     "atspeed_op_gemm_noalloc", "atspeed_op_status", "atspeed_op_gemm_swiglu", "atspeed_op_rmsnorm", "atspeed_op_attention_scratch", "atspeed_op_attention",
     "atspeed_op_batch_plan", "atspeed_op_rope_append", "atspeed_op_tree_attention_workspace", "atspeed_op_tree_attention",
-    "atspeed_op_adjust_logits",
+    "atspeed_op_adjust_logits", "atspeed_op_capture_id",
 ]
 
 
@@ -134,6 +134,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "atspeed_op_tree_attention_workspace": (ctypes.c_size_t, []),
         "atspeed_op_tree_attention": (c_int, [vp, ctypes.POINTER(KvPages), vp, ctypes.c_int64, c_int, c_int, c_int, vp, vp,
                                               vp, c_int, vp, c_int, ctypes.c_float, vp, ctypes.c_int64, vp, vp]),
+        "atspeed_op_capture_id": (ctypes.c_uint64, [vp]),
         "atspeed_op_adjust_logits": (c_int, [vp, vp, c_int, ctypes.c_int64, c_int, c_int, vp,
                                              ctypes.POINTER(LogitRulesDesc), vp, c_int, vp, vp, c_int, ctypes.c_int64]),
     }
@@ -555,17 +556,24 @@ _tree_ws: Dict[Tuple[int, int], torch.Tensor] = {}
 TREE_ATTENTION_COUNTER_BYTES = 4096
 
 
+def _new_tree_workspace(device, stream: int) -> torch.Tensor:
+    """Allocated and its counters zeroed on the stream whose calls use it, so that both come before them."""
+    on = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    with torch.cuda.stream(on):
+        w = torch.empty(load().atspeed_op_tree_attention_workspace(), dtype=torch.uint8, device=device)
+        w[:TREE_ATTENTION_COUNTER_BYTES].zero_()
+    return w
+
+
 def op_tree_attention_workspace(device, stream: int) -> torch.Tensor:
     """The attention's workspace of one stream (calls on one stream follow each other; two streams' would not).  While a stream
     is captured that has none, one of the graph's own memory, whose counters the graph itself clears."""
     key = (device.index or 0, stream)
     if key not in _tree_ws:
-        if torch.cuda.is_current_stream_capturing():
-            w = torch.empty(load().atspeed_op_tree_attention_workspace(), dtype=torch.uint8, device=device)
-            w[:TREE_ATTENTION_COUNTER_BYTES].zero_()
+        w = _new_tree_workspace(device, stream)
+        if load().atspeed_op_capture_id(stream):
             return w
-        _tree_ws[key] = torch.zeros(load().atspeed_op_tree_attention_workspace(), dtype=torch.uint8, device=device)
-        torch.cuda.current_stream(device).synchronize()   # (the zeros come before a call on whatever stream)
+        _tree_ws[key] = w
     return _tree_ws[key]
 
 

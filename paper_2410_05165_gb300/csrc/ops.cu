@@ -279,6 +279,16 @@ atspeed_status atspeed_op_gemm_noalloc(atspeed_stream stream, const void* d_W, c
   return gemm_status(gemm_launch(a, s, kNoAllocGrid, kNoAllocGrid, (cudaStream_t)stream, false, eb, sizeof eb));
 }
 
+uint64_t atspeed_op_capture_id(atspeed_stream stream) {
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+  unsigned long long id = 0;
+  if (cudaStreamGetCaptureInfo((cudaStream_t)stream, &status, &id) != cudaSuccess) {
+    cudaGetLastError();   // (the legacy stream beside a capture, or no GPU: not captured)
+    return 0;
+  }
+  return status == cudaStreamCaptureStatusActive ? id : 0;
+}
+
 /* See include/atspeed.h.  Reads (and clears) the error words that the operators' bounded waits set. */
 atspeed_status atspeed_op_status(atspeed_stream stream, void* d_ws) {
   unsigned int* words[3] = {nullptr, nullptr, nullptr};

@@ -183,3 +183,28 @@ def test_outputs_on_a_stream_stay_until_the_current_one_has_read_them(ats, op):
     assert other.data_ptr() != at
     torch.cuda.synchronize()
     assert torch.equal(kept, want)
+
+
+def test_attention_on_a_stream_that_a_capture_forks_to(ats):
+    """The workspace of a captured call is of the stream that the call is on, not of the one that was current: its counters are
+    zeroed before the call, and its memory is not given to the capturing stream's next tensors."""
+    kc, vc = (torch.randn(60, 16, 2, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(9, 4, 64, device="cuda").to(torch.bfloat16)
+    args = (_dev([0, 1, 9]), _dev([300, 100]), _dev(np.arange(60).reshape(2, 30)))
+    want = ats.op_tree_attention(q, kc, vc, *args)
+    out = torch.zeros(3, *q.shape, dtype=q.dtype, device="cuda")
+    main, side, g = torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=main):
+        side.wait_stream(main)
+        others = []
+        for i in range(3):
+            ats.op_tree_attention(q, kc, vc, *args, out=out[i], stream=side)
+            others.append(torch.full((50_000_000,), 255, dtype=torch.uint8, device="cuda"))   # (more than a workspace)
+        main.wait_stream(side)
+    for _ in range(5):
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want) for o in out) and all(bool((x == 255).all()) for x in others)
+    assert ats.op_status(noalloc=True) == ats.OK
