@@ -553,6 +553,7 @@ def op_rope_append(qkv: torch.Tensor, n_heads: int, kc: torch.Tensor, vc: torch.
 
 
 _tree_ws: Dict[Tuple[int, int], torch.Tensor] = {}
+_graph_ws: Dict[Tuple[int, int], Tuple[int, torch.Tensor]] = {}   # of the last capture that a stream was part of
 TREE_ATTENTION_COUNTER_BYTES = 4096
 
 
@@ -566,14 +567,17 @@ def _new_tree_workspace(device, stream: int) -> torch.Tensor:
 
 
 def op_tree_attention_workspace(device, stream: int) -> torch.Tensor:
-    """The attention's workspace of one stream (calls on one stream follow each other; two streams' would not).  While a stream
-    is captured that has none, one of the graph's own memory, whose counters the graph itself clears."""
+    """The attention's workspace of one stream (calls on one stream follow each other; two streams' would not).  Calls that are
+    captured have one of their own, whatever the stream had before: a graph is replayed on any stream, beside this one's calls
+    and other graphs.  It is of the graph's own memory, and the graph clears its counters before the first call."""
     key = (device.index or 0, stream)
+    capture = load().atspeed_op_capture_id(stream)
+    if capture:
+        if _graph_ws.get(key, (0, None))[0] != capture:
+            _graph_ws[key] = (capture, _new_tree_workspace(device, stream))
+        return _graph_ws[key][1]
     if key not in _tree_ws:
-        w = _new_tree_workspace(device, stream)
-        if load().atspeed_op_capture_id(stream):
-            return w
-        _tree_ws[key] = w
+        _tree_ws[key] = _new_tree_workspace(device, stream)
     return _tree_ws[key]
 
 

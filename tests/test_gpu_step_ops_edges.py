@@ -208,3 +208,66 @@ def test_attention_on_a_stream_that_a_capture_forks_to(ats):
         torch.cuda.synchronize()
         assert all(torch.equal(o, want) for o in out) and all(bool((x == 255).all()) for x in others)
     assert ats.op_status(noalloc=True) == ats.OK
+
+
+def test_captured_attention_shares_no_workspace(ats, monkeypatch):
+    """Two graphs captured on a stream that had a workspace: each has its own, one for all its calls, and replays beside each
+    other and beside calls on that stream are right."""
+    from paper_2410_05165_gb300 import binding
+    kc, vc = (torch.randn(300, 16, 1, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+    qs = torch.randn(3, 4, 8, 64, device="cuda").to(torch.bfloat16)
+    args = (_dev([0, 4]), _dev([4700]), _dev(np.arange(300)[None]))   # (one block, cut for many CTAs)
+    want = torch.stack([ats.op_tree_attention(q, kc, vc, *args) for q in qs])
+    got = torch.zeros_like(want)
+    torch.cuda.synchronize()
+    lib, used = binding.load(), []
+
+    class Watched:
+        def __getattr__(self, name):
+            f = getattr(lib, name)
+            if name != "atspeed_op_tree_attention":
+                return f
+            return lambda *a: used.append(a[-1]) or f(*a)
+
+    warm = torch.cuda.Stream()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    with monkeypatch.context() as m:
+        m.setattr(binding, "load", Watched)
+        with torch.cuda.stream(warm):
+            ats.op_tree_attention(qs[2], kc, vc, *args, out=got[2])
+        warm.synchronize()
+        for i, g in enumerate(graphs):
+            with torch.cuda.graph(g, stream=warm):
+                for _ in range(4):
+                    ats.op_tree_attention(qs[i], kc, vc, *args, out=got[i])
+    assert len(used) == 9 and len({used[0], used[1], used[5]}) == 3
+    assert len(set(used[1:5])) == 1 and len(set(used[5:])) == 1   # (one a graph, zeroed once)
+    assert not {used[1], used[5]} & {w.data_ptr() for w in binding._tree_ws.values()}
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        got.zero_()
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for g, s in zip(graphs, streams):
+                with torch.cuda.stream(s):
+                    g.replay()
+            with torch.cuda.stream(warm):
+                ats.op_tree_attention(qs[2], kc, vc, *args, out=got[2])
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+    assert ats.op_status(noalloc=True) == ats.OK
+
+
+def test_attention_on_two_streams_at_once(ats):
+    kc, vc = (torch.randn(300, 16, 1, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+    qs = torch.randn(2, 4, 8, 64, device="cuda").to(torch.bfloat16)
+    args = (_dev([0, 4]), _dev([4700]), _dev(np.arange(300)[None]))
+    want = torch.stack([ats.op_tree_attention(q, kc, vc, *args) for q in qs])
+    got = torch.zeros_like(want)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            ats.op_tree_attention(qs[i], kc, vc, *args, out=got[i], stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and ats.op_status(noalloc=True) == ats.OK
