@@ -397,9 +397,12 @@ def op_status(noalloc: bool = False, stream=None) -> int:
     ws = None if noalloc else op_workspace().data_ptr()
     status = int(load().atspeed_op_status(_stream(stream), ws))
     if noalloc and status != 0:   # a call that gave up leaves its counters as they are
-        for (device, st), w in _tree_ws.items():
-            with torch.cuda.stream(torch.cuda.ExternalStream(st, device=device)):
-                w[:TREE_ATTENTION_COUNTER_BYTES].zero_()
+        for device in {d for d, _ in _tree_ws}:   # (from here, not from their streams: some may be gone)
+            torch.cuda.synchronize(device)
+        for w in _tree_ws.values():
+            w[:TREE_ATTENTION_COUNTER_BYTES].zero_()
+        for device in {d for d, _ in _tree_ws}:
+            torch.cuda.synchronize(device)
     return status
 
 

@@ -271,3 +271,27 @@ def test_attention_on_two_streams_at_once(ats):
             ats.op_tree_attention(qs[i], kc, vc, *args, out=got[i], stream=s)
     torch.cuda.synchronize()
     assert torch.equal(got, want) and ats.op_status(noalloc=True) == ats.OK
+
+
+def test_a_timeout_once_read_asks_nothing_of_a_stream_that_is_gone(ats, monkeypatch):
+    """(The status is a fake's.)  The workspace of a stream that its owner has destroyed is cleared with the others."""
+    import ctypes
+
+    from paper_2410_05165_gb300 import binding
+    rt, handle = torch.cuda.cudart(), ctypes.c_size_t()
+    assert int(rt.cudaStreamCreate(ctypes.addressof(handle))) == 0
+    w = binding.op_tree_attention_workspace(torch.device("cuda", 0), handle.value)
+    torch.cuda.synchronize()
+    assert int(rt.cudaStreamDestroy(handle.value)) == 0
+    w[:64] = 1
+
+    class Failed:
+        @staticmethod
+        def atspeed_op_status(stream, ws):
+            return binding.E_TIMEOUT
+
+    with monkeypatch.context() as m:
+        m.setattr(binding, "load", lambda: Failed)
+        assert binding.op_status(noalloc=True) == binding.E_TIMEOUT
+    assert int(w[:binding.TREE_ATTENTION_COUNTER_BYTES].sum()) == 0
+    binding._tree_ws.pop((0, handle.value))
