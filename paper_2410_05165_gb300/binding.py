@@ -448,20 +448,29 @@ def _refuse(what: str):
     raise AtSpeedError(E_ARG, what)
 
 
-def _tensor(t: Optional[torch.Tensor], dtype, n: int, what: str) -> Optional[int]:
-    """The address of a contiguous device tensor of the given type with n elements or more; None for None."""
+def _gpu(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> int:
+    """The GPU of a call: its tensors' and its stream's, and the current one, on which the library launches.  (By numbers: ten
+    comparisons of torch.device objects cost a call a microsecond more.)"""
+    gpu = t.get_device()
+    if gpu < 0 or gpu != torch._C._cuda_getDevice() or (stream is not None and stream.device.index != gpu):
+        _refuse(f"tensors on {t.device}, stream on {'it' if stream is None else stream.device}: not both the current device")
+    return gpu
+
+
+def _tensor(t: Optional[torch.Tensor], dtype, n: int, what: str, gpu: int) -> Optional[int]:
+    """The address of a contiguous tensor on a GPU of the given type with n elements or more; None for None."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.numel() < n or not t.is_cuda or not t.is_contiguous():
-        _refuse(f"{what}: {dtype} on the device, contiguous, {n} elements or more, not {tuple(t.shape)} {t.dtype} {t.device}")
+    if t.dtype is not dtype or t.numel() < n or t.get_device() != gpu or not t.is_contiguous():
+        _refuse(f"{what}: {dtype} on GPU {gpu}, contiguous, {n} elements or more, not {tuple(t.shape)} {t.dtype} {t.device}")
     return t.data_ptr()
 
 
-def _given(t: Optional[torch.Tensor], dtype, n: int, what: str) -> int:
+def _given(t: Optional[torch.Tensor], dtype, n: int, what: str, gpu: int) -> int:
     """The same for an argument that has to be there."""
     if t is None:
         _refuse(f"{what}: missing")
-    return _tensor(t, dtype, n, what)
+    return _tensor(t, dtype, n, what, gpu)
 
 
 def _outputs(device, stream, *specs) -> List[torch.Tensor]:
@@ -481,14 +490,14 @@ def _raw_stream(stream: Optional[torch.cuda.Stream], device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
 
-def _kv_pages(kc: torch.Tensor, vc: torch.Tensor) -> KvPages:
+def _kv_pages(kc: torch.Tensor, vc: torch.Tensor, gpu: int) -> KvPages:
     """Caches [pages][page_size][kv heads][head_dim], any strides but the last (a head-by-head cache: transpose(1, 2))."""
     shape, ks, vs = kc.shape, kc.stride(), vc.stride()
     kt, vt = _DTYPES.get(kc.dtype), _DTYPES.get(vc.dtype)
-    if len(shape) != 4 or shape != vc.shape or ks[3] != 1 or vs[3] != 1 or kt is None or vt is None or not (kc.is_cuda and
-                                                                                                            vc.is_cuda):
-        _refuse(f"caches: two [pages][page_size][heads][head_dim] on the device, not {tuple(shape)} {kc.dtype} and "
-                f"{tuple(vc.shape)} {vc.dtype}")
+    if (len(shape) != 4 or shape != vc.shape or ks[3] != 1 or vs[3] != 1 or kt is None or vt is None or kc.get_device() != gpu or
+            vc.get_device() != gpu):
+        _refuse(f"caches: two [pages][page_size][heads][head_dim] on GPU {gpu}, not {tuple(shape)} {kc.dtype} {kc.device} and "
+                f"{tuple(vc.shape)} {vc.dtype} {vc.device}")
     return KvPages.from_buffer_copy(_KV_PACK(kc.data_ptr(), vc.data_ptr(), kt, vt, shape[0], shape[1], shape[2], shape[3],
                                              ks[0], ks[1], ks[2], vs[0], vs[1], vs[2]))   # (0.5 us; field by field 1.3)
 
@@ -522,12 +531,12 @@ def op_batch_plan(q_len: torch.Tensor, kv_len: torch.Tensor, block_table: torch.
                   n_free: torch.Tensor, page_size: int, max_tokens: int, parent: Optional[torch.Tensor] = None,
                   mask_words: int = 0, stream=None) -> BatchPlan:
     """Pages, slots, positions and tree masks of a step from the requests' lengths; block_table is extended in place."""
-    n, T, i32, dev = q_len.numel(), max_tokens, torch.int32, q_len.device
+    n, T, i32, dev, gpu = q_len.numel(), max_tokens, torch.int32, q_len.device, _gpu(q_len, stream)
     if block_table.dim() != 2 or block_table.shape[0] != n or T <= 0 or n == 0 or (parent is not None and mask_words <= 0):
         _refuse(f"{n} requests, {T} tokens, block_table {tuple(block_table.shape)}, {mask_words} mask words")
-    q_ptr, kv_ptr, up_ptr = _given(q_len, i32, n, "q_len"), _given(kv_len, i32, n, "kv_len"), _tensor(parent, i32, T, "parent")
-    table_ptr = _given(block_table, i32, n, "block_table")
-    free_ptr, n_free_ptr = _given(free, i32, 1, "free"), _given(n_free, i32, 1, "n_free")
+    q_ptr, kv_ptr, up_ptr = _given(q_len, i32, n, "q_len", gpu), _given(kv_len, i32, n, "kv_len", gpu), _tensor(parent, i32, T, "parent", gpu)
+    table_ptr = _given(block_table, i32, n, "block_table", gpu)
+    free_ptr, n_free_ptr = _given(free, i32, 1, "free", gpu), _given(n_free, i32, 1, "n_free", gpu)
     cu_q, ctx_len, state, pages, req, pos, slot, *trees = _outputs(
         dev, stream, (n + 1, i32), (n, i32), (n, i32), (2, i32), (T, i32), (T, i32), (T, torch.int64),
         *([((T, mask_words), i32)] if parent is not None else []))
@@ -543,14 +552,15 @@ def op_rope_append(qkv: torch.Tensor, n_heads: int, kc: torch.Tensor, vc: torch.
                    pos: Optional[torch.Tensor] = None, theta: float = 10000.0, stream=None) -> torch.Tensor:
     """Rotates q and k of fused QKV rows [T][(heads + 2 kv heads) * head_dim], stores k and v by slot, returns q
     [T][heads][head_dim]."""
-    pages = _kv_pages(kc, vc)
+    dev, gpu = qkv.device, _gpu(qkv, stream)
+    pages = _kv_pages(kc, vc, gpu)
     hd, src = pages.head_dim, _DTYPES.get(qkv.dtype)
-    if qkv.dim() != 2 or src is None or not qkv.is_cuda or qkv.stride(1) != 1 or qkv.shape[1] != (n_heads + 2 * pages.n_kv_heads) * hd:
-        _refuse(f"qkv: [T][({n_heads} + 2 * {pages.n_kv_heads}) * {hd}] on the device, not {tuple(qkv.shape)} {qkv.dtype}")
+    if qkv.dim() != 2 or src is None or qkv.stride(1) != 1 or qkv.shape[1] != (n_heads + 2 * pages.n_kv_heads) * hd:
+        _refuse(f"qkv: [T][({n_heads} + 2 * {pages.n_kv_heads}) * {hd}], not {tuple(qkv.shape)} {qkv.dtype}")
     T = qkv.shape[0]
-    q, = _outputs(qkv.device, stream, ((T, n_heads, hd), kc.dtype))
-    _check(load().atspeed_op_rope_append(_raw_stream(stream, qkv.device), qkv.data_ptr(), src, qkv.stride(0), T, n_heads, pages,
-                                         _given(slot, torch.int64, T, "slot"), _tensor(pos, torch.int32, T, "pos"), theta,
+    q, = _outputs(dev, stream, ((T, n_heads, hd), kc.dtype))
+    _check(load().atspeed_op_rope_append(_raw_stream(stream, dev), qkv.data_ptr(), src, qkv.stride(0), T, n_heads, pages,
+                                         _given(slot, torch.int64, T, "slot", gpu), _tensor(pos, torch.int32, T, "pos", gpu), theta,
                                          q.data_ptr() if n_heads else None, n_heads * hd))
     return q
 
@@ -589,26 +599,27 @@ def op_tree_attention(q: torch.Tensor, kc: torch.Tensor, vc: torch.Tensor, cu_q:
                       out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of q [T][heads][head_dim] (rows any stride apart) over the batch's paged caches and, by the mask's bits
     (None: causal), the step's own tokens.  scale: 1 / sqrt(head_dim) by default."""
-    pages = _kv_pages(kc, vc)
+    dev, gpu = q.device, _gpu(q, stream)
+    pages = _kv_pages(kc, vc, gpu)
     n, hd = ctx_len.numel(), pages.head_dim
-    if q.dim() != 3 or q.dtype is not kc.dtype or q.shape[2] != hd or q.stride(2) != 1 or q.stride(1) != hd or not q.is_cuda:
-        _refuse(f"q: [T][heads][{hd}] of {kc.dtype} on the device, each row contiguous, not {tuple(q.shape)} {q.dtype}")
+    if q.dim() != 3 or q.dtype is not kc.dtype or q.shape[2] != hd or q.stride(2) != 1 or q.stride(1) != hd:
+        _refuse(f"q: [T][heads][{hd}] of {kc.dtype}, each row contiguous, not {tuple(q.shape)} {q.dtype}")
     T, H, _ = q.shape
     if out is None:
-        out, = _outputs(q.device, stream, (q.shape, q.dtype))
-    elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1 or out.stride(1) != hd or not out.is_cuda:
-        _refuse(f"out: as q {tuple(q.shape)} {q.dtype}, each row contiguous, not {tuple(out.shape)} {out.dtype}")
+        out, = _outputs(dev, stream, (q.shape, q.dtype))
+    elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1 or out.stride(1) != hd or out.get_device() != gpu:
+        _refuse(f"out: as q {tuple(q.shape)} {q.dtype} on {dev}, each row contiguous, not {tuple(out.shape)} {out.dtype} {out.device}")
     if block_table.dim() != 2 or block_table.shape[0] < n or (mask is not None and (mask.dim() != 2 or mask.shape[0] < T)):
         _refuse(f"block_table: [{n}][width] and mask: [{T}][words], not {tuple(block_table.shape)} and "
                 f"{None if mask is None else tuple(mask.shape)}")
-    st = _raw_stream(stream, q.device)
+    st = _raw_stream(stream, dev)
     _check(load().atspeed_op_tree_attention(st, pages, q.data_ptr(), q.stride(0), H, n, T,
-                                            _given(cu_q, torch.int32, n + 1, "cu_q"), _given(ctx_len, torch.int32, 1, "ctx_len"),
-                                            _given(block_table, torch.int32, n, "block_table"), block_table.shape[1],
-                                            _tensor(mask, torch.int32, T, "mask"), mask.shape[1] if mask is not None else 0,
+                                            _given(cu_q, torch.int32, n + 1, "cu_q", gpu), _given(ctx_len, torch.int32, 1, "ctx_len", gpu),
+                                            _given(block_table, torch.int32, n, "block_table", gpu), block_table.shape[1],
+                                            _tensor(mask, torch.int32, T, "mask", gpu), mask.shape[1] if mask is not None else 0,
                                             hd ** -0.5 if scale is None else scale, out.data_ptr(), out.stride(0),
-                                            _tensor(lse, torch.float32, T * H, "lse"),
-                                            op_tree_attention_workspace(q.device, st).data_ptr()))
+                                            _tensor(lse, torch.float32, T * H, "lse", gpu),
+                                            op_tree_attention_workspace(dev, st).data_ptr()))
     return out
 
 
@@ -627,34 +638,39 @@ class LogitRules:
         self._keep = (hist, hist_off, prompt_len, repetition, frequency, presence, temperature, bias_off, bias_tok, bias_val,
                       grammar, tree_tok, cu_q)
         self.n_req = n_req
+        gpu = self.gpu = next((t.get_device() for t in self._keep if t is not None), None)   # (no tensor: of any)
+        if gpu == -1:
+            _refuse("rules on the CPU")
         self.desc = LogitRulesDesc(
-            n_req, _tensor(hist, i32, 0, "hist"), _tensor(hist_off, i32, n_req + 1, "hist_off"),
-            _tensor(prompt_len, i32, n_req, "prompt_len"), _tensor(repetition, f32, n_req, "repetition"),
-            _tensor(frequency, f32, n_req, "frequency"), _tensor(presence, f32, n_req, "presence"),
-            _tensor(temperature, f32, n_req, "temperature"), _tensor(bias_off, i32, n_req + 1, "bias_off"),
-            _tensor(bias_tok, i32, 0, "bias_tok"),
-            _tensor(bias_val, f32, 0 if bias_tok is None else bias_tok.numel(), "bias_val"), _tensor(grammar, i32, 0, "grammar"),
+            n_req, _tensor(hist, i32, 0, "hist", gpu), _tensor(hist_off, i32, n_req + 1, "hist_off", gpu),
+            _tensor(prompt_len, i32, n_req, "prompt_len", gpu), _tensor(repetition, f32, n_req, "repetition", gpu),
+            _tensor(frequency, f32, n_req, "frequency", gpu), _tensor(presence, f32, n_req, "presence", gpu),
+            _tensor(temperature, f32, n_req, "temperature", gpu), _tensor(bias_off, i32, n_req + 1, "bias_off", gpu),
+            _tensor(bias_tok, i32, 0, "bias_tok", gpu),
+            _tensor(bias_val, f32, 0 if bias_tok is None else bias_tok.numel(), "bias_val", gpu), _tensor(grammar, i32, 0, "grammar", gpu),
             0 if grammar is None else grammar.shape[1], 0 if grammar is None else grammar.shape[0],
-            _tensor(tree_tok, i32, 0, "tree_tok"), _tensor(cu_q, i32, n_req + 1, "cu_q"))
+            _tensor(tree_tok, i32, 0, "tree_tok", gpu), _tensor(cu_q, i32, n_req + 1, "cu_q", gpu))
 
 
 def op_adjust_logits(logits: torch.Tensor, req: torch.Tensor, rules: LogitRules, mask: Optional[torch.Tensor] = None,
                      state: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype=None,
                      stream=None) -> torch.Tensor:
     """Rules on logits [R][vocab] (rows any stride apart) of requests req [R]; out may be logits itself."""
-    it = _DTYPES.get(logits.dtype)
-    if logits.dim() != 2 or it is None or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] != 1):
-        _refuse(f"logits: [R][vocab] on the device, not {tuple(logits.shape)} {logits.dtype}")
+    it, dev, gpu = _DTYPES.get(logits.dtype), logits.device, _gpu(logits, stream)
+    if logits.dim() != 2 or it is None or (logits.stride(1) != 1 and logits.shape[1] != 1):
+        _refuse(f"logits: [R][vocab], not {tuple(logits.shape)} {logits.dtype}")
     R, V = logits.shape
+    if rules.gpu not in (None, gpu):
+        _refuse(f"rules on GPU {rules.gpu}, logits on {dev}")
     if out is None:
-        out, = _outputs(logits.device, stream, ((R, V), out_dtype or logits.dtype))
+        out, = _outputs(dev, stream, ((R, V), out_dtype or logits.dtype))
     ot = _DTYPES.get(out.dtype)
-    if out.shape != logits.shape or ot is None or not out.is_cuda or (out.stride(1) != 1 and V != 1):
-        _refuse(f"out: [{R}][{V}] on the device, not {tuple(out.shape)} {out.dtype}")
+    if out.shape != logits.shape or ot is None or out.get_device() != gpu or (out.stride(1) != 1 and V != 1):
+        _refuse(f"out: [{R}][{V}] on {dev}, not {tuple(out.shape)} {out.dtype} {out.device}")
     if mask is not None and (mask.dim() != 2 or mask.shape[0] < R):
         _refuse(f"mask: [{R}][words], not {tuple(mask.shape)}")
-    _check(load().atspeed_op_adjust_logits(_raw_stream(stream, logits.device), logits.data_ptr(), it, logits.stride(0), R, V,
-                                           _given(req, torch.int32, R, "req"), rules.desc,
-                                           _tensor(mask, torch.int32, R, "mask"), mask.shape[1] if mask is not None else 0,
-                                           _tensor(state, torch.int32, R, "state"), out.data_ptr(), ot, out.stride(0)))
+    _check(load().atspeed_op_adjust_logits(_raw_stream(stream, dev), logits.data_ptr(), it, logits.stride(0), R, V,
+                                           _given(req, torch.int32, R, "req", gpu), rules.desc,
+                                           _tensor(mask, torch.int32, R, "mask", gpu), mask.shape[1] if mask is not None else 0,
+                                           _tensor(state, torch.int32, R, "state", gpu), out.data_ptr(), ot, out.stride(0)))
     return out
