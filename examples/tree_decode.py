@@ -81,8 +81,7 @@ class Decoder:
         self._prefill()
 
     def _plan(self, q_len: Sequence[int], parent=None) -> "ats.BatchPlan":
-        free = _i32(self.free or [0])
-        plan = ats.op_batch_plan(_i32(q_len), _i32(self.kv_len), self.table, free, _i32([len(self.free)]), PAGE, MAX_TOKENS,
+        plan = ats.op_batch_plan(_i32(q_len), _i32(self.kv_len), self.table, _i32(self.free), _i32([len(self.free)]), PAGE, MAX_TOKENS,
                                  parent=parent, mask_words=MASK_WORDS if parent is not None else 0)
         if int(plan.state.max()) != ats.PLAN_OK:
             raise RuntimeError(f"not all users can be served: {plan.state.tolist()}")

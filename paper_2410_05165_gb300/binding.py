@@ -536,7 +536,9 @@ def op_batch_plan(q_len: torch.Tensor, kv_len: torch.Tensor, block_table: torch.
         _refuse(f"{n} requests, {T} tokens, block_table {tuple(block_table.shape)}, {mask_words} mask words")
     q_ptr, kv_ptr, up_ptr = _given(q_len, i32, n, "q_len", gpu), _given(kv_len, i32, n, "kv_len", gpu), _tensor(parent, i32, T, "parent", gpu)
     table_ptr = _given(block_table, i32, n, "block_table", gpu)
-    free_ptr, n_free_ptr = _given(free, i32, 1, "free", gpu), _given(n_free, i32, 1, "n_free", gpu)
+    free_ptr, n_free_ptr = _given(free, i32, 0, "free", gpu), _given(n_free, i32, 1, "n_free", gpu)
+    if free.numel() == 0:   # (n_free is 0: nothing is read of an address that has to be there)
+        free_ptr = n_free_ptr
     cu_q, ctx_len, state, pages, req, pos, slot, *trees = _outputs(
         dev, stream, (n + 1, i32), (n, i32), (n, i32), (2, i32), (T, i32), (T, i32), (T, torch.int64),
         *([((T, mask_words), i32)] if parent is not None else []))

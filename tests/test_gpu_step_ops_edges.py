@@ -295,3 +295,14 @@ def test_a_timeout_once_read_asks_nothing_of_a_stream_that_is_gone(ats, monkeypa
         assert binding.op_status(noalloc=True) == binding.E_TIMEOUT
     assert int(w[:binding.TREE_ATTENTION_COUNTER_BYTES].sum()) == 0
     binding._tree_ws.pop((0, handle.value))
+
+
+# ---------------------------------------------------------------------------------------------------
+# nothing to take, nothing listed, one row
+# ---------------------------------------------------------------------------------------------------
+def test_plan_with_no_free_page(ats):
+    """An empty free list: requests that need no page are served, the others are not."""
+    table = _dev([[4, 0], [7, 0]])
+    p = ats.op_batch_plan(_dev([1, 1]), _dev([15, 16]), table, _dev(np.zeros(0, np.int32)), _dev([0]), 16, 2)
+    assert p.state.tolist() == [ats.PLAN_OK, ats.PLAN_NO_PAGES] and p.slot.tolist() == [4 * 16 + 15, -1]
+    assert int(p.used) == 0 and table.tolist() == [[4, 0], [7, 0]]
