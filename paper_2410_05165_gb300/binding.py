@@ -636,6 +636,8 @@ class LogitRules:
                          next((t.numel() - 1 for t in (hist_off, bias_off, cu_q) if t is not None), 0))
         if grammar is not None and grammar.dim() != 2:
             _refuse(f"grammar: [states][words], not {tuple(grammar.shape)}")
+        if bias_tok is not None and bias_tok.numel() == 0:   # (lists without an entry have no address)
+            bias_off = bias_tok = bias_val = None
         f32, i32 = torch.float32, torch.int32
         self._keep = (hist, hist_off, prompt_len, repetition, frequency, presence, temperature, bias_off, bias_tok, bias_val,
                       grammar, tree_tok, cu_q)

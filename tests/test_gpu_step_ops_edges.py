@@ -306,3 +306,12 @@ def test_plan_with_no_free_page(ats):
     p = ats.op_batch_plan(_dev([1, 1]), _dev([15, 16]), table, _dev(np.zeros(0, np.int32)), _dev([0]), 16, 2)
     assert p.state.tolist() == [ats.PLAN_OK, ats.PLAN_NO_PAGES] and p.slot.tolist() == [4 * 16 + 15, -1]
     assert int(p.used) == 0 and table.tolist() == [[4, 0], [7, 0]]
+
+
+def test_no_bias_listed(ats):
+    """Lists of biases that hold none in this step."""
+    x = torch.randn(3, 100, device="cuda")
+    none = _dev(np.zeros(0, np.int32))
+    rules = ats.LogitRules(n_req=2, bias_off=_dev([0, 0, 0]), bias_tok=none, bias_val=none.float(),
+                           temperature=torch.full((2,), 2.0, device="cuda"))
+    assert torch.equal(ats.op_adjust_logits(x, _dev([0, 1, 1]), rules), x / 2)
