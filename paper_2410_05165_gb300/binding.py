@@ -502,6 +502,11 @@ def _kv_pages(kc: torch.Tensor, vc: torch.Tensor, gpu: int) -> KvPages:
                                              ks[0], ks[1], ks[2], vs[0], vs[1], vs[2]))   # (0.5 us; field by field 1.3)
 
 
+def _pitch(t: torch.Tensor, width: int) -> int:
+    """Elements from a row of `width` to the next; the stride of a single row means nothing."""
+    return t.stride(0) if t.shape[0] != 1 else width
+
+
 class BatchPlan:
     """Outputs of op_batch_plan (see atspeed_op_batch_plan)."""
     __slots__ = ("cu_q", "ctx_len", "state", "pages", "req", "pos", "slot", "mask")
@@ -561,7 +566,7 @@ def op_rope_append(qkv: torch.Tensor, n_heads: int, kc: torch.Tensor, vc: torch.
         _refuse(f"qkv: [T][({n_heads} + 2 * {pages.n_kv_heads}) * {hd}], not {tuple(qkv.shape)} {qkv.dtype}")
     T = qkv.shape[0]
     q, = _outputs(dev, stream, ((T, n_heads, hd), kc.dtype))
-    _check(load().atspeed_op_rope_append(_raw_stream(stream, dev), qkv.data_ptr(), src, qkv.stride(0), T, n_heads, pages,
+    _check(load().atspeed_op_rope_append(_raw_stream(stream, dev), qkv.data_ptr(), src, _pitch(qkv, qkv.shape[1]), T, n_heads, pages,
                                          _given(slot, torch.int64, T, "slot", gpu), _tensor(pos, torch.int32, T, "pos", gpu), theta,
                                          q.data_ptr() if n_heads else None, n_heads * hd))
     return q
@@ -604,22 +609,22 @@ def op_tree_attention(q: torch.Tensor, kc: torch.Tensor, vc: torch.Tensor, cu_q:
     dev, gpu = q.device, _gpu(q, stream)
     pages = _kv_pages(kc, vc, gpu)
     n, hd = ctx_len.numel(), pages.head_dim
-    if q.dim() != 3 or q.dtype is not kc.dtype or q.shape[2] != hd or q.stride(2) != 1 or q.stride(1) != hd:
+    if q.dim() != 3 or q.dtype is not kc.dtype or q.shape[2] != hd or q.stride(2) != 1 or (q.stride(1) != hd and q.shape[1] != 1):
         _refuse(f"q: [T][heads][{hd}] of {kc.dtype}, each row contiguous, not {tuple(q.shape)} {q.dtype}")
     T, H, _ = q.shape
     if out is None:
         out, = _outputs(dev, stream, (q.shape, q.dtype))
-    elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1 or out.stride(1) != hd or out.get_device() != gpu:
+    elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1 or (out.stride(1) != hd and H != 1) or out.get_device() != gpu:
         _refuse(f"out: as q {tuple(q.shape)} {q.dtype} on {dev}, each row contiguous, not {tuple(out.shape)} {out.dtype} {out.device}")
     if block_table.dim() != 2 or block_table.shape[0] < n or (mask is not None and (mask.dim() != 2 or mask.shape[0] < T)):
         _refuse(f"block_table: [{n}][width] and mask: [{T}][words], not {tuple(block_table.shape)} and "
                 f"{None if mask is None else tuple(mask.shape)}")
     st = _raw_stream(stream, dev)
-    _check(load().atspeed_op_tree_attention(st, pages, q.data_ptr(), q.stride(0), H, n, T,
+    _check(load().atspeed_op_tree_attention(st, pages, q.data_ptr(), _pitch(q, H * hd), H, n, T,
                                             _given(cu_q, torch.int32, n + 1, "cu_q", gpu), _given(ctx_len, torch.int32, 1, "ctx_len", gpu),
                                             _given(block_table, torch.int32, n, "block_table", gpu), block_table.shape[1],
                                             _tensor(mask, torch.int32, T, "mask", gpu), mask.shape[1] if mask is not None else 0,
-                                            hd ** -0.5 if scale is None else scale, out.data_ptr(), out.stride(0),
+                                            hd ** -0.5 if scale is None else scale, out.data_ptr(), _pitch(out, H * hd),
                                             _tensor(lse, torch.float32, T * H, "lse", gpu),
                                             op_tree_attention_workspace(dev, st).data_ptr()))
     return out
@@ -673,8 +678,8 @@ def op_adjust_logits(logits: torch.Tensor, req: torch.Tensor, rules: LogitRules,
         _refuse(f"out: [{R}][{V}] on {dev}, not {tuple(out.shape)} {out.dtype} {out.device}")
     if mask is not None and (mask.dim() != 2 or mask.shape[0] < R):
         _refuse(f"mask: [{R}][words], not {tuple(mask.shape)}")
-    _check(load().atspeed_op_adjust_logits(_raw_stream(stream, dev), logits.data_ptr(), it, logits.stride(0), R, V,
+    _check(load().atspeed_op_adjust_logits(_raw_stream(stream, dev), logits.data_ptr(), it, _pitch(logits, V), R, V,
                                            _given(req, torch.int32, R, "req", gpu), rules.desc,
                                            _tensor(mask, torch.int32, R, "mask", gpu), mask.shape[1] if mask is not None else 0,
-                                           _tensor(state, torch.int32, R, "state", gpu), out.data_ptr(), ot, out.stride(0)))
+                                           _tensor(state, torch.int32, R, "state", gpu), out.data_ptr(), ot, _pitch(out, V)))
     return out

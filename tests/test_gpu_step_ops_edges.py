@@ -315,3 +315,36 @@ def test_no_bias_listed(ats):
     rules = ats.LogitRules(n_req=2, bias_off=_dev([0, 0, 0]), bias_tok=none, bias_val=none.float(),
                            temperature=torch.full((2,), 2.0, device="cuda"))
     assert torch.equal(ats.op_adjust_logits(x, _dev([0, 1, 1]), rules), x / 2)
+
+
+def test_one_row_of_any_stride(ats):
+    """The distance between rows means nothing where there is one: logits and projections as columns that were transposed."""
+    col = torch.randn(1003, 1, device="cuda")
+    rules = ats.LogitRules(n_req=1, temperature=torch.full((1,), 2.0, device="cuda"))
+    out = torch.empty(1003, 1, device="cuda").t()
+    assert torch.equal(ats.op_adjust_logits(col.t(), _dev([0]), rules), col.t() / 2)
+    assert torch.equal(ats.op_adjust_logits(col.t(), _dev([0]), rules, out=out), col.t() / 2)
+    kc, vc = (torch.randn(4, 16, 2, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+    qkv = torch.randn(8 * 64, 1, device="cuda")
+    slot = torch.tensor([35], device="cuda")
+    q = ats.op_rope_append(qkv.t(), 4, kc, vc, slot)
+    assert torch.equal(q.flatten(), qkv[:256, 0].to(torch.bfloat16))
+    assert torch.equal(kc[2, 3].flatten(), qkv[256:384, 0].to(torch.bfloat16))
+    args = (kc, vc, _dev([0, 1]), _dev([35]), _dev([[0, 1, 2]]))
+    odd = torch.as_strided(q.clone(), (1, 4, 64), (1, 64, 1))
+    assert torch.equal(ats.op_tree_attention(odd, *args), ats.op_tree_attention(q, *args))
+    into = torch.empty_like(q)
+    ats.op_tree_attention(q, *args, out=torch.as_strided(into, (1, 4, 64), (1, 64, 1)))
+    assert torch.equal(into, ats.op_tree_attention(q, *args))
+
+
+def test_one_head_of_any_stride(ats):
+    kc, vc = (torch.randn(4, 16, 1, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(3, 1, 64, device="cuda").to(torch.bfloat16)
+    args = (kc, vc, _dev([0, 3]), _dev([40]), _dev([[0, 1, 2]]))
+    other = q.reshape(1, 3, 64).transpose(0, 1)   # (the heads' stride is that of all tokens)
+    assert other.stride(1) != 64
+    out = torch.empty(1, 3, 64, dtype=q.dtype, device="cuda").transpose(0, 1)
+    want = ats.op_tree_attention(q, *args)
+    assert torch.equal(ats.op_tree_attention(other, *args), want)
+    assert torch.equal(ats.op_tree_attention(q, *args, out=out), want)
