@@ -167,27 +167,29 @@ __global__ void __launch_bounds__(kThreads, 4) adjust_logits_kernel(const __grid
         uint32_t* c = sm + w * words;
         if (!(atomicOr(c + i, kListed) & kListed)) reinterpret_cast<uint16_t*>(c + kRegion)[atomicAdd(&s_n[w], 1)] = (uint16_t)i;
       };
-      // (kBatch entries a thread at once; few are among the CTA's tokens, and those are read again)
-      for (int k_at = h0 + tid; k_at < h1; k_at += kBatch * kThreads) {
+      // (kBatch entries a thread at once; few are among the CTA's tokens, and those are read again.  What is left is counted, not
+      // the places: a step past the end of lists that end near 2^31 would come round to negative ones)
+      const int* at = a.r.d_hist + h0 + (long long)tid;
+      for (int left = h1 - h0 - tid; left > 0; left -= kBatch * kThreads, at += kBatch * kThreads) {
         uint32_t hits = 0;
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
-          const int k = k_at + j * kThreads, v = k < h1 ? __ldg(a.r.d_hist + k) : -1;
+          const int v = j * kThreads < left ? __ldg(at + j * kThreads) : -1;
           if ((unsigned)v < (unsigned)a.V && (unsigned)(v - v0 + 8) < (unsigned)(kChunk + 16)) hits |= 1u << j;
         }
 #pragma unroll 1
         for (; hits; hits &= hits - 1) {
-          const int k = k_at + (__ffs(hits) - 1) * kThreads;
-          each(__ldg(a.r.d_hist + k), [&](int w, int i) {
-            if (k < p) atomicOr(sm + w * words + i, kPrompt);
+          const int j = (__ffs(hits) - 1) * kThreads;
+          each(__ldg(at + j), [&](int w, int i) {
+            if (h1 - left + j < p) atomicOr(sm + w * words + i, kPrompt);
             else atomicAdd(sm + w * words + i, 1u);
             enlist(w, i);
           });
         }
       }
-      for (int k = k0 + tid; k < k1; k += kThreads)
+      for (unsigned k = k0 + tid; k < (unsigned)k1; k += kThreads)
         each(__ldg(a.r.d_bias_tok + k), [&](int w, int i) {   // (the later entry)
-          atomicMax(sm + w * words + kRegion + kRegion / 2 + i, (uint32_t)(k - k0) + 1u);
+          atomicMax(sm + w * words + kRegion + kRegion / 2 + i, k - k0 + 1u);
           enlist(w, i);
         });
       __syncthreads();

@@ -348,3 +348,18 @@ def test_one_head_of_any_stride(ats):
     want = ats.op_tree_attention(q, *args)
     assert torch.equal(ats.op_tree_attention(other, *args), want)
     assert torch.equal(ats.op_tree_attention(q, *args, out=out), want)
+
+
+def test_lists_that_end_near_31_bits(ats):
+    """Entries at the end of lists of 2^31 - 1: the places past them do not come round to negative ones."""
+    end, V = (1 << 31) - 1, 100
+    hist, bias_tok = (torch.empty(end, dtype=torch.int32, device="cuda") for _ in range(2))
+    bias_val = torch.empty(end, device="cuda")
+    hist[-3:] = _dev([7, 9, 9])
+    bias_tok[-2:], bias_val[-2:] = _dev([7, 50]), torch.tensor([2.0, -1.0], device="cuda")
+    rules = ats.LogitRules(hist=hist, hist_off=_dev([end - 3, end]), frequency=torch.full((1,), 0.5, device="cuda"),
+                           bias_off=_dev([end - 2, end]), bias_tok=bias_tok, bias_val=bias_val)
+    x = torch.zeros(2, V, device="cuda")
+    want = x.clone()
+    want[:, 7], want[:, 9], want[:, 50] = 1.5, -1.0, -1.0
+    assert torch.equal(ats.op_adjust_logits(x, _dev([0, 0]), rules), want)
