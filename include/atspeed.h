@@ -334,8 +334,8 @@ typedef struct {
 typedef enum {
   ATSPEED_PLAN_OK = 0,
   ATSPEED_PLAN_NO_PAGES = 1, /* the free pages did not reach to it */
-  ATSPEED_PLAN_LIMIT = 2     /* negative length, more pages than its table row, tokens past max_tokens or past
-                              * the mask's 32 * mask_words bits */
+  ATSPEED_PLAN_LIMIT = 2     /* negative length, positions past 2^31 - 2, more pages than its table row, tokens past
+                              * max_tokens or past the mask's 32 * mask_words bits */
 } atspeed_plan_state;
 
 /* Block tables and slot maps of a step from the requests' lengths.

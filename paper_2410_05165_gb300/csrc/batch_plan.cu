@@ -23,6 +23,11 @@ struct PlanArgs {
   uint32_t* mask;
 };
 
+// Pages of a served request's tokens (unsigned: the sum may pass 2^31).
+__device__ __forceinline__ int pages_of(const PlanArgs& a, int tokens) {
+  return (int)(((unsigned)tokens + (unsigned)a.page - 1u) / (unsigned)a.page);
+}
+
 // Inclusive sums over the CTA's threads of two values each.
 __device__ __forceinline__ void block_scan2(long long& a, long long& b, long long (*red)[2]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -53,7 +58,8 @@ __global__ void __launch_bounds__(kThreads) batch_plan_kernel(PlanArgs a) {
     const long long ql = a.q_len[b], kv = a.kv_len[b];
     q = max(0LL, ql);
     const long long need = (kv + q + a.page - 1) / a.page;
-    const bool ok = ql >= 0 && kv >= 0 && need <= a.width && first + q <= a.T && (!a.mask || q <= 32LL * a.words);
+    const bool ok = ql >= 0 && kv >= 0 && kv + q <= 0x7fffffff && need <= a.width && first + q <= a.T &&
+                    (!a.mask || q <= 32LL * a.words);
     fresh = ok ? need - (kv + a.page - 1) / a.page : 0;
     return ok;
   };
@@ -102,8 +108,7 @@ __global__ void __launch_bounds__(kThreads) batch_plan_kernel(PlanArgs a) {
   // table entries of the new pages, a thread a request
   for (int b = blockIdx.x * kThreads + tid; b < a.n; b += gridDim.x * kThreads) {
     if (base[b] < 0) continue;
-    const int kv = a.kv_len[b], have = (kv + a.page - 1) / a.page;
-    const int need = (int)(((long long)kv + a.q_len[b] + a.page - 1) / a.page);
+    const int kv = a.kv_len[b], have = pages_of(a, kv), need = pages_of(a, kv + a.q_len[b]);
     for (int j = have; j < need; ++j) a.table[(size_t)b * a.width + j] = a.free[base[b] + j - have];
   }
   // tokens
@@ -121,12 +126,12 @@ __global__ void __launch_bounds__(kThreads) batch_plan_kernel(PlanArgs a) {
     const int i = t - start[b], kv = a.kv_len[b];
     long long slot = -1;
     if (base[b] >= 0) {
-      const int p = kv + i, col = p / a.page, have = (kv + a.page - 1) / a.page;
+      const int p = kv + i, col = p / a.page, have = pages_of(a, kv);
       const int id = col < have ? a.table[(size_t)b * a.width + col] : a.free[base[b] + col - have];
       slot = (long long)id * a.page + p % a.page;
     }
     a.req[t] = b;
-    a.pos[t] = kv + depth;
+    a.pos[t] = (int)((unsigned)kv + depth);
     a.slot[t] = slot;
   };
   if (!a.mask) {

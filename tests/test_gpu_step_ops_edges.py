@@ -363,3 +363,14 @@ def test_lists_that_end_near_31_bits(ats):
     want = x.clone()
     want[:, 7], want[:, 9], want[:, 50] = 1.5, -1.0, -1.0
     assert torch.equal(ats.op_adjust_logits(x, _dev([0, 0]), rules), want)
+
+
+def test_plan_of_positions_near_31_bits(ats):
+    """Pages of 2^30 tokens and a request whose last position is 2^31 - 2; the next one would need a position past that."""
+    page, kv = 1 << 30, (1 << 31) - 9
+    table = _dev([[5, 6, -7], [8, 9, -7], [-7, -7, -7]])
+    p = ats.op_batch_plan(_dev([8, 9, 2]), _dev([kv, kv, 0]), table, _dev([3]), _dev([1]), page, 20)
+    assert p.state.tolist() == [ats.PLAN_OK, ats.PLAN_LIMIT, ats.PLAN_OK] and p.ctx_len.tolist() == [kv, -1, 0]
+    assert table.tolist() == [[5, 6, -7], [8, 9, -7], [3, -7, -7]]
+    assert p.pos.tolist()[:8] == [kv + i for i in range(8)] and p.pos.tolist()[17:] == [0, 1, 0]
+    assert p.slot.tolist() == [6 * page + kv - page + i for i in range(8)] + [-1] * 9 + [3 * page, 3 * page + 1, -1]
