@@ -374,9 +374,13 @@ atspeed_status atspeed_op_rope_append(atspeed_stream stream, const void *d_qkv, 
 /* Attention of a step's tokens over their requests' caches: token i of request b attends to the cache positions
  * p < ctx_len[b] and to the positions ctx_len[b] + a of those new tokens a of its request whose bit is set in its row of
  * d_mask [T][mask_words] (d_mask NULL: a <= i, causal), scores scale * q.k, softmax in 32 bits (weights rounded to the
- * type of V for the product with V; where that is F16, weights below 2^-32 of a row's largest may count as 0 there).  Query head h reads key head h / (n_heads / n_kv_heads).  Keys and values that a
- * token does not attend to never reach its result, whatever they hold (a cache row that was never written, an infinity, a
- * NaN); a token that attends to nothing gets zeros (and a log-sum-exp of -infinity).  Requests with ctx_len < 0 get zeros.
+ * type of V for the product with V; where that is F16, weights below 2^-32 of a row's largest may count as 0 there).
+ * Query head h reads key head h / (n_heads / n_kv_heads).  Keys and values that a token does not attend to never reach its
+ * result, whatever they hold (a cache row that was never written, an infinity, a NaN); a token that attends to nothing gets
+ * zeros (and a log-sum-exp of -infinity).  Requests with ctx_len < 0 get zeros.
+ * Rows of d_out and d_lse that belong to no request (before cu_q[0], from cu_q[n_req] on) are left as they are, so that a
+ * step can be divided among calls over neighbouring requests, each with its own kind of mask; where such rows are read
+ * later (a step padded to T rows), fill them first.
  *   d_q [T] rows of n_heads * head_dim, q_stride elements apart, of the cache's k_type; d_out the same with out_stride;
  *   d_lse NULL or [T][n_heads]: natural log of the sum of exp(score);
  *   d_cu_q [n_req+1], d_ctx_len [n_req], d_block_table [n_req][table_width] (entries past the last page of a request are not

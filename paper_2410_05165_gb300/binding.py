@@ -605,7 +605,8 @@ def op_tree_attention(q: torch.Tensor, kc: torch.Tensor, vc: torch.Tensor, cu_q:
                       block_table: torch.Tensor, mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
                       out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of q [T][heads][head_dim] (rows any stride apart) over the batch's paged caches and, by the mask's bits
-    (None: causal), the step's own tokens.  scale: 1 / sqrt(head_dim) by default."""
+    (None: causal), the step's own tokens.  scale: 1 / sqrt(head_dim) by default.  Rows of no request (those past the last
+    token of a padded step) are not written: without out they hold whatever the memory held."""
     dev, gpu = q.device, _gpu(q, stream)
     pages = _kv_pages(kc, vc, gpu)
     n, hd = ctx_len.numel(), pages.head_dim

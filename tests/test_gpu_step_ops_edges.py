@@ -374,3 +374,23 @@ def test_plan_of_positions_near_31_bits(ats):
     assert table.tolist() == [[5, 6, -7], [8, 9, -7], [3, -7, -7]]
     assert p.pos.tolist()[:8] == [kv + i for i in range(8)] and p.pos.tolist()[17:] == [0, 1, 0]
     assert p.slot.tolist() == [6 * page + kv - page + i for i in range(8)] + [-1] * 9 + [3 * page, 3 * page + 1, -1]
+
+
+# ---------------------------------------------------------------------------------------------------
+# rows of no request
+# ---------------------------------------------------------------------------------------------------
+def test_rows_of_no_request_are_left_as_they_are(ats):
+    """So that a step can be divided among calls over neighbouring requests, each with its own kind of mask."""
+    kc, vc = (torch.randn(12, 16, 2, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(40, 4, 64, device="cuda").to(torch.bfloat16)
+    cu, ctx, table = _dev([0, 5, 6, 30]), _dev([20, 33, 10]), _dev([[0, 1, 2, 3], [4, 5, 6, 7], [8, 9, 10, 11]])
+    lse = torch.full((40, 4), 7.0, device="cuda")
+    out = torch.full_like(q, 3.0)
+    ats.op_tree_attention(q, kc, vc, cu, ctx, table, out=out, lse=lse)
+    assert bool((out[30:] == 3).all()) and bool((lse[30:] == 7).all())
+    parts = torch.full_like(q, 3.0)
+    ats.op_tree_attention(q, kc, vc, cu[2:], ctx[2:], table[2:], out=parts)
+    assert bool((parts[:6] == 3).all())
+    ats.op_tree_attention(q, kc, vc, cu[:3], ctx[:2], table[:2], out=parts)
+    tol = 2.0 ** -8 * out.float().abs() + 2.0 ** -7 * vc.float().abs().max()   # (each call divides its key ranges its own way)
+    assert bool(((parts.float() - out.float()).abs() <= tol).all())
