@@ -388,8 +388,9 @@ atspeed_status atspeed_op_rope_append(atspeed_stream stream, const void *d_qkv, 
  * head_dim 32, 64 or 128; page_size 16, 32, 64, 128 or 256; n_heads a multiple of n_kv_heads, at most 128 times it;
  * n_req <= 16384 (ATSPEED_E_SHAPE); scale > 0; rows and strides 16-byte aligned (ATSPEED_E_ARG).
  * d_ws: atspeed_op_tree_attention_workspace() bytes, 256-byte aligned, the first ATSPEED_TREE_ATTENTION_COUNTER_BYTES of them
- * zero-filled before its first use, of one stream (or graph) at a time (every call leaves its counters zeroed).  The first call on a device is made outside stream capture.  Long key ranges are divided by the lengths of the whole call, in an
- * order that the lengths alone fix: the same call gives the same bits, a request's last bits may differ in another batch.
+ * zero-filled before its first use, of one stream (or graph) at a time (every call leaves its counters zeroed).  The first
+ * call on a device is made outside stream capture.  Long key ranges are divided by the lengths of the whole call, in an order
+ * that the lengths alone fix: the same call gives the same bits, a request's last bits may differ in another batch.
  * Device-side timeouts surface through atspeed_op_status(stream, NULL); after one, zero those bytes again. */
 #define ATSPEED_TREE_ATTENTION_COUNTER_BYTES 4096
 /* The id of the capture (into a CUDA graph) that `stream` is part of, 0 for a stream that is not captured: a workspace used by
@@ -414,7 +415,8 @@ atspeed_status atspeed_op_tree_attention(atspeed_stream stream, const atspeed_kv
  *   d_grammar[s * grammar_stride ..], lowest bit first, become -infinity, whatever their logit (a state of
  *   n_states or above allows no token);
  *   x /= temperature (a temperature that is not above 0: not divided).
- * Tokens outside [0, vocab) are ignored.  Arithmetic in 32 bits, one rounding to the output's type. */
+ * Tokens outside [0, vocab) are ignored.  Arithmetic in 32 bits (the quotients within 1.5 units in the last place: by a
+ * reciprocal rounded once per request), one rounding to the output's type. */
 typedef struct {
   int n_req;
   const int32_t *d_hist, *d_hist_off, *d_prompt_len;

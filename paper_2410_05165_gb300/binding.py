@@ -539,7 +539,8 @@ def op_batch_plan(q_len: torch.Tensor, kv_len: torch.Tensor, block_table: torch.
     n, T, i32, dev, gpu = q_len.numel(), max_tokens, torch.int32, q_len.device, _gpu(q_len, stream)
     if block_table.dim() != 2 or block_table.shape[0] != n or T <= 0 or n == 0 or (parent is not None and mask_words <= 0):
         _refuse(f"{n} requests, {T} tokens, block_table {tuple(block_table.shape)}, {mask_words} mask words")
-    q_ptr, kv_ptr, up_ptr = _given(q_len, i32, n, "q_len", gpu), _given(kv_len, i32, n, "kv_len", gpu), _tensor(parent, i32, T, "parent", gpu)
+    q_ptr, kv_ptr = _given(q_len, i32, n, "q_len", gpu), _given(kv_len, i32, n, "kv_len", gpu)
+    up_ptr = _tensor(parent, i32, T, "parent", gpu)
     table_ptr = _given(block_table, i32, n, "block_table", gpu)
     free_ptr, n_free_ptr = _given(free, i32, 0, "free", gpu), _given(n_free, i32, 1, "n_free", gpu)
     if free.numel() == 0:   # (n_free is 0: nothing is read of an address that has to be there)
@@ -615,14 +616,17 @@ def op_tree_attention(q: torch.Tensor, kc: torch.Tensor, vc: torch.Tensor, cu_q:
     T, H, _ = q.shape
     if out is None:
         out, = _outputs(dev, stream, (q.shape, q.dtype))
-    elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1 or (out.stride(1) != hd and H != 1) or out.get_device() != gpu:
-        _refuse(f"out: as q {tuple(q.shape)} {q.dtype} on {dev}, each row contiguous, not {tuple(out.shape)} {out.dtype} {out.device}")
+    elif (out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1 or (out.stride(1) != hd and H != 1) or
+          out.get_device() != gpu):
+        _refuse(f"out: as q {tuple(q.shape)} {q.dtype} on {dev}, each row contiguous, not {tuple(out.shape)} {out.dtype} "
+                f"{out.device}")
     if block_table.dim() != 2 or block_table.shape[0] < n or (mask is not None and (mask.dim() != 2 or mask.shape[0] < T)):
         _refuse(f"block_table: [{n}][width] and mask: [{T}][words], not {tuple(block_table.shape)} and "
                 f"{None if mask is None else tuple(mask.shape)}")
     st = _raw_stream(stream, dev)
     _check(load().atspeed_op_tree_attention(st, pages, q.data_ptr(), _pitch(q, H * hd), H, n, T,
-                                            _given(cu_q, torch.int32, n + 1, "cu_q", gpu), _given(ctx_len, torch.int32, 1, "ctx_len", gpu),
+                                            _given(cu_q, torch.int32, n + 1, "cu_q", gpu),
+                                            _given(ctx_len, torch.int32, 1, "ctx_len", gpu),
                                             _given(block_table, torch.int32, n, "block_table", gpu), block_table.shape[1],
                                             _tensor(mask, torch.int32, T, "mask", gpu), mask.shape[1] if mask is not None else 0,
                                             hd ** -0.5 if scale is None else scale, out.data_ptr(), _pitch(out, H * hd),
@@ -657,7 +661,8 @@ class LogitRules:
             _tensor(frequency, f32, n_req, "frequency", gpu), _tensor(presence, f32, n_req, "presence", gpu),
             _tensor(temperature, f32, n_req, "temperature", gpu), _tensor(bias_off, i32, n_req + 1, "bias_off", gpu),
             _tensor(bias_tok, i32, 0, "bias_tok", gpu),
-            _tensor(bias_val, f32, 0 if bias_tok is None else bias_tok.numel(), "bias_val", gpu), _tensor(grammar, i32, 0, "grammar", gpu),
+            _tensor(bias_val, f32, 0 if bias_tok is None else bias_tok.numel(), "bias_val", gpu),
+            _tensor(grammar, i32, 0, "grammar", gpu),
             0 if grammar is None else grammar.shape[1], 0 if grammar is None else grammar.shape[0],
             _tensor(tree_tok, i32, 0, "tree_tok", gpu), _tensor(cu_q, i32, n_req + 1, "cu_q", gpu))
 

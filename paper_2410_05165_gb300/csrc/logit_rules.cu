@@ -1,8 +1,8 @@
 // Penalties, biases, grammar masks and temperature on next-token logits (atspeed_op_adjust_logits).
 //   c(v) = occurrences of v in the request's output and on the row's path in its tree, seen(v) = c(v) > 0 or v in the prompt
 //   x <- seen ? (x > 0 ? x / rep : x * rep) : x;  x <- x - freq c - pres [c > 0] + bias(v);  forbidden: -inf;  x <- x / temp
-// Bound: HBM (each logit read and written once).  3840 rows of 33024 (32 bits) take 237 us, 4.3 TB/s; with the temperature alone
-// 172, a plain copy 152.  509 rows of 100003 (bf16) with histories of up to 8000 tokens take 114 us, 1.8 TB/s: there each piece
+// Bound: HBM (each logit read and written once).  3840 rows of 33024 (32 bits) take 240 us, 4.2 TB/s; with the temperature alone
+// 172, a plain copy 152.  509 rows of 100003 (bf16) with histories of up to 8000 tokens take 117 us, 1.8 TB/s: there each piece
 // of a row goes through the whole history, whose loads wait for the request's, and a CTA has too few bytes under way meanwhile
 // (without histories 85 us, a copy 40).  Pieces twice as long leave two CTAs an SM for the table's sake and take 154 us.
 //
@@ -348,9 +348,10 @@ extern "C" atspeed_status atspeed_op_adjust_logits(atspeed_stream stream, const 
   a.in_place = d_out == d_logits;
   // Pieces of 4096 tokens (7 more for rows that begin between 16-byte addresses).  Rows a CTA: a request's list is made once for
   // those that follow each other, and more CTAs than run at once even out their ends.  us for 1 / 2 / 4 / 8 / 16 rows: 3840 rows of
-  // 33024, 240 a request, 335 / 261 / 237 / 237 / 254; 509 rows of 100003, one a request, 114 / 131 / 144 / 160 / 212.
-  // Neighbouring CTAs take a row's pieces one after the other (3840 rows: 237, row after row 254), except where every row has
-  // a history of its own, whose long ones then spread (509 rows: 120 and 114).
+  // 33024, 240 a request, 328 / 266 / 243 / 244 / 261; 509 rows of 100003, one a request, 117 / 140 / 158 / 178 / 230.
+  // Neighbouring CTAs take a row's pieces one after the other (3840 rows: 243, row after row 260), except where every row has
+  // a history of its own, whose long ones then spread (509 rows: 123 and 117).  (n_req that counts more requests than the rows
+  // are of makes it fewer rows a CTA than would do: slower, not wrong.)
   a.chunks = (unsigned)((vocab + 7LL + kChunk - 1) / kChunk);
   a.rows = std::min(4, std::max(1, R / std::max(1, r.n_req)));
   a.groups = (unsigned)((R + a.rows - 1LL) / a.rows);

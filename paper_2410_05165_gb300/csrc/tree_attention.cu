@@ -31,7 +31,8 @@
 //
 // Roles (384 threads): warp 0 copies (TMA), warps 1 and 2 issue the products of a stream each, warp 3 loads Q, warps 4-7 and
 // 8-11 run the streams' softmax.  A stream's warps keep their place in the walk over the blocks in shared memory: beside a
-// row of S it does not fit the registers, and spilled it cost 20 to 75% of the time where the HBM is the bound.
+// row of S it does not fit the registers, and spilled it cost 20 to 75% of the time where the HBM is the bound (8 to 12 bytes
+// of a thread's still are spilled).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -128,7 +129,9 @@ __device__ __forceinline__ int block_rows(const TreeAttnArgs& a, const Request& 
 // What a block costs beside its tiles (its Q, its pipeline's start, its masks and its result), in tiles, so that ranges of equal
 // units take equal times.  Measured at heads of 128, against no cost at all: 61 single tokens 208 -> 188 us with 1 (a CTA has
 // up to three blocks, another one long one); 16 trees of 240 tokens 107 -> 99 us with 2 to 6; a causal prompt of 4001 tokens
-// loses instead, 390 -> 403 us (its blocks are all of one kind and long).
+// loses instead, 390 -> 403 us (its blocks are all of one kind and long).  Since ends move to blocks' borders (below) trees of
+// 240 tokens are the same either way; 40 of 60 tokens, 32 heads on 8 of 128 / 64 / 32, took 84.6 / 68.3 / 60 us with no cost and
+// 82.6 / 64.2 / 58 like this, the 61 single tokens 215 / 166 / 139 and 212 / 160 / 136 (cold L2).
 __device__ __forceinline__ int block_cost(const TreeAttnArgs& a, const Request& r, int blk) {
   return block_rows(a, r, blk) <= a.rt ? 1 : a.mask ? 4 : 0;
 }
@@ -283,6 +286,7 @@ __device__ __forceinline__ void hold64(uint32_t* x) {
                    "+r"(x[j + 7]), "+r"(x[j + 8]), "+r"(x[j + 9]), "+r"(x[j + 10]), "+r"(x[j + 11]), "+r"(x[j + 12]),
                    "+r"(x[j + 13]), "+r"(x[j + 14]), "+r"(x[j + 15]));
 }
+// The instruction, good to 2^-22: below what P's 16 bits keep, and in the joins below the roundings of P that they sum.
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
