@@ -437,6 +437,79 @@ atspeed_status atspeed_op_adjust_logits(atspeed_stream stream, const void *d_log
                                         const uint32_t *d_mask, int mask_words, const int32_t *d_state, void *d_out,
                                         atspeed_dtype out_type, int64_t ld_out);
 
+/* ----------------------------------------------------------------------------------------------
+ * What follows a step's logits: the best continuations of every request's beams, the block tables of the chosen ones, the
+ * copies that sharing pages asks for, and the place of an accepted path in the cache.  Each writes new state from old state
+ * that it leaves as it is (the caches' contents excepted), on the device alone, so that a loop of plan -> rope_append ->
+ * tree_attention -> adjust_logits -> beam_select -> fork_pages -> copy_pages (drafted trees: compact_tokens -> fork_pages) neither
+ * copies to nor waits for the host.  (Sec. 2's beam search over a whole vocabulary; the paper has no counterpart of the rest.)
+ * ---------------------------------------------------------------------------------------------- */
+
+/* The `width` best continuations of each request's beams.  Request b's beams are the rows d_cu_beam[b] .. d_cu_beam[b+1]-1 of the
+ * logits [R][vocab] (F32, BF16 or F16, ld elements between rows; a logit that is NaN counts as -infinity, +infinity as the type's
+ * largest number).  Row r is in grammar state s = d_state[r] (d_state NULL, or a negative one: every token is allowed; else
+ * those whose bit is set in d_grammar[s * grammar_stride ..], lowest bit first; none in a state of n_states or above).
+ *   score(r, v) = d_score[r] + log p_r(v) of the allowed tokens v, p_r the softmax over the allowed logits (ATSPEED_NORM_MASKED) or over
+ *   all of the row (ATSPEED_NORM_FULL);  d_score NULL: 0;
+ *   d_final[r] >= 0 (d_final NULL: none): the beam has ended, its one continuation is that token with the score d_score[r].
+ * Higher scores come first, compared in 64 bits (the sum of a row's exponentials in 32); of equal ones the lower row, then the
+ * larger logit, then the lower token.  A score of -infinity (in 32 bits) or NaN is never chosen.
+ * Outputs [n_req][width], best first: d_token, d_parent (the row), d_out_score (rounded to 32 bits); places without a
+ * continuation hold -1, -1, -infinity.  Rows of no request are not read.
+ * width 1 .. 256, vocab up to 2^30 (ATSPEED_E_SHAPE).  d_ws: atspeed_op_beam_select_workspace(R, vocab, width) bytes, 16-byte aligned, whatever they
+ * hold, of this call alone until it is done. */
+size_t atspeed_op_beam_select_workspace(int R, int vocab, int width);
+atspeed_status atspeed_op_beam_select(atspeed_stream stream, const void *d_logits, atspeed_dtype type, int64_t ld, int R, int vocab,
+                                      const float *d_score, const int32_t *d_final, int n_req, const int32_t *d_cu_beam, int width,
+                                      const int32_t *d_state, const uint32_t *d_grammar, int64_t grammar_stride, int n_states,
+                                      atspeed_norm_mode norm, int32_t *d_token, int32_t *d_parent, float *d_out_score, void *d_ws);
+
+/* New rows of block tables from old ones: beams go on from their parents, ended or rejected ones give their pages back.
+ * Page counts: d_ref[page] is the number of rows (and of whatever else the caller counts) that hold a page; 0: free.
+ *   d_table [n_old][table_width], page_size as in batch_plan;  old row p holds its first ceil(held / page_size) entries, where
+ *     held = d_kv_len[p] + (d_q_len and served ? d_q_len[p] : 0), served: d_old_state NULL or d_old_state[p] = ATSPEED_PLAN_OK
+ *     (d_kv_len, d_q_len, d_old_state: the plan's inputs and its output);
+ *   d_free [*d_n_free], of which the first *d_used (NULL: 0) have been handed out since d_ref was made (the plan's d_pages):
+ *     each of those counts one holder more;
+ *   d_parent [n_new]: each new row's old row, negative: an empty row (NULL: row j goes on from row j, n_new = n_old);
+ *   d_length [n_new]: the tokens it keeps (NULL: all that its parent holds).
+ * A new row keeps its parent's first ceil(length / page_size) pages.  Full ones are shared.  The last one, if not full, will be
+ * written to: the child of its parent that keeps the most tokens (the first of those) goes on in it if nothing else held it
+ * (d_ref at most 1); any other child gets the next page of d_free, from the used ones on, in the order of the rows, and has to
+ * be given a copy of it.
+ * Outputs (overlapping no input): d_new_table [n_new][table_width], -1 behind the kept pages;  d_new_len [n_new] tokens kept, -1 if not
+ * served;  d_new_state [n_new] an atspeed_plan_state (NO_PAGES: no page was left for its copy; LIMIT: a parent of n_old or above,
+ * a length below 0 or above what the parent holds, or more pages than table_width), a row that is not served holds nothing;  d_src,
+ * d_dst [n_new] pages to copy from and to, -1: none;  d_new_ref [n_pages];  d_new_free [n_pages], *d_new_n_free: the pages
+ * whose new count is 0 or less, ascending, -1 behind them.
+ * Entries outside [0, n_pages) are handed on, not counted, not copied.  n_old, n_new <= 16384, n_pages <= 2^26 (ATSPEED_E_SHAPE). */
+atspeed_status atspeed_op_fork_pages(atspeed_stream stream, int n_old, int n_new, const int32_t *d_table, int table_width,
+                                     int page_size, const int32_t *d_kv_len, const int32_t *d_q_len, const int32_t *d_old_state,
+                                     const int32_t *d_parent, const int32_t *d_length, int n_pages, const int32_t *d_ref,
+                                     const int32_t *d_free, const int32_t *d_n_free, const int32_t *d_used, int32_t *d_new_table,
+                                     int32_t *d_new_len, int32_t *d_new_state, int32_t *d_src, int32_t *d_dst, int32_t *d_new_ref,
+                                     int32_t *d_new_free, int32_t *d_new_n_free);
+
+/* Copies pages of n_layers caches of one geometry (types, sizes and strides as the first one's; ATSPEED_E_ARG otherwise): for each
+ * j < n with d_src[j], d_dst[j] both pages of the cache, the first ((d_length[j] - 1) mod page_size) + 1 tokens (d_length NULL:
+ * the whole page; a length below 1: none) of page d_src[j] to page d_dst[j], keys and values of all heads.  A page is written by one
+ * copy at most and read by none that is written in the same call (fork_pages' pairs are such; others leave either content).
+ * head_dim a multiple of 8 (ATSPEED_E_SHAPE). */
+atspeed_status atspeed_op_copy_pages(atspeed_stream stream, const atspeed_kv_pages *layers, int n_layers, int n, const int32_t *d_src,
+                                     const int32_t *d_dst, const int32_t *d_length);
+
+/* Moves what a step keeps of its new tokens behind the cached ones, in n_layers caches of one geometry.  Request b keeps its
+ * tokens d_keep[b][0 .. d_n_keep[b]) (indices among the request's, ascending: an accepted path of a tree whose parents come
+ * before their children); the list ends at the first entry that is not below the request's tokens or not above the one before it.
+ * Keys and values of token d_keep[b][i] go from cache row d_slot[d_cu_q[b] + d_keep[b][i]] to d_slot[d_cu_q[b] + i] (the plan's; moves
+ * from or to a row outside the cache are left out).  d_new_len [n_req] = d_kv_len[b] + the tokens kept; requests
+ * with d_state[b] other than ATSPEED_PLAN_OK (d_state NULL: none) keep nothing, d_kv_len [n_req] are the plan's.
+ * T: rows of d_slot (entries of d_cu_q are taken within 0 .. T).  head_dim a multiple of 8 (ATSPEED_E_SHAPE). */
+atspeed_status atspeed_op_compact_tokens(atspeed_stream stream, const atspeed_kv_pages *layers, int n_layers, int n_req, int T,
+                                         const int64_t *d_slot, const int32_t *d_cu_q, const int32_t *d_kv_len,
+                                         const int32_t *d_state, const int32_t *d_keep, int keep_width, const int32_t *d_n_keep,
+                                         int32_t *d_new_len);
+
 #ifdef __cplusplus
 }
 #endif

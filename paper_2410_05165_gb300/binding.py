@@ -31,7 +31,8 @@ EXPORTS = [
     "atspeed_debug_node_logits", "atspeed_debug_node_lse", "atspeed_debug_buffer", "atspeed_set_tree", "atspeed_op_workspace_bytes", "atspeed_op_gemm",
     "atspeed_op_gemm_noalloc", "atspeed_op_status", "atspeed_op_gemm_swiglu", "atspeed_op_rmsnorm", "atspeed_op_attention_scratch", "atspeed_op_attention",
     "atspeed_op_batch_plan", "atspeed_op_rope_append", "atspeed_op_tree_attention_workspace", "atspeed_op_tree_attention",
-    "atspeed_op_adjust_logits", "atspeed_op_capture_id",
+    "atspeed_op_adjust_logits", "atspeed_op_capture_id", "atspeed_op_beam_select_workspace", "atspeed_op_beam_select",
+    "atspeed_op_fork_pages", "atspeed_op_copy_pages", "atspeed_op_compact_tokens",
 ]
 
 
@@ -137,6 +138,13 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "atspeed_op_capture_id": (ctypes.c_uint64, [vp]),
         "atspeed_op_adjust_logits": (c_int, [vp, vp, c_int, ctypes.c_int64, c_int, c_int, vp,
                                              ctypes.POINTER(LogitRulesDesc), vp, c_int, vp, vp, c_int, ctypes.c_int64]),
+        "atspeed_op_beam_select_workspace": (ctypes.c_size_t, [c_int, c_int, c_int]),
+        "atspeed_op_beam_select": (c_int, [vp, vp, c_int, ctypes.c_int64, c_int, c_int, vp, vp, c_int, vp, c_int, vp, vp,
+                                           ctypes.c_int64, c_int, c_int, vp, vp, vp, vp]),
+        "atspeed_op_fork_pages": (c_int, [vp, c_int, c_int, vp, c_int, c_int, vp, vp, vp, vp, vp, c_int, vp, vp, vp, vp, vp, vp, vp, vp,
+                                          vp, vp, vp, vp]),
+        "atspeed_op_copy_pages": (c_int, [vp, ctypes.POINTER(KvPages), c_int, c_int, vp, vp, vp]),
+        "atspeed_op_compact_tokens": (c_int, [vp, ctypes.POINTER(KvPages), c_int, c_int, c_int, vp, vp, vp, vp, vp, c_int, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -689,3 +697,132 @@ def op_adjust_logits(logits: torch.Tensor, req: torch.Tensor, rules: LogitRules,
                                            _tensor(mask, torch.int32, R, "mask", gpu), mask.shape[1] if mask is not None else 0,
                                            _tensor(state, torch.int32, R, "state", gpu), out.data_ptr(), ot, _pitch(out, V)))
     return out
+
+
+# ---------------------------------------------------------------------------------------------------
+# what follows a step's logits: beam selection, fork of block tables, copies of pages, compaction of an accepted path
+# ---------------------------------------------------------------------------------------------------
+class BeamChoice:
+    """Outputs of op_beam_select [n][width], best first (see atspeed_op_beam_select)."""
+    __slots__ = ("token", "parent", "score")
+
+    def __init__(self, token, parent, score):
+        self.token = token      # int32, -1: no continuation
+        self.parent = parent    # int32, the row of the logits, -1: none
+        self.score = score      # float32, -infinity: none
+
+
+def op_beam_select(logits: torch.Tensor, cu_beam: torch.Tensor, width: int, score: Optional[torch.Tensor] = None,
+                   final: Optional[torch.Tensor] = None, grammar: Optional[torch.Tensor] = None,
+                   state: Optional[torch.Tensor] = None, norm: int = NORM_MASKED, stream=None) -> BeamChoice:
+    """The best continuations of each request's beams, rows cu_beam[b] .. cu_beam[b + 1] - 1 of logits [R][vocab] (any stride apart)."""
+    it, dev, gpu = _DTYPES.get(logits.dtype), logits.device, _gpu(logits, stream)
+    if logits.dim() != 2 or it is None or (logits.stride(1) != 1 and logits.shape[1] != 1):
+        _refuse(f"logits: [R][vocab], not {tuple(logits.shape)} {logits.dtype}")
+    (R, V), n, i32, f32 = logits.shape, cu_beam.numel() - 1, torch.int32, torch.float32
+    if n < 1 or R < 1 or V < 1 or width < 1 or (state is None) != (grammar is None) or (grammar is not None and grammar.dim() != 2):
+        _refuse(f"{n} requests, {R} rows of {V}, width {width}, state {'missing' if state is None else 'given'}, grammar "
+                f"{'missing' if grammar is None else tuple(grammar.shape)}")
+    lib = load()
+    cu_ptr, score_ptr = _given(cu_beam, i32, 2, "cu_beam", gpu), _tensor(score, f32, R, "score", gpu)
+    final_ptr, state_ptr = _tensor(final, i32, R, "final", gpu), _tensor(state, i32, R, "state", gpu)
+    words, states, grammar_ptr = 0, 0, None
+    if grammar is not None:
+        states, words = grammar.shape
+        grammar_ptr = _tensor(grammar, i32, 1, "grammar", gpu)
+    token, parent, out, ws = _outputs(dev, stream, ((n, width), i32), ((n, width), i32), ((n, width), f32),
+                                      ((lib.atspeed_op_beam_select_workspace(R, V, width),), torch.uint8))
+    _check(lib.atspeed_op_beam_select(_raw_stream(stream, dev), logits.data_ptr(), it, _pitch(logits, V), R, V, score_ptr, final_ptr,
+                                      n, cu_ptr, width, state_ptr, grammar_ptr, words, states, norm, token.data_ptr(),
+                                      parent.data_ptr(), out.data_ptr(), ws.data_ptr()))
+    return BeamChoice(token, parent, out)
+
+
+class PageFork:
+    """Outputs of op_fork_pages (see atspeed_op_fork_pages)."""
+    __slots__ = ("table", "kv_len", "state", "src", "dst", "ref", "free", "n_free")
+
+    def __init__(self, table, kv_len, state, src, dst, ref, free, n_free):
+        self.table = table      # [m][width] int32, -1 behind a row's pages
+        self.kv_len = kv_len    # [m] int32, -1: not served
+        self.state = state      # [m] int32, PLAN_*
+        self.src = src          # [m] int32, page to copy from, -1: none
+        self.dst = dst          # [m] int32, page to copy to, -1: none
+        self.ref = ref          # [pages] int32, who holds a page
+        self.free = free        # [pages] int32, free pages, -1 behind them
+        self.n_free = n_free    # [1] int32
+
+
+def op_fork_pages(table: torch.Tensor, kv_len: torch.Tensor, ref: torch.Tensor, free: torch.Tensor, n_free: torch.Tensor,
+                  page_size: int, q_len: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None,
+                  used: Optional[torch.Tensor] = None, parent: Optional[torch.Tensor] = None,
+                  length: Optional[torch.Tensor] = None, out: Optional[PageFork] = None, stream=None) -> PageFork:
+    """New rows of block tables, page counts and free list from old ones, which stay as they are.  used: the plan's count of pages
+    taken (BatchPlan.pages or .used); out: a fork of the same sizes to write into, not the one that the inputs are from."""
+    i32, dev, gpu = torch.int32, table.device, _gpu(table, stream)
+    n, pages = kv_len.numel(), ref.numel()
+    if table.dim() != 2 or table.shape[0] != n or n < 1 or pages < 1 or (parent is None and length is not None and length.numel() != n):
+        _refuse(f"{n} rows, table {tuple(table.shape)}, {pages} pages, {'no parents' if parent is None else parent.numel()}")
+    m, width = n if parent is None else parent.numel(), table.shape[1]
+    ins = (_given(table, i32, n, "table", gpu), width, page_size, _given(kv_len, i32, n, "kv_len", gpu), _tensor(q_len, i32, n, "q_len", gpu),
+           _tensor(state, i32, n, "state", gpu), _tensor(parent, i32, 1, "parent", gpu), _tensor(length, i32, m, "length", gpu), pages,
+           _given(ref, i32, pages, "ref", gpu))
+    n_free_ptr = _given(n_free, i32, 1, "n_free", gpu)
+    free_ptr = _given(free, i32, 0, "free", gpu) if free.numel() else n_free_ptr   # (n_free is 0: nothing is read of it)
+    used_ptr = _tensor(used, i32, 1, "used", gpu)
+    if out is None:
+        out = PageFork(*_outputs(dev, stream, ((m, width), i32), ((m,), i32), ((m,), i32), ((m,), i32), ((m,), i32), ((pages,), i32),
+                                 ((pages,), i32), ((1,), i32)))
+        outs = [getattr(out, k).data_ptr() for k in PageFork.__slots__]
+    else:
+        if out.table.shape != (m, width):
+            _refuse(f"out.table: [{m}][{width}], not {tuple(out.table.shape)}")
+        outs = [_given(getattr(out, k), i32, size, "out." + k, gpu)
+                for k, size in zip(PageFork.__slots__, (m * width, m, m, m, m, pages, pages, 1))]
+    _check(load().atspeed_op_fork_pages(_raw_stream(stream, dev), n, m, *ins, free_ptr, n_free_ptr, used_ptr, *outs))
+    return out
+
+
+class CacheLayers:
+    """All layers' caches, [(K, V), ..] of one geometry, each [pages][page_size][kv heads][head_dim] (any strides but the last): what
+    op_copy_pages and op_compact_tokens move rows in.  Made once; keeps the tensors alive."""
+
+    def __init__(self, caches: Sequence[Tuple[torch.Tensor, torch.Tensor]]):
+        if not caches:
+            _refuse("no layers")
+        self._keep = [tuple(c) for c in caches]
+        self.device = caches[0][0].device
+        self.gpu = caches[0][0].get_device()
+        if self.gpu < 0:
+            _refuse("caches on the CPU")
+        self.n = len(caches)
+        self.desc = (KvPages * self.n)(*[_kv_pages(k, v, self.gpu) for k, v in caches])
+
+    def _on(self, stream) -> int:
+        if self.gpu != torch._C._cuda_getDevice() or (stream is not None and stream.device.index != self.gpu):
+            _refuse(f"caches on {self.device}, stream on {'it' if stream is None else stream.device}: not both the current device")
+        return self.gpu
+
+
+def op_copy_pages(layers: CacheLayers, src: torch.Tensor, dst: torch.Tensor, length: Optional[torch.Tensor] = None,
+                  stream=None) -> None:
+    """The first ((length - 1) mod page size) + 1 tokens (None: all) of pages src to pages dst, K and V of all layers; -1: none."""
+    gpu, n, i32 = layers._on(stream), src.numel(), torch.int32
+    if n < 1:
+        _refuse("no pages")
+    _check(load().atspeed_op_copy_pages(_raw_stream(stream, layers.device), layers.desc, layers.n, n, _given(src, i32, n, "src", gpu),
+                                        _given(dst, i32, n, "dst", gpu), _tensor(length, i32, n, "length", gpu)))
+
+
+def op_compact_tokens(layers: CacheLayers, slot: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor, keep: torch.Tensor,
+                      n_keep: torch.Tensor, state: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Moves the kept ones keep [n][..] (n_keep [n] of them, ascending) of each request's new tokens behind the cached ones, K and V of
+    all layers; slot, cu_q, state: the plan's.  Returns the cached tokens of each request [n]."""
+    gpu, n, i32 = layers._on(stream), kv_len.numel(), torch.int32
+    if n < 1 or keep.dim() != 2 or keep.shape[0] != n or keep.shape[1] < 1 or slot.numel() < 1:
+        _refuse(f"{n} requests, {slot.numel()} slots, keep {tuple(keep.shape)}")
+    ins = (slot.numel(), _given(slot, torch.int64, 1, "slot", gpu), _given(cu_q, i32, n + 1, "cu_q", gpu), _given(kv_len, i32, n, "kv_len", gpu),
+           _tensor(state, i32, n, "state", gpu), _given(keep, i32, n, "keep", gpu), keep.shape[1], _given(n_keep, i32, n, "n_keep", gpu))
+    new_len, = _outputs(layers.device, stream, ((n,), i32))
+    _check(load().atspeed_op_compact_tokens(_raw_stream(stream, layers.device), layers.desc, layers.n, n, *ins, new_len.data_ptr()))
+    return new_len

@@ -19,7 +19,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libatspeed.so")
 
 SOURCES = ["api.cu", "ops.cu", "gemm.cu", "gemm_cluster.cu", "gemm_pair.cu", "attention.cu", "norm.cu", "select.cu", "tree_ops.cu", "fwd.cu",
-           "batch_plan.cu", "rope_append.cu", "tree_attention.cu", "logit_rules.cu"]
+           "batch_plan.cu", "rope_append.cu", "tree_attention.cu", "logit_rules.cu",
+           "beam_select.cu", "fork_pages.cu", "move_rows.cu"]
 EXTRA = {}
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC,
