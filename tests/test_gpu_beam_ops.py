@@ -212,6 +212,26 @@ def test_select_values_that_are_not_finite(ats):
         _check_select(ats, logits.to(dtype), [5], 300 - 44, score=[-1, -2, -3, -4, -5])
 
 
+@pytest.mark.parametrize("at", [1000.0, 2.0 ** 20, -2.0 ** 20, 3e6, -1e9, 1e30, -3e38])
+def test_select_logits_far_out(ats, at):
+    """Maxima on both sides of where sums change their units; a row's parts on both sides."""
+    V = 9000
+    g = torch.Generator("cuda").manual_seed(1)
+    logits = (torch.randn(4, V, generator=g, device="cuda") * 3 + at).contiguous()
+    logits[1, ::3] = -5.0
+    logits[2, 4096:] -= 1e7 if abs(at) < 1e8 else 0.0
+    for dtype in (torch.float32, torch.bfloat16):
+        for r in range(4):
+            x = logits[r:r + 1].to(dtype)
+            lp, _ = _log_probs(_rows(x), dtype, np.ones((1, V), bool), False)
+            got = ats.op_beam_select(x, _dev([0, 1]), 20)
+            best = np.sort(lp[0])[::-1][:20]
+            out = got.score[0].double().cpu().numpy()
+            # (where only the differences of far out logits count: a difference, a product, the constant of a term's exponent, 2.3 steps of
+            # differences of up to 100 that count)
+            assert (np.abs(out - best) <= _tolerance(V) + 230 * 2.0 ** -24 + np.abs(best) * 2.0 ** -24).all(), (dtype, r)
+
+
 def test_select_scores_far_out(ats):
     """Beams marked as empty by a score far down or -infinity, and scores of any size."""
     logits = _logits(4, 6, 5000, torch.float32)
