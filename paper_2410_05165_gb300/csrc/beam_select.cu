@@ -13,6 +13,7 @@
 //
 // Sums of a row do not depend on where the row begins in memory: rows with the same logits have the same bits.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "step_ops.cuh"
@@ -21,8 +22,7 @@ namespace atspeed {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kPer = 16;                    // logits of a thread in a tile
-constexpr int kTile = kThreads * kPer;
+constexpr int kVec = 4;                     // 16-byte vectors of a thread in a tile
 constexpr int kList = 1024;                 // candidates that a piece's list holds
 constexpr int kMaxWidth = 256;
 constexpr int kRankThreads = 1024, kRankList = 2048;
@@ -64,28 +64,51 @@ __device__ __forceinline__ unsigned long long key_of(double x) {
 
 template <int TYPE>
 struct In {
-  static constexpr int N = TYPE == ATSPEED_F32 ? 4 : 8;   // logits of 16 bytes
+  static constexpr int SIZE = TYPE == ATSPEED_F32 ? 4 : 2, N = 16 / SIZE;   // N: logits of 16 bytes
+  static constexpr int TILE = kThreads * kVec * N;
+  static constexpr uint32_t NONE = TYPE == ATSPEED_F32 ? 0xff800000u : TYPE == ATSPEED_F16 ? 0xfc00u : 0xff80u;   // -infinity
+  static constexpr uint32_t MOST = TYPE == ATSPEED_F32 ? 0x7f7fffffu : TYPE == ATSPEED_F16 ? 0x7bffu : 0x7f7fu;
+  static __device__ __forceinline__ float value(uint32_t bits) {
+    if constexpr (TYPE == ATSPEED_F32) return __uint_as_float(bits);
+    else return unpack2(bits, TYPE == ATSPEED_F16).x;
+  }
+};
+// A thread's logits of a tile, as they are in memory; which of them it is by constants alone.
+template <int TYPE>
+struct Tile {
+  uint32_t w[kVec][4];
+  __device__ __forceinline__ float at(int v, int j) const {
+    if constexpr (TYPE == ATSPEED_F32) return __uint_as_float(w[v][j]);
+    else if constexpr (TYPE == ATSPEED_BF16) return __uint_as_float(j & 1 ? w[v][j / 2] & 0xffff0000u : w[v][j / 2] << 16);
+    else return j & 1 ? unpack2(w[v][j / 2], true).y : unpack2(w[v][j / 2], true).x;
+  }
+  __device__ __forceinline__ void set(int v, int j, uint32_t bits) {
+    if constexpr (TYPE == ATSPEED_F32) w[v][j] = bits;
+    else w[v][j / 2] = j & 1 ? (w[v][j / 2] & 0xffffu) | bits << 16 : (w[v][j / 2] & 0xffff0000u) | bits;
+  }
 };
 
-// The largest t with at least `want` of the warp's keys (E a lane, all valid ones above kNone) at or above it, or a
-// smaller one with at most `most` there; kNone + 1 where there are fewer than `want`.
-template <int E>
-__device__ uint32_t warp_threshold(const uint32_t (&k)[E], int want, int most) {
+// The largest t with at least `want` of n keys in shared memory at or above it, or a smaller one with at most `most` there; 0
+// where fewer than `want` are above kNone.  A warp.
+__device__ __forceinline__ uint32_t threshold_of(const uint32_t* keys, int n, int want, int most) {
+  const int lane = threadIdx.x & 31;
   uint32_t lo = 0xffffffffu, hi = 0;
   int valid = 0;
-#pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (k[e] > kNone) lo = min(lo, k[e]), hi = max(hi, k[e]), ++valid;
+#pragma unroll 4
+  for (int i = lane; i < n; i += 32) {
+    const uint32_t k = keys[i];
+    if (k > kNone) lo = min(lo, k), hi = max(hi, k), ++valid;
+  }
   valid = __reduce_add_sync(0xffffffffu, valid);
-  if (valid < want) return kNone + 1;
+  if (valid < want) return 0;
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
   if (valid <= most) return lo;
   while (lo < hi) {   // at least `want` at lo, fewer above hi
     const uint32_t mid = lo + (hi - lo) / 2 + 1;
     int c = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) c += k[e] >= mid;
+#pragma unroll 8
+    for (int i = lane; i < n; i += 32) c += keys[i] >= mid;
     c = __reduce_add_sync(0xffffffffu, c);
     if (c >= want) {
       lo = mid;
@@ -100,8 +123,11 @@ __device__ uint32_t warp_threshold(const uint32_t (&k)[E], int want, int most) {
 struct Shared {
   uint32_t key[kList];
   int tok[kList];
-  uint32_t group[4 * kThreads];
-  int n, count[kWarps];
+  uint32_t group[kVec * kThreads];
+  uint32_t from;
+  int n;             // candidates in the list, once they are known
+  int more[3];       // what tiles add to it, one after the other
+  int count[kWarps];
   float m[kWarps], s[kWarps];
 };
 
@@ -117,7 +143,7 @@ __device__ __forceinline__ int block_count(int v, Shared& sh) {   // the sum ove
 }
 
 // Cuts the list to its W best (equal keys: the lower tokens); returns the W-th key.  Every thread of the CTA.
-__device__ uint32_t cut_list(Shared& sh, int W) {
+__device__ __noinline__ uint32_t cut_list(Shared& sh, int W) {
   constexpr int E = kList / kThreads;
   const int n = sh.n;
   uint32_t k[E];
@@ -188,134 +214,195 @@ __device__ __forceinline__ float rescale(float m, float M) {
                           : NEAR ? fmaf(m, kLog2e, -unit_of(M)) : (m - M) * kLog2e);
 }
 
+// The W best of a tile's tokens [t0, end), where more than the list holds are at or above `from`, exactly: into the list behind its `had`
+// candidates (equal ones in the tokens' order).  Reads the tile again.  Every thread of the CTA; returns what the list then holds.
 template <int TYPE>
-__global__ void __launch_bounds__(kThreads) beam_pieces_kernel(const __grid_constant__ SelectArgs a) {
-  constexpr int N = In<TYPE>::N, SIZE = 16 / N;
+__device__ __noinline__ int put_exactly(const SelectArgs& a, const char* in, const uint32_t* allowed, int t0, int end, uint32_t from, int had,
+                                        Shared& sh) {
+  const int tid = threadIdx.x;
+  const auto key = [&](int t) {
+    if (t >= end || (allowed && !(__ldg(allowed + (t >> 5)) >> (t & 31) & 1))) return 0u;
+    using Bits = std::conditional_t<In<TYPE>::SIZE == 4, uint32_t, uint16_t>;
+    const float y = In<TYPE>::value(__ldg(reinterpret_cast<const Bits*>(in) + t));
+    const uint32_t k = y == y ? key_of(fminf(y, In<TYPE>::value(In<TYPE>::MOST))) : 0u;
+    return k >= from ? k : 0u;
+  };
+  uint32_t lo = from, hi = 0xffffffffu;
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo) / 2 + 1;
+    int c = 0;
+    for (int t = t0 + tid; t < t0 + In<TYPE>::TILE; t += kThreads) c += key(t) >= mid;
+    if (block_count(c, sh) >= a.W) lo = mid;
+    else hi = mid - 1;
+  }
+  int above = 0;
+  for (int t = t0 + tid; t < t0 + In<TYPE>::TILE; t += kThreads) above += key(t) > lo;
+  above = block_count(above, sh);
+  if (tid == 0) sh.n = had;
+  __syncthreads();
+  int at = had + above, room = a.W - above;   // of the equal ones (at least one)
+  for (int t1 = t0; t1 < t0 + In<TYPE>::TILE; t1 += kThreads) {
+    const uint32_t k = key(t1 + tid);
+    const unsigned same = __ballot_sync(0xffffffffu, k == lo);
+    const int all = room > 0 ? block_count((tid & 31) == 0 ? __popc(same) : 0, sh) : 0;   // (sh.count: the warps')
+    int place = -1;
+    if (k > lo) {
+      place = atomicAdd(&sh.n, 1);
+    } else if (k == lo) {
+      int nth = __popc(same & ((1u << (tid & 31)) - 1u));
+      for (int w = 0; w < tid >> 5; ++w) nth += sh.count[w];
+      if (nth < room) place = at + nth;
+    }
+    if (place >= 0) {
+      sh.key[place] = k;
+      sh.tok[place] = t1 + tid;
+    }
+    at += min(room, all);
+    room -= min(room, all);
+  }
+  __syncthreads();
+  return at;
+}
+
+// ALIGNED: every row begins at a multiple of 16 bytes.
+template <int TYPE, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(const __grid_constant__ SelectArgs a) {
+  constexpr int N = In<TYPE>::N, SIZE = In<TYPE>::SIZE, TILE = In<TYPE>::TILE;
   __shared__ Shared sh;
   const int row = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_launch_dependents();
+  const int begin = piece * a.span, end = min(a.V, begin + a.span);
+  const char* in = static_cast<const char*>(a.logits) + (long long)row * a.ld * SIZE;
+  const unsigned lead = ALIGNED ? 0u : (unsigned)(reinterpret_cast<uintptr_t>(in) & 15);   // bytes that the row begins behind a 16-byte word
+  const auto token = [&](int t0, int v) { return t0 + (v * kThreads + tid) * N; };   // the first of a vector
+  // A thread's logits of a tile, wherever the row begins: the 16-byte words that they lie in, shifted.  At a row's ends one by one.
+  const auto load = [&](int t0, Tile<TYPE>& x) {
+    if (ALIGNED && t0 + TILE <= end) {
+#pragma unroll
+      for (int v = 0; v < kVec; ++v) {
+        const uint4 p = __ldcs(reinterpret_cast<const uint4*>(in + (long long)token(t0, v) * SIZE));
+        x.w[v][0] = p.x, x.w[v][1] = p.y, x.w[v][2] = p.z, x.w[v][3] = p.w;
+      }
+      return;
+    }
+    if (!ALIGNED && t0 > 0 && t0 + TILE + N <= end) {
+      uint4 p[kVec], q[kVec];
+#pragma unroll
+      for (int v = 0; v < kVec; ++v) {
+        const uint4* at = reinterpret_cast<const uint4*>(in + (long long)token(t0, v) * SIZE - lead);
+        p[v] = __ldg(at);
+        q[v] = __ldg(at + 1);   // (lead 0: not needed; the other words of a line that is read anyway)
+      }
+#pragma unroll
+      for (int v = 0; v < kVec; ++v) {
+        uint32_t y[8] = {p[v].x, p[v].y, p[v].z, p[v].w, q[v].x, q[v].y, q[v].z, q[v].w};
+        if (lead & 8) {
+#pragma unroll
+          for (int j = 0; j < 6; ++j) y[j] = y[j + 2];
+        }
+        if (lead & 4) {
+#pragma unroll
+          for (int j = 0; j < 5; ++j) y[j] = y[j + 1];
+        }
+        if (SIZE == 2 && (lead & 2)) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] = __funnelshift_r(y[j], y[j + 1], 16);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x.w[v][j] = y[j];
+      }
+      return;
+    }
+#pragma unroll
+    for (int v = 0; v < kVec; ++v) {
+      const int t = token(t0, v);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (SIZE == 4) {
+          x.w[v][j] = t + j < end ? __ldg(reinterpret_cast<const uint32_t*>(in) + t + j) : In<TYPE>::NONE;
+        } else {
+          const uint16_t* h = reinterpret_cast<const uint16_t*>(in);
+          const uint32_t lo = t + 2 * j < end ? __ldg(h + t + 2 * j) : In<TYPE>::NONE;
+          const uint32_t hi = t + 2 * j + 1 < end ? __ldg(h + t + 2 * j + 1) : In<TYPE>::NONE;
+          x.w[v][j] = lo | hi << 16;
+        }
+      }
+    }
+  };
   const int cu0 = __ldg(a.cu), cu1 = __ldg(a.cu + a.n_req);
   if (row < cu0 || row >= cu1 || (a.final && __ldg(a.final + row) >= 0)) return;   // (the other kernel knows as much)
   const int st = a.state ? __ldg(a.state + row) : -1;
   const uint32_t* allowed = st >= 0 && st < a.n_states ? a.grammar + st * a.grammar_stride : nullptr;
   const bool nothing = st >= a.n_states && a.state;
-  const int begin = piece * a.span, end = min(a.V, begin + a.span);
-  const char* in = static_cast<const char*>(a.logits) + (long long)row * a.ld * SIZE;
-  const unsigned lead = (unsigned)(reinterpret_cast<uintptr_t>(in) & 15);   // bytes that the row begins behind a 16-byte word
-  if (tid == 0) sh.n = 0;
+  Tile<TYPE> x;
+  load(begin, x);
+  if (tid < 3) sh.more[tid] = 0;
   float m = -INFINITY, s = 0.f;   // the thread's maximum and sum
   uint32_t floor = kNone;         // only what is above it is a candidate
   bool open = true;               // .. and fewer than W are known at or above a bound
+  int n = 0, again = 0;           // candidates in the list; how many there may be before the bound is looked for anew
   __syncthreads();
-  for (int t0 = begin; t0 < end; t0 += kTile) {
-    float x[kPer];   // token t0 + (i / N * kThreads + tid) * N + i % N
-    const auto token = [&](int i) { return t0 + (i / N * kThreads + tid) * N + i % N; };
-    // A thread's logits of a vector, wherever the row begins: the 16-byte words that they lie in, shifted.  At the row's ends one by one.
-    uint4 w[kPer / N];
-    if (t0 + kTile <= end && lead == 0) {
+  for (int t0 = begin, turn = 0; t0 < end; t0 += TILE, turn = turn == 2 ? 0 : turn + 1) {
+    const auto each = [&](auto&& f) {
 #pragma unroll
-      for (int v = 0; v < kPer / N; ++v) w[v] = __ldcs(reinterpret_cast<const uint4*>(in + (long long)token(v * N) * SIZE));
-    } else {
+      for (int v = 0; v < kVec; ++v)
 #pragma unroll
-      for (int v = 0; v < kPer / N; ++v) {
-        const int t = token(v * N);
-        const char* at = in + (long long)t * SIZE - lead;
-        if (t + 2 * N <= a.V && t + N <= end && t > 0) {
-          const uint4 p = __ldg(reinterpret_cast<const uint4*>(at));
-          w[v] = p;
-          if (lead) {
-            const uint4 q = __ldg(reinterpret_cast<const uint4*>(at) + 1);
-            uint32_t y[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
-            if (lead & 8) {
-#pragma unroll
-              for (int j = 0; j < 6; ++j) y[j] = y[j + 2];
-            }
-            if (lead & 4) {
-#pragma unroll
-              for (int j = 0; j < 5; ++j) y[j] = y[j + 1];
-            }
-            if (SIZE == 2 && (lead & 2)) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) y[j] = __funnelshift_r(y[j], y[j + 1], 16);
-            }
-            w[v] = make_uint4(y[0], y[1], y[2], y[3]);
-          }
-        } else {
-          uint32_t y[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if constexpr (SIZE == 4) {
-              y[j] = t + j < end ? __ldg(reinterpret_cast<const uint32_t*>(in) + t + j) : 0xff800000u;
-            } else {
-              const uint16_t* h = reinterpret_cast<const uint16_t*>(in);
-              const uint32_t none = TYPE == ATSPEED_F16 ? 0xfc00u : 0xff80u;
-              const uint32_t lo = t + 2 * j < end ? __ldg(h + t + 2 * j) : none, hi = t + 2 * j + 1 < end ? __ldg(h + t + 2 * j + 1) : none;
-              y[j] = lo | hi << 16;
-            }
-          }
-          w[v] = make_uint4(y[0], y[1], y[2], y[3]);
-        }
-      }
-    }
-#pragma unroll
-    for (int v = 0; v < kPer / N; ++v) {
-      const uint32_t y[4] = {w[v].x, w[v].y, w[v].z, w[v].w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (SIZE == 4) {
-          x[v * N + j] = __uint_as_float(y[j]);
-        } else {
-          const float2 f = unpack2(y[j], TYPE == ATSPEED_F16);
-          x[v * N + 2 * j] = f.x;
-          x[v * N + 2 * j + 1] = f.y;
-        }
-      }
-    }
-    uint32_t ok = 0xffffffffu;   // bit i: token(i) is allowed
+        for (int j = 0; j < N; ++j) f(v, j);
+    };
+    uint32_t ok = 0xffffffffu;   // bit v N + j: that token is allowed
     if (allowed) {
       ok = 0;
 #pragma unroll
-      for (int v = 0; v < kPer / N; ++v) {   // (a vector's bits lie in one word)
-        const int t = token(v * N);
+      for (int v = 0; v < kVec; ++v) {   // (a vector's bits lie in one word)
+        const int t = token(t0, v);
         if (t < end) ok |= (__ldg(allowed + (t >> 5)) >> (t & 31) & ((1u << N) - 1)) << v * N;
       }
     } else if (nothing) {
       ok = 0;
     }
-    if (ok != 0xffffffffu && !a.full) {
+    const bool hidden = allowed || nothing;
+    const auto hide = [&] {
+      each([&](int v, int j) {
+        if (!(ok >> (v * N + j) & 1)) x.set(v, j, In<TYPE>::NONE);
+      });
+    };
+    float vm[kVec], top;   // of the vectors, of all (a NaN is passed over)
+    const auto tops = [&] {
 #pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (!(ok >> i & 1)) x[i] = -INFINITY;
-    }
-    float top = x[0];   // (a NaN is passed over)
+      for (int v = 0; v < kVec; ++v) {
+        vm[v] = fmaxf(x.at(v, 0), x.at(v, 1));
 #pragma unroll
-    for (int i = 1; i < kPer; ++i) top = fmaxf(top, x[i]);
-    top = fmaxf(top, -INFINITY);
+        for (int j = 2; j < N; ++j) vm[v] = fmaxf(vm[v], x.at(v, j));
+        vm[v] = fmaxf(vm[v], -INFINITY);
+      }
+      top = vm[0];
+#pragma unroll
+      for (int v = 1; v < kVec; ++v) top = fmaxf(top, vm[v]);
+    };
+    if (hidden && !a.full) hide();
+    tops();
     float sum = 0.f, M = fmaxf(m, top);
     if (M > -INFINITY) {
       if (fabsf(M) < kFar) {
         const float u = unit_of(M);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) sum += exp2_approx(fmaf(x[i], kLog2e, -u));
+        float more = 0.f;
+        each([&](int v, int j) { (j & 1 ? more : sum) += exp2_approx(fmaf(x.at(v, j), kLog2e, -u)); });
+        sum += more;
       } else {
         sum = NAN;
       }
       if (sum != sum) {   // a NaN (it counts as -infinity), an infinity (as the type's largest), logits far out
-        constexpr float most = TYPE == ATSPEED_F32 ? 3.40282347e38f : TYPE == ATSPEED_BF16 ? 3.38953139e38f : 65504.f;
-        top = -INFINITY;
-        sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          x[i] = x[i] == x[i] ? fminf(x[i], most) : -INFINITY;
-          top = fmaxf(top, x[i]);
-        }
+        each([&](int v, int j) {
+          const float y = x.at(v, j);
+          if (y != y) x.set(v, j, In<TYPE>::NONE);
+          else if (y == INFINITY) x.set(v, j, In<TYPE>::MOST);
+        });
+        tops();
         M = fmaxf(m, top);
+        sum = 0.f;
         const bool near = fabsf(M) < kFar;
         const float u = unit_of(M);
-        if (M > -INFINITY) {
-#pragma unroll
-          for (int i = 0; i < kPer; ++i) sum += exp2_approx(near ? fmaf(x[i], kLog2e, -u) : (x[i] - M) * kLog2e);
-        }
+        if (M > -INFINITY) each([&](int v, int j) { sum += exp2_approx(near ? fmaf(x.at(v, j), kLog2e, -u) : (x.at(v, j) - M) * kLog2e); });
       }
       if (M > m) {
         s = m > -INFINITY ? s * rescale(m, M) : 0.f;
@@ -323,130 +410,98 @@ __global__ void __launch_bounds__(kThreads) beam_pieces_kernel(const __grid_cons
       }
     }
     s += sum;
-    if (ok != 0xffffffffu && a.full) {
-      top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        if (!(ok >> i & 1)) x[i] = -INFINITY;
-        top = fmaxf(top, x[i]);
-      }
+    if (hidden && a.full) {
+      hide();
+      tops();
     }
-    uint32_t from = floor + 1;
+    uint32_t from = floor + 1, bound = 0;
     if (open) {   // from the W-th of the groups' maxima on
-      if (a.W <= kThreads / 4) {
+      int groups = kThreads;
+      if (a.W <= 32) {
         sh.group[tid] = key_of(top);
-        __syncthreads();
-        uint32_t e[kThreads / 32];
-#pragma unroll
-        for (int i = 0; i < kThreads / 32; ++i) e[i] = sh.group[i * 32 + lane];
-        from = max(from, warp_threshold(e, a.W, a.W + a.W / 4));
+      } else if (a.W <= 128) {
+        sh.group[tid] = key_of(fmaxf(vm[0], vm[1]));
+        sh.group[kThreads + tid] = key_of(fmaxf(vm[2], vm[3]));
+        groups = 2 * kThreads;
       } else {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float g = x[q];
-#pragma unroll
-          for (int i = 1; i < kPer / 4; ++i) g = fmaxf(g, x[4 * i + q]);
-          sh.group[q * kThreads + tid] = key_of(g);
-        }
-        __syncthreads();
-        uint32_t e[4 * kThreads / 32];
-#pragma unroll
-        for (int i = 0; i < 4 * kThreads / 32; ++i) e[i] = sh.group[i * 32 + lane];
-        from = max(from, warp_threshold(e, a.W, a.W + a.W / 4));
+        for (int v = 0; v < kVec; ++v) sh.group[v * kThreads + tid] = key_of(vm[v]);
+        groups = kVec * kThreads;
       }
+      __syncthreads();
+      if (warp == 0) {
+        const uint32_t t = threshold_of(sh.group, groups, a.W, a.W + a.W / 4);
+        if (lane == 0) sh.from = t;
+      }
+      __syncthreads();
+      bound = sh.from;
+      from = max(from, bound);
     }
     const float least = value_of(from);
-    const int had = sh.n;
-    __syncthreads();
-    if (top >= least) {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (x[i] >= least) {
-          const int at = atomicAdd(&sh.n, 1);
+    if (top >= least)
+      each([&](int v, int j) {
+        const float y = x.at(v, j);
+        if (y >= least) {
+          const int at = n + atomicAdd(&sh.more[turn], 1);
           if (at < kList) {
-            sh.key[at] = key_of(x[i]);
-            sh.tok[at] = token(i);
+            sh.key[at] = key_of(y);
+            sh.tok[at] = token(t0, v) + j;
           }
         }
-    }
+      });
+    if (tid == 0) sh.more[turn == 2 ? 0 : turn + 1] = 0;   // (last read two barriers ago)
     __syncthreads();
-    if (sh.n > kList) {   // too many: the tile's W best exactly, equal ones in the tokens' order
-      uint32_t k[kPer];
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) k[i] = x[i] >= least ? key_of(x[i]) : 0u;
-      uint32_t lo = from, hi = 0xffffffffu;
-      while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2 + 1;
-        int c = 0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) c += k[i] >= mid;
-        if (block_count(c, sh) >= a.W) lo = mid;
-        else hi = mid - 1;
-      }
-      int above = 0;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) above += k[i] > lo;
-      int room = a.W - block_count(above, sh);   // for equal ones (at least one)
-      __syncthreads();
-      if (tid == 0) sh.n = had;
-      __syncthreads();
-      const auto put = [&](int i, int at) {
-        sh.key[at] = k[i];
-        sh.tok[at] = token(i);
-      };
-#pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (k[i] > lo) put(i, atomicAdd(&sh.n, 1));
-      __syncthreads();
-      int at0 = sh.n;
-      // (a thread's tokens follow each other in its vectors, the vectors of all threads in the tile)
-#pragma unroll
-      for (int v = 0; v < kPer / N; ++v) {
-        int mine = 0;
-#pragma unroll
-        for (int j = 0; j < N; ++j) mine += k[v * N + j] == lo;
-        int upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int y = __shfl_up_sync(0xffffffffu, upto, o);
-          if (lane >= o) upto += y;
-        }
-        __syncthreads();
-        if (lane == 31) sh.count[warp] = upto;
-        __syncthreads();
-        int nth = upto - mine, all = 0;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          if (w < warp) nth += sh.count[w];
-          all += sh.count[w];
-        }
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (k[v * N + j] == lo) {
-            if (nth < room) put(v * N + j, at0 + nth);
-            ++nth;
-          }
-        at0 += min(room, all);
-        room -= min(room, all);
-      }
-      __syncthreads();
-      if (tid == 0) sh.n = at0;
-      __syncthreads();
-    }
-    if (open && from > kNone + 1) {   // (W of the tile's are at `from` or above: a later token there comes after them)
+    const int had = n;
+    n += sh.more[turn];
+    if (n > kList) n = put_exactly<TYPE>(a, in, allowed, t0, end, from, had, sh);
+    if (t0 + TILE < end) load(t0 + TILE, x);
+    if (bound) {   // (W of the tile's are at `from` or above: a later token there comes after them)
       open = false;
       floor = from;
+      again = n + a.W / 2;
     }
-    if (sh.n > kList / 2) {
+    if (n > kList / 2) {
+      if (tid == 0) sh.n = n;
       open = false;
-      floor = cut_list(sh, a.W);
+      floor = max(floor, cut_list(sh, a.W));
+      n = a.W;
+      again = n + a.W / 2;
+    } else if (!open && n > again && t0 + TILE < end) {   // a better bound: the W-th (or so) of the list
+      if (warp == 0) {
+        const uint32_t t = threshold_of(sh.key, n, a.W, a.W + a.W / 4);
+        if (lane == 0) sh.from = t;
+      }
+      __syncthreads();
+      floor = max(floor, sh.from);
+      again = n + a.W / 2;
+    }
+  }
+  // hands on the list, or what is at or above a bound that leaves few enough
+  const long long at = (long long)row * a.pieces + piece;
+  uint32_t from = 0;
+  if (n > a.cap) {
+    if (warp == 0) {
+      const uint32_t t = threshold_of(sh.key, n, a.W, a.cap);
+      int c = 0;
+      for (int i = lane; i < n; i += 32) c += sh.key[i] >= t;
+      c = __reduce_add_sync(0xffffffffu, c);
+      if (lane == 0) {
+        sh.from = t;
+        sh.n = c;
+      }
+    }
+    __syncthreads();
+    from = sh.from;
+    if (sh.n > a.cap) {   // (equal ones)
+      __syncthreads();
+      if (tid == 0) sh.n = n;
+      cut_list(sh, a.W);
+      n = a.W;
+      from = 0;
     }
     __syncthreads();
   }
-  if (sh.n > a.cap) cut_list(sh, a.W);
-  const long long at = (long long)row * a.pieces + piece;
-  for (int i = tid; i < sh.n; i += kThreads)
-    a.cand[at * a.cap + i] = make_uint2(__float_as_uint(value_of(sh.key[i])), (uint32_t)sh.tok[i]);
+  if (tid == 0) sh.n = 0;
   // the piece's sum, in one order
   float M = warp_max(m);
   if (lane == 0) sh.m[warp] = M;
@@ -455,6 +510,8 @@ __global__ void __launch_bounds__(kThreads) beam_pieces_kernel(const __grid_cons
   for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sh.m[w]);
   const float sum = warp_sum(m > -INFINITY ? s * rescale(m, M) : 0.f);
   if (lane == 0) sh.s[warp] = sum;
+  for (int i = tid; i < n; i += kThreads)
+    if (sh.key[i] >= from) a.cand[at * a.cap + atomicAdd(&sh.n, 1)] = make_uint2(__float_as_uint(value_of(sh.key[i])), (uint32_t)sh.tok[i]);
   __syncthreads();
   if (tid == 0) {
     float all = 0.f;
@@ -473,7 +530,7 @@ struct Entry {
 // score = cum + ((x - off) - more)
 struct Row {
   double off, more;
-  float cum;
+  float cum, off32, more32;
   int final;   // the one token of an ended beam; -1
 };
 
@@ -523,93 +580,129 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
   const int lists = max(0, r1 - r0) * a.pieces;
   if (tid == 0) sh.n = 0;
   pdl_wait();
-  for (int r = r0 + tid; r < r1; r += kRankThreads) {
-    Row w = {0.0, 0.0, a.score ? __ldg(a.score + r) : 0.f, a.final ? __ldg(a.final + r) : -1};
-    if (w.final < 0) {
+  const auto row_at = [&](int r) -> Row& { return r - r0 < kRows ? sh.row[r - r0] : a.rows[r]; };
+  // A row's maximum and sum from its pieces: many pieces by a warp, few by a thread; then its logarithm.
+  // (Sums as multiples of 2^-32, whole numbers: a row's is at least 0.7 and at most 1.5 times its length.)
+  const auto whole = [&](float s) { return (unsigned long long)(s * 0x1p32f); };
+  const auto set_row = [&](int r, float M, unsigned long long s) {
+    Row w = {0.0, 0.0, a.score ? __ldg(a.score + r) : 0.f, 0.f, 0.f, -1};
+    const double l = log((double)s * 0x1p-32);
+    if (fabsf(M) < kFar) w.off = (double)unit_of(M) * kLn2 + l - (double)M * kEta;
+    else w.off = (double)M, w.more = l;
+    w.off32 = (float)w.off, w.more32 = (float)w.more;
+    row_at(r) = w;
+  };
+  const auto final_of = [&](int r) { return a.final ? __ldg(a.final + r) : -1; };
+  const auto set_final = [&](int r, int f) { row_at(r) = {0.0, 0.0, a.score ? __ldg(a.score + r) : 0.f, 0.f, 0.f, f}; };
+  if (a.pieces <= 2) {
+    for (int r = r0 + tid; r < r1; r += kRankThreads) {
+      const int f = final_of(r);
+      if (f >= 0) {
+        set_final(r, f);
+        continue;
+      }
       const Header* h = a.head + (long long)r * a.pieces;
-      float M = -INFINITY;
-      for (int p = 0; p < a.pieces; ++p) M = fmaxf(M, h[p].m);
-      double s = 0.0;
-      for (int p = 0; p < a.pieces; ++p)
-        if (h[p].m > -INFINITY) s += (double)(h[p].s * rescale(h[p].m, M));   
-      const double l = log(s);
-      if (fabsf(M) < kFar) w.off = (double)unit_of(M) * kLn2 + l - (double)M * kEta;
-      else w.off = (double)M, w.more = l;
+      const float m0 = h[0].m, s0 = h[0].s, m1 = a.pieces > 1 ? h[1].m : -INFINITY, s1 = a.pieces > 1 ? h[1].s : 0.f;
+      const float M = fmaxf(m0, m1);
+      set_row(r, M, M > -INFINITY ? whole(s0 * rescale(m0, M)) + whole(s1 * rescale(m1, M)) : 0ull);
     }
-    if (r - r0 < kRows) sh.row[r - r0] = w;
-    else a.rows[r] = w;
+  } else {
+    for (int base = r0; base < r1; base += kRankThreads) {   // (a thousand rows at a time, whose sums wait in the list's place)
+      const int last = min(r1, base + kRankThreads);
+      for (int r = base + warp; r < last; r += kRankThreads / 32) {
+        const Header* h = a.head + (long long)r * a.pieces;
+        const bool live = final_of(r) < 0;
+        float M = -INFINITY;
+        for (int p = lane; live && p < a.pieces; p += 32) M = fmaxf(M, h[p].m);
+        M = warp_max(M);
+        unsigned long long s = 0;
+        for (int p = lane; live && p < a.pieces; p += 32)
+          if (h[p].m > -INFINITY) s += whole(h[p].s * rescale(h[p].m, M));
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lane == 0) {
+          sh.group[r - base] = __float_as_uint(M);
+          sh.score[r - base] = s;
+        }
+      }
+      __syncthreads();
+      if (base + tid < last) {
+        const int r = base + tid, f = final_of(r);
+        if (f >= 0) set_final(r, f);
+        else set_row(r, __uint_as_float(sh.group[tid]), sh.score[tid]);
+      }
+      __syncthreads();
+    }
   }
   __syncthreads();
-  // Candidate `at` of list l, in 32 bits: between low and high.
+  // Candidates: a thread has place `at` of list my_list and of every lists_at_once-th list from there.
   const int lists_at_once = kRankThreads / a.cap, at = tid % a.cap, my_list = tid / a.cap;
-  struct Found {
-    float x, low, high;
-    uint32_t tok;
-    int row;
-  };
-  const auto row_of = [&](int r) -> const Row& { return r - r0 < kRows ? sh.row[r - r0] : a.rows[r]; };
-  const auto look = [&](int l, const uint2& c, int n, Found& f) {   // c, n: of that list
-    f.row = r0 + l / a.pieces;
-    const Row& w = row_of(f.row);
-    if (w.final >= 0) {
-      f.tok = (uint32_t)w.final, f.x = 0.f, f.low = f.high = w.cum;
-      return at == 0 && l % a.pieces == 0;
-    }
-    f.x = __uint_as_float(c.x), f.tok = c.y;
-    const float off = (float)w.off, more = (float)w.more;
-    const float y = w.cum + ((f.x - off) - more), e = 0x1p-21f * (fabsf(w.cum) + fabsf(f.x) + fabsf(off) + fabsf(more));
-    f.low = y - e, f.high = y + e;
-    return at < n;
-  };
   const auto fetch = [&](int l, uint2& c, int& n) {
     const long long h = (long long)r0 * a.pieces + l;
     c = a.cand[h * a.cap + at];
     n = a.head[h].n;
   };
-  float from = -INFINITY;   // what is below it (in 32 bits) is not among the W best
-  if (lists > lists_at_once) {   // more than a step's: from the W-th of the threads' best on
-    float g = -INFINITY;
-    for (int l = my_list; l < lists; l += 4 * lists_at_once) {
-      uint2 c[4];
-      int n[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (l + q * lists_at_once < lists) fetch(l + q * lists_at_once, c[q], n[q]);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        Found f;
-        if (l + q * lists_at_once < lists && look(l + q * lists_at_once, c[q], n[q], f)) g = fmaxf(g, f.low);   // (not a NaN)
-      }
+  // Its score in 32 bits, and how far that may be off (four roundings); false: there is none
+  const auto look = [&](int l, uint2& c, int n, float& y, float& e) {
+    const Row& w = row_at(r0 + l / a.pieces);
+    if (w.final >= 0) {
+      c = make_uint2(0u, (uint32_t)w.final);
+      y = w.cum, e = 0.f;
+      return at == 0 && l % a.pieces == 0;
     }
-    sh.group[tid] = key_of(g);
-    __syncthreads();
-    if (warp == 0) {
-      uint32_t k[kRankThreads / 32];
+    const float x = __uint_as_float(c.x);
+    y = w.cum + ((x - w.off32) - w.more32);
+    e = 0x1p-21f * (fabsf(w.cum) + fabsf(x) + fabsf(w.off32) + fabsf(w.more32));
+    return at < n;
+  };
+  // what is below `from` is not among the W best: the W-th of the threads' best (some of them have W candidates, or they are few)
+  constexpr int kHold = 4;
+  const bool hold = lists <= kHold * lists_at_once;
+  uint2 c[kHold];
+  int cn[kHold];
+  float g = -INFINITY;
+  for (int l0 = 0; l0 < lists; l0 += kHold * lists_at_once) {
 #pragma unroll
-      for (int i = 0; i < kRankThreads / 32; ++i) k[i] = sh.group[i * 32 + lane];
-      const uint32_t t = warp_threshold(k, a.W, a.W + a.W / 4);
-      if (lane == 0) sh.from = t;
+    for (int q = 0; q < kHold; ++q) {
+      cn[q] = 0;
+      const int l = l0 + q * lists_at_once + my_list;
+      if (l < lists) fetch(l, c[q], cn[q]);
     }
-    __syncthreads();
-    if (sh.from > kNone + 1) from = value_of(sh.from);
+#pragma unroll
+    for (int q = 0; q < kHold; ++q) {
+      const int l = l0 + q * lists_at_once + my_list;
+      float y, e;
+      if (l < lists && look(l, c[q], cn[q], y, e)) g = fmaxf(g, y - e);   // (not a NaN)
+    }
   }
-  for (int l0 = 0; l0 < lists; l0 += lists_at_once) {
+  sh.group[tid] = key_of(g);
+  __syncthreads();
+  if (warp == 0) {
+    const uint32_t t = threshold_of(sh.group, kRankThreads, a.W, a.W + a.W / 4);
+    if (lane == 0) sh.from = t;
+  }
+  __syncthreads();
+  float from = sh.from ? value_of(sh.from) : -INFINITY;
+  const auto put = [&](int l, uint2 c, int n) {
+    float y, e;
+    if (!look(l, c, n, y, e) || y + e < from) return;
+    const int r = r0 + l / a.pieces;
+    const Row& w = row_at(r);
+    const float x = __uint_as_float(c.x);
+    const double z = w.final >= 0 ? (double)w.cum : (double)w.cum + (((double)x - w.off) - w.more);
+    if (!((float)z > -INFINITY)) return;
+    const int to = atomicAdd(&sh.n, 1);
+    sh.score[to] = key_of(z + 0.0);   // (-0: 0)
+    sh.rest[to] = (unsigned long long)(~(uint32_t)r) << 32 | key_of(x);
+    sh.tok[to] = c.y;
+  };
+#pragma unroll 1
+  for (int l0 = 0, q = 0; l0 < lists; l0 += lists_at_once, ++q) {
     const int l = l0 + my_list;
-    if (my_list < lists_at_once && l < lists) {
-      uint2 c;
-      int n;
-      Found f;
-      fetch(l, c, n);
-      if (look(l, c, n, f) && !(f.high < from)) {
-        const Row& w = row_of(f.row);
-        const double y = w.final >= 0 ? (double)w.cum : (double)w.cum + (((double)f.x - w.off) - w.more);
-        if ((float)y > -INFINITY) {
-          const int to = atomicAdd(&sh.n, 1);
-          sh.score[to] = key_of(y + 0.0);   // (-0: 0)
-          sh.rest[to] = (unsigned long long)(~(uint32_t)f.row) << 32 | key_of(f.x);
-          sh.tok[to] = f.tok;
-        }
-      }
+    if (l < lists) {
+      uint2 x = q == 0 ? c[0] : q == 1 ? c[1] : q == 2 ? c[2] : c[3];
+      int n = q == 0 ? cn[0] : q == 1 ? cn[1] : q == 2 ? cn[2] : cn[3];
+      if (!hold) fetch(l, x, n);
+      put(l, x, n);
     }
     if (l0 + lists_at_once >= lists) break;
     __syncthreads();
@@ -643,9 +736,10 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
   }
 }
 
+constexpr int kTile = In<ATSPEED_F32>::TILE;
 // Pieces of a row: enough CTAs for every SM to have four, none shorter than a tile.
 int pieces_of(int R, int V) {
-  const long long tiles = (V + kTile - 1LL) / kTile;
+  const long long tiles = (V + kTile - 1LL) / kTile;   // (of the smaller tile)
   return (int)std::max(1LL, std::min(tiles, (608LL + R - 1) / R));
 }
 int cap_of(int W) {   
@@ -702,9 +796,11 @@ extern "C" atspeed_status atspeed_op_beam_select(atspeed_stream stream, const vo
   static std::atomic<unsigned long long> done{0};
   if (smem_attr_once(done, beam_rank_kernel, (int)sizeof(RankShared)) != cudaSuccess) return ATSPEED_E_CUDA;
   const int grid = R * l.pieces;
-  if (type == ATSPEED_F32) beam_pieces_kernel<ATSPEED_F32><<<grid, kThreads, 0, (cudaStream_t)stream>>>(a);
-  else if (type == ATSPEED_BF16) beam_pieces_kernel<ATSPEED_BF16><<<grid, kThreads, 0, (cudaStream_t)stream>>>(a);
-  else beam_pieces_kernel<ATSPEED_F16><<<grid, kThreads, 0, (cudaStream_t)stream>>>(a);
+  const bool aligned = aligned16(d_logits) && ld * dtype_size(type) % 16 == 0;
+  const auto go = [&](auto kernel) { kernel<<<grid, kThreads, 0, (cudaStream_t)stream>>>(a); };
+  if (type == ATSPEED_F32) aligned ? go(beam_pieces_kernel<ATSPEED_F32, true>) : go(beam_pieces_kernel<ATSPEED_F32, false>);
+  else if (type == ATSPEED_BF16) aligned ? go(beam_pieces_kernel<ATSPEED_BF16, true>) : go(beam_pieces_kernel<ATSPEED_BF16, false>);
+  else aligned ? go(beam_pieces_kernel<ATSPEED_F16, true>) : go(beam_pieces_kernel<ATSPEED_F16, false>);
   if (launch_status() != ATSPEED_OK) return ATSPEED_E_CUDA;
   // (it may start while the last of the pieces are read, and waits for them)
   cudaLaunchConfig_t cfg = {};
