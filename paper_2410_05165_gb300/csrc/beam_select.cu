@@ -4,12 +4,12 @@
 //
 // Two launches.  The first reads the logits, a CTA a piece of a row: the piece's maximum, its sum of exponentials and the
 // candidates among its logits, which are at least its W best (within a row the order is the logits').  The second, a CTA a
-// request, makes log s_r of the pieces, scores the candidates in 64 bits and ranks the best.
+// request, makes log s_r of the pieces, scores the candidates and ranks the best.
 //
-// Candidates of a piece: W of the largest values of 256 (1024) groups of its first tile lie at or above the W-th largest group maximum, so what is
-// below it is none; behind that tile only what is above it.  What is left goes to a list in shared memory, that is cut to
-// the W best when it is half full.  A tile that holds more than fits (equal logits, a mask of the type's lowest value) is
-// searched exactly.
+// Candidates of a piece: its tokens form groups (256 or 1024; each a thread's, strided over the whole piece) whose maxima stay in
+// registers while the logits stream by.  W of these maxima, so W logits, are at or above the W-th largest of them: the groups that
+// reach that bound, little more than W of them, are read again (from L2) for what is at or above it.  Where that is more than
+// a list holds (equal logits, a mask of the type's lowest value) the W best are searched exactly.
 //
 // Sums of a row do not depend on where the row begins in memory: rows with the same logits have the same bits.
 #include <algorithm>
@@ -24,6 +24,7 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kVec = 4;                     // 16-byte vectors of a thread in a tile
 constexpr int kList = 1024;                 // candidates that a piece's list holds
+constexpr int kGroups = kThreads * kVec;
 constexpr int kMaxWidth = 256;
 constexpr int kRankThreads = 1024, kRankList = 2048;
 constexpr uint32_t kNone = 0x007fffffu;     // the key of -infinity
@@ -123,11 +124,10 @@ __device__ __forceinline__ uint32_t threshold_of(const uint32_t* keys, int n, in
 struct Shared {
   uint32_t key[kList];
   int tok[kList];
-  uint32_t group[kVec * kThreads];
+  uint32_t group[kGroups];   // groups' maxima
+  uint16_t read[kGroups];    // the groups to be read again
+  int n, n_read, count[kWarps];
   uint32_t from;
-  int n;             // candidates in the list, once they are known
-  int more[3];       // what tiles add to it, one after the other
-  int count[kWarps];
   float m[kWarps], s[kWarps];
 };
 
@@ -140,56 +140,6 @@ __device__ __forceinline__ int block_count(int v, Shared& sh) {   // the sum ove
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) t += sh.count[w];
   return t;
-}
-
-// Cuts the list to its W best (equal keys: the lower tokens); returns the W-th key.  Every thread of the CTA.
-__device__ __noinline__ uint32_t cut_list(Shared& sh, int W) {
-  constexpr int E = kList / kThreads;
-  const int n = sh.n;
-  uint32_t k[E];
-  int t[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int i = e * kThreads + threadIdx.x;
-    k[e] = i < n ? sh.key[i] : 0u;
-    t[e] = i < n ? sh.tok[i] : 0;
-  }
-  uint32_t lo = kNone + 1, hi = 0xffffffffu;
-  while (lo < hi) {   // (n > W: at least W at lo)
-    const uint32_t mid = lo + (hi - lo) / 2 + 1;
-    int c = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) c += k[e] >= mid;
-    if (block_count(c, sh) >= W) lo = mid;
-    else hi = mid - 1;
-  }
-  int above = 0;
-#pragma unroll
-  for (int e = 0; e < E; ++e) above += k[e] > lo;
-  above = block_count(above, sh);
-  // of the keys at lo, those with fewer than W - above lower tokens
-  bool keep[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    keep[e] = k[e] > lo;
-    if (k[e] == lo) {
-      int before = 0;
-      for (int i = 0; i < n; ++i) before += sh.key[i] == lo && sh.tok[i] < t[e];
-      keep[e] = above + before < W;
-    }
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) sh.n = 0;
-  __syncthreads();
-#pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (keep[e]) {
-      const int at = atomicAdd(&sh.n, 1);
-      sh.key[at] = k[e];
-      sh.tok[at] = t[e];
-    }
-  __syncthreads();
-  return lo;
 }
 
 // A sum of exponentials below a maximum m: for |m| < kFar in units of the whole power of two 2^unit_of(m), its terms 2^(x l - unit)
@@ -214,54 +164,63 @@ __device__ __forceinline__ float rescale(float m, float M) {
                           : NEAR ? fmaf(m, kLog2e, -unit_of(M)) : (m - M) * kLog2e);
 }
 
-// The W best of a tile's tokens [t0, end), where more than the list holds are at or above `from`, exactly: into the list behind its `had`
-// candidates (equal ones in the tokens' order).  Reads the tile again.  Every thread of the CTA; returns what the list then holds.
+// A token's key, 0 if it is not a candidate at or above `from`.
 template <int TYPE>
-__device__ __noinline__ int put_exactly(const SelectArgs& a, const char* in, const uint32_t* allowed, int t0, int end, uint32_t from, int had,
-                                        Shared& sh) {
+__device__ __forceinline__ uint32_t key_at(const char* in, const uint32_t* allowed, int t, uint32_t from) {
+  if (allowed && !(__ldg(allowed + (t >> 5)) >> (t & 31) & 1)) return 0u;
+  using Bits = std::conditional_t<In<TYPE>::SIZE == 4, uint32_t, uint16_t>;
+  const float y = In<TYPE>::value(__ldg(reinterpret_cast<const Bits*>(in) + t));
+  const uint32_t k = y == y ? key_of(fminf(y, In<TYPE>::value(In<TYPE>::MOST))) : 0u;   // (NaN: -infinity)
+  return k >= from ? k : 0u;
+}
+
+// The W best of the tokens [begin, end), of which more than W are at or above `from`, exactly (equal ones in the tokens' order), into the
+// list.  Every thread of the CTA.
+template <int TYPE>
+__device__ __noinline__ void put_exactly(const char* in, const uint32_t* allowed, int begin, int end, uint32_t from, int W, Shared& sh) {
   const int tid = threadIdx.x;
-  const auto key = [&](int t) {
-    if (t >= end || (allowed && !(__ldg(allowed + (t >> 5)) >> (t & 31) & 1))) return 0u;
-    using Bits = std::conditional_t<In<TYPE>::SIZE == 4, uint32_t, uint16_t>;
-    const float y = In<TYPE>::value(__ldg(reinterpret_cast<const Bits*>(in) + t));
-    const uint32_t k = y == y ? key_of(fminf(y, In<TYPE>::value(In<TYPE>::MOST))) : 0u;
-    return k >= from ? k : 0u;
+  const auto count = [&](uint32_t least) {
+    int c = 0;
+    for (int t = begin + tid; t < end; t += kThreads) c += key_at<TYPE>(in, allowed, t, least) != 0;
+    return block_count(c, sh);
   };
   uint32_t lo = from, hi = 0xffffffffu;
-  while (lo < hi) {
-    const uint32_t mid = lo + (hi - lo) / 2 + 1;
-    int c = 0;
-    for (int t = t0 + tid; t < t0 + In<TYPE>::TILE; t += kThreads) c += key(t) >= mid;
-    if (block_count(c, sh) >= a.W) lo = mid;
-    else hi = mid - 1;
+  int above = count(lo + 1);
+  if (above >= W) {   // at least W at lo + 1, fewer above hi
+    ++lo;
+    while (lo < hi) {
+      const uint32_t mid = lo + (hi - lo) / 2 + 1;
+      if (count(mid) >= W) lo = mid;
+      else hi = mid - 1;
+    }
+    above = count(lo + 1);
   }
-  int above = 0;
-  for (int t = t0 + tid; t < t0 + In<TYPE>::TILE; t += kThreads) above += key(t) > lo;
-  above = block_count(above, sh);
-  if (tid == 0) sh.n = had;
+  if (tid == 0) sh.n = 0;
   __syncthreads();
-  int at = had + above, room = a.W - above;   // of the equal ones (at least one)
-  for (int t1 = t0; t1 < t0 + In<TYPE>::TILE; t1 += kThreads) {
-    const uint32_t k = key(t1 + tid);
+  int at = above, room = W - above;   // of the equal ones
+  for (int t0 = begin; t0 < end; t0 += kThreads) {
+    const int t = t0 + tid;
+    const uint32_t k = t < end ? key_at<TYPE>(in, allowed, t, lo) : 0u;
     const unsigned same = __ballot_sync(0xffffffffu, k == lo);
     const int all = room > 0 ? block_count((tid & 31) == 0 ? __popc(same) : 0, sh) : 0;   // (sh.count: the warps')
     int place = -1;
     if (k > lo) {
       place = atomicAdd(&sh.n, 1);
-    } else if (k == lo) {
+    } else if (k == lo && room > 0) {
       int nth = __popc(same & ((1u << (tid & 31)) - 1u));
       for (int w = 0; w < tid >> 5; ++w) nth += sh.count[w];
       if (nth < room) place = at + nth;
     }
     if (place >= 0) {
       sh.key[place] = k;
-      sh.tok[place] = t1 + tid;
+      sh.tok[place] = t;
     }
     at += min(room, all);
     room -= min(room, all);
   }
   __syncthreads();
-  return at;
+  if (tid == 0) sh.n = at;
+  __syncthreads();
 }
 
 // ALIGNED: every row begins at a multiple of 16 bytes.
@@ -332,39 +291,22 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
   const int cu0 = __ldg(a.cu), cu1 = __ldg(a.cu + a.n_req);
   if (row < cu0 || row >= cu1 || (a.final && __ldg(a.final + row) >= 0)) return;   // (the other kernel knows as much)
   const int st = a.state ? __ldg(a.state + row) : -1;
-  const uint32_t* allowed = st >= 0 && st < a.n_states ? a.grammar + st * a.grammar_stride : nullptr;
-  const bool nothing = st >= a.n_states && a.state;
-  Tile<TYPE> x;
-  load(begin, x);
-  if (tid < 3) sh.more[tid] = 0;
+  const bool nothing = a.state && st >= a.n_states;
+  const uint32_t* allowed = st >= 0 && !nothing ? a.grammar + st * a.grammar_stride : nullptr;
   float m = -INFINITY, s = 0.f;   // the thread's maximum and sum
-  uint32_t floor = kNone;         // only what is above it is a candidate
-  bool open = true;               // .. and fewer than W are known at or above a bound
-  int n = 0, again = 0;           // candidates in the list; how many there may be before the bound is looked for anew
-  __syncthreads();
-  for (int t0 = begin, turn = 0; t0 < end; t0 += TILE, turn = turn == 2 ? 0 : turn + 1) {
+  float best[kVec];               // .. and the largest candidates in its vectors' places: a group's maximum each
+#pragma unroll
+  for (int v = 0; v < kVec; ++v) best[v] = -INFINITY;
+  Tile<TYPE> next;
+  load(begin, next);
+  for (int t0 = begin; t0 < end; t0 += TILE) {
+    Tile<TYPE> x = next;
+    if (t0 + TILE < end) load(t0 + TILE, next);
     const auto each = [&](auto&& f) {
 #pragma unroll
       for (int v = 0; v < kVec; ++v)
 #pragma unroll
         for (int j = 0; j < N; ++j) f(v, j);
-    };
-    uint32_t ok = 0xffffffffu;   // bit v N + j: that token is allowed
-    if (allowed) {
-      ok = 0;
-#pragma unroll
-      for (int v = 0; v < kVec; ++v) {   // (a vector's bits lie in one word)
-        const int t = token(t0, v);
-        if (t < end) ok |= (__ldg(allowed + (t >> 5)) >> (t & 31) & ((1u << N) - 1)) << v * N;
-      }
-    } else if (nothing) {
-      ok = 0;
-    }
-    const bool hidden = allowed || nothing;
-    const auto hide = [&] {
-      each([&](int v, int j) {
-        if (!(ok >> (v * N + j) & 1)) x.set(v, j, In<TYPE>::NONE);
-      });
     };
     float vm[kVec], top;   // of the vectors, of all (a NaN is passed over)
     const auto tops = [&] {
@@ -379,7 +321,20 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
 #pragma unroll
       for (int v = 1; v < kVec; ++v) top = fmaxf(top, vm[v]);
     };
-    if (hidden && !a.full) hide();
+    uint32_t ok = 0;   // bit v N + j: that token is allowed
+    const auto hide = [&] {
+      each([&](int v, int j) {
+        if (!(ok >> (v * N + j) & 1)) x.set(v, j, In<TYPE>::NONE);
+      });
+    };
+    if (allowed) {
+#pragma unroll
+      for (int v = 0; v < kVec; ++v) {   // (a vector's bits lie in one word)
+        const int t = token(t0, v);
+        if (t < end) ok |= (__ldg(allowed + (t >> 5)) >> (t & 31) & ((1u << N) - 1)) << v * N;
+      }
+      if (!a.full) hide();
+    }
     tops();
     float sum = 0.f, M = fmaxf(m, top);
     if (M > -INFINITY) {
@@ -410,113 +365,71 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
       }
     }
     s += sum;
-    if (hidden && a.full) {
+    if (allowed && a.full) {
       hide();
       tops();
     }
-    uint32_t from = floor + 1, bound = 0;
-    if (open) {   // from the W-th of the groups' maxima on
-      int groups = kThreads;
-      if (a.W <= 32) {
-        sh.group[tid] = key_of(top);
-      } else if (a.W <= 128) {
-        sh.group[tid] = key_of(fmaxf(vm[0], vm[1]));
-        sh.group[kThreads + tid] = key_of(fmaxf(vm[2], vm[3]));
-        groups = 2 * kThreads;
-      } else {
 #pragma unroll
-        for (int v = 0; v < kVec; ++v) sh.group[v * kThreads + tid] = key_of(vm[v]);
-        groups = kVec * kThreads;
-      }
-      __syncthreads();
-      if (warp == 0) {
-        const uint32_t t = threshold_of(sh.group, groups, a.W, a.W + a.W / 4);
-        if (lane == 0) sh.from = t;
-      }
-      __syncthreads();
-      bound = sh.from;
-      from = max(from, bound);
-    }
-    const float least = value_of(from);
-    if (top >= least)
-      each([&](int v, int j) {
-        const float y = x.at(v, j);
-        if (y >= least) {
-          const int at = n + atomicAdd(&sh.more[turn], 1);
-          if (at < kList) {
-            sh.key[at] = key_of(y);
-            sh.tok[at] = token(t0, v) + j;
-          }
+    for (int v = 0; v < kVec; ++v) best[v] = fmaxf(best[v], vm[v]);
+  }
+  // the W-th largest of the groups' maxima, or a smaller value with little more above it
+  const bool wide = a.W > kThreads / 4;   // (a group a vector's place, not a thread)
+  if (wide) {
+#pragma unroll
+    for (int v = 0; v < kVec; ++v) sh.group[v * kThreads + tid] = key_of(best[v]);
+  } else {
+    sh.group[tid] = key_of(fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])));
+  }
+  static_assert(kVec == 4, "vectors of a thread");
+  const float wm = warp_max(m);
+  if (lane == 0) sh.m[warp] = wm;
+  if (tid == 0) sh.n = sh.n_read = 0;
+  __syncthreads();
+  float M = sh.m[0];
+#pragma unroll
+  for (int w = 1; w < kWarps; ++w) M = fmaxf(M, sh.m[w]);
+  const float ws = warp_sum(m > -INFINITY ? s * rescale(m, M) : 0.f);
+  if (lane == 0) sh.s[warp] = ws;
+  if (warp == 0) {
+    const uint32_t t = threshold_of(sh.group, wide ? kGroups : kThreads, a.W, a.W + a.W / 4);
+    if (lane == 0) sh.from = t ? t : kNone + 1;
+  }
+  __syncthreads();
+  const uint32_t from = sh.from;
+  for (int g = tid; g < (wide ? kGroups : kThreads); g += kThreads)
+    if (sh.group[g] >= from) sh.read[atomicAdd(&sh.n_read, 1)] = (uint16_t)g;
+  __syncthreads();
+  const int vectors = wide ? 1 : kVec, tiles = (end - begin + TILE - 1) / TILE;   // (of a group in a tile)
+  const int reads = nothing ? 0 : sh.n_read * vectors * tiles;
+  for (int i = tid; i < reads; i += kThreads) {
+    const int g = sh.read[i % sh.n_read], k = i / sh.n_read;
+    const int v = wide ? g / kThreads : k % kVec, t = begin + k / vectors * TILE + (v * kThreads + g % kThreads) * N;
+    uint32_t key[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) key[j] = t + j < end ? key_at<TYPE>(in, allowed, t + j, from) : 0u;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (key[j]) {
+        const int at = atomicAdd(&sh.n, 1);
+        if (at < kList) {
+          sh.key[at] = key[j];
+          sh.tok[at] = t + j;
         }
-      });
-    if (tid == 0) sh.more[turn == 2 ? 0 : turn + 1] = 0;   // (last read two barriers ago)
-    __syncthreads();
-    const int had = n;
-    n += sh.more[turn];
-    if (n > kList) n = put_exactly<TYPE>(a, in, allowed, t0, end, from, had, sh);
-    if (t0 + TILE < end) load(t0 + TILE, x);
-    if (bound) {   // (W of the tile's are at `from` or above: a later token there comes after them)
-      open = false;
-      floor = from;
-      again = n + a.W / 2;
-    }
-    if (n > kList / 2) {
-      if (tid == 0) sh.n = n;
-      open = false;
-      floor = max(floor, cut_list(sh, a.W));
-      n = a.W;
-      again = n + a.W / 2;
-    } else if (!open && n > again && t0 + TILE < end) {   // a better bound: the W-th (or so) of the list
-      if (warp == 0) {
-        const uint32_t t = threshold_of(sh.key, n, a.W, a.W + a.W / 4);
-        if (lane == 0) sh.from = t;
       }
-      __syncthreads();
-      floor = max(floor, sh.from);
-      again = n + a.W / 2;
-    }
   }
-  // hands on the list, or what is at or above a bound that leaves few enough
+  __syncthreads();
+  if (sh.n > a.cap) {
+    __syncthreads();
+    put_exactly<TYPE>(in, allowed, begin, end, from, a.W, sh);
+  }
   const long long at = (long long)row * a.pieces + piece;
-  uint32_t from = 0;
-  if (n > a.cap) {
-    if (warp == 0) {
-      const uint32_t t = threshold_of(sh.key, n, a.W, a.cap);
-      int c = 0;
-      for (int i = lane; i < n; i += 32) c += sh.key[i] >= t;
-      c = __reduce_add_sync(0xffffffffu, c);
-      if (lane == 0) {
-        sh.from = t;
-        sh.n = c;
-      }
-    }
-    __syncthreads();
-    from = sh.from;
-    if (sh.n > a.cap) {   // (equal ones)
-      __syncthreads();
-      if (tid == 0) sh.n = n;
-      cut_list(sh, a.W);
-      n = a.W;
-      from = 0;
-    }
-    __syncthreads();
-  }
-  if (tid == 0) sh.n = 0;
-  // the piece's sum, in one order
-  float M = warp_max(m);
-  if (lane == 0) sh.m[warp] = M;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sh.m[w]);
-  const float sum = warp_sum(m > -INFINITY ? s * rescale(m, M) : 0.f);
-  if (lane == 0) sh.s[warp] = sum;
+  const int n = sh.n;
   for (int i = tid; i < n; i += kThreads)
-    if (sh.key[i] >= from) a.cand[at * a.cap + atomicAdd(&sh.n, 1)] = make_uint2(__float_as_uint(value_of(sh.key[i])), (uint32_t)sh.tok[i]);
-  __syncthreads();
+    a.cand[at * a.cap + i] = make_uint2(__float_as_uint(value_of(sh.key[i])), (uint32_t)sh.tok[i]);
   if (tid == 0) {
     float all = 0.f;
-    for (int w = 0; w < kWarps; ++w) all += sh.s[w];
-    a.head[at] = {M, all, sh.n, 0};
+    for (int w = 0; w < kWarps; ++w) all += sh.s[w];   // (in one order)
+    a.head[at] = {M, all, n, 0};
   }
 }
 
@@ -580,6 +493,24 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
   const int lists = max(0, r1 - r0) * a.pieces;
   if (tid == 0) sh.n = 0;
   pdl_wait();
+  // Candidates: a thread has place `at` of list my_list and of every lists_at_once-th list from there.
+  const int lists_at_once = kRankThreads / a.cap, at = tid % a.cap, my_list = tid / a.cap;
+  const auto fetch = [&](int l, uint2& c, int& n) {
+    const long long h = (long long)r0 * a.pieces + l;
+    c = a.cand[h * a.cap + at];
+    n = a.head[h].n;
+  };
+  constexpr int kHold = 4;
+  const bool hold = lists <= kHold * lists_at_once;
+  uint2 c[kHold];
+  int cn[kHold];
+#pragma unroll
+  for (int q = 0; q < kHold; ++q) {   // (the first ones are under way while the rows' sums are made)
+    cn[q] = 0;
+    const int l = q * lists_at_once + my_list;
+    if (l < lists) fetch(l, c[q], cn[q]);
+  }
+  const auto row_of = [&](int l) { return r0 + (a.pieces == 1 ? l : l / a.pieces); };
   const auto row_at = [&](int r) -> Row& { return r - r0 < kRows ? sh.row[r - r0] : a.rows[r]; };
   // A row's maximum and sum from its pieces: many pieces by a warp, few by a thread; then its logarithm.
   // (Sums as multiples of 2^-32, whole numbers: a row's is at least 0.7 and at most 1.5 times its length.)
@@ -634,20 +565,14 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
     }
   }
   __syncthreads();
-  // Candidates: a thread has place `at` of list my_list and of every lists_at_once-th list from there.
-  const int lists_at_once = kRankThreads / a.cap, at = tid % a.cap, my_list = tid / a.cap;
-  const auto fetch = [&](int l, uint2& c, int& n) {
-    const long long h = (long long)r0 * a.pieces + l;
-    c = a.cand[h * a.cap + at];
-    n = a.head[h].n;
-  };
   // Its score in 32 bits, and how far that may be off (four roundings); false: there is none
   const auto look = [&](int l, uint2& c, int n, float& y, float& e) {
-    const Row& w = row_at(r0 + l / a.pieces);
+    const int r = row_of(l);
+    const Row& w = row_at(r);
     if (w.final >= 0) {
       c = make_uint2(0u, (uint32_t)w.final);
       y = w.cum, e = 0.f;
-      return at == 0 && l % a.pieces == 0;
+      return at == 0 && l == (r - r0) * a.pieces;
     }
     const float x = __uint_as_float(c.x);
     y = w.cum + ((x - w.off32) - w.more32);
@@ -655,17 +580,15 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
     return at < n;
   };
   // what is below `from` is not among the W best: the W-th of the threads' best (some of them have W candidates, or they are few)
-  constexpr int kHold = 4;
-  const bool hold = lists <= kHold * lists_at_once;
-  uint2 c[kHold];
-  int cn[kHold];
   float g = -INFINITY;
   for (int l0 = 0; l0 < lists; l0 += kHold * lists_at_once) {
+    if (l0) {
 #pragma unroll
-    for (int q = 0; q < kHold; ++q) {
-      cn[q] = 0;
-      const int l = l0 + q * lists_at_once + my_list;
-      if (l < lists) fetch(l, c[q], cn[q]);
+      for (int q = 0; q < kHold; ++q) {
+        cn[q] = 0;
+        const int l = l0 + q * lists_at_once + my_list;
+        if (l < lists) fetch(l, c[q], cn[q]);
+      }
     }
 #pragma unroll
     for (int q = 0; q < kHold; ++q) {
@@ -685,16 +608,22 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
   const auto put = [&](int l, uint2 c, int n) {
     float y, e;
     if (!look(l, c, n, y, e) || y + e < from) return;
-    const int r = r0 + l / a.pieces;
-    const Row& w = row_at(r);
-    const float x = __uint_as_float(c.x);
-    const double z = w.final >= 0 ? (double)w.cum : (double)w.cum + (((double)x - w.off) - w.more);
-    if (!((float)z > -INFINITY)) return;
     const int to = atomicAdd(&sh.n, 1);
-    sh.score[to] = key_of(z + 0.0);   // (-0: 0)
-    sh.rest[to] = (unsigned long long)(~(uint32_t)r) << 32 | key_of(x);
+    sh.rest[to] = (unsigned long long)(uint32_t)row_of(l) << 32 | c.x;
     sh.tok[to] = c.y;
   };
+  // scores of the list's entries from i0 on, in 64 bits (0: it is not to be chosen)
+  const auto finish = [&](int i0, int n) {
+    for (int i = i0 + tid; i < n; i += kRankThreads) {
+      const int r = (int)(sh.rest[i] >> 32);
+      const float x = __uint_as_float((uint32_t)sh.rest[i]);
+      const Row& w = row_at(r);
+      const double z = w.final >= 0 ? (double)w.cum : (double)w.cum + (((double)x - w.off) - w.more);
+      sh.score[i] = (float)z > -INFINITY ? key_of(z + 0.0) : 0ull;   // (-0: 0)
+      sh.rest[i] = (unsigned long long)~(uint32_t)r << 32 | key_of(x);
+    }
+  };
+  int done = 0;   // entries that have their scores
 #pragma unroll 1
   for (int l0 = 0, q = 0; l0 < lists; l0 += lists_at_once, ++q) {
     const int l = l0 + my_list;
@@ -708,13 +637,16 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
     __syncthreads();
     const int n = sh.n;
     if (n > kRankList - kRankThreads) {   // the W best stay
+      finish(done, n);
+      done = min(n, a.W);
+      __syncthreads();
       rank_list(sh, n, a.W, [&](int r, const Entry& e) { sh.best[r] = e; });
       __syncthreads();
       for (int j = tid; j < min(n, a.W); j += kRankThreads) sh.score[j] = sh.best[j].score, sh.rest[j] = sh.best[j].rest, sh.tok[j] = sh.best[j].tok;
       if (tid == 0) {
         sh.n = min(n, a.W);
         // (in 32 bits, rounded down)
-        sh.from = n >= a.W ? key_of(__double2float_rd(score_of(sh.best[a.W - 1].score))) : 0u;
+        sh.from = n >= a.W && sh.best[a.W - 1].score ? key_of(__double2float_rd(score_of(sh.best[a.W - 1].score))) : 0u;
       }
       __syncthreads();
       if (sh.from) from = fmaxf(from, value_of(sh.from));
@@ -723,11 +655,13 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
   }
   __syncthreads();
   const int n = sh.n;
+  finish(done, n);
+  __syncthreads();
   const long long o = (long long)b * a.W;
   rank_list(sh, n, a.W, [&](int r, const Entry& e) {
-    a.token[o + r] = (int)e.tok;
-    a.parent[o + r] = (int)~(uint32_t)(e.rest >> 32);
-    a.out_score[o + r] = (float)score_of(e.score);
+    a.token[o + r] = e.score ? (int)e.tok : -1;
+    a.parent[o + r] = e.score ? (int)~(uint32_t)(e.rest >> 32) : -1;
+    a.out_score[o + r] = e.score ? (float)score_of(e.score) : -INFINITY;
   });
   for (int j = n + tid; j < a.W; j += kRankThreads) {
     a.token[o + j] = -1;
@@ -744,7 +678,7 @@ int pieces_of(int R, int V) {
 }
 int cap_of(int W) {   
   int cap = 32;
-  while (cap < W + std::max(8, W / 4)) cap *= 2;
+  while (cap < W + W / 2 + 8) cap *= 2;
   return cap;
 }
 
