@@ -68,37 +68,40 @@ struct In {
   static constexpr int SIZE = TYPE == ATSPEED_F32 ? 4 : 2, N = 16 / SIZE;   // N: logits of 16 bytes
   static constexpr int TILE = kThreads * kVec * N;
   static constexpr uint32_t NONE = TYPE == ATSPEED_F32 ? 0xff800000u : TYPE == ATSPEED_F16 ? 0xfc00u : 0xff80u;   // -infinity
+  static constexpr uint32_t PAIR = SIZE == 4 ? NONE : NONE * 0x10001u;   // a word of such
   static constexpr uint32_t MOST = TYPE == ATSPEED_F32 ? 0x7f7fffffu : TYPE == ATSPEED_F16 ? 0x7bffu : 0x7f7fu;
   static __device__ __forceinline__ float value(uint32_t bits) {
     if constexpr (TYPE == ATSPEED_F32) return __uint_as_float(bits);
     else return unpack2(bits, TYPE == ATSPEED_F16).x;
   }
 };
-// A thread's logits of a tile, as they are in memory; which of them it is by constants alone.
+// Logit j of a vector; of a thread's logits of a tile, as they are in memory (which of them it is by constants alone).
+template <int TYPE>
+__device__ __forceinline__ float vector_at(const uint32_t (&w)[4], int j) {
+  if constexpr (TYPE == ATSPEED_F32) return __uint_as_float(w[j]);
+  else if constexpr (TYPE == ATSPEED_BF16) return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+  else return j & 1 ? unpack2(w[j / 2], true).y : unpack2(w[j / 2], true).x;
+}
 template <int TYPE>
 struct Tile {
   uint32_t w[kVec][4];
-  __device__ __forceinline__ float at(int v, int j) const {
-    if constexpr (TYPE == ATSPEED_F32) return __uint_as_float(w[v][j]);
-    else if constexpr (TYPE == ATSPEED_BF16) return __uint_as_float(j & 1 ? w[v][j / 2] & 0xffff0000u : w[v][j / 2] << 16);
-    else return j & 1 ? unpack2(w[v][j / 2], true).y : unpack2(w[v][j / 2], true).x;
-  }
+  __device__ __forceinline__ float at(int v, int j) const { return vector_at<TYPE>(w[v], j); }
   __device__ __forceinline__ void set(int v, int j, uint32_t bits) {
     if constexpr (TYPE == ATSPEED_F32) w[v][j] = bits;
     else w[v][j / 2] = j & 1 ? (w[v][j / 2] & 0xffffu) | bits << 16 : (w[v][j / 2] & 0xffff0000u) | bits;
   }
 };
 
-// The largest t with at least `want` of n keys in shared memory at or above it, or a smaller one with at most `most` there; 0
+// The largest t with at least `want` of 32 E keys in shared memory at or above it, or a smaller one with at most `most` there; 0
 // where fewer than `want` are above kNone.  A warp.
-__device__ __forceinline__ uint32_t threshold_of(const uint32_t* keys, int n, int want, int most) {
-  const int lane = threadIdx.x & 31;
-  uint32_t lo = 0xffffffffu, hi = 0;
+template <int E>
+__device__ __forceinline__ uint32_t threshold_of(const uint32_t* keys, int want, int most) {
+  uint32_t k[E], lo = 0xffffffffu, hi = 0;
   int valid = 0;
-#pragma unroll 4
-  for (int i = lane; i < n; i += 32) {
-    const uint32_t k = keys[i];
-    if (k > kNone) lo = min(lo, k), hi = max(hi, k), ++valid;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    k[e] = keys[e * 32 + (threadIdx.x & 31)];
+    if (k[e] > kNone) lo = min(lo, k[e]), hi = max(hi, k[e]), ++valid;
   }
   valid = __reduce_add_sync(0xffffffffu, valid);
   if (valid < want) return 0;
@@ -108,8 +111,8 @@ __device__ __forceinline__ uint32_t threshold_of(const uint32_t* keys, int n, in
   while (lo < hi) {   // at least `want` at lo, fewer above hi
     const uint32_t mid = lo + (hi - lo) / 2 + 1;
     int c = 0;
-#pragma unroll 8
-    for (int i = lane; i < n; i += 32) c += keys[i] >= mid;
+#pragma unroll
+    for (int e = 0; e < E; ++e) c += k[e] >= mid;
     c = __reduce_add_sync(0xffffffffu, c);
     if (c >= want) {
       lo = mid;
@@ -234,13 +237,33 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
   const char* in = static_cast<const char*>(a.logits) + (long long)row * a.ld * SIZE;
   const unsigned lead = ALIGNED ? 0u : (unsigned)(reinterpret_cast<uintptr_t>(in) & 15);   // bytes that the row begins behind a 16-byte word
   const auto token = [&](int t0, int v) { return t0 + (v * kThreads + tid) * N; };   // the first of a vector
+  const auto tail = [&](int t, uint32_t (&w)[4]) {   // a vector's logits one by one
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (SIZE == 4) {
+        w[j] = t + j < end ? __ldg(reinterpret_cast<const uint32_t*>(in) + t + j) : In<TYPE>::NONE;
+      } else {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(in);
+        const uint32_t lo = t + 2 * j < end ? __ldg(h + t + 2 * j) : In<TYPE>::NONE;
+        const uint32_t hi = t + 2 * j + 1 < end ? __ldg(h + t + 2 * j + 1) : In<TYPE>::NONE;
+        w[j] = lo | hi << 16;
+      }
+    }
+  };
   // A thread's logits of a tile, wherever the row begins: the 16-byte words that they lie in, shifted.  At a row's ends one by one.
   const auto load = [&](int t0, Tile<TYPE>& x) {
-    if (ALIGNED && t0 + TILE <= end) {
+    if (ALIGNED) {   // (a vector at the row's end: its tokens past it count as -infinity)
 #pragma unroll
       for (int v = 0; v < kVec; ++v) {
-        const uint4 p = __ldcs(reinterpret_cast<const uint4*>(in + (long long)token(t0, v) * SIZE));
+        const int t = token(t0, v);
+        uint4 p = make_uint4(In<TYPE>::PAIR, In<TYPE>::PAIR, In<TYPE>::PAIR, In<TYPE>::PAIR);
+        if (t + N <= end) p = __ldg(reinterpret_cast<const uint4*>(in + (long long)t * SIZE));
         x.w[v][0] = p.x, x.w[v][1] = p.y, x.w[v][2] = p.z, x.w[v][3] = p.w;
+      }
+      if (t0 + TILE > end) {
+#pragma unroll
+        for (int v = 0; v < kVec; ++v)
+          if (token(t0, v) < end && token(t0, v) + N > end) tail(token(t0, v), x.w[v]);
       }
       return;
     }
@@ -273,35 +296,23 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
       return;
     }
 #pragma unroll
-    for (int v = 0; v < kVec; ++v) {
-      const int t = token(t0, v);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (SIZE == 4) {
-          x.w[v][j] = t + j < end ? __ldg(reinterpret_cast<const uint32_t*>(in) + t + j) : In<TYPE>::NONE;
-        } else {
-          const uint16_t* h = reinterpret_cast<const uint16_t*>(in);
-          const uint32_t lo = t + 2 * j < end ? __ldg(h + t + 2 * j) : In<TYPE>::NONE;
-          const uint32_t hi = t + 2 * j + 1 < end ? __ldg(h + t + 2 * j + 1) : In<TYPE>::NONE;
-          x.w[v][j] = lo | hi << 16;
-        }
-      }
-    }
+    for (int v = 0; v < kVec; ++v) tail(token(t0, v), x.w[v]);
   };
+  Tile<TYPE> x;
+  load(begin, x);
   const int cu0 = __ldg(a.cu), cu1 = __ldg(a.cu + a.n_req);
   if (row < cu0 || row >= cu1 || (a.final && __ldg(a.final + row) >= 0)) return;   // (the other kernel knows as much)
   const int st = a.state ? __ldg(a.state + row) : -1;
   const bool nothing = a.state && st >= a.n_states;
   const uint32_t* allowed = st >= 0 && !nothing ? a.grammar + st * a.grammar_stride : nullptr;
   float m = -INFINITY, s = 0.f;   // the thread's maximum and sum
+  float unit = -INFINITY;         // unit_of(m), a NaN where m is far out
   float best[kVec];               // .. and the largest candidates in its vectors' places: a group's maximum each
 #pragma unroll
   for (int v = 0; v < kVec; ++v) best[v] = -INFINITY;
-  Tile<TYPE> next;
-  load(begin, next);
   for (int t0 = begin; t0 < end; t0 += TILE) {
-    Tile<TYPE> x = next;
-    if (t0 + TILE < end) load(t0 + TILE, next);
+    if (t0 > begin) load(t0, x);
+    if (t0 + warp * 32 * N >= end) break;   // (nothing of the last tile is this warp's)
     const auto each = [&](auto&& f) {
 #pragma unroll
       for (int v = 0; v < kVec; ++v)
@@ -336,35 +347,29 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
       if (!a.full) hide();
     }
     tops();
-    float sum = 0.f, M = fmaxf(m, top);
-    if (M > -INFINITY) {
-      if (fabsf(M) < kFar) {
-        const float u = unit_of(M);
-        float more = 0.f;
-        each([&](int v, int j) { (j & 1 ? more : sum) += exp2_approx(fmaf(x.at(v, j), kLog2e, -u)); });
-        sum += more;
+    float M = fmaxf(m, top);
+    const auto unit_at = [&] { return fabsf(M) < kFar ? unit_of(M) : NAN; };
+    float u = unit_at(), sum = 0.f, more = 0.f;
+    each([&](int v, int j) { (j & 1 ? more : sum) += exp2_approx(fmaf(x.at(v, j), kLog2e, -u)); });
+    sum += fmaf(s, exp2_approx(unit - u), more);
+    if (sum != sum) {   // a NaN (it counts as -infinity), an infinity (as the type's largest), a maximum far out or of -infinity
+      each([&](int v, int j) {
+        const float y = x.at(v, j);
+        if (y != y) x.set(v, j, In<TYPE>::NONE);
+        else if (y == INFINITY) x.set(v, j, In<TYPE>::MOST);
+      });
+      tops();
+      M = fmaxf(m, top);
+      u = unit_at();
+      sum = 0.f;
+      if (M > -INFINITY) {
+        each([&](int v, int j) { sum += exp2_approx(u == u ? fmaf(x.at(v, j), kLog2e, -u) : (x.at(v, j) - M) * kLog2e); });
+        if (m > -INFINITY) sum += s * rescale(m, M);
       } else {
-        sum = NAN;
-      }
-      if (sum != sum) {   // a NaN (it counts as -infinity), an infinity (as the type's largest), logits far out
-        each([&](int v, int j) {
-          const float y = x.at(v, j);
-          if (y != y) x.set(v, j, In<TYPE>::NONE);
-          else if (y == INFINITY) x.set(v, j, In<TYPE>::MOST);
-        });
-        tops();
-        M = fmaxf(m, top);
-        sum = 0.f;
-        const bool near = fabsf(M) < kFar;
-        const float u = unit_of(M);
-        if (M > -INFINITY) each([&](int v, int j) { sum += exp2_approx(near ? fmaf(x.at(v, j), kLog2e, -u) : (x.at(v, j) - M) * kLog2e); });
-      }
-      if (M > m) {
-        s = m > -INFINITY ? s * rescale(m, M) : 0.f;
-        m = M;
+        u = -INFINITY;
       }
     }
-    s += sum;
+    m = M, s = sum, unit = u;
     if (allowed && a.full) {
       hide();
       tops();
@@ -373,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
     for (int v = 0; v < kVec; ++v) best[v] = fmaxf(best[v], vm[v]);
   }
   // the W-th largest of the groups' maxima, or a smaller value with little more above it
-  const bool wide = a.W > kThreads / 4;   // (a group a vector's place, not a thread)
+  const bool wide = a.W > kThreads / 16;   // (a group a vector's place, not a thread)
   if (wide) {
 #pragma unroll
     for (int v = 0; v < kVec; ++v) sh.group[v * kThreads + tid] = key_of(best[v]);
@@ -391,11 +396,12 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
   const float ws = warp_sum(m > -INFINITY ? s * rescale(m, M) : 0.f);
   if (lane == 0) sh.s[warp] = ws;
   if (warp == 0) {
-    const uint32_t t = threshold_of(sh.group, wide ? kGroups : kThreads, a.W, a.W + a.W / 4);
+    const uint32_t t = wide ? threshold_of<kGroups / 32>(sh.group, a.W, a.W + a.W / 4) : threshold_of<kThreads / 32>(sh.group, a.W, a.W + a.W / 4);
     if (lane == 0) sh.from = t ? t : kNone + 1;
   }
   __syncthreads();
   const uint32_t from = sh.from;
+  const float least = value_of(from);
   for (int g = tid; g < (wide ? kGroups : kThreads); g += kThreads)
     if (sh.group[g] >= from) sh.read[atomicAdd(&sh.n_read, 1)] = (uint16_t)g;
   __syncthreads();
@@ -404,15 +410,19 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
   for (int i = tid; i < reads; i += kThreads) {
     const int g = sh.read[i % sh.n_read], k = i / sh.n_read;
     const int v = wide ? g / kThreads : k % kVec, t = begin + k / vectors * TILE + (v * kThreads + g % kThreads) * N;
-    uint32_t key[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) key[j] = t + j < end ? key_at<TYPE>(in, allowed, t + j, from) : 0u;
+    uint32_t w[4];
+    if (ALIGNED && t + N <= end) {
+      const uint4 p = __ldg(reinterpret_cast<const uint4*>(in + (long long)t * SIZE));
+      w[0] = p.x, w[1] = p.y, w[2] = p.z, w[3] = p.w;
+    } else {
+      tail(t, w);
+    }
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      if (key[j]) {
+      if (vector_at<TYPE>(w, j) >= least && (!allowed || (__ldg(allowed + (t >> 5)) >> (t & 31) + j & 1))) {
         const int at = atomicAdd(&sh.n, 1);
         if (at < kList) {
-          sh.key[at] = key[j];
+          sh.key[at] = key_of(fminf(vector_at<TYPE>(w, j), In<TYPE>::value(In<TYPE>::MOST)));
           sh.tok[at] = t + j;
         }
       }
@@ -600,7 +610,7 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
   sh.group[tid] = key_of(g);
   __syncthreads();
   if (warp == 0) {
-    const uint32_t t = threshold_of(sh.group, kRankThreads, a.W, a.W + a.W / 4);
+    const uint32_t t = threshold_of<kRankThreads / 32>(sh.group, a.W, a.W + a.W / 4);
     if (lane == 0) sh.from = t;
   }
   __syncthreads();
