@@ -68,7 +68,6 @@ struct In {
   static constexpr int SIZE = TYPE == ATSPEED_F32 ? 4 : 2, N = 16 / SIZE;   // N: logits of 16 bytes
   static constexpr int TILE = kThreads * kVec * N;
   static constexpr uint32_t NONE = TYPE == ATSPEED_F32 ? 0xff800000u : TYPE == ATSPEED_F16 ? 0xfc00u : 0xff80u;   // -infinity
-  static constexpr uint32_t PAIR = SIZE == 4 ? NONE : NONE * 0x10001u;   // a word of such
   static constexpr uint32_t MOST = TYPE == ATSPEED_F32 ? 0x7f7fffffu : TYPE == ATSPEED_F16 ? 0x7bffu : 0x7f7fu;
   static __device__ __forceinline__ float value(uint32_t bits) {
     if constexpr (TYPE == ATSPEED_F32) return __uint_as_float(bits);
@@ -226,58 +225,71 @@ __device__ __noinline__ void put_exactly(const char* in, const uint32_t* allowed
   __syncthreads();
 }
 
+// A tile's 16-byte words on their way through shared memory, a warp's 32 of a vector in a row, and the one behind them.
+constexpr int kStages = 3;
+struct Stage {
+  uint4 word[kWarps][kVec][33];
+};
+union PieceShared {
+  Stage ring[kStages];   // while the logits stream by
+  Shared sh;             // then
+};
+
+// The first `bytes` of 16 from device to shared memory, zeros behind them.
+__device__ __forceinline__ void copy16(void* to, const void* from, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
+}
+
 // ALIGNED: every row begins at a multiple of 16 bytes.
 template <int TYPE, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(const __grid_constant__ SelectArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) beam_pieces_kernel(const __grid_constant__ SelectArgs a) {
   constexpr int N = In<TYPE>::N, SIZE = In<TYPE>::SIZE, TILE = In<TYPE>::TILE;
-  __shared__ Shared sh;
+  extern __shared__ __align__(16) unsigned char raw[];
+  PieceShared& shared = *reinterpret_cast<PieceShared*>(raw);
+  Shared& sh = shared.sh;
   const int row = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_launch_dependents();
   const int begin = piece * a.span, end = min(a.V, begin + a.span);
   const char* in = static_cast<const char*>(a.logits) + (long long)row * a.ld * SIZE;
   const unsigned lead = ALIGNED ? 0u : (unsigned)(reinterpret_cast<uintptr_t>(in) & 15);   // bytes that the row begins behind a 16-byte word
   const auto token = [&](int t0, int v) { return t0 + (v * kThreads + tid) * N; };   // the first of a vector
-  const auto tail = [&](int t, uint32_t (&w)[4]) {   // a vector's logits one by one
+  // (A word that the row begins in holds bytes of it, so it may be read; behind the piece's end nothing is.)
+  const auto fetch = [&](int t0, int stage) {
+    if (t0 < end) {
+      const char* from = in - lead + (long long)token(t0, 0) * SIZE;
+      auto& to = shared.ring[stage].word[warp];
+      if (t0 + TILE + N <= end) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if constexpr (SIZE == 4) {
-        w[j] = t + j < end ? __ldg(reinterpret_cast<const uint32_t*>(in) + t + j) : In<TYPE>::NONE;
+        for (int v = 0; v < kVec; ++v) copy16(&to[v][lane], from + v * kThreads * 16, 16);
+        if (!ALIGNED && lane < kVec) copy16(&to[lane][32], from + (lane * kThreads + 32 - lane) * 16, 16);
       } else {
-        const uint16_t* h = reinterpret_cast<const uint16_t*>(in);
-        const uint32_t lo = t + 2 * j < end ? __ldg(h + t + 2 * j) : In<TYPE>::NONE;
-        const uint32_t hi = t + 2 * j + 1 < end ? __ldg(h + t + 2 * j + 1) : In<TYPE>::NONE;
-        w[j] = lo | hi << 16;
+        const char* stop = in + (long long)end * SIZE;
+        const auto some = [&](uint4* to, const char* from) {
+          const long long left = stop - from;
+          copy16(to, left > 0 ? from : in, left > 0 ? (int)min(16ll, left) : 0);
+        };
+#pragma unroll
+        for (int v = 0; v < kVec; ++v) some(&to[v][lane], from + v * kThreads * 16);
+        if (!ALIGNED && lane < kVec) some(&to[lane][32], from + (lane * kThreads + 32 - lane) * 16);
       }
     }
+    copies_done();
   };
-  // A thread's logits of a tile, wherever the row begins: the 16-byte words that they lie in, shifted.  At a row's ends one by one.
-  const auto load = [&](int t0, Tile<TYPE>& x) {
-    if (ALIGNED) {   // (a vector at the row's end: its tokens past it count as -infinity)
+  // A thread's logits of a tile, wherever the row begins: its words, shifted.
+  const auto take = [&](int t0, int stage, Tile<TYPE>& x) {
+    const auto& at = shared.ring[stage].word[warp];
 #pragma unroll
-      for (int v = 0; v < kVec; ++v) {
-        const int t = token(t0, v);
-        uint4 p = make_uint4(In<TYPE>::PAIR, In<TYPE>::PAIR, In<TYPE>::PAIR, In<TYPE>::PAIR);
-        if (t + N <= end) p = __ldg(reinterpret_cast<const uint4*>(in + (long long)t * SIZE));
-        x.w[v][0] = p.x, x.w[v][1] = p.y, x.w[v][2] = p.z, x.w[v][3] = p.w;
-      }
-      if (t0 + TILE > end) {
-#pragma unroll
-        for (int v = 0; v < kVec; ++v)
-          if (token(t0, v) < end && token(t0, v) + N > end) tail(token(t0, v), x.w[v]);
-      }
-      return;
-    }
-    if (!ALIGNED && t0 > 0 && t0 + TILE + N <= end) {
-      uint4 p[kVec], q[kVec];
-#pragma unroll
-      for (int v = 0; v < kVec; ++v) {
-        const uint4* at = reinterpret_cast<const uint4*>(in + (long long)token(t0, v) * SIZE - lead);
-        p[v] = __ldg(at);
-        q[v] = __ldg(at + 1);   // (lead 0: not needed; the other words of a line that is read anyway)
-      }
-#pragma unroll
-      for (int v = 0; v < kVec; ++v) {
-        uint32_t y[8] = {p[v].x, p[v].y, p[v].z, p[v].w, q[v].x, q[v].y, q[v].z, q[v].w};
+    for (int v = 0; v < kVec; ++v) {
+      const uint4 p = at[v][lane];
+      x.w[v][0] = p.x, x.w[v][1] = p.y, x.w[v][2] = p.z, x.w[v][3] = p.w;
+      if (!ALIGNED && lead) {
+        const uint4 q = at[v][lane + 1];
+        uint32_t y[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
         if (lead & 8) {
 #pragma unroll
           for (int j = 0; j < 6; ++j) y[j] = y[j + 2];
@@ -293,26 +305,37 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
 #pragma unroll
         for (int j = 0; j < 4; ++j) x.w[v][j] = y[j];
       }
-      return;
     }
+    if (t0 + TILE > end) {
 #pragma unroll
-    for (int v = 0; v < kVec; ++v) tail(token(t0, v), x.w[v]);
+      for (int v = 0; v < kVec; ++v)
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (token(t0, v) + j >= end) x.set(v, j, In<TYPE>::NONE);
+    }
   };
-  Tile<TYPE> x;
-  load(begin, x);
+  fetch(begin, 0);
+  fetch(begin + TILE, 1);
   const int cu0 = __ldg(a.cu), cu1 = __ldg(a.cu + a.n_req);
-  if (row < cu0 || row >= cu1 || (a.final && __ldg(a.final + row) >= 0)) return;   // (the other kernel knows as much)
+  if (row < cu0 || row >= cu1 || (a.final && __ldg(a.final + row) >= 0)) {   // (the other kernel knows as much)
+    copies_wait<0>();
+    return;
+  }
   const int st = a.state ? __ldg(a.state + row) : -1;
   const bool nothing = a.state && st >= a.n_states;
   const uint32_t* allowed = st >= 0 && !nothing ? a.grammar + st * a.grammar_stride : nullptr;
   float m = -INFINITY, s = 0.f;   // the thread's maximum and sum
-  float unit = -INFINITY;         // unit_of(m), a NaN where m is far out
+  float unit = 0.f;               // unit_of(m), a NaN where m is far out
   float best[kVec];               // .. and the largest candidates in its vectors' places: a group's maximum each
 #pragma unroll
   for (int v = 0; v < kVec; ++v) best[v] = -INFINITY;
-  for (int t0 = begin; t0 < end; t0 += TILE) {
-    if (t0 > begin) load(t0, x);
+  for (int t0 = begin, stage = 0; t0 < end; t0 += TILE, stage = stage == kStages - 1 ? 0 : stage + 1) {
+    copies_wait<1>();
+    if (!ALIGNED) __syncwarp();
     if (t0 + warp * 32 * N >= end) break;   // (nothing of the last tile is this warp's)
+    Tile<TYPE> x;
+    take(t0, stage, x);
+    fetch(t0 + 2 * TILE, stage == 0 ? kStages - 1 : stage - 1);   // (where the tile before this one was)
     const auto each = [&](auto&& f) {
 #pragma unroll
       for (int v = 0; v < kVec; ++v)
@@ -326,7 +349,6 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
         vm[v] = fmaxf(x.at(v, 0), x.at(v, 1));
 #pragma unroll
         for (int j = 2; j < N; ++j) vm[v] = fmaxf(vm[v], x.at(v, j));
-        vm[v] = fmaxf(vm[v], -INFINITY);
       }
       top = vm[0];
 #pragma unroll
@@ -348,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
     }
     tops();
     float M = fmaxf(m, top);
-    const auto unit_at = [&] { return fabsf(M) < kFar ? unit_of(M) : NAN; };
+    const auto unit_at = [&] { return fabsf(M) < kFar ? unit_of(M) : M == -INFINITY ? 0.f : NAN; };   // (nothing yet: any will do)
     float u = unit_at(), sum = 0.f, more = 0.f;
     each([&](int v, int j) { (j & 1 ? more : sum) += exp2_approx(fmaf(x.at(v, j), kLog2e, -u)); });
     sum += fmaf(s, exp2_approx(unit - u), more);
@@ -365,8 +387,6 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
       if (M > -INFINITY) {
         each([&](int v, int j) { sum += exp2_approx(u == u ? fmaf(x.at(v, j), kLog2e, -u) : (x.at(v, j) - M) * kLog2e); });
         if (m > -INFINITY) sum += s * rescale(m, M);
-      } else {
-        u = -INFINITY;
       }
     }
     m = M, s = sum, unit = u;
@@ -377,6 +397,7 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
 #pragma unroll
     for (int v = 0; v < kVec; ++v) best[v] = fmaxf(best[v], vm[v]);
   }
+  __syncthreads();   // (the ring is read)
   // the W-th largest of the groups' maxima, or a smaller value with little more above it
   const bool wide = a.W > kThreads / 16;   // (a group a vector's place, not a thread)
   if (wide) {
@@ -415,7 +436,17 @@ __global__ void __launch_bounds__(kThreads, ALIGNED ? 4 : 3) beam_pieces_kernel(
       const uint4 p = __ldg(reinterpret_cast<const uint4*>(in + (long long)t * SIZE));
       w[0] = p.x, w[1] = p.y, w[2] = p.z, w[3] = p.w;
     } else {
-      tail(t, w);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (SIZE == 4) {
+          w[j] = t + j < end ? __ldg(reinterpret_cast<const uint32_t*>(in) + t + j) : In<TYPE>::NONE;
+        } else {
+          const uint16_t* h = reinterpret_cast<const uint16_t*>(in);
+          const uint32_t lo = t + 2 * j < end ? __ldg(h + t + 2 * j) : In<TYPE>::NONE;
+          const uint32_t hi = t + 2 * j + 1 < end ? __ldg(h + t + 2 * j + 1) : In<TYPE>::NONE;
+          w[j] = lo | hi << 16;
+        }
+      }
     }
 #pragma unroll
     for (int j = 0; j < N; ++j)
@@ -741,11 +772,18 @@ extern "C" atspeed_status atspeed_op_beam_select(atspeed_stream stream, const vo
   if (smem_attr_once(done, beam_rank_kernel, (int)sizeof(RankShared)) != cudaSuccess) return ATSPEED_E_CUDA;
   const int grid = R * l.pieces;
   const bool aligned = aligned16(d_logits) && ld * dtype_size(type) % 16 == 0;
-  const auto go = [&](auto kernel) { kernel<<<grid, kThreads, 0, (cudaStream_t)stream>>>(a); };
-  if (type == ATSPEED_F32) aligned ? go(beam_pieces_kernel<ATSPEED_F32, true>) : go(beam_pieces_kernel<ATSPEED_F32, false>);
-  else if (type == ATSPEED_BF16) aligned ? go(beam_pieces_kernel<ATSPEED_BF16, true>) : go(beam_pieces_kernel<ATSPEED_BF16, false>);
-  else aligned ? go(beam_pieces_kernel<ATSPEED_F16, true>) : go(beam_pieces_kernel<ATSPEED_F16, false>);
-  if (launch_status() != ATSPEED_OK) return ATSPEED_E_CUDA;
+  static std::atomic<unsigned long long> ready[6];
+  const auto go = [&](auto kernel, int i) {
+    if (smem_attr_once(ready[i], kernel, (int)sizeof(PieceShared)) != cudaSuccess) return ATSPEED_E_CUDA;
+    kernel<<<grid, kThreads, sizeof(PieceShared), (cudaStream_t)stream>>>(a);
+    return launch_status();
+  };
+  const atspeed_status launched =
+      type == ATSPEED_F32    ? aligned ? go(beam_pieces_kernel<ATSPEED_F32, true>, 0) : go(beam_pieces_kernel<ATSPEED_F32, false>, 1)
+      : type == ATSPEED_BF16 ? aligned ? go(beam_pieces_kernel<ATSPEED_BF16, true>, 2) : go(beam_pieces_kernel<ATSPEED_BF16, false>, 3)
+      : aligned              ? go(beam_pieces_kernel<ATSPEED_F16, true>, 4)
+                             : go(beam_pieces_kernel<ATSPEED_F16, false>, 5);
+  if (launched != ATSPEED_OK) return launched;
   // (it may start while the last of the pieces are read, and waits for them)
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(n_req), cfg.blockDim = dim3(kRankThreads), cfg.dynamicSmemBytes = sizeof(RankShared), cfg.stream = (cudaStream_t)stream;
