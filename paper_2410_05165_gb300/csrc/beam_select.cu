@@ -35,6 +35,25 @@ struct Header {   // of a piece
   int pad;
 };
 
+// log(s 2^-32) to 2^-31, s > 0.  With s = 2^e f, f in [2/3, 4/3): log f = 2 atanh z = 2 (z + z^3 / 3 + ..), z = (f - 1) / (f + 1), |z| <= 1/5; z in
+// two 32-bit parts (its quotient and what that leaves, times the derivative 1 / (1 - z^2)), the rest of the series in one.  (The 64-bit logarithm takes 1.3 us here.)
+__device__ __forceinline__ double log_of(unsigned long long s) {
+  int e = 63 - __clzll(s);
+  const unsigned long long f = s << (63 - e);                       // 1.f in 64 bits
+  float hi = (float)(uint32_t)(f >> 40) * 0x1p-23f, lo = (float)(uint32_t)(f >> 16 & 0xffffff) * 0x1p-47f;   // (24 bits each)
+  if (hi >= 4.f / 3.f) hi *= 0.5f, lo *= 0.5f, ++e;
+  const float up = hi - 1.f, down = hi + 1.f, down_lo = (hi - (down - 1.f)) + lo;
+  const float z = __fdividef(up, down);
+  const float z_lo = __fdividef(fmaf(-z, down, up) + (lo - z * down_lo), down), q = z * z;
+  float p = 1.f / 13.f;
+  p = fmaf(p, q, 1.f / 11.f);
+  p = fmaf(p, q, 1.f / 9.f);
+  p = fmaf(p, q, 1.f / 7.f);
+  p = fmaf(p, q, 1.f / 5.f);
+  p = fmaf(p, q, 1.f / 3.f);
+  return fma((double)(e - 32), 0.69314718055994530942, (double)(z + z) + (double)fmaf(z + z, q * p, (z_lo + z_lo) * (1.f + q)));
+}
+
 struct SelectArgs {
   const void* logits;
   long long ld;
@@ -109,10 +128,10 @@ __device__ __forceinline__ uint32_t threshold_of(const uint32_t* keys, int want,
   if (valid <= most) return lo;
   while (lo < hi) {   // at least `want` at lo, fewer above hi
     const uint32_t mid = lo + (hi - lo) / 2 + 1;
-    int c = 0;
+    int part[4] = {};   // (four sums, so that none waits for itself)
 #pragma unroll
-    for (int e = 0; e < E; ++e) c += k[e] >= mid;
-    c = __reduce_add_sync(0xffffffffu, c);
+    for (int e = 0; e < E; ++e) part[e & 3] += k[e] >= mid;
+    const int c = __reduce_add_sync(0xffffffffu, (part[0] + part[1]) + (part[2] + part[3]));
     if (c >= want) {
       lo = mid;
       if (c <= most) break;
@@ -280,6 +299,23 @@ __global__ void __launch_bounds__(kThreads, 4) beam_pieces_kernel(const __grid_c
     }
     copies_done();
   };
+  const auto shift = [&](const uint4& p, const uint4& q, uint32_t (&w)[4]) {   // the 16 bytes that begin `lead` bytes into p
+    uint32_t y[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+    if (lead & 8) {
+#pragma unroll
+      for (int j = 0; j < 6; ++j) y[j] = y[j + 2];
+    }
+    if (lead & 4) {
+#pragma unroll
+      for (int j = 0; j < 5; ++j) y[j] = y[j + 1];
+    }
+    if (SIZE == 2 && (lead & 2)) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = __funnelshift_r(y[j], y[j + 1], 16);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = y[j];
+  };
   // A thread's logits of a tile, wherever the row begins: its words, shifted.
   const auto take = [&](int t0, int stage, Tile<TYPE>& x) {
     const auto& at = shared.ring[stage].word[warp];
@@ -287,24 +323,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_pieces_kernel(const __grid_c
     for (int v = 0; v < kVec; ++v) {
       const uint4 p = at[v][lane];
       x.w[v][0] = p.x, x.w[v][1] = p.y, x.w[v][2] = p.z, x.w[v][3] = p.w;
-      if (!ALIGNED && lead) {
-        const uint4 q = at[v][lane + 1];
-        uint32_t y[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
-        if (lead & 8) {
-#pragma unroll
-          for (int j = 0; j < 6; ++j) y[j] = y[j + 2];
-        }
-        if (lead & 4) {
-#pragma unroll
-          for (int j = 0; j < 5; ++j) y[j] = y[j + 1];
-        }
-        if (SIZE == 2 && (lead & 2)) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) y[j] = __funnelshift_r(y[j], y[j + 1], 16);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x.w[v][j] = y[j];
-      }
+      if (!ALIGNED && lead) shift(p, at[v][lane + 1], x.w[v]);
     }
     if (t0 + TILE > end) {
 #pragma unroll
@@ -312,6 +331,27 @@ __global__ void __launch_bounds__(kThreads, 4) beam_pieces_kernel(const __grid_c
 #pragma unroll
         for (int j = 0; j < N; ++j)
           if (token(t0, v) + j >= end) x.set(v, j, In<TYPE>::NONE);
+    }
+  };
+  // The vector of logits from token t on, -infinity behind the end; by the words that it lies in or one by one.
+  const auto vector = [&](int t, uint32_t (&w)[4]) {
+    if (t + 2 * N <= end) {
+      const uint4* at = reinterpret_cast<const uint4*>(in - lead + (long long)t * SIZE);
+      const uint4 p = __ldg(at);
+      w[0] = p.x, w[1] = p.y, w[2] = p.z, w[3] = p.w;
+      if (!ALIGNED && lead) shift(p, __ldg(at + 1), w);
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (SIZE == 4) {
+        w[j] = t + j < end ? __ldg(reinterpret_cast<const uint32_t*>(in) + t + j) : In<TYPE>::NONE;
+      } else {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(in);
+        const uint32_t lo = t + 2 * j < end ? __ldg(h + t + 2 * j) : In<TYPE>::NONE;
+        const uint32_t hi = t + 2 * j + 1 < end ? __ldg(h + t + 2 * j + 1) : In<TYPE>::NONE;
+        w[j] = lo | hi << 16;
+      }
     }
   };
   fetch(begin, 0);
@@ -398,8 +438,8 @@ __global__ void __launch_bounds__(kThreads, 4) beam_pieces_kernel(const __grid_c
     for (int v = 0; v < kVec; ++v) best[v] = fmaxf(best[v], vm[v]);
   }
   __syncthreads();   // (the ring is read)
-  // the W-th largest of the groups' maxima, or a smaller value with little more above it
-  const bool wide = a.W > kThreads / 16;   // (a group a vector's place, not a thread)
+  // the W-th largest of the groups' maxima, or a smaller value with little more above it: of the threads', for many of their vectors' places
+  const bool wide = a.W > kThreads / 4;
   if (wide) {
 #pragma unroll
     for (int v = 0; v < kVec; ++v) sh.group[v * kThreads + tid] = key_of(best[v]);
@@ -417,46 +457,41 @@ __global__ void __launch_bounds__(kThreads, 4) beam_pieces_kernel(const __grid_c
   const float ws = warp_sum(m > -INFINITY ? s * rescale(m, M) : 0.f);
   if (lane == 0) sh.s[warp] = ws;
   if (warp == 0) {
-    const uint32_t t = wide ? threshold_of<kGroups / 32>(sh.group, a.W, a.W + a.W / 4) : threshold_of<kThreads / 32>(sh.group, a.W, a.W + a.W / 4);
+    const uint32_t t = wide ? threshold_of<kGroups / 32>(sh.group, a.W, a.W + a.W / 8) : threshold_of<kThreads / 32>(sh.group, a.W, a.W + a.W / 8);
     if (lane == 0) sh.from = t ? t : kNone + 1;
   }
   __syncthreads();
   const uint32_t from = sh.from;
   const float least = value_of(from);
-  for (int g = tid; g < (wide ? kGroups : kThreads); g += kThreads)
-    if (sh.group[g] >= from) sh.read[atomicAdd(&sh.n_read, 1)] = (uint16_t)g;
-  __syncthreads();
-  const int vectors = wide ? 1 : kVec, tiles = (end - begin + TILE - 1) / TILE;   // (of a group in a tile)
-  const int reads = nothing ? 0 : sh.n_read * vectors * tiles;
-  for (int i = tid; i < reads; i += kThreads) {
-    const int g = sh.read[i % sh.n_read], k = i / sh.n_read;
-    const int v = wide ? g / kThreads : k % kVec, t = begin + k / vectors * TILE + (v * kThreads + g % kThreads) * N;
-    uint32_t w[4];
-    if (ALIGNED && t + N <= end) {
-      const uint4 p = __ldg(reinterpret_cast<const uint4*>(in + (long long)t * SIZE));
-      w[0] = p.x, w[1] = p.y, w[2] = p.z, w[3] = p.w;
-    } else {
+  if (!nothing) {   // (nothing is allowed in the row)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (SIZE == 4) {
-          w[j] = t + j < end ? __ldg(reinterpret_cast<const uint32_t*>(in) + t + j) : In<TYPE>::NONE;
-        } else {
-          const uint16_t* h = reinterpret_cast<const uint16_t*>(in);
-          const uint32_t lo = t + 2 * j < end ? __ldg(h + t + 2 * j) : In<TYPE>::NONE;
-          const uint32_t hi = t + 2 * j + 1 < end ? __ldg(h + t + 2 * j + 1) : In<TYPE>::NONE;
-          w[j] = lo | hi << 16;
-        }
-      }
+    for (int v = 0; v < kVec; ++v)
+      if (best[v] >= least) sh.read[atomicAdd(&sh.n_read, 1)] = (uint16_t)(v * kThreads + tid);
+  }
+  __syncthreads();
+  const int n_read = sh.n_read, reads = n_read * ((end - begin + TILE - 1) / TILE);
+  constexpr int kAtOnce = 4;
+  for (int i0 = tid; i0 < reads; i0 += kAtOnce * kThreads) {
+    uint32_t w[kAtOnce][4], ok[kAtOnce];
+    int t[kAtOnce];
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      const int i = i0 + q * kThreads, tile = i / n_read;
+      t[q] = i < reads ? begin + tile * TILE + sh.read[i - tile * n_read] * N : end;
+      vector(t[q], w[q]);
+      ok[q] = allowed && t[q] < end ? __ldg(allowed + (t[q] >> 5)) >> (t[q] & 31) : 0xffffffffu;
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (vector_at<TYPE>(w, j) >= least && (!allowed || (__ldg(allowed + (t >> 5)) >> (t & 31) + j & 1))) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < kList) {
-          sh.key[at] = key_of(fminf(vector_at<TYPE>(w, j), In<TYPE>::value(In<TYPE>::MOST)));
-          sh.tok[at] = t + j;
+    for (int q = 0; q < kAtOnce; ++q)
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (vector_at<TYPE>(w[q], j) >= least && (ok[q] >> j & 1)) {
+          const int at = atomicAdd(&sh.n, 1);
+          if (at < kList) {
+            sh.key[at] = key_of(fminf(vector_at<TYPE>(w[q], j), In<TYPE>::value(In<TYPE>::MOST)));
+            sh.tok[at] = t[q] + j;
+          }
         }
-      }
   }
   __syncthreads();
   if (sh.n > a.cap) {
@@ -533,6 +568,9 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
   const int r1 = min(min(a.R, __ldg(a.cu + a.n_req)), __ldg(a.cu + b + 1));
   const int lists = max(0, r1 - r0) * a.pieces;
   if (tid == 0) sh.n = 0;
+  // (the first thousand rows' inputs, before the sums are there)
+  const float my_cum = a.score && r0 + tid < r1 ? __ldg(a.score + r0 + tid) : 0.f;
+  const int my_final = a.final && r0 + tid < r1 ? __ldg(a.final + r0 + tid) : -1;
   pdl_wait();
   // Candidates: a thread has place `at` of list my_list and of every lists_at_once-th list from there.
   const int lists_at_once = kRankThreads / a.cap, at = tid % a.cap, my_list = tid / a.cap;
@@ -556,26 +594,22 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
   // A row's maximum and sum from its pieces: many pieces by a warp, few by a thread; then its logarithm.
   // (Sums as multiples of 2^-32, whole numbers: a row's is at least 0.7 and at most 1.5 times its length.)
   const auto whole = [&](float s) { return (unsigned long long)(s * 0x1p32f); };
-  const auto set_row = [&](int r, float M, unsigned long long s) {
-    Row w = {0.0, 0.0, a.score ? __ldg(a.score + r) : 0.f, 0.f, 0.f, -1};
-    const double l = log((double)s * 0x1p-32);
-    if (fabsf(M) < kFar) w.off = (double)unit_of(M) * kLn2 + l - (double)M * kEta;
-    else w.off = (double)M, w.more = l;
-    w.off32 = (float)w.off, w.more32 = (float)w.more;
+  const auto set_row = [&](int r, float M, unsigned long long s) {   // r: r0 + tid and every thousandth from there
+    const bool first = r - r0 < kRankThreads;
+    Row w = {0.0, 0.0, first ? my_cum : a.score ? __ldg(a.score + r) : 0.f, 0.f, 0.f, first ? my_final : a.final ? __ldg(a.final + r) : -1};
+    if (w.final < 0 && s) {   // (no sum: no candidates)
+      const double l = log_of(s);
+      if (fabsf(M) < kFar) w.off = (double)unit_of(M) * kLn2 + l - (double)M * kEta;
+      else w.off = (double)M, w.more = l;
+      w.off32 = (float)w.off, w.more32 = (float)w.more;
+    }
     row_at(r) = w;
   };
-  const auto final_of = [&](int r) { return a.final ? __ldg(a.final + r) : -1; };
-  const auto set_final = [&](int r, int f) { row_at(r) = {0.0, 0.0, a.score ? __ldg(a.score + r) : 0.f, 0.f, 0.f, f}; };
   if (a.pieces <= 2) {
     for (int r = r0 + tid; r < r1; r += kRankThreads) {
-      const int f = final_of(r);
-      if (f >= 0) {
-        set_final(r, f);
-        continue;
-      }
       const Header* h = a.head + (long long)r * a.pieces;
       const float m0 = h[0].m, s0 = h[0].s, m1 = a.pieces > 1 ? h[1].m : -INFINITY, s1 = a.pieces > 1 ? h[1].s : 0.f;
-      const float M = fmaxf(m0, m1);
+      const float M = fmaxf(m0, m1);   // (an ended beam's mean nothing)
       set_row(r, M, M > -INFINITY ? whole(s0 * rescale(m0, M)) + whole(s1 * rescale(m1, M)) : 0ull);
     }
   } else {
@@ -583,12 +617,12 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
       const int last = min(r1, base + kRankThreads);
       for (int r = base + warp; r < last; r += kRankThreads / 32) {
         const Header* h = a.head + (long long)r * a.pieces;
-        const bool live = final_of(r) < 0;
-        float M = -INFINITY;
-        for (int p = lane; live && p < a.pieces; p += 32) M = fmaxf(M, h[p].m);
+        const float m0 = lane < a.pieces ? h[lane].m : -INFINITY, s0 = lane < a.pieces ? h[lane].s : 0.f;
+        float M = m0;
+        for (int p = lane + 32; p < a.pieces; p += 32) M = fmaxf(M, h[p].m);
         M = warp_max(M);
-        unsigned long long s = 0;
-        for (int p = lane; live && p < a.pieces; p += 32)
+        unsigned long long s = m0 > -INFINITY ? whole(s0 * rescale(m0, M)) : 0ull;
+        for (int p = lane + 32; p < a.pieces; p += 32)
           if (h[p].m > -INFINITY) s += whole(h[p].s * rescale(h[p].m, M));
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
         if (lane == 0) {
@@ -597,11 +631,7 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
         }
       }
       __syncthreads();
-      if (base + tid < last) {
-        const int r = base + tid, f = final_of(r);
-        if (f >= 0) set_final(r, f);
-        else set_row(r, __uint_as_float(sh.group[tid]), sh.score[tid]);
-      }
+      if (base + tid < last) set_row(base + tid, __uint_as_float(sh.group[tid]), sh.score[tid]);
       __syncthreads();
     }
   }
@@ -638,10 +668,15 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
       if (l < lists && look(l, c[q], cn[q], y, e)) g = fmaxf(g, y - e);   // (not a NaN)
     }
   }
-  sh.group[tid] = key_of(g);
+  const bool many = a.W > 64;
+  if (!many) {   // (of four threads each)
+    g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 1));
+    g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
+  }
+  if (many || tid % 4 == 0) sh.group[many ? tid : tid / 4] = key_of(g);
   __syncthreads();
   if (warp == 0) {
-    const uint32_t t = threshold_of<kRankThreads / 32>(sh.group, a.W, a.W + a.W / 4);
+    const uint32_t t = many ? threshold_of<kRankThreads / 32>(sh.group, a.W, a.W + a.W / 8) : threshold_of<kRankThreads / 128>(sh.group, a.W, a.W + a.W / 8);
     if (lane == 0) sh.from = t;
   }
   __syncthreads();
