@@ -6,9 +6,10 @@
 // candidates among its logits, which are at least its W best (within a row the order is the logits').  The second, a CTA a
 // request, makes log s_r of the pieces, scores the candidates and ranks the best.
 //
-// Candidates of a piece: its tokens form groups (256 or 1024; each a thread's, strided over the whole piece) whose maxima stay in
+// Candidates of a piece: its tokens form groups (512; a place of a thread's each, strided over the whole piece) whose maxima stay in
 // registers while the logits stream by.  W of these maxima, so W logits, are at or above the W-th largest of them: the groups that
-// reach that bound, little more than W of them, are read again (from L2) for what is at or above it.  Where that is more than
+// reach that bound, little more than W of them, are read again for what is at or above it: in the one tile that holds the
+// maximum, or in all if the next best reaches the bound too.  Where that is more than
 // a list holds (equal logits, a mask of the type's lowest value) the W best are searched exactly.
 //
 // Sums of a row do not depend on where the row begins in memory: rows with the same logits have the same bits.
@@ -21,7 +22,7 @@
 namespace atspeed {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 128, kWarps = kThreads / 32, kCtas = 6;   // (CTAs an SM)
 constexpr int kVec = 4;                     // 16-byte vectors of a thread in a tile
 constexpr int kList = 1024;                 // candidates that a piece's list holds
 constexpr int kGroups = kThreads * kVec;
@@ -35,25 +36,6 @@ struct Header {   // of a piece
   int pad;
 };
 
-// log(s 2^-32) to 2^-31, s > 0.  With s = 2^e f, f in [2/3, 4/3): log f = 2 atanh z = 2 (z + z^3 / 3 + ..), z = (f - 1) / (f + 1), |z| <= 1/5; z in
-// two 32-bit parts (its quotient and what that leaves, times the derivative 1 / (1 - z^2)), the rest of the series in one.  (The 64-bit logarithm takes 1.3 us here.)
-__device__ __forceinline__ double log_of(unsigned long long s) {
-  int e = 63 - __clzll(s);
-  const unsigned long long f = s << (63 - e);                       // 1.f in 64 bits
-  float hi = (float)(uint32_t)(f >> 40) * 0x1p-23f, lo = (float)(uint32_t)(f >> 16 & 0xffffff) * 0x1p-47f;   // (24 bits each)
-  if (hi >= 4.f / 3.f) hi *= 0.5f, lo *= 0.5f, ++e;
-  const float up = hi - 1.f, down = hi + 1.f, down_lo = (hi - (down - 1.f)) + lo;
-  const float z = __fdividef(up, down);
-  const float z_lo = __fdividef(fmaf(-z, down, up) + (lo - z * down_lo), down), q = z * z;
-  float p = 1.f / 13.f;
-  p = fmaf(p, q, 1.f / 11.f);
-  p = fmaf(p, q, 1.f / 9.f);
-  p = fmaf(p, q, 1.f / 7.f);
-  p = fmaf(p, q, 1.f / 5.f);
-  p = fmaf(p, q, 1.f / 3.f);
-  return fma((double)(e - 32), 0.69314718055994530942, (double)(z + z) + (double)fmaf(z + z, q * p, (z_lo + z_lo) * (1.f + q)));
-}
-
 struct SelectArgs {
   const void* logits;
   long long ld;
@@ -64,11 +46,13 @@ struct SelectArgs {
   long long grammar_stride;
   int n_states;
   bool full;
+  uint32_t per_piece;   // 2^32 / pieces, rounded up
   int *token, *parent;
   float* out_score;
   Header* head;
   uint2* cand;   // (logit, token)
   struct Row* rows;   // [R]
+  struct Quick* quick;
 };
 
 // Order-preserving maps to whole numbers.
@@ -77,10 +61,23 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
-__device__ __forceinline__ unsigned long long key_of(double x) {
-  const unsigned long long b = (unsigned long long)__double_as_longlong(x);
-  return b >> 63 ? ~b : b | 1ull << 63;
+
+// Sums in two 32-bit parts, the larger rounded to nearest (64-bit arithmetic has a hundred clocks of latency here: with it the ranking of
+// ten beams took 2 us more).
+struct Two {
+  float hi, lo;
+};
+__device__ __forceinline__ Two two_sum(float a, float b) {   // a + b exactly (Knuth)
+  const float s = a + b, c = s - a;
+  return {s, (a - (s - c)) + (b - c)};
 }
+__device__ __forceinline__ Two add_low(Two a, float lo) {   // |lo| << |a.hi|; what is not finite has no lower part
+  if (!(fabsf(a.hi) < INFINITY)) return {a.hi, 0.f};
+  lo += a.lo;
+  const float hi = a.hi + lo;
+  return {hi, lo - (hi - a.hi)};
+}
+__device__ __forceinline__ unsigned long long key_of(Two a) { return (unsigned long long)key_of(a.hi) << 32 | key_of(a.lo); }
 
 template <int TYPE>
 struct In {
@@ -110,28 +107,35 @@ struct Tile {
   }
 };
 
-// The largest t with at least `want` of 32 E keys in shared memory at or above it, or a smaller one with at most `most` there; 0
-// where fewer than `want` are above kNone.  A warp.
-template <int E>
-__device__ __forceinline__ uint32_t threshold_of(const uint32_t* keys, int want, int most) {
-  uint32_t k[E], lo = 0xffffffffu, hi = 0;
-  int valid = 0;
+// The largest t with at least `want` of the CTA's keys (E a thread) at or above it, or a smaller one with at most `most` there; 0
+// where fewer than `want` are above kNone.  Every thread of the CTA; scratch: 3 words a warp.  (The barriers count: by one warp, with
+// the keys in shared memory, it took twice as long.)
+template <int E, int WARPS>
+__device__ __forceinline__ uint32_t threshold_of(const uint32_t (&k)[E], int want, int most, uint32_t* scratch) {
+  uint32_t lo = 0xffffffffu, hi = 0, valid = 0;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    k[e] = keys[e * 32 + (threadIdx.x & 31)];
+  for (int e = 0; e < E; ++e)
     if (k[e] > kNone) lo = min(lo, k[e]), hi = max(hi, k[e]), ++valid;
-  }
-  valid = __reduce_add_sync(0xffffffffu, valid);
-  if (valid < want) return 0;
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
-  if (valid <= most) return lo;
+  valid = __reduce_add_sync(0xffffffffu, valid);
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) {
+    uint32_t* at = scratch + threadIdx.x / 32;
+    at[0] = lo, at[WARPS] = hi, at[2 * WARPS] = valid;
+  }
+  __syncthreads();
+  const bool have = lane < WARPS;
+  lo = __reduce_min_sync(0xffffffffu, have ? scratch[lane] : 0xffffffffu);
+  hi = __reduce_max_sync(0xffffffffu, have ? scratch[WARPS + lane] : 0u);
+  valid = __reduce_add_sync(0xffffffffu, have ? scratch[2 * WARPS + lane] : 0u);
+  if ((int)valid < want) return 0;
+  if ((int)valid <= most) return lo;
   while (lo < hi) {   // at least `want` at lo, fewer above hi
     const uint32_t mid = lo + (hi - lo) / 2 + 1;
-    int part[4] = {};   // (four sums, so that none waits for itself)
+    int c = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) part[e & 3] += k[e] >= mid;
-    const int c = __reduce_add_sync(0xffffffffu, (part[0] + part[1]) + (part[2] + part[3]));
+    for (int e = 0; e < E; ++e) c += __syncthreads_count(k[e] >= mid);
     if (c >= want) {
       lo = mid;
       if (c <= most) break;
@@ -145,10 +149,9 @@ __device__ __forceinline__ uint32_t threshold_of(const uint32_t* keys, int want,
 struct Shared {
   uint32_t key[kList];
   int tok[kList];
-  uint32_t group[kGroups];   // groups' maxima
-  uint16_t read[kGroups];    // the groups to be read again
-  int n, n_read, count[kWarps];
-  uint32_t from;
+  uint32_t scratch[3 * kWarps];
+  int read[kGroups];         // vectors to be read again: from the front by their first tokens, from the back in every tile
+  int n, n_read, n_every, count[kWarps];
   float m[kWarps], s[kWarps];
 };
 
@@ -168,7 +171,8 @@ __device__ __forceinline__ int block_count(int v, Shared& sh) {   // the sum ove
 // kFar on, where x l has no bits left for that, in units of e^m.
 // e^x as 2^(x l) is off by a factor e^(x kEta), which the scores take back for the row's maximum.
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr double kLn2 = 0.69314718055994530942, kEta = (double)kLog2e * kLn2 - 1.0;
+constexpr double kLn2 = 0.69314718055994530942;
+constexpr float kLn2Hi = (float)kLn2, kLn2Lo = (float)(kLn2 - (double)kLn2Hi), kEta = (float)((double)kLog2e * kLn2 - 1.0);
 constexpr float kFar = 0x1p20f;
 
 __device__ __forceinline__ float unit_of(float m) { return rintf(m * kLog2e); }
@@ -245,7 +249,7 @@ __device__ __noinline__ void put_exactly(const char* in, const uint32_t* allowed
 }
 
 // A tile's 16-byte words on their way through shared memory, a warp's 32 of a vector in a row, and the one behind them.
-constexpr int kStages = 3;
+constexpr int kStages = 3;   // (two tiles under way)
 struct Stage {
   uint4 word[kWarps][kVec][33];
 };
@@ -266,7 +270,7 @@ __device__ __forceinline__ void copies_wait() {
 
 // ALIGNED: every row begins at a multiple of 16 bytes.
 template <int TYPE, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads, 4) beam_pieces_kernel(const __grid_constant__ SelectArgs a) {
+__global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __grid_constant__ SelectArgs a) {
   constexpr int N = In<TYPE>::N, SIZE = In<TYPE>::SIZE, TILE = In<TYPE>::TILE;
   extern __shared__ __align__(16) unsigned char raw[];
   PieceShared& shared = *reinterpret_cast<PieceShared*>(raw);
@@ -366,14 +370,16 @@ __global__ void __launch_bounds__(kThreads, 4) beam_pieces_kernel(const __grid_c
   const uint32_t* allowed = st >= 0 && !nothing ? a.grammar + st * a.grammar_stride : nullptr;
   float m = -INFINITY, s = 0.f;   // the thread's maximum and sum
   float unit = 0.f;               // unit_of(m), a NaN where m is far out
-  float best[kVec];               // .. and the largest candidates in its vectors' places: a group's maximum each
+  // .. and of its vectors' places, each a group: the largest candidate, the tile that it is in, and the largest of any place's other tiles
+  float best[kVec], second = -INFINITY;
+  int where[kVec];
 #pragma unroll
-  for (int v = 0; v < kVec; ++v) best[v] = -INFINITY;
+  for (int v = 0; v < kVec; ++v) best[v] = -INFINITY, where[v] = begin;
+  Tile<TYPE> x;
   for (int t0 = begin, stage = 0; t0 < end; t0 += TILE, stage = stage == kStages - 1 ? 0 : stage + 1) {
     copies_wait<1>();
     if (!ALIGNED) __syncwarp();
     if (t0 + warp * 32 * N >= end) break;   // (nothing of the last tile is this warp's)
-    Tile<TYPE> x;
     take(t0, stage, x);
     fetch(t0 + 2 * TILE, stage == 0 ? kStages - 1 : stage - 1);   // (where the tile before this one was)
     const auto each = [&](auto&& f) {
@@ -435,63 +441,99 @@ __global__ void __launch_bounds__(kThreads, 4) beam_pieces_kernel(const __grid_c
       tops();
     }
 #pragma unroll
-    for (int v = 0; v < kVec; ++v) best[v] = fmaxf(best[v], vm[v]);
+    for (int v = 0; v < kVec; ++v) {
+      second = fmaxf(second, fminf(best[v], vm[v]));
+      where[v] = vm[v] > best[v] ? t0 : where[v];
+      best[v] = fmaxf(best[v], vm[v]);
+    }
   }
   __syncthreads();   // (the ring is read)
   // the W-th largest of the groups' maxima, or a smaller value with little more above it: of the threads', for many of their vectors' places
-  const bool wide = a.W > kThreads / 4;
-  if (wide) {
-#pragma unroll
-    for (int v = 0; v < kVec; ++v) sh.group[v * kThreads + tid] = key_of(best[v]);
-  } else {
-    sh.group[tid] = key_of(fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])));
-  }
-  static_assert(kVec == 4, "vectors of a thread");
   const float wm = warp_max(m);
   if (lane == 0) sh.m[warp] = wm;
-  if (tid == 0) sh.n = sh.n_read = 0;
-  __syncthreads();
+  if (tid == 0) sh.n = sh.n_read = sh.n_every = 0;
+  uint32_t from;
+  if (a.W <= kThreads / 4) {
+    static_assert(kVec == 4, "vectors of a thread");
+    const uint32_t k[1] = {key_of(fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])))};
+    from = threshold_of<1, kWarps>(k, a.W, a.W + a.W / 8, sh.scratch);
+  } else {
+    uint32_t k[kVec];
+#pragma unroll
+    for (int v = 0; v < kVec; ++v) k[v] = key_of(best[v]);
+    from = threshold_of<kVec, kWarps>(k, a.W, a.W + a.W / 8, sh.scratch);
+  }
+  if (!from) from = kNone + 1;
   float M = sh.m[0];
 #pragma unroll
   for (int w = 1; w < kWarps; ++w) M = fmaxf(M, sh.m[w]);
   const float ws = warp_sum(m > -INFINITY ? s * rescale(m, M) : 0.f);
   if (lane == 0) sh.s[warp] = ws;
-  if (warp == 0) {
-    const uint32_t t = wide ? threshold_of<kGroups / 32>(sh.group, a.W, a.W + a.W / 8) : threshold_of<kThreads / 32>(sh.group, a.W, a.W + a.W / 8);
-    if (lane == 0) sh.from = t ? t : kNone + 1;
-  }
-  __syncthreads();
-  const uint32_t from = sh.from;
   const float least = value_of(from);
-  if (!nothing) {   // (nothing is allowed in the row)
+  // The candidates among count vectors of logits w from token t(q) on (bits ok: those allowed), in the list: places for all of a
+  // thread's at once.
+  const auto keep = [&](auto&& at, int q, int j, auto&& t, int place) {
+    if (place >= kList) return;
+    sh.key[place] = key_of(fminf(at(q, j), In<TYPE>::value(In<TYPE>::MOST)));
+    sh.tok[place] = t(q) + j;
+  };
+  const auto gather = [&](auto&& at, auto&& ok, auto&& t) {
+    uint32_t hits[kVec];
+    int all = 0;
 #pragma unroll
-    for (int v = 0; v < kVec; ++v)
-      if (best[v] >= least) sh.read[atomicAdd(&sh.n_read, 1)] = (uint16_t)(v * kThreads + tid);
+    for (int q = 0; q < kVec; ++q) {
+      hits[q] = 0;
+#pragma unroll
+      for (int j = 0; j < N; ++j) hits[q] |= (at(q, j) >= least ? 1u : 0u) << j;
+      hits[q] &= ok(q);
+      all += __popc(hits[q]);
+    }
+    if (!all) return;
+    int place = atomicAdd(&sh.n, all);
+#pragma unroll
+    for (int q = 0; q < kVec; ++q) {
+      if (!hits[q]) continue;
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (hits[q] >> j & 1) keep(at, q, j, t, place++);
+    }
+  };
+  const int tiles = (end - begin + TILE - 1) / TILE;
+  if (nothing) {   // (nothing is allowed in the row)
+  } else if (tiles == 1) {   // (the tile is at hand, where the warp has any of it)
+    if (m > -INFINITY)
+      gather([&](int q, int j) { return x.at(q, j); }, [&](int q) { return best[q] >= least ? 0xffffffffu : 0u; }, [&](int q) { return token(begin, q); });
+  } else {
+    const bool every = second >= least;   // (of a place's tiles: then all are read, else the one with the maximum)
+    int mine = 0;
+#pragma unroll
+    for (int v = 0; v < kVec; ++v) mine += best[v] >= least;
+    if (mine) {
+      int at = atomicAdd(every ? &sh.n_every : &sh.n_read, mine);
+#pragma unroll
+      for (int v = 0; v < kVec; ++v)
+        if (best[v] >= least) sh.read[every ? kGroups - 1 - at++ : at++] = token(every ? 0 : where[v], v);
+    }
   }
   __syncthreads();
-  const int n_read = sh.n_read, reads = n_read * ((end - begin + TILE - 1) / TILE);
-  constexpr int kAtOnce = 4;
-  for (int i0 = tid; i0 < reads; i0 += kAtOnce * kThreads) {
-    uint32_t w[kAtOnce][4], ok[kAtOnce];
-    int t[kAtOnce];
+  const int n_one = sh.n_read, n_every = sh.n_every, reads = n_one + n_every * tiles;
+  for (int i0 = tid; i0 < reads; i0 += kVec * kThreads) {
+    uint32_t w[kVec][4], ok[kVec];
+    int t[kVec];
 #pragma unroll
-    for (int q = 0; q < kAtOnce; ++q) {
-      const int i = i0 + q * kThreads, tile = i / n_read;
-      t[q] = i < reads ? begin + tile * TILE + sh.read[i - tile * n_read] * N : end;
+    for (int q = 0; q < kVec; ++q) {
+      const int i = i0 + q * kThreads;
+      t[q] = end;
+      if (i < n_one) {
+        t[q] = sh.read[i];
+      } else if (i < reads) {
+        const int tile = (i - n_one) / n_every;
+        t[q] = begin + tile * TILE + sh.read[kGroups - 1 - (i - n_one - tile * n_every)];
+      }
       vector(t[q], w[q]);
       ok[q] = allowed && t[q] < end ? __ldg(allowed + (t[q] >> 5)) >> (t[q] & 31) : 0xffffffffu;
     }
-#pragma unroll
-    for (int q = 0; q < kAtOnce; ++q)
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (vector_at<TYPE>(w[q], j) >= least && (ok[q] >> j & 1)) {
-          const int at = atomicAdd(&sh.n, 1);
-          if (at < kList) {
-            sh.key[at] = key_of(fminf(vector_at<TYPE>(w[q], j), In<TYPE>::value(In<TYPE>::MOST)));
-            sh.tok[at] = t[q] + j;
-          }
-        }
+    gather([&](int q, int j) { return vector_at<TYPE>(w[q], j); }, [&](int q) { return ok[q]; }, [&](int q) { return t[q]; });
   }
   __syncthreads();
   if (sh.n > a.cap) {
@@ -516,27 +558,63 @@ struct Entry {
   uint32_t tok;
 };
 
+// n log 2 + log(s 2^-32) + more to 2^-29, s > 0.  With s = 2^e f, f in [2/3, 4/3): log f = 2 atanh z = 2 (z + z^3 / 3 + ..),
+// z = (f - 1) / (f + 1), |z| <= 1/5; z in two parts (its quotient and what that leaves, times the derivative 1 / (1 - z^2)), the rest of the
+// series in one.
+__device__ __forceinline__ Two log_of(unsigned long long s, int n, float more) {
+  int e = 63 - __clzll(s);
+  const unsigned long long f = s << (63 - e);                       // 1.f in 64 bits
+  float hi = (float)(uint32_t)(f >> 40) * 0x1p-23f, lo = (float)(uint32_t)(f >> 16 & 0xffffff) * 0x1p-47f;   // (24 bits each)
+  if (hi >= 4.f / 3.f) hi *= 0.5f, lo *= 0.5f, ++e;
+  const float up = hi - 1.f, down = hi + 1.f, down_lo = (hi - (down - 1.f)) + lo;
+  const float z = __fdividef(up, down);
+  const float z_lo = __fdividef(fmaf(-z, down, up) + (lo - z * down_lo), down), q = z * z;
+  float p = 1.f / 13.f;
+  p = fmaf(p, q, 1.f / 11.f);
+  p = fmaf(p, q, 1.f / 9.f);
+  p = fmaf(p, q, 1.f / 7.f);
+  p = fmaf(p, q, 1.f / 5.f);
+  p = fmaf(p, q, 1.f / 3.f);
+  const float k = (float)(n + e - 32), twos = k * kLn2Hi;
+  const float low = fmaf(k, kLn2Hi, -twos) + k * kLn2Lo + fmaf(z + z, q * p, (z_lo + z_lo) * (1.f + q)) + more;
+  return add_low(two_sum(twos, z + z), low);
+}
+
 // score = cum + ((x - off) - more)
-struct Row {
-  double off, more;
-  float cum, off32, more32;
+struct alignas(16) Row {
+  Two off, more;
+  float cum;
   int final;   // the one token of an ended beam; -1
+  int pad[2];
+  __device__ __forceinline__ Two score(float x) const {
+    if (final >= 0) return {cum, 0.f};
+    Two t = two_sum(x, -off.hi);
+    t.lo -= off.lo;
+    if (more.hi != 0.f) {
+      const float lo = t.lo - more.lo;
+      t = two_sum(t.hi, -more.hi);
+      t.lo += lo;
+    }
+    return add_low(two_sum(cum, t.hi), t.lo);
+  }
+};
+
+// The same in 32 bits for a first look: bias + x, off by 2^-21 (|that| + size) at most; size < 0: the beam has ended.
+struct Quick {
+  float bias, size;
 };
 
 constexpr int kRows = 256;   // that shared memory holds (of more: device memory)
 struct RankShared {
   unsigned long long score[kRankList], rest[kRankList];
   uint32_t tok[kRankList];
-  uint32_t group[kRankThreads];
+  uint32_t scratch[3 * kRankThreads / 32];
+  float top[kRankThreads];   // rows' maxima, on the way to their logarithms
   Row row[kRows];
+  Quick quick[kRows];
   Entry best[kMaxWidth];
-  int n;
-  uint32_t from;
+  int n, hits[2];
 };
-
-__device__ __forceinline__ double score_of(unsigned long long k) {
-  return __longlong_as_double((long long)(k >> 63 ? k ^ 1ull << 63 : ~k));
-}
 
 // Ranks the list's n entries and hands each that is among the W best to put(rank, entry).  Every thread of the CTA; several threads
 // an entry, neighbours in a warp.
@@ -544,9 +622,10 @@ template <class Put>
 __device__ __forceinline__ void rank_list(const RankShared& sh, int n, int W, Put&& put) {
   int share = 32;   // threads an entry
   while (share > 1 && share * n > kRankThreads) share >>= 1;
-  const int per = kRankThreads / share, sub = threadIdx.x % share;
+  const int per = kRankThreads / share, sub = threadIdx.x & (share - 1), mine = threadIdx.x / share;
   for (int j0 = 0; j0 < n; j0 += per) {
-    const int j = j0 + threadIdx.x / share;
+    if (j0 + (threadIdx.x & ~31) / share >= n) break;   // (the warp has none)
+    const int j = j0 + mine;
     Entry e = {0, 0, 0};
     if (j < n) e = {sh.score[j], sh.rest[j], sh.tok[j]};
     int r = 0;
@@ -567,49 +646,49 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
   const int r0 = max(max(0, __ldg(a.cu)), __ldg(a.cu + b));
   const int r1 = min(min(a.R, __ldg(a.cu + a.n_req)), __ldg(a.cu + b + 1));
   const int lists = max(0, r1 - r0) * a.pieces;
-  if (tid == 0) sh.n = 0;
+  if (tid == 0) sh.n = sh.hits[0] = 0;
   // (the first thousand rows' inputs, before the sums are there)
   const float my_cum = a.score && r0 + tid < r1 ? __ldg(a.score + r0 + tid) : 0.f;
   const int my_final = a.final && r0 + tid < r1 ? __ldg(a.final + r0 + tid) : -1;
   pdl_wait();
-  // Candidates: a thread has place `at` of list my_list and of every lists_at_once-th list from there.
-  const int lists_at_once = kRankThreads / a.cap, at = tid % a.cap, my_list = tid / a.cap;
+  // Candidates: a thread has place `at` of list my_list and of every at_once-th list from there; kHold of them in a round, the
+  // first of which are under way while the rows' sums are made.
+  const int at_once = kRankThreads / a.cap, at = tid & (a.cap - 1), my_list = tid / a.cap;
+  constexpr int kHold = 16, kBatch = 4;
   const auto fetch = [&](int l, uint2& c, int& n) {
+    if (l >= lists) return;
     const long long h = (long long)r0 * a.pieces + l;
     c = a.cand[h * a.cap + at];
     n = a.head[h].n;
   };
-  constexpr int kHold = 4;
-  const bool hold = lists <= kHold * lists_at_once;
-  uint2 c[kHold];
-  int cn[kHold];
+  uint2 c[kBatch];
+  int cn[kBatch];
 #pragma unroll
-  for (int q = 0; q < kHold; ++q) {   // (the first ones are under way while the rows' sums are made)
-    cn[q] = 0;
-    const int l = q * lists_at_once + my_list;
-    if (l < lists) fetch(l, c[q], cn[q]);
-  }
-  const auto row_of = [&](int l) { return r0 + (a.pieces == 1 ? l : l / a.pieces); };
+  for (int q = 0; q < kBatch; ++q) fetch(q * at_once + my_list, c[q], cn[q]);
+  const auto row_of = [&](int l) { return r0 + (a.pieces == 1 ? l : (int)__umulhi((unsigned)l, a.per_piece)); };
   const auto row_at = [&](int r) -> Row& { return r - r0 < kRows ? sh.row[r - r0] : a.rows[r]; };
-  // A row's maximum and sum from its pieces: many pieces by a warp, few by a thread; then its logarithm.
+  const auto quick_at = [&](int r) -> Quick& { return r - r0 < kRows ? sh.quick[r - r0] : a.quick[r]; };
+  // A row's maximum and sum from its pieces, many by a warp, few by a thread; then its logarithm.
   // (Sums as multiples of 2^-32, whole numbers: a row's is at least 0.7 and at most 1.5 times its length.)
   const auto whole = [&](float s) { return (unsigned long long)(s * 0x1p32f); };
   const auto set_row = [&](int r, float M, unsigned long long s) {   // r: r0 + tid and every thousandth from there
-    const bool first = r - r0 < kRankThreads;
-    Row w = {0.0, 0.0, first ? my_cum : a.score ? __ldg(a.score + r) : 0.f, 0.f, 0.f, first ? my_final : a.final ? __ldg(a.final + r) : -1};
-    if (w.final < 0 && s) {   // (no sum: no candidates)
-      const double l = log_of(s);
-      if (fabsf(M) < kFar) w.off = (double)unit_of(M) * kLn2 + l - (double)M * kEta;
-      else w.off = (double)M, w.more = l;
-      w.off32 = (float)w.off, w.more32 = (float)w.more;
+    const bool first = r - r0 < kRankThreads, near = fabsf(M) < kFar;
+    Row w = {};
+    w.cum = first ? my_cum : a.score ? __ldg(a.score + r) : 0.f;
+    w.final = first ? my_final : a.final ? __ldg(a.final + r) : -1;
+    if (s) {   // (no sum: no candidates; an ended beam's means nothing)
+      const Two l = log_of(s, near ? (int)unit_of(M) : 0, near ? -M * kEta : 0.f);
+      if (near) w.off = l;
+      else w.off = {M, 0.f}, w.more = l;
     }
     row_at(r) = w;
+    quick_at(r) = w.final >= 0 ? Quick{w.cum, -1.f} : Quick{w.cum - w.off.hi - w.more.hi, fabsf(w.cum) + fabsf(w.off.hi) + fabsf(w.more.hi)};
   };
   if (a.pieces <= 2) {
     for (int r = r0 + tid; r < r1; r += kRankThreads) {
       const Header* h = a.head + (long long)r * a.pieces;
       const float m0 = h[0].m, s0 = h[0].s, m1 = a.pieces > 1 ? h[1].m : -INFINITY, s1 = a.pieces > 1 ? h[1].s : 0.f;
-      const float M = fmaxf(m0, m1);   // (an ended beam's mean nothing)
+      const float M = fmaxf(m0, m1);
       set_row(r, M, M > -INFINITY ? whole(s0 * rescale(m0, M)) + whole(s1 * rescale(m1, M)) : 0ull);
     }
   } else {
@@ -626,118 +705,104 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
           if (h[p].m > -INFINITY) s += whole(h[p].s * rescale(h[p].m, M));
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
         if (lane == 0) {
-          sh.group[r - base] = __float_as_uint(M);
+          sh.top[r - base] = M;
           sh.score[r - base] = s;
         }
       }
       __syncthreads();
-      if (base + tid < last) set_row(base + tid, __uint_as_float(sh.group[tid]), sh.score[tid]);
+      if (base + tid < last) set_row(base + tid, sh.top[tid], sh.score[tid]);
       __syncthreads();
     }
   }
   __syncthreads();
-  // Its score in 32 bits, and how far that may be off (four roundings); false: there is none
-  const auto look = [&](int l, uint2& c, int n, float& y, float& e) {
+  // whether list l has candidate c (n: its length), and in `high` and `low` what its score is between
+  const auto look = [&](int l, const uint2& c, int n, float& high, float& low) {
+    const int r = row_of(l);
+    const Quick w = quick_at(r);
+    const bool ended = w.size < 0.f;
+    if (ended ? at != 0 || l != (r - r0) * a.pieces : at >= n) return;
+    const float y = ended ? w.bias : w.bias + __uint_as_float(c.x), e = ended ? 0.f : 0x1p-21f * (fabsf(y) + w.size);
+    high = y + e, low = fmaxf(low, y - e);   // (a NaN is passed over)
+  };
+  float hi[kHold];   // of a round's candidates: not above it
+  float g = -INFINITY;
+  const auto round = [&](int l0) {
+#pragma unroll
+    for (int q0 = 0; q0 < kHold; q0 += kBatch) {
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q) hi[q0 + q] = -INFINITY;
+      if (l0 + q0 * at_once >= lists) continue;
+      if (l0 || q0) {
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) fetch(l0 + (q0 + q) * at_once + my_list, c[q], cn[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q)
+        if (l0 + (q0 + q) * at_once + my_list < lists) look(l0 + (q0 + q) * at_once + my_list, c[q], cn[q], hi[q0 + q], g);
+    }
+  };
+  const int per_round = kHold * at_once;
+  for (int l0 = 0; l0 < lists; l0 += per_round) round(l0);
+  // what is below `from` is not among the W best: the W-th of the threads' best
+  const uint32_t group[1] = {key_of(g)}, bound = threshold_of<1, kRankThreads / 32>(group, a.W, a.W + a.W / 8, sh.scratch);
+  float from = bound ? value_of(bound) : -INFINITY;
+  const auto put = [&](int l) {
+    uint2 x;
+    int n;
+    fetch(l, x, n);
     const int r = row_of(l);
     const Row& w = row_at(r);
-    if (w.final >= 0) {
-      c = make_uint2(0u, (uint32_t)w.final);
-      y = w.cum, e = 0.f;
-      return at == 0 && l == (r - r0) * a.pieces;
-    }
-    const float x = __uint_as_float(c.x);
-    y = w.cum + ((x - w.off32) - w.more32);
-    e = 0x1p-21f * (fabsf(w.cum) + fabsf(x) + fabsf(w.off32) + fabsf(w.more32));
-    return at < n;
-  };
-  // what is below `from` is not among the W best: the W-th of the threads' best (some of them have W candidates, or they are few)
-  float g = -INFINITY;
-  for (int l0 = 0; l0 < lists; l0 += kHold * lists_at_once) {
-    if (l0) {
-#pragma unroll
-      for (int q = 0; q < kHold; ++q) {
-        cn[q] = 0;
-        const int l = l0 + q * lists_at_once + my_list;
-        if (l < lists) fetch(l, c[q], cn[q]);
-      }
-    }
-#pragma unroll
-    for (int q = 0; q < kHold; ++q) {
-      const int l = l0 + q * lists_at_once + my_list;
-      float y, e;
-      if (l < lists && look(l, c[q], cn[q], y, e)) g = fmaxf(g, y - e);   // (not a NaN)
-    }
-  }
-  const bool many = a.W > 64;
-  if (!many) {   // (of four threads each)
-    g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 1));
-    g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
-  }
-  if (many || tid % 4 == 0) sh.group[many ? tid : tid / 4] = key_of(g);
-  __syncthreads();
-  if (warp == 0) {
-    const uint32_t t = many ? threshold_of<kRankThreads / 32>(sh.group, a.W, a.W + a.W / 8) : threshold_of<kRankThreads / 128>(sh.group, a.W, a.W + a.W / 8);
-    if (lane == 0) sh.from = t;
-  }
-  __syncthreads();
-  float from = sh.from ? value_of(sh.from) : -INFINITY;
-  const auto put = [&](int l, uint2 c, int n) {
-    float y, e;
-    if (!look(l, c, n, y, e) || y + e < from) return;
+    if (w.final >= 0) x = make_uint2(0u, (uint32_t)w.final);
+    const Two y = w.score(__uint_as_float(x.x));
+    if (!(y.hi > -INFINITY)) return;
     const int to = atomicAdd(&sh.n, 1);
-    sh.rest[to] = (unsigned long long)(uint32_t)row_of(l) << 32 | c.x;
-    sh.tok[to] = c.y;
+    sh.score[to] = key_of(y);
+    sh.rest[to] = (unsigned long long)~(uint32_t)r << 32 | key_of(__uint_as_float(x.x));
+    sh.tok[to] = x.y;
   };
-  // scores of the list's entries from i0 on, in 64 bits (0: it is not to be chosen)
-  const auto finish = [&](int i0, int n) {
-    for (int i = i0 + tid; i < n; i += kRankThreads) {
-      const int r = (int)(sh.rest[i] >> 32);
-      const float x = __uint_as_float((uint32_t)sh.rest[i]);
-      const Row& w = row_at(r);
-      const double z = w.final >= 0 ? (double)w.cum : (double)w.cum + (((double)x - w.off) - w.more);
-      sh.score[i] = (float)z > -INFINITY ? key_of(z + 0.0) : 0ull;   // (-0: 0)
-      sh.rest[i] = (unsigned long long)~(uint32_t)r << 32 | key_of(x);
+  for (int l0 = 0, turn = 0; l0 < lists; l0 += per_round, turn ^= 1) {
+    if (lists > per_round) {
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q) fetch(q * at_once + my_list, c[q], cn[q]);   // (round 0 takes these)
+      round(l0);
     }
-  };
-  int done = 0;   // entries that have their scores
-#pragma unroll 1
-  for (int l0 = 0, q = 0; l0 < lists; l0 += lists_at_once, ++q) {
-    const int l = l0 + my_list;
-    if (l < lists) {
-      uint2 x = q == 0 ? c[0] : q == 1 ? c[1] : q == 2 ? c[2] : c[3];
-      int n = q == 0 ? cn[0] : q == 1 ? cn[1] : q == 2 ? cn[2] : cn[3];
-      if (!hold) fetch(l, x, n);
-      put(l, x, n);
-    }
-    if (l0 + lists_at_once >= lists) break;
+    uint32_t hits = 0;
+#pragma unroll
+    for (int q = 0; q < kHold; ++q) hits |= (hi[q] >= from && hi[q] > -INFINITY ? 1u : 0u) << q;
+    const int mine = __reduce_add_sync(0xffffffffu, __popc(hits));
+    if (lane == 0 && mine) atomicAdd(&sh.hits[turn], mine);
     __syncthreads();
-    const int n = sh.n;
-    if (n > kRankList - kRankThreads) {   // the W best stay
-      finish(done, n);
-      done = min(n, a.W);
-      __syncthreads();
-      rank_list(sh, n, a.W, [&](int r, const Entry& e) { sh.best[r] = e; });
-      __syncthreads();
-      for (int j = tid; j < min(n, a.W); j += kRankThreads) sh.score[j] = sh.best[j].score, sh.rest[j] = sh.best[j].rest, sh.tok[j] = sh.best[j].tok;
-      if (tid == 0) {
-        sh.n = min(n, a.W);
-        // (in 32 bits, rounded down)
-        sh.from = n >= a.W && sh.best[a.W - 1].score ? key_of(__double2float_rd(score_of(sh.best[a.W - 1].score))) : 0u;
+    const int all = sh.hits[turn], had = sh.n;
+    if (tid == 0) sh.hits[turn ^ 1] = 0;
+    if (had + all <= kRankList) {
+      __syncthreads();   // (everyone knows `had`)
+#pragma unroll 1
+      for (; hits; hits &= hits - 1) put(l0 + (__ffs(hits) - 1) * at_once + my_list);
+    } else {   // a step at a time, of which the W best stay
+#pragma unroll 1
+      for (int q = 0; q < kHold; ++q) {
+        __syncthreads();
+        if (hits >> q & 1) put(l0 + q * at_once + my_list);
+        __syncthreads();
+        const int n = sh.n;
+        if (n <= kRankList - kRankThreads) continue;
+        rank_list(sh, n, a.W, [&](int r, const Entry& e) { sh.best[r] = e; });
+        __syncthreads();
+        const int left = min(n, a.W);
+        for (int j = tid; j < left; j += kRankThreads) sh.score[j] = sh.best[j].score, sh.rest[j] = sh.best[j].rest, sh.tok[j] = sh.best[j].tok;
+        if (tid == 0) sh.n = left;
+        if (n >= a.W) from = fmaxf(from, value_of((uint32_t)(sh.best[a.W - 1].score >> 32)));
       }
-      __syncthreads();
-      if (sh.from) from = fmaxf(from, value_of(sh.from));
     }
     __syncthreads();
   }
   __syncthreads();
   const int n = sh.n;
-  finish(done, n);
-  __syncthreads();
   const long long o = (long long)b * a.W;
   rank_list(sh, n, a.W, [&](int r, const Entry& e) {
-    a.token[o + r] = e.score ? (int)e.tok : -1;
-    a.parent[o + r] = e.score ? (int)~(uint32_t)(e.rest >> 32) : -1;
-    a.out_score[o + r] = e.score ? (float)score_of(e.score) : -INFINITY;
+    a.token[o + r] = (int)e.tok;
+    a.parent[o + r] = (int)~(uint32_t)(e.rest >> 32);
+    a.out_score[o + r] = value_of((uint32_t)(e.score >> 32));
   });
   for (int j = n + tid; j < a.W; j += kRankThreads) {
     a.token[o + j] = -1;
@@ -747,10 +812,11 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
 }
 
 constexpr int kTile = In<ATSPEED_F32>::TILE;
-// Pieces of a row: enough CTAs for every SM to have four, none shorter than a tile.
+// Pieces of a row: as many CTAs as run at once, none shorter than a tile (of 32-bit logits, whatever the type).
 int pieces_of(int R, int V) {
-  const long long tiles = (V + kTile - 1LL) / kTile;   // (of the smaller tile)
-  return (int)std::max(1LL, std::min(tiles, (608LL + R - 1) / R));
+  const long long tiles = (V + kTile - 1LL) / kTile, most = std::max(1LL, std::min(tiles, (152LL * kCtas + R - 1) / R));
+  const long long span = (tiles + most - 1) / most;
+  return (int)((tiles + span - 1) / span);
 }
 int cap_of(int W) {   
   int cap = 32;
@@ -760,15 +826,16 @@ int cap_of(int W) {
 
 struct Layout {
   int pieces;
-  size_t cand, rows, bytes;
+  size_t cand, rows, quick, bytes;
 };
 Layout layout_of(int R, int V, int W) {
   Layout l;
   l.pieces = pieces_of(R, V);
   const size_t n = (size_t)R * l.pieces;
   l.cand = n * sizeof(Header);
-  l.rows = l.cand + n * cap_of(W) * sizeof(uint2);
-  l.bytes = l.rows + (size_t)R * sizeof(Row);
+  l.rows = (l.cand + n * cap_of(W) * sizeof(uint2) + 15) / 16 * 16;
+  l.quick = l.rows + (size_t)R * sizeof(Row);
+  l.bytes = l.quick + (size_t)R * sizeof(Quick);
   return l;
 }
 
@@ -799,10 +866,11 @@ extern "C" atspeed_status atspeed_op_beam_select(atspeed_stream stream, const vo
   a.span = (int)(((vocab + (long long)l.pieces - 1) / l.pieces + kTile - 1) / kTile * kTile);
   a.score = d_score, a.final = d_final, a.cu = d_cu_beam, a.state = d_state, a.grammar = d_grammar;
   a.grammar_stride = grammar_stride, a.n_states = d_state ? n_states : 0, a.full = norm == ATSPEED_NORM_FULL;
+  a.per_piece = l.pieces > 1 ? (uint32_t)((0x100000000ll + l.pieces - 1) / l.pieces) : 0u;
   a.token = d_token, a.parent = d_parent, a.out_score = d_out_score;
   char* ws = static_cast<char*>(d_ws);
   a.head = reinterpret_cast<Header*>(ws), a.cand = reinterpret_cast<uint2*>(ws + l.cand);
-  a.rows = reinterpret_cast<Row*>(ws + l.rows);
+  a.rows = reinterpret_cast<Row*>(ws + l.rows), a.quick = reinterpret_cast<Quick*>(ws + l.quick);
   static std::atomic<unsigned long long> done{0};
   if (smem_attr_once(done, beam_rank_kernel, (int)sizeof(RankShared)) != cudaSuccess) return ATSPEED_E_CUDA;
   const int grid = R * l.pieces;

@@ -240,6 +240,10 @@ def test_select_scores_far_out(ats):
     assert (got.token == -1).all()
     got = _check_select(ats, logits, [6], 5, score=[float("nan")] * 6)
     assert (got.token == -1).all()
+    # (a row of score +infinity comes first, by its logits)
+    got = ats.op_beam_select(logits, _dev([0, 6]), 5, score=_dev(np.array([0, 1, np.inf, 0, 0, 0], np.float32), torch.float32))
+    assert got.parent[0].tolist() == [2] * 5 and got.score[0].tolist() == [float("inf")] * 5
+    assert got.token[0].tolist() == torch.sort(logits[2], descending=True).indices[:5].tolist()
     # (a row whose score swallows its logits' differences: by the logits)
     got = ats.op_beam_select(logits, _dev([0, 1]), 5, score=_dev(np.full(6, -1e20, np.float32), torch.float32))
     assert got.token[0].tolist() == torch.sort(logits[0], descending=True).indices[:5].tolist()
