@@ -770,15 +770,18 @@ def op_fork_pages(table: torch.Tensor, kv_len: torch.Tensor, ref: torch.Tensor, 
     n_free_ptr = _given(n_free, i32, 1, "n_free", gpu)
     free_ptr = _given(free, i32, 0, "free", gpu) if free.numel() else n_free_ptr   # (n_free is 0: nothing is read of it)
     used_ptr = _tensor(used, i32, 1, "used", gpu)
-    if out is None:
-        out = PageFork(*_outputs(dev, stream, ((m, width), i32), ((m,), i32), ((m,), i32), ((m,), i32), ((m,), i32), ((pages,), i32),
-                                 ((pages,), i32), ((1,), i32)))
-        outs = [getattr(out, k).data_ptr() for k in PageFork.__slots__]
+    if out is None:   # (one tensor and views of it, the counts at its start: eight tensors take longer)
+        cells = m * width
+        whole, = _outputs(dev, stream, ((2 * pages + cells + 4 * m + 1,), i32))
+        new_ref, new_free, new_table, new_len, new_state, src, dst, left = whole.split_with_sizes((pages, pages, cells, m, m, m, m, 1))
+        out, at = PageFork(new_table.view(m, width), new_len, new_state, src, dst, new_ref, new_free, left), whole.data_ptr()
+        rows = at + 8 * pages + 4 * cells
+        outs = (at + 8 * pages, rows, rows + 4 * m, rows + 8 * m, rows + 12 * m, at, at + 4 * pages, rows + 16 * m)
     else:
         if out.table.shape != (m, width):
             _refuse(f"out.table: [{m}][{width}], not {tuple(out.table.shape)}")
-        outs = [_given(getattr(out, k), i32, size, "out." + k, gpu)
-                for k, size in zip(PageFork.__slots__, (m * width, m, m, m, m, pages, pages, 1))]
+        sizes = (m * width, m, m, m, m, pages, pages, 1)
+        outs = [_given(getattr(out, k), i32, size, "out." + k, gpu) for k, size in zip(PageFork.__slots__, sizes)]
     _check(load().atspeed_op_fork_pages(_raw_stream(stream, dev), n, m, *ins, free_ptr, n_free_ptr, used_ptr, *outs))
     return out
 

@@ -639,7 +639,7 @@ __device__ __forceinline__ void rank_list(const RankShared& sh, int n, int W, Pu
   }
 }
 
-__global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_constant__ SelectArgs a) {
+__global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid_constant__ SelectArgs a) {
   extern __shared__ __align__(16) unsigned char raw[];
   RankShared& sh = *reinterpret_cast<RankShared*>(raw);
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -812,9 +812,11 @@ __global__ void __launch_bounds__(kRankThreads) beam_rank_kernel(const __grid_co
 }
 
 constexpr int kTile = In<ATSPEED_F32>::TILE;
-// Pieces of a row: as many CTAs as run at once, none shorter than a tile (of 32-bit logits, whatever the type).
+// Pieces of a row: up to two CTAs an SM, none shorter than four tiles (of 32-bit logits, whatever the type).  Each costs a bound and more
+// candidates to rank.  us for 1 / 2 / 4 / 9 / 17 pieces of 33024 logits: 10 rows 12.4 / 11.1 / 10.6 / 10.3 / 11.2, 16 rows 13.2 / 11.5 /
+// 11.4 / 12.1 / 12.5, 320 rows 15.9 / 16.0 / 20.2 / 25.6 / 43, 3840 rows 100 / 112 / 155 / 357 / 580.
 int pieces_of(int R, int V) {
-  const long long tiles = (V + kTile - 1LL) / kTile, most = std::max(1LL, std::min(tiles, (152LL * kCtas + R - 1) / R));
+  const long long tiles = (V + kTile - 1LL) / kTile, most = std::max(1LL, std::min((tiles + 3) / 4, 304LL / R));
   const long long span = (tiles + most - 1) / most;
   return (int)((tiles + span - 1) / span);
 }

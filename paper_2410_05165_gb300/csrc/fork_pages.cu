@@ -4,10 +4,10 @@
 //   count' = count + handed out - old rows that hold the page + new rows that hold it;  free' = {page : count' <= 0}
 // Bound: latency, for large tables HBM (the old entries in, the new ones out).
 //
-// One launch of clusters of eight CTAs.  Every CTA works out for itself which children are heirs and which page a copy gets (a few
-// bytes a row, from L2, and one sum over the rows) instead of waiting for another launch.  The first cluster then makes the counts
-// and the free list, in phases with the cluster's barrier between them; the other clusters write the rows.  An old row and the
-// child that counts for it cancel: only the entries that a row gains or loses touch a count.
+// One launch.  Every CTA works out for itself which children are heirs and which page a copy gets (a few bytes a row, from L2, and
+// one sum over the rows) instead of waiting for another launch.  The first CTA, or for many pages a cluster of eight, then makes the counts
+// and the free list, in phases with its barrier between them; the others write the rows, a warp some hundred entries.
+// An old row and the child that counts for it cancel: only the entries that a row gains or loses touch a count.
 #include <algorithm>
 
 #include "common.cuh"
@@ -17,11 +17,12 @@ namespace atspeed {
 namespace {
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
-constexpr int kCluster = 8;
+constexpr int kPiece = 512;   // entries of a row that a warp writes
 constexpr int kMaxPages = 1 << 26;
 
 struct ForkArgs {
   int n_old, n_new, width, page, n_pages;
+  bool wide;   // counts at multiples of 16 bytes
   const int *table, *kv_len, *q_len, *old_state, *parent, *length, *ref, *free, *n_free, *used;
   int *new_table, *new_len, *new_state, *src, *dst, *new_ref, *new_free, *new_n_free;
 };
@@ -55,13 +56,19 @@ __device__ __forceinline__ Child child_of(const ForkArgs& a, int j) {
 
 constexpr int kNoCopy = -1, kNoPage = -2;   // in place of a copy's number
 
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) fork_pages_kernel(const __grid_constant__ ForkArgs a) {
+// kCluster: CTAs that make the counts (and those of every cluster).
+template <int kCluster>
+__global__ void __launch_bounds__(kThreads, 1) fork_pages_kernel(const __grid_constant__ ForkArgs a) {
   extern __shared__ __align__(16) unsigned char raw[];
   unsigned long long* heir = reinterpret_cast<unsigned long long*>(raw);   // [n_old] (len, ~j) of its best child, 0: none
   int* copy = reinterpret_cast<int*>(heir + a.n_old);                     // [n_new] which of the copies it is
-  __shared__ int s_sum[kWarps], s_count[kCluster];
+  __shared__ int s_sum[kWarps], s_count[8];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rank = (int)cluster_ctarank();
+  const int rank = kCluster > 1 ? (int)cluster_ctarank() : 0;
+  const auto sync_all = [] {   // of the CTAs that make the counts
+    if constexpr (kCluster > 1) cluster_sync();
+    else __syncthreads();
+  };
   const auto scan = [&](int v, int& all) {   // the sum over the threads before this one
     int x = v;
 #pragma unroll
@@ -88,6 +95,13 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) for
   const auto in_pool = [&](int e) { return (unsigned)e < (unsigned)a.n_pages; };
   const int n_free = max(0, __ldg(a.n_free)), used = a.used ? min(n_free, max(0, __ldg(a.used))) : 0;
 
+  if (blockIdx.x < kCluster) {   // the old counts, under way meanwhile
+    const int step = kCluster * kThreads, first = rank * kThreads + tid, n4 = a.wide ? a.n_pages / 4 : 0;
+#pragma unroll 4
+    for (int p = first; p < n4; p += step) reinterpret_cast<int4*>(a.new_ref)[p] = __ldg(reinterpret_cast<const int4*>(a.ref) + p);
+#pragma unroll 4
+    for (int p = 4 * n4 + first; p < a.n_pages; p += step) a.new_ref[p] = __ldg(a.ref + p);
+  }
   for (int p = tid; p < a.n_old; p += kThreads) heir[p] = 0;
   __syncthreads();
   for (int j = tid; j < a.n_new; j += kThreads) {
@@ -122,17 +136,24 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) for
   __syncthreads();
   const auto fresh_page = [&](int j) { return __ldg(a.free + used + copy[j]); };
 
-  if (blockIdx.x >= kCluster) {   // rows, a warp each
-    const int warps = (gridDim.x - kCluster) * kWarps;
-    for (int j = (blockIdx.x - kCluster) * kWarps + warp; j < a.n_new; j += warps) {
+  if (blockIdx.x >= kCluster) {   // rows, a warp a piece of one
+    const int warps = (gridDim.x - kCluster) * kWarps, pieces = (a.width + kPiece - 1) / kPiece;
+    for (long long it = (blockIdx.x - kCluster) * kWarps + warp; it < (long long)a.n_new * pieces; it += warps) {
+      const int j = (int)(it / pieces), i0 = (int)(it % pieces) * kPiece + lane, i1 = min(a.width, i0 - lane + kPiece);
       const Child c = child_of(a, j);
       const int k = copy[j];
       const bool served = c.state == ATSPEED_PLAN_OK && k != kNoPage;
       const int kept = served ? c.kept : 0, fresh = k >= 0 ? fresh_page(j) : -1;
       const int* from = a.table + (long long)max(0, c.parent) * a.width;
       int* to = a.new_table + (long long)j * a.width;
-      for (int i = lane; i < a.width; i += 32) to[i] = i < kept ? (k >= 0 && i == kept - 1 ? fresh : __ldg(from + i)) : -1;
-      if (lane == 0) {
+      const int own = k >= 0 ? kept - 1 : kept;   // entries from the parent
+#pragma unroll 8
+      for (int i = i0; i < i1; i += 32) {
+        int e = i < kept ? fresh : -1;
+        if (i < own) e = __ldg(from + i);
+        to[i] = e;
+      }
+      if (i0 == 0) {
         a.new_len[j] = served ? c.len : -1;
         a.new_state[j] = c.state != ATSPEED_PLAN_OK ? c.state : served ? ATSPEED_PLAN_OK : ATSPEED_PLAN_NO_PAGES;
         a.src[j] = k >= 0 ? last_entry(c) : -1;
@@ -141,55 +162,110 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) for
     }
     return;
   }
-  // counts: the old ones, then what changes
-  for (int p = rank * kThreads + tid; p < a.n_pages; p += kCluster * kThreads) a.new_ref[p] = __ldg(a.ref + p);
-  cluster_sync();
+  // counts: what changes
+  sync_all();   // (the old ones are there)
   const auto add = [&](int e, int v) {
     if (in_pool(e)) atomicAdd(a.new_ref + e, v);
   };
   for (int i = rank * kThreads + tid; i < used; i += kCluster * kThreads) add(__ldg(a.free + i), 1);
-  for (int j = rank * kWarps + warp; j < a.n_new; j += kCluster * kWarps) {
-    const Child c = child_of(a, j);
-    if (c.parent < 0 || c.state != ATSPEED_PLAN_OK || copy[j] == kNoPage) continue;
-    const int* from = a.table + (long long)c.parent * a.width;
-    const int kept = c.kept - (copy[j] >= 0);
-    if (is_heir(c, j)) {   // (with its parent's own hold)
-      for (int i = kept + lane, n = held_pages(a, c.parent); i < n; i += 32) add(__ldg(from + i), -1);
-    } else {
-      for (int i = lane; i < kept; i += 32) add(__ldg(from + i), 1);
+  // New rows, then old ones that no heir counts for: a lane finds out about one, the warp walks through their entries.
+  // (entries i0 .. i1 of row p get v; what a warp does one after the other here is a chain of four reads a row)
+  const int my_warp = rank * kWarps + warp, all_warps = kCluster * kWarps;
+  const auto walk = [&](int p, int i0, int i1, int v) {
+    unsigned rows = __ballot_sync(0xffffffffu, i0 < i1);
+    while (rows) {
+      int e[4], from[4], to[4], by[4], at[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int l = rows ? __ffs(rows) - 1 : 0;
+        from[q] = __shfl_sync(0xffffffffu, i0, l) + lane, to[q] = rows ? __shfl_sync(0xffffffffu, i1, l) : 0;
+        by[q] = __shfl_sync(0xffffffffu, v, l), at[q] = __shfl_sync(0xffffffffu, p, l);
+        rows &= rows - 1;
+        e[q] = from[q] < to[q] ? __ldg(a.table + (long long)at[q] * a.width + from[q]) : -1;
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) add(e[q], by[q]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll 8
+        for (int i = from[q] + 32; i < to[q]; i += 32) add(__ldg(a.table + (long long)at[q] * a.width + i), by[q]);
     }
-    if (lane == 0 && copy[j] >= 0) add(fresh_page(j), 1);
+  };
+  for (int j0 = my_warp; j0 < a.n_new; j0 += 32 * all_warps) {
+    const int j = j0 + lane * all_warps;
+    int p = 0, from = 0, to = 0, v = 1;
+    if (j < a.n_new) {
+      const Child c = child_of(a, j);
+      if (c.parent >= 0 && c.state == ATSPEED_PLAN_OK && copy[j] != kNoPage) {
+        const int kept = c.kept - (copy[j] >= 0);
+        p = c.parent, to = kept;
+        if (is_heir(c, j)) from = kept, to = held_pages(a, p), v = -1;   // (with its parent's own hold)
+        if (copy[j] >= 0) add(fresh_page(j), 1);
+      }
+    }
+    walk(p, from, to, v);
   }
-  for (int p = rank * kWarps + warp; p < a.n_old; p += kCluster * kWarps) {
-    if (heir[p] && copy[~(uint32_t)heir[p]] != kNoPage) continue;   // (its heir has counted for it)
-    const int* from = a.table + (long long)p * a.width;
-    for (int i = lane, n = held_pages(a, p); i < n; i += 32) add(__ldg(from + i), -1);
+  for (int p0 = my_warp; p0 < a.n_old; p0 += 32 * all_warps) {
+    const int p = p0 + lane * all_warps;
+    const bool own = p < a.n_old && !(heir[p] && copy[~(uint32_t)heir[p]] != kNoPage);
+    walk(p, 0, own ? held_pages(a, p) : 0, -1);
   }
-  cluster_sync();
-  // the free list: every CTA a range of pages, in order
-  const int share = (int)((a.n_pages + (long long)kCluster * kThreads - 1) / (kCluster * kThreads)) * kThreads;
-  const int p0 = (int)min((long long)a.n_pages, (long long)rank * share), p1 = min(a.n_pages, p0 + share);
+  sync_all();
+  // the free list: every warp a range of pages, in order, 128 at a time; which of them are free stays in a lane's bits
+  constexpr int kHeld = 16;
+  const int steps = (int)((a.n_pages + 128ll * kWarps * kCluster - 1) / (128ll * kWarps * kCluster));
+  const long long p0 = 128ll * steps * (rank * kWarps + warp) + 4 * lane;   // the lane's first four
+  const auto free_of = [&](int step) {
+    const long long p = p0 + 128ll * step;
+    uint32_t bits = 0;
+    if (a.wide && p + 4 <= a.n_pages) {
+      const int4 n = __ldcg(reinterpret_cast<const int4*>(a.new_ref + p));
+      return (n.x <= 0 ? 1u : 0u) | (n.y <= 0 ? 2u : 0u) | (n.z <= 0 ? 4u : 0u) | (n.w <= 0 ? 8u : 0u);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bits |= (p + i < a.n_pages && __ldcg(a.new_ref + p + i) <= 0 ? 1u : 0u) << i;
+    return bits;
+  };
+  unsigned long long held = 0;
   int zeros = 0;
-  for (int p = p0 + tid; p < p1; p += kThreads) zeros += __ldcg(a.new_ref + p) <= 0;
-  scan(zeros, all);
-  if (tid < kCluster) {
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(mapa_u32(&s_count[rank], tid)), "r"(all) : "memory");
+#pragma unroll 4
+  for (int t = 0; t < steps; ++t) {
+    const uint32_t bits = free_of(t);
+    if (t < kHeld) held |= (unsigned long long)bits << 4 * t;
+    zeros += __popc(bits);
   }
-  cluster_sync();
-  int at = 0, total = 0;
-  for (int r = 0; r < kCluster; ++r) {
-    at += r < rank ? s_count[r] : 0;
-    total += s_count[r];
+  zeros = __reduce_add_sync(0xffffffffu, zeros);
+  int at = scan(lane == 0 ? zeros : 0, all), total = all;   // (lane 0's is the warp's)
+  at = __shfl_sync(0xffffffffu, at, 0);
+  if constexpr (kCluster > 1) {
+    if (tid < kCluster)
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(mapa_u32(&s_count[rank], tid)), "r"(all) : "memory");
+    cluster_sync();
+    total = 0;
+    for (int r = 0; r < kCluster; ++r) {
+      at += r < rank ? s_count[r] : 0;
+      total += s_count[r];
+    }
   }
-  for (int p = p0; p < p1; p += kThreads) {
-    const bool is_free = p + tid < p1 && __ldcg(a.new_ref + p + tid) <= 0;
-    const int before = scan(is_free, all);
-    if (is_free) a.new_free[at + before] = p + tid;
-    at += all;
+  for (int t = 0; t < steps; ++t) {
+    const uint32_t bits = t < kHeld ? (uint32_t)(held >> 4 * t) & 15u : free_of(t);
+    const int mine = __popc(bits);
+    int x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    int to = at + x - mine;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (bits >> i & 1) a.new_free[to++] = (int)(p0 + 128ll * t + i);
+    at += __shfl_sync(0xffffffffu, x, 31);
   }
+#pragma unroll 4
   for (int i = total + rank * kThreads + tid; i < a.n_pages; i += kCluster * kThreads) a.new_free[i] = -1;
   if (rank == 0 && tid == 0) *a.new_n_free = total;
-  cluster_sync();   // (no CTA leaves while others may write to its counts)
+  if constexpr (kCluster > 1) cluster_sync();   // (no CTA leaves while others may write to its counts)
 }
 
 }  // namespace
@@ -209,14 +285,25 @@ extern "C" atspeed_status atspeed_op_fork_pages(atspeed_stream stream, int n_old
     return ATSPEED_E_ARG;
   if ((!d_parent && n_old != n_new) || d_new_table == d_table || d_new_ref == d_ref || d_new_free == d_free) return ATSPEED_E_ARG;
   if (n_old > kMaxRequests || n_new > kMaxRequests || n_pages > kMaxPages) return ATSPEED_E_SHAPE;
-  const ForkArgs a = {n_old,  n_new,  table_width, page_size,   n_pages,   d_table,   d_kv_len, d_q_len, d_old_state, d_parent,  d_length,
+  const ForkArgs a = {n_old,  n_new,  table_width, page_size,   n_pages,   aligned16(d_ref) && aligned16(d_new_ref), d_table,   d_kv_len, d_q_len, d_old_state, d_parent,  d_length,
                       d_ref,  d_free, d_n_free,    d_used,      d_new_table, d_new_len, d_new_state, d_src, d_dst, d_new_ref, d_new_free,
                       d_new_n_free};
   const int smem = n_old * (int)sizeof(unsigned long long) + n_new * (int)sizeof(int);
-  static std::atomic<unsigned long long> done{0};
-  if (smem_attr_once(done, fork_pages_kernel, kMaxRequests * 12) != cudaSuccess) return ATSPEED_E_CUDA;
-  // one cluster for the counts, and of the others what fills the GPU where there are rows enough (a warp a row)
-  const int clusters = 1 + std::min(17, (n_new + kCluster * kWarps - 1) / (kCluster * kWarps));
-  fork_pages_kernel<<<clusters * kCluster, kThreads, smem, (cudaStream_t)stream>>>(a);
-  return launch_status();
+  // Rows by as many CTAs as there is work for, up to the SMs that are left.  One CTA makes the counts of few pages and rows.
+  const long long warps = (long long)n_new * ((table_width + kPiece - 1) / kPiece);
+  const int writers = (int)std::min(136LL, (warps + kWarps - 1) / kWarps);
+  static std::atomic<unsigned long long> done[2];
+  if (n_pages <= 16384 && n_old + n_new <= 128) {
+    if (smem_attr_once(done[0], fork_pages_kernel<1>, kMaxRequests * 12) != cudaSuccess) return ATSPEED_E_CUDA;
+    fork_pages_kernel<1><<<1 + writers, kThreads, smem, (cudaStream_t)stream>>>(a);
+    return launch_status();
+  }
+  if (smem_attr_once(done[1], fork_pages_kernel<8>, kMaxRequests * 12) != cudaSuccess) return ATSPEED_E_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(8 + (writers + 7) / 8 * 8), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = smem, cfg.stream = (cudaStream_t)stream;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = 8, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr, cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, fork_pages_kernel<8>, a) == cudaSuccess ? ATSPEED_OK : ATSPEED_E_CUDA;
 }

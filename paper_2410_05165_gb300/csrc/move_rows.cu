@@ -37,57 +37,135 @@ struct CompactArgs {
   Layers l;
 };
 
-// A CTA takes (copy, layer, K or V) after (copy, layer, K or V).
+// Copies from `from` to `to` what a warp has of one layer's K or V: i-th vectors at at(i), i < n, eight under way a lane.
+template <class At>
+__device__ __forceinline__ void warp_copy(uint4* to, const uint4* from, int n, At&& at) {
+  const int lane = threadIdx.x & 31;
+  for (int i0 = lane; i0 < n; i0 += 32 * kBatch) {
+    uint4 x[kBatch];
+    long long o[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (i0 + 32 * q < n) {
+        o[q] = at(i0 + 32 * q);
+        x[q] = from[o[q]];
+      }
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (i0 + 32 * q < n) to[o[q]] = x[q];
+  }
+}
+
+// A warp takes some rows (512 vectors, a row at least) of a copy in one layer's K or V after some rows.  Copies come and go with the lengths,
+// so every CTA lists 256 of them at a time with the rows that they have, and the grid's warps share those out: with a CTA a (copy,
+// layer, K or V) and pairs of -1 among them, 59 copies of 8 of 16 tokens in 32 layers of 32 heads of 128 took 118 us.
 __global__ void __launch_bounds__(kThreads) copy_pages_kernel(const __grid_constant__ CopyArgs a) {
+  __shared__ int s_upto[kThreads], s_src[kThreads], s_dst[kThreads], s_rows[kThreads], s_warp[kWarps];
   const Geometry& g = a.g;
-  const long long items = 2LL * a.n * a.layers;
-  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-    const int j = (int)(it / (2 * a.layers)), lv = (int)(it % (2 * a.layers));
-    const int src = __ldg(a.src + j), dst = __ldg(a.dst + j);
-    if ((unsigned)src >= (unsigned)g.n_pages || (unsigned)dst >= (unsigned)g.n_pages || src == dst) continue;
-    const int len = a.length ? __ldg(a.length + j) : g.page;
-    if (len < 1) continue;
-    const int rows = (len - 1) % g.page + 1;
-    const bool v = lv & 1;
-    uint4* base = a.l.at[lv >> 1][lv & 1];
-    const long long sp = v ? g.v_page : g.k_page, st = v ? g.v_token : g.k_token, sh = v ? g.v_head : g.k_head;
-    const int row = g.heads * g.vecs;
-    const long long all = (long long)rows * row;
-    for (long long i = threadIdx.x; i < all; i += kThreads) {
-      const int t = (int)(i / row), h = (int)(i % row) / g.vecs, c = (int)(i % row) % g.vecs;
-      const long long at = t * st + h * sh + c;
-      base[dst * sp + at] = base[src * sp + at];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, all_warps = gridDim.x * kWarps;
+  const int row = g.heads * g.vecs, some = max(1, 512 / row);   // vectors of a row, rows that a warp takes at once
+  long long turn = blockIdx.x * kWarps + warp;                  // this warp's next piece of work
+  for (int j0 = 0; j0 < a.n; j0 += kThreads) {
+    const int j = j0 + tid;
+    int src = -1, dst = -1, rows = 0;
+    if (j < a.n) {
+      src = __ldg(a.src + j), dst = __ldg(a.dst + j);
+      const int len = a.length ? __ldg(a.length + j) : g.page;
+      if ((unsigned)src < (unsigned)g.n_pages && (unsigned)dst < (unsigned)g.n_pages && src != dst && len > 0) rows = (len - 1) % g.page + 1;
     }
+    int upto = (rows + some - 1) / some;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    __syncthreads();   // (the list before this one is done with)
+    if (lane == 31) s_warp[warp] = upto;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) upto += s_warp[w];
+    s_upto[tid] = upto, s_src[tid] = src, s_dst[tid] = dst, s_rows[tid] = rows;
+    __syncthreads();
+    const int units = s_upto[kThreads - 1];
+    const long long work = (long long)units * 2 * a.layers;
+    for (; turn < work; turn += all_warps) {
+      const int lv = (int)(turn / units), u = (int)(turn % units);
+      int c = 0;   // the first copy whose work ends behind u
+#pragma unroll
+      for (int step = kThreads / 2; step > 0; step >>= 1)
+        if (s_upto[c + step - 1] <= u) c += step;
+      const int t0 = (u - (c ? s_upto[c - 1] : 0)) * some, n = min(some, s_rows[c] - t0);
+      const bool v = lv & 1;
+      uint4* base = a.l.at[lv >> 1][lv & 1];
+      const long long sp = v ? g.v_page : g.k_page, st = v ? g.v_token : g.k_token, sh = v ? g.v_head : g.k_head;
+      uint4* to = base + s_dst[c] * sp + t0 * st;
+      const uint4* from = base + s_src[c] * sp + t0 * st;
+      if (sh == g.vecs && (n == 1 || st == row)) {
+        warp_copy(to, from, n * row, [](int i) { return (long long)i; });
+      } else {
+        warp_copy(to, from, n * row, [&](int i) {
+          const int t = i / row, r = i - t * row, h = r / g.vecs;
+          return t * st + h * sh + (r - h * g.vecs);
+        });
+      }
+    }
+    turn -= work;   // (the next list's first work goes to those that have none of this one's)
   }
 }
 
 // The moves of a request: a thread has 16 bytes of a row, in one layer's K or V, and moves them for token after token, so that a
 // row is read before a later move of the same bytes writes to it (a kept token's place is never behind its own).
+constexpr int kMoves = 64;   // that the CTA works out at a time
 __global__ void __launch_bounds__(kThreads) compact_tokens_kernel(const __grid_constant__ CompactArgs a) {
+  __shared__ int s_count;
+  __shared__ long long s_from[kMoves], s_to[kMoves];   // vectors from the base, to: -1 if it does not move
   const Geometry& g = a.g;
   const int b = blockIdx.x, lv = blockIdx.y, tid = threadIdx.x;
   const int q0 = min(a.T, max(0, __ldg(a.cu_q + b))), q = min(a.T, __ldg(a.cu_q + b + 1)) - q0;
-  int n = !a.state || __ldg(a.state + b) == ATSPEED_PLAN_OK ? min(a.keep_width, __ldg(a.n_keep + b)) : 0;
+  const int n = !a.state || __ldg(a.state + b) == ATSPEED_PLAN_OK ? max(0, min(a.keep_width, __ldg(a.n_keep + b))) : 0;
   const int* keep = a.keep + (long long)b * a.keep_width;
-  int count = 0;   // of the list up to its first entry that is out of order
-  for (int last = -1; count < n; ++count) {
-    const int k = __ldg(keep + count);
-    if (k <= last || k >= q) break;
-    last = k;
+  if (tid == 0) s_count = n;
+  __syncthreads();
+  for (int i = tid; i < n; i += kThreads) {   // the list ends at its first entry that is out of order
+    const int k = __ldg(keep + i), before = i ? __ldg(keep + i - 1) : -1;
+    if (k <= before || k >= q) atomicMin(&s_count, i);
   }
+  __syncthreads();
+  const int count = s_count;
   if (a.new_len && lv == 0 && blockIdx.z == 0 && tid == 0) a.new_len[b] = __ldg(a.kv_len + b) + count;
   const bool v = lv & 1;
   uint4* base = a.l.at[lv >> 1][lv & 1];
   const long long sp = v ? g.v_page : g.k_page, st = v ? g.v_token : g.k_token, sh = v ? g.v_head : g.k_head;
-  const long long rows = (long long)g.n_pages * g.page;
-  for (int i = blockIdx.z * kThreads + tid; i < g.heads * g.vecs; i += gridDim.z * kThreads) {
-    uint4* at = base + i / g.vecs * sh + i % g.vecs;
-    for (int m = 0; m < count; ++m) {
-      const int k = __ldg(keep + m);
-      if (k == m) continue;
-      const long long from = __ldg(a.slot + q0 + k), to = __ldg(a.slot + q0 + m);
-      if ((unsigned long long)from >= (unsigned long long)rows || (unsigned long long)to >= (unsigned long long)rows) continue;
-      at[to / g.page * sp + to % g.page * st] = at[from / g.page * sp + from % g.page * st];
+  const unsigned long long rows = (unsigned long long)g.n_pages * g.page;
+  for (int m0 = 0; m0 < count; m0 += kMoves) {
+    if (m0) __syncthreads();
+    if (tid < kMoves && m0 + tid < count) {
+      const int k = __ldg(keep + m0 + tid);
+      const unsigned long long from = (unsigned long long)__ldg(a.slot + q0 + k), to = (unsigned long long)__ldg(a.slot + q0 + m0 + tid);
+      const auto at = [&](unsigned long long row) {
+        const unsigned long long page = row >> 32 ? row / g.page : (unsigned)row / (unsigned)g.page;
+        return (long long)page * sp + (long long)(row - page * g.page) * st;
+      };
+      const bool moves = k != m0 + tid && from < rows && to < rows;   // (negative slots are large ones)
+      s_from[tid] = moves ? at(from) : 0;
+      s_to[tid] = moves ? at(to) : -1;
+    }
+    __syncthreads();
+    const int moves = min(kMoves, count - m0);
+    for (int i = blockIdx.z * kThreads + tid; i < g.heads * g.vecs; i += gridDim.z * kThreads) {
+      uint4* at = base + i / g.vecs * sh + i % g.vecs;
+      // (four reads, then as many writes: those go to places before any later token's)
+      for (int t = 0; t < moves; t += 4) {
+        uint4 x[4];
+        long long to[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          to[j] = t + j < moves ? s_to[t + j] : -1;
+          if (to[j] >= 0) x[j] = at[s_from[t + j]];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (to[j] >= 0) at[to[j]] = x[j];
+      }
     }
   }
 }
@@ -128,7 +206,8 @@ extern "C" atspeed_status atspeed_op_copy_pages(atspeed_stream stream, const ats
   a.n = n, a.src = d_src, a.dst = d_dst, a.length = d_length;
   for (int first = 0; first < n_layers; first += kLayers) {
     a.layers = set_layers(a.l, layers, first, n_layers);
-    const int grid = (int)std::min(152LL * 8, 2LL * n * a.layers);
+    // (four CTAs an SM; few copies: a warp a row at most)
+    const int grid = (int)std::min(152LL * 4, (2LL * n * a.layers * std::min(64, a.g.page) + kWarps - 1) / kWarps);
     copy_pages_kernel<<<grid, kThreads, 0, (cudaStream_t)stream>>>(a);
   }
   return launch_status();
