@@ -6,7 +6,7 @@
 // candidates among its logits, which are at least its W best (within a row the order is the logits').  The second, a CTA a
 // request, makes log s_r of the pieces, scores the candidates and ranks the best.
 //
-// Candidates of a piece: its tokens form groups (512; a place of a thread's each, strided over the whole piece) whose maxima stay in
+// Candidates of a piece: its tokens form groups (128 to 512, each some of a thread's, strided over the whole piece) whose maxima stay in
 // registers while the logits stream by.  W of these maxima, so W logits, are at or above the W-th largest of them: the groups that
 // reach that bound, little more than W of them, are read again for what is at or above it: in the one tile that holds the
 // maximum, or in all if the next best reaches the bound too.  Where that is more than
@@ -181,6 +181,22 @@ __device__ __forceinline__ float exp2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// The even and the odd ones of a thread's 2^(x l + c), i < kVec N, added up (two at a time: an instruction less for each).
+template <int COUNT, class X>
+__device__ __forceinline__ void sum_exp2(X&& x, float c, float& even, float& odd) {
+  unsigned long long l, add, sum = 0, y;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(l) : "f"(kLog2e));
+  asm("mov.b64 %0, {%1, %1};" : "=l"(add) : "f"(c));
+#pragma unroll
+  for (int i = 0; i < COUNT; i += 2) {
+    float a, b;
+    asm("{\n .reg .b64 p;\n mov.b64 p, {%1, %2};\n fma.rn.f32x2 %0, p, %3, %4;\n}" : "=l"(y) : "f"(x(i)), "f"(x(i + 1)), "l"(l), "l"(add));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(y));
+    a = exp2_approx(a), b = exp2_approx(b);
+    asm("{\n .reg .b64 p;\n mov.b64 p, {%1, %2};\n add.rn.f32x2 %0, %0, p;\n}" : "+l"(sum) : "f"(a), "f"(b));
+  }
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(even), "=f"(odd) : "l"(sum));
+}
 // What a sum below m is worth below M >= m.
 __device__ __forceinline__ float rescale(float m, float M) {
   if (m == M) return 1.f;
@@ -303,32 +319,33 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
     }
     copies_done();
   };
-  const auto shift = [&](const uint4& p, const uint4& q, uint32_t (&w)[4]) {   // the 16 bytes that begin `lead` bytes into p
-    uint32_t y[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
-    if (lead & 8) {
+  // the 16 bytes that begin `lead` bytes into p: words from the (lead / 4)-th on, each with the half that follows it
+  const auto shift_by = [&](auto words, const uint4& p, const uint4& q, uint32_t (&w)[4]) {
+    const uint32_t y[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
 #pragma unroll
-      for (int j = 0; j < 6; ++j) y[j] = y[j + 2];
+    for (int j = 0; j < 4; ++j) w[j] = SIZE == 2 ? __funnelshift_r(y[j + words], y[j + words + 1], lead * 8) : y[j + words];   // (its low 5 bits: 0 or 16)
+  };
+  const auto with_words = [&](auto&& f) {
+    switch (lead / 4) {
+      case 0: f(std::integral_constant<int, 0>()); break;
+      case 1: f(std::integral_constant<int, 1>()); break;
+      case 2: f(std::integral_constant<int, 2>()); break;
+      default: f(std::integral_constant<int, 3>());
     }
-    if (lead & 4) {
-#pragma unroll
-      for (int j = 0; j < 5; ++j) y[j] = y[j + 1];
-    }
-    if (SIZE == 2 && (lead & 2)) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = __funnelshift_r(y[j], y[j + 1], 16);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = y[j];
   };
   // A thread's logits of a tile, wherever the row begins: its words, shifted.
   const auto take = [&](int t0, int stage, Tile<TYPE>& x) {
     const auto& at = shared.ring[stage].word[warp];
+    const auto words = [&](auto k) {
 #pragma unroll
-    for (int v = 0; v < kVec; ++v) {
-      const uint4 p = at[v][lane];
-      x.w[v][0] = p.x, x.w[v][1] = p.y, x.w[v][2] = p.z, x.w[v][3] = p.w;
-      if (!ALIGNED && lead) shift(p, at[v][lane + 1], x.w[v]);
-    }
+      for (int v = 0; v < kVec; ++v) {
+        const uint4 p = at[v][lane];
+        if constexpr (ALIGNED) x.w[v][0] = p.x, x.w[v][1] = p.y, x.w[v][2] = p.z, x.w[v][3] = p.w;
+        else shift_by(k, p, at[v][lane + 1], x.w[v]);
+      }
+    };
+    if constexpr (ALIGNED) words(0);
+    else with_words(words);
     if (t0 + TILE > end) {
 #pragma unroll
       for (int v = 0; v < kVec; ++v)
@@ -343,7 +360,10 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
       const uint4* at = reinterpret_cast<const uint4*>(in - lead + (long long)t * SIZE);
       const uint4 p = __ldg(at);
       w[0] = p.x, w[1] = p.y, w[2] = p.z, w[3] = p.w;
-      if (!ALIGNED && lead) shift(p, __ldg(at + 1), w);
+      if (!ALIGNED && lead) {
+        const uint4 q = __ldg(at + 1);
+        with_words([&](auto k) { shift_by(k, p, q, w); });
+      }
       return;
     }
 #pragma unroll
@@ -418,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
     float M = fmaxf(m, top);
     const auto unit_at = [&] { return fabsf(M) < kFar ? unit_of(M) : M == -INFINITY ? 0.f : NAN; };   // (nothing yet: any will do)
     float u = unit_at(), sum = 0.f, more = 0.f;
-    each([&](int v, int j) { (j & 1 ? more : sum) += exp2_approx(fmaf(x.at(v, j), kLog2e, -u)); });
+    sum_exp2<kVec * N>([&](int i) { return x.at(i / N, i % N); }, -u, sum, more);
     sum += fmaf(s, exp2_approx(unit - u), more);
     if (sum != sum) {   // a NaN (it counts as -infinity), an infinity (as the type's largest), a maximum far out or of -infinity
       each([&](int v, int j) {
@@ -457,6 +477,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
     static_assert(kVec == 4, "vectors of a thread");
     const uint32_t k[1] = {key_of(fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])))};
     from = threshold_of<1, kWarps>(k, a.W, a.W + a.W / 8, sh.scratch);
+  } else if (a.W <= 96) {
+    const uint32_t k[2] = {key_of(fmaxf(best[0], best[1])), key_of(fmaxf(best[2], best[3]))};
+    from = threshold_of<2, kWarps>(k, a.W, a.W + a.W / 8, sh.scratch);
   } else {
     uint32_t k[kVec];
 #pragma unroll
@@ -536,14 +559,38 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
     gather([&](int q, int j) { return vector_at<TYPE>(w[q], j); }, [&](int q) { return ok[q]; }, [&](int q) { return t[q]; });
   }
   __syncthreads();
-  if (sh.n > a.cap) {
-    __syncthreads();
-    put_exactly<TYPE>(in, allowed, begin, end, from, a.W, sh);
-  }
   const long long at = (long long)row * a.pieces + piece;
-  const int n = sh.n;
-  for (int i = tid; i < n; i += kThreads)
-    a.cand[at * a.cap + i] = make_uint2(__float_as_uint(value_of(sh.key[i])), (uint32_t)sh.tok[i]);
+  int n = sh.n;
+  const auto hand_on = [&](int i, int to) { a.cand[at * a.cap + to] = make_uint2(__float_as_uint(value_of(sh.key[i])), (uint32_t)sh.tok[i]); };
+  const auto hand_on_best = [&] {   // what is at or above a bound among those of the list; false: too many are equal
+    uint32_t k[kList / kThreads];
+#pragma unroll
+    for (int q = 0; q < kList / kThreads; ++q) k[q] = q * kThreads + tid < n ? sh.key[q * kThreads + tid] : 0u;
+    const uint32_t bound = threshold_of<kList / kThreads, kWarps>(k, a.W, a.cap, sh.scratch);
+    int left = 0, mine = 0;
+#pragma unroll
+    for (int q = 0; q < kList / kThreads; ++q) {
+      left += __syncthreads_count(k[q] >= bound);
+      mine += k[q] >= bound;
+    }
+    if (left > a.cap) return false;
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    int to = mine ? atomicAdd(&sh.n, mine) : 0;
+#pragma unroll
+    for (int q = 0; q < kList / kThreads; ++q)
+      if (k[q] >= bound) hand_on(q * kThreads + tid, to++);
+    n = left;
+    return true;
+  };
+  if (n <= a.cap || n > kList || !hand_on_best()) {
+    if (n > a.cap) {
+      __syncthreads();
+      put_exactly<TYPE>(in, allowed, begin, end, from, a.W, sh);
+      n = sh.n;
+    }
+    for (int i = tid; i < n; i += kThreads) hand_on(i, i);
+  }
   if (tid == 0) {
     float all = 0.f;
     for (int w = 0; w < kWarps; ++w) all += sh.s[w];   // (in one order)

@@ -249,8 +249,8 @@ def test_select_scores_far_out(ats):
     assert got.token[0].tolist() == torch.sort(logits[0], descending=True).indices[:5].tolist()
 
 
-@pytest.mark.parametrize("order", ["up", "down", "lane", "tile"])
-@pytest.mark.parametrize("width", [10, 256])
+@pytest.mark.parametrize("order", ["up", "down", "lane", "tile", "few", "row"])
+@pytest.mark.parametrize("width", [10, 80, 256])
 def test_select_orders_that_meet_one_group(ats, order, width):
     """The best tokens in one thread's places, in one tile, or every one better than those before it."""
     V, R = 41000, 2
@@ -261,7 +261,10 @@ def test_select_orders_that_meet_one_group(ats, order, width):
         x = base[::-1]
     else:
         x = np.random.default_rng(0).permutation(base[:V - 2000] - 8)
-        hot = np.arange(2000) * 16 % V if order == "lane" else 20000 + np.arange(2000)
+        i = np.arange(2000)
+        hot = {"lane": i * 16 % V, "tile": 20000 + i, "few": i // 100 + i % 20 * 2048 + i % 100 // 20 * 300,   # a hundred places of each 2048
+               "row": i // 20 + i % 20 * 2048}[order]
+        assert len(set(hot.tolist())) == 2000
         x = np.concatenate([x, np.zeros(2000)])
         x[hot] = np.linspace(0, 8, 2000)
     logits = torch.from_numpy(np.tile(x, (R, 1)).astype(np.float32)).to("cuda")
