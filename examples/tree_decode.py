@@ -133,9 +133,12 @@ class Decoder:
         state = torch.where(plan.req < 0, -1, plan.pos & 1).to(torch.int32)
         ats.op_adjust_logits(logits, plan.req, rules, mask=plan.mask, state=state, out=logits)
         best, first = logits.argmax(dim=1).tolist(), 0
+        self.path = []   # each user's tokens of this step that are accepted
         for b in range(n):
             at = len(chains[b]) - 1   # the last accepted token; then down the tree as long as a draft is what was chosen
+            self.path.append(list(range(at)))
             while at is not None:
+                self.path[b].append(at)
                 self.text[b].append(best[first + at])
                 at = next((j for j in range(len(chains[b]), q_len[b])
                            if parents[b][j] == at and parts[b][j] == self.text[b][-1]), None)
