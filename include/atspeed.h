@@ -452,10 +452,10 @@ atspeed_status atspeed_op_adjust_logits(atspeed_stream stream, const void *d_log
  *   score(r, v) = d_score[r] + log p_r(v) of the allowed tokens v, p_r the softmax over the allowed logits (ATSPEED_NORM_MASKED) or over
  *   all of the row (ATSPEED_NORM_FULL);  d_score NULL: 0;
  *   d_final[r] >= 0 (d_final NULL: none): the beam has ended, its one continuation is that token with the score d_score[r].
- * Higher scores come first, compared in 64 bits (the sum of a row's exponentials in 32); of equal ones the lower row, then the
- * larger logit, then the lower token.  A score of -infinity (in 32 bits) or NaN is never chosen.
+ * Higher scores come first, compared in two 32-bit parts (48 bits; the terms of a row's sum have 22); of equal ones the lower row, then
+ * the larger logit, then the lower token.  A score of -infinity (in 32 bits) or NaN is never chosen.
  * Outputs [n_req][width], best first: d_token, d_parent (the row), d_out_score (rounded to 32 bits); places without a
- * continuation hold -1, -1, -infinity.  Rows of no request are not read.
+ * continuation hold -1, -1, -infinity.  Rows of no request do not count.
  * width 1 .. 256, vocab up to 2^30 (ATSPEED_E_SHAPE).  d_ws: atspeed_op_beam_select_workspace(R, vocab, width) bytes, 16-byte aligned, whatever they
  * hold, of this call alone until it is done. */
 size_t atspeed_op_beam_select_workspace(int R, int vocab, int width);

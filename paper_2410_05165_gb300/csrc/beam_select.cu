@@ -1,18 +1,23 @@
 // Beam search's selection over beams and vocabulary (atspeed_op_beam_select).
 //   score(r, v) = cum_r + ((x_rv - m_r) - log s_r),  m_r = max x_r,  s_r = sum_v exp(x_rv - m_r);  the best W of a request's rows
-// Bound: HBM (each logit read once).
+// Bound: HBM (each logit read once).  3840 rows of 33024 (32 bits, W = 80) take 99 us, 5.1 TB/s: 75 of them the logits alone (a copy's rate), 3
+// the bounds, 10 the second reads, 10 the ranking.  732 rows of 100003 (bf16, at odd addresses, W = 32) 38 us, 3.9 TB/s, where
+// unpacking and exponentials take as long as the bytes.  Ten rows of 33024 11 us: latency, half of it the ranking's.
 //
 // Two launches.  The first reads the logits, a CTA a piece of a row: the piece's maximum, its sum of exponentials and the
 // candidates among its logits, which are at least its W best (within a row the order is the logits').  The second, a CTA a
-// request, makes log s_r of the pieces, scores the candidates and ranks the best.
+// request, makes log s_r of the pieces, looks at the candidates in 32 bits and ranks those that may be among the best.
 //
 // Candidates of a piece: its tokens form groups (128 to 512, each some of a thread's, strided over the whole piece) whose maxima stay in
 // registers while the logits stream by.  W of these maxima, so W logits, are at or above the W-th largest of them: the groups that
 // reach that bound, little more than W of them, are read again for what is at or above it: in the one tile that holds the
-// maximum, or in all if the next best reaches the bound too.  Where that is more than
-// a list holds (equal logits, a mask of the type's lowest value) the W best are searched exactly.
+// maximum, or in all if the next best reaches the bound too.  (Logits held against a bound as they come: 290 us for the 3840 rows; every
+// tile of those groups read again: 116.)  Of more than are handed on, a bound among them leaves fewer; where the logits are equal or
+// more than a list holds reach the bound (a mask of the type's lowest value), the W best are searched exactly.
 //
-// Sums of a row do not depend on where the row begins in memory: rows with the same logits have the same bits.
+// Logits come through a ring of asynchronous copies, two tiles ahead: 64 to 80 KB an SM under way.  CTAs of 128 threads, so that few of an
+// SM's are at their bounds, which take a fifth of a row's time, while the others read.  Sums of a row do not depend on where the
+// row begins in memory, so that rows with the same logits have the same bits.
 #include <algorithm>
 #include <type_traits>
 
@@ -22,7 +27,7 @@
 namespace atspeed {
 namespace {
 
-constexpr int kThreads = 128, kWarps = kThreads / 32, kCtas = 6;   // (CTAs an SM)
+constexpr int kThreads = 128, kWarps = kThreads / 32, kCtas = 5;   // (CTAs an SM)
 constexpr int kVec = 4;                     // 16-byte vectors of a thread in a tile
 constexpr int kList = 1024;                 // candidates that a piece's list holds
 constexpr int kGroups = kThreads * kVec;
@@ -32,8 +37,6 @@ constexpr uint32_t kNone = 0x007fffffu;     // the key of -infinity
 
 struct Header {   // of a piece
   float m, s;
-  int n;
-  int pad;
 };
 
 struct SelectArgs {
@@ -151,7 +154,7 @@ struct Shared {
   int tok[kList];
   uint32_t scratch[3 * kWarps];
   int read[kGroups];         // vectors to be read again: from the front by their first tokens, from the back in every tile
-  int n, n_read, n_every, count[kWarps];
+  int n, n_reads, count[kWarps];   // n_reads: those at the front, and 65536 times those at the back
   float m[kWarps], s[kWarps];
 };
 
@@ -390,11 +393,11 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
   const uint32_t* allowed = st >= 0 && !nothing ? a.grammar + st * a.grammar_stride : nullptr;
   float m = -INFINITY, s = 0.f;   // the thread's maximum and sum
   float unit = 0.f;               // unit_of(m), a NaN where m is far out
-  // .. and of its vectors' places, each a group: the largest candidate, the tile that it is in, and the largest of any place's other tiles
-  float best[kVec], second = -INFINITY;
+  // .. and of each of its vectors' places: the largest candidate, the tile that it is in, and the largest of the other tiles
+  float best[kVec], second[kVec];
   int where[kVec];
 #pragma unroll
-  for (int v = 0; v < kVec; ++v) best[v] = -INFINITY, where[v] = begin;
+  for (int v = 0; v < kVec; ++v) best[v] = second[v] = -INFINITY, where[v] = begin;
   Tile<TYPE> x;
   for (int t0 = begin, stage = 0; t0 < end; t0 += TILE, stage = stage == kStages - 1 ? 0 : stage + 1) {
     copies_wait<1>();
@@ -462,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
     }
 #pragma unroll
     for (int v = 0; v < kVec; ++v) {
-      second = fmaxf(second, fminf(best[v], vm[v]));
+      second[v] = fmaxf(second[v], fminf(best[v], vm[v]));
       where[v] = vm[v] > best[v] ? t0 : where[v];
       best[v] = fmaxf(best[v], vm[v]);
     }
@@ -471,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
   // the W-th largest of the groups' maxima, or a smaller value with little more above it: of the threads', for many of their vectors' places
   const float wm = warp_max(m);
   if (lane == 0) sh.m[warp] = wm;
-  if (tid == 0) sh.n = sh.n_read = sh.n_every = 0;
+  if (tid == 0) sh.n = sh.n_reads = 0;
   uint32_t from;
   if (a.W <= kThreads / 4) {
     static_assert(kVec == 4, "vectors of a thread");
@@ -493,8 +496,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
   const float ws = warp_sum(m > -INFINITY ? s * rescale(m, M) : 0.f);
   if (lane == 0) sh.s[warp] = ws;
   const float least = value_of(from);
-  // The candidates among count vectors of logits w from token t(q) on (bits ok: those allowed), in the list: places for all of a
-  // thread's at once.
+  // The candidates among kVec vectors, logits at(q, j) of the tokens from t(q) on (those of the bits ok(q)), into the list: places for all
+  // of a thread's at once.
   const auto keep = [&](auto&& at, int q, int j, auto&& t, int place) {
     if (place >= kList) return;
     sh.key[place] = key_of(fminf(at(q, j), In<TYPE>::value(In<TYPE>::MOST)));
@@ -527,19 +530,25 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
     if (m > -INFINITY)
       gather([&](int q, int j) { return x.at(q, j); }, [&](int q) { return best[q] >= least ? 0xffffffffu : 0u; }, [&](int q) { return token(begin, q); });
   } else {
-    const bool every = second >= least;   // (of a place's tiles: then all are read, else the one with the maximum)
-    int mine = 0;
+    int one = 0, every = 0;   // places to be read in the tile with the maximum, in every tile
 #pragma unroll
-    for (int v = 0; v < kVec; ++v) mine += best[v] >= least;
-    if (mine) {
-      int at = atomicAdd(every ? &sh.n_every : &sh.n_read, mine);
+    for (int v = 0; v < kVec; ++v) {
+      every += second[v] >= least;
+      one += best[v] >= least && !(second[v] >= least);
+    }
+    if (one | every) {
+      const int at = atomicAdd(&sh.n_reads, one | every << 16);
+      int front = at & 0xffff, back = kGroups - (at >> 16);
 #pragma unroll
       for (int v = 0; v < kVec; ++v)
-        if (best[v] >= least) sh.read[every ? kGroups - 1 - at++ : at++] = token(every ? 0 : where[v], v);
+        if (best[v] >= least) {
+          if (second[v] >= least) sh.read[--back] = token(0, v);
+          else sh.read[front++] = token(where[v], v);
+        }
     }
   }
   __syncthreads();
-  const int n_one = sh.n_read, n_every = sh.n_every, reads = n_one + n_every * tiles;
+  const int n_one = sh.n_reads & 0xffff, n_every = sh.n_reads >> 16, reads = n_one + n_every * tiles;
   for (int i0 = tid; i0 < reads; i0 += kVec * kThreads) {
     uint32_t w[kVec][4], ok[kVec];
     int t[kVec];
@@ -591,10 +600,11 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
     }
     for (int i = tid; i < n; i += kThreads) hand_on(i, i);
   }
+  for (int i = n + tid; i < a.cap; i += kThreads) a.cand[at * a.cap + i] = make_uint2(0xff800000u, 0u);   // (-infinity: none)
   if (tid == 0) {
     float all = 0.f;
     for (int w = 0; w < kWarps; ++w) all += sh.s[w];   // (in one order)
-    a.head[at] = {M, all, n, 0};
+    a.head[at] = {M, all};
   }
 }
 
@@ -651,12 +661,13 @@ struct Quick {
   float bias, size;
 };
 
+constexpr int kMostCtas = 304, kManyPieces = kMostCtas / 3 + 1;   // of the first launch where rows are in pieces; rows of three pieces or more
 constexpr int kRows = 256;   // that shared memory holds (of more: device memory)
 struct RankShared {
   unsigned long long score[kRankList], rest[kRankList];
   uint32_t tok[kRankList];
   uint32_t scratch[3 * kRankThreads / 32];
-  float top[kRankThreads];   // rows' maxima, on the way to their logarithms
+  float top[kManyPieces];   // rows' maxima, on the way to their logarithms
   Row row[kRows];
   Quick quick[kRows];
   Entry best[kMaxWidth];
@@ -701,17 +712,11 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
   // Candidates: a thread has place `at` of list my_list and of every at_once-th list from there; kHold of them in a round, the
   // first of which are under way while the rows' sums are made.
   const int at_once = kRankThreads / a.cap, at = tid & (a.cap - 1), my_list = tid / a.cap;
-  constexpr int kHold = 16, kBatch = 4;
-  const auto fetch = [&](int l, uint2& c, int& n) {
-    if (l >= lists) return;
-    const long long h = (long long)r0 * a.pieces + l;
-    c = a.cand[h * a.cap + at];
-    n = a.head[h].n;
-  };
+  constexpr int kHold = 16, kBatch = 8;
+  const auto fetch = [&](int l) { return l < lists ? a.cand[((long long)r0 * a.pieces + l) * a.cap + at] : make_uint2(0xff800000u, 0u); };
   uint2 c[kBatch];
-  int cn[kBatch];
 #pragma unroll
-  for (int q = 0; q < kBatch; ++q) fetch(q * at_once + my_list, c[q], cn[q]);
+  for (int q = 0; q < kBatch; ++q) c[q] = fetch(q * at_once + my_list);
   const auto row_of = [&](int l) { return r0 + (a.pieces == 1 ? l : (int)__umulhi((unsigned)l, a.per_piece)); };
   const auto row_at = [&](int r) -> Row& { return r - r0 < kRows ? sh.row[r - r0] : a.rows[r]; };
   const auto quick_at = [&](int r) -> Quick& { return r - r0 < kRows ? sh.quick[r - r0] : a.quick[r]; };
@@ -739,36 +744,35 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
       set_row(r, M, M > -INFINITY ? whole(s0 * rescale(m0, M)) + whole(s1 * rescale(m1, M)) : 0ull);
     }
   } else {
-    for (int base = r0; base < r1; base += kRankThreads) {   // (a thousand rows at a time, whose sums wait in the list's place)
-      const int last = min(r1, base + kRankThreads);
-      for (int r = base + warp; r < last; r += kRankThreads / 32) {
-        const Header* h = a.head + (long long)r * a.pieces;
-        const float m0 = lane < a.pieces ? h[lane].m : -INFINITY, s0 = lane < a.pieces ? h[lane].s : 0.f;
-        float M = m0;
-        for (int p = lane + 32; p < a.pieces; p += 32) M = fmaxf(M, h[p].m);
-        M = warp_max(M);
-        unsigned long long s = m0 > -INFINITY ? whole(s0 * rescale(m0, M)) : 0ull;
-        for (int p = lane + 32; p < a.pieces; p += 32)
-          if (h[p].m > -INFINITY) s += whole(h[p].s * rescale(h[p].m, M));
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (lane == 0) {
-          sh.top[r - base] = M;
-          sh.score[r - base] = s;
-        }
+    // (rows of three pieces or more are fewer than kManyPieces; their sums wait in the list's place)
+    for (int r = r0 + warp; r < r1; r += kRankThreads / 32) {
+      const Header* h = a.head + (long long)r * a.pieces;
+      const float m0 = lane < a.pieces ? h[lane].m : -INFINITY, s0 = lane < a.pieces ? h[lane].s : 0.f;
+      float M = m0;
+      for (int p = lane + 32; p < a.pieces; p += 32) M = fmaxf(M, h[p].m);
+      M = warp_max(M);
+      unsigned long long s = m0 > -INFINITY ? whole(s0 * rescale(m0, M)) : 0ull;
+      for (int p = lane + 32; p < a.pieces; p += 32)
+        if (h[p].m > -INFINITY) s += whole(h[p].s * rescale(h[p].m, M));
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      if (lane == 0) {
+        sh.top[r - r0] = M;
+        sh.score[r - r0] = s;
       }
-      __syncthreads();
-      if (base + tid < last) set_row(base + tid, sh.top[tid], sh.score[tid]);
-      __syncthreads();
     }
+    __syncthreads();
+    if (tid < r1 - r0) set_row(r0 + tid, sh.top[tid], sh.score[tid]);
   }
   __syncthreads();
-  // whether list l has candidate c (n: its length), and in `high` and `low` what its score is between
-  const auto look = [&](int l, const uint2& c, int n, float& high, float& low) {
+  // in `high` and `low` what the score of candidate c of list l is between, if it has one there
+  const auto look = [&](int l, const uint2& c, float& high, float& low) {
     const int r = row_of(l);
     const Quick w = quick_at(r);
-    const bool ended = w.size < 0.f;
-    if (ended ? at != 0 || l != (r - r0) * a.pieces : at >= n) return;
-    const float y = ended ? w.bias : w.bias + __uint_as_float(c.x), e = ended ? 0.f : 0x1p-21f * (fabsf(y) + w.size);
+    float y = w.bias + __uint_as_float(c.x), e = 0x1p-21f * (fabsf(y) + w.size);
+    if (w.size < 0.f) {
+      if (at != 0 || l != (r - r0) * a.pieces) return;
+      y = w.bias, e = 0.f;
+    }
     high = y + e, low = fmaxf(low, y - e);   // (a NaN is passed over)
   };
   float hi[kHold];   // of a round's candidates: not above it
@@ -781,11 +785,11 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
       if (l0 + q0 * at_once >= lists) continue;
       if (l0 || q0) {
 #pragma unroll
-        for (int q = 0; q < kBatch; ++q) fetch(l0 + (q0 + q) * at_once + my_list, c[q], cn[q]);
+        for (int q = 0; q < kBatch; ++q) c[q] = fetch(l0 + (q0 + q) * at_once + my_list);
       }
 #pragma unroll
       for (int q = 0; q < kBatch; ++q)
-        if (l0 + (q0 + q) * at_once + my_list < lists) look(l0 + (q0 + q) * at_once + my_list, c[q], cn[q], hi[q0 + q], g);
+        if (l0 + (q0 + q) * at_once + my_list < lists) look(l0 + (q0 + q) * at_once + my_list, c[q], hi[q0 + q], g);
     }
   };
   const int per_round = kHold * at_once;
@@ -794,9 +798,7 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
   const uint32_t group[1] = {key_of(g)}, bound = threshold_of<1, kRankThreads / 32>(group, a.W, a.W + a.W / 8, sh.scratch);
   float from = bound ? value_of(bound) : -INFINITY;
   const auto put = [&](int l) {
-    uint2 x;
-    int n;
-    fetch(l, x, n);
+    uint2 x = fetch(l);
     const int r = row_of(l);
     const Row& w = row_at(r);
     if (w.final >= 0) x = make_uint2(0u, (uint32_t)w.final);
@@ -810,7 +812,7 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
   for (int l0 = 0, turn = 0; l0 < lists; l0 += per_round, turn ^= 1) {
     if (lists > per_round) {
 #pragma unroll
-      for (int q = 0; q < kBatch; ++q) fetch(q * at_once + my_list, c[q], cn[q]);   // (round 0 takes these)
+      for (int q = 0; q < kBatch; ++q) c[q] = fetch(q * at_once + my_list);   // (round 0 takes these)
       round(l0);
     }
     uint32_t hits = 0;
@@ -862,8 +864,9 @@ constexpr int kTile = In<ATSPEED_F32>::TILE;
 // Pieces of a row: up to two CTAs an SM, none shorter than four tiles (of 32-bit logits, whatever the type).  Each costs a bound and more
 // candidates to rank.  us for 1 / 2 / 4 / 9 / 17 pieces of 33024 logits: 10 rows 12.4 / 11.1 / 10.6 / 10.3 / 11.2, 16 rows 13.2 / 11.5 /
 // 11.4 / 12.1 / 12.5, 320 rows 15.9 / 16.0 / 20.2 / 25.6 / 43, 3840 rows 100 / 112 / 155 / 357 / 580.
+static_assert(kManyPieces <= kRankThreads, "a thread a row of several pieces");
 int pieces_of(int R, int V) {
-  const long long tiles = (V + kTile - 1LL) / kTile, most = std::max(1LL, std::min((tiles + 3) / 4, 304LL / R));
+  const long long tiles = (V + kTile - 1LL) / kTile, most = std::max(1LL, std::min((tiles + 3) / 4, (long long)kMostCtas / R));
   const long long span = (tiles + most - 1) / most;
   return (int)((tiles + span - 1) / span);
 }

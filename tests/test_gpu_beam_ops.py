@@ -133,7 +133,7 @@ def test_select_strides(ats, dtype, pitch, lead):
     _check_select(ats, _logits(7, 9, V, dtype, pitch=pitch, lead=lead), [4, 5], 33, score=np.linspace(-1, -3, 9))
 
 
-@pytest.mark.parametrize("R,V,width", [(1, 33024, 40), (1, 200003, 256), (700, 5000, 17), (1300, 700, 8)])
+@pytest.mark.parametrize("R,V,width", [(1, 33024, 40), (1, 200003, 256), (1, 300007, 30), (101, 40000, 12), (150, 40001, 12), (700, 5000, 17), (2600, 700, 8)])
 def test_select_one_piece_and_many(ats, R, V, width):
     counts = [R] if R == 1 else [R // 4, 1, R - R // 4 - 1]
     _check_select(ats, _logits(R, R, V, torch.float32), counts, width, score=-np.random.default_rng(R).exponential(2.0, R))
