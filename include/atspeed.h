@@ -456,13 +456,27 @@ atspeed_status atspeed_op_adjust_logits(atspeed_stream stream, const void *d_log
  * the larger logit, then the lower token.  A score of -infinity (in 32 bits) or NaN is never chosen.
  * Outputs [n_req][width], best first: d_token, d_parent (the row), d_out_score (rounded to 32 bits); places without a
  * continuation hold -1, -1, -infinity.  Rows of no request do not count.
- * width 1 .. 256, vocab up to 2^30 (ATSPEED_E_SHAPE).  d_ws: atspeed_op_beam_select_workspace(R, vocab, width) bytes, 16-byte aligned, whatever they
- * hold, of this call alone until it is done. */
+ * width 1 .. 256, vocab up to 2^30 (ATSPEED_E_SHAPE). */
+typedef struct {
+  const void *d_logits;
+  int64_t ld;
+  atspeed_dtype type;
+  int R, vocab, n_req, width;
+  atspeed_norm_mode norm;
+  const int32_t *d_cu_beam;
+  const float *d_score;
+  const int32_t *d_final, *d_state;
+  const uint32_t *d_grammar;
+  int64_t grammar_stride; /* words */
+  int n_states;
+  int32_t *d_token, *d_parent;
+  float *d_out_score;
+} atspeed_beams;
+
+/* d_ws: atspeed_op_beam_select_workspace(R, vocab, width) bytes, 16-byte aligned, whatever they hold, of this call alone until it is
+ * done. */
 size_t atspeed_op_beam_select_workspace(int R, int vocab, int width);
-atspeed_status atspeed_op_beam_select(atspeed_stream stream, const void *d_logits, atspeed_dtype type, int64_t ld, int R, int vocab,
-                                      const float *d_score, const int32_t *d_final, int n_req, const int32_t *d_cu_beam, int width,
-                                      const int32_t *d_state, const uint32_t *d_grammar, int64_t grammar_stride, int n_states,
-                                      atspeed_norm_mode norm, int32_t *d_token, int32_t *d_parent, float *d_out_score, void *d_ws);
+atspeed_status atspeed_op_beam_select(atspeed_stream stream, const atspeed_beams *beams, void *d_ws);
 
 /* New rows of block tables from old ones: beams go on from their parents, ended or rejected ones give their pages back.
  * Page counts: d_ref[page] is the number of rows (and of whatever else the caller counts) that hold a page; 0: free.
@@ -483,12 +497,12 @@ atspeed_status atspeed_op_beam_select(atspeed_stream stream, const void *d_logit
  * d_dst [n_new] pages to copy from and to, -1: none;  d_new_ref [n_pages];  d_new_free [n_pages], *d_new_n_free: the pages
  * whose new count is 0 or less, ascending, -1 behind them.
  * Entries outside [0, n_pages) are handed on, not counted, not copied.  n_old, n_new <= 16384, n_pages <= 2^26 (ATSPEED_E_SHAPE). */
-atspeed_status atspeed_op_fork_pages(atspeed_stream stream, int n_old, int n_new, const int32_t *d_table, int table_width,
-                                     int page_size, const int32_t *d_kv_len, const int32_t *d_q_len, const int32_t *d_old_state,
-                                     const int32_t *d_parent, const int32_t *d_length, int n_pages, const int32_t *d_ref,
-                                     const int32_t *d_free, const int32_t *d_n_free, const int32_t *d_used, int32_t *d_new_table,
-                                     int32_t *d_new_len, int32_t *d_new_state, int32_t *d_src, int32_t *d_dst, int32_t *d_new_ref,
-                                     int32_t *d_new_free, int32_t *d_new_n_free);
+typedef struct {
+  int n_old, n_new, table_width, page_size, n_pages;
+  const int32_t *d_table, *d_kv_len, *d_q_len, *d_old_state, *d_parent, *d_length, *d_ref, *d_free, *d_n_free, *d_used;
+  int32_t *d_new_table, *d_new_len, *d_new_state, *d_src, *d_dst, *d_new_ref, *d_new_free, *d_new_n_free;
+} atspeed_page_fork;
+atspeed_status atspeed_op_fork_pages(atspeed_stream stream, const atspeed_page_fork *fork);
 
 /* Copies pages of n_layers caches of one geometry (types, sizes and strides as the first one's; ATSPEED_E_ARG otherwise): for each
  * j < n with d_src[j], d_dst[j] both pages of the cache, the first ((d_length[j] - 1) mod page_size) + 1 tokens (d_length NULL:

@@ -84,6 +84,24 @@ class LogitRulesDesc(ctypes.Structure):
                                                      ("d_tree_tok", ctypes.c_void_p), ("d_cu_q", ctypes.c_void_p)]
 
 
+class BeamsDesc(ctypes.Structure):
+    _fields_ = [("d_logits", ctypes.c_void_p), ("ld", ctypes.c_int64), ("type", ctypes.c_int), ("R", ctypes.c_int), ("vocab", ctypes.c_int),
+                ("n_req", ctypes.c_int), ("width", ctypes.c_int), ("norm", ctypes.c_int), ("d_cu_beam", ctypes.c_void_p),
+                ("d_score", ctypes.c_void_p), ("d_final", ctypes.c_void_p), ("d_state", ctypes.c_void_p), ("d_grammar", ctypes.c_void_p),
+                ("grammar_stride", ctypes.c_int64), ("n_states", ctypes.c_int), ("d_token", ctypes.c_void_p),
+                ("d_parent", ctypes.c_void_p), ("d_out_score", ctypes.c_void_p)]
+
+
+class PageForkDesc(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int) for f in ("n_old", "n_new", "table_width", "page_size", "n_pages")] + [(f, ctypes.c_void_p) for f in (
+        "d_table", "d_kv_len", "d_q_len", "d_old_state", "d_parent", "d_length", "d_ref", "d_free", "d_n_free", "d_used", "d_new_table",
+        "d_new_len", "d_new_state", "d_src", "d_dst", "d_new_ref", "d_new_free", "d_new_n_free")]
+
+
+# (packed whole and passed by address: as arguments of their own the fields of a fork take 2 us more)
+_BEAMS_PACK, _FORK_PACK = struct.Struct("@PqiiiiiiPPPPPqiPPP").pack, struct.Struct("@iiiii18P").pack
+assert struct.calcsize("@PqiiiiiiPPPPPqiPPP") == ctypes.sizeof(BeamsDesc) and struct.calcsize("@iiiii18P") == ctypes.sizeof(PageForkDesc)
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -139,10 +157,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "atspeed_op_adjust_logits": (c_int, [vp, vp, c_int, ctypes.c_int64, c_int, c_int, vp,
                                              ctypes.POINTER(LogitRulesDesc), vp, c_int, vp, vp, c_int, ctypes.c_int64]),
         "atspeed_op_beam_select_workspace": (ctypes.c_size_t, [c_int, c_int, c_int]),
-        "atspeed_op_beam_select": (c_int, [vp, vp, c_int, ctypes.c_int64, c_int, c_int, vp, vp, c_int, vp, c_int, vp, vp,
-                                           ctypes.c_int64, c_int, c_int, vp, vp, vp, vp]),
-        "atspeed_op_fork_pages": (c_int, [vp, c_int, c_int, vp, c_int, c_int, vp, vp, vp, vp, vp, c_int, vp, vp, vp, vp, vp, vp, vp, vp,
-                                          vp, vp, vp, vp]),
+        "atspeed_op_beam_select": (c_int, [vp, ctypes.c_char_p, vp]),   # (an atspeed_beams and an atspeed_page_fork as bytes)
+        "atspeed_op_fork_pages": (c_int, [vp, ctypes.c_char_p]),
         "atspeed_op_copy_pages": (c_int, [vp, ctypes.POINTER(KvPages), c_int, c_int, vp, vp, vp]),
         "atspeed_op_compact_tokens": (c_int, [vp, ctypes.POINTER(KvPages), c_int, c_int, c_int, vp, vp, vp, vp, vp, c_int, vp, vp]),
     }
@@ -724,17 +740,17 @@ def op_beam_select(logits: torch.Tensor, cu_beam: torch.Tensor, width: int, scor
         _refuse(f"{n} requests, {R} rows of {V}, width {width}, state {'missing' if state is None else 'given'}, grammar "
                 f"{'missing' if grammar is None else tuple(grammar.shape)}")
     lib = load()
-    cu_ptr, score_ptr = _given(cu_beam, i32, 2, "cu_beam", gpu), _tensor(score, f32, R, "score", gpu)
-    final_ptr, state_ptr = _tensor(final, i32, R, "final", gpu), _tensor(state, i32, R, "state", gpu)
-    words, states, grammar_ptr = 0, 0, None
+    cu_ptr, score_ptr = _given(cu_beam, i32, 2, "cu_beam", gpu), _tensor(score, f32, R, "score", gpu) or 0
+    final_ptr, state_ptr = _tensor(final, i32, R, "final", gpu) or 0, _tensor(state, i32, R, "state", gpu) or 0
+    words, states, grammar_ptr = 0, 0, 0
     if grammar is not None:
         states, words = grammar.shape
         grammar_ptr = _tensor(grammar, i32, 1, "grammar", gpu)
     token, parent, out, ws = _outputs(dev, stream, ((n, width), i32), ((n, width), i32), ((n, width), f32),
                                       ((lib.atspeed_op_beam_select_workspace(R, V, width),), torch.uint8))
-    _check(lib.atspeed_op_beam_select(_raw_stream(stream, dev), logits.data_ptr(), it, _pitch(logits, V), R, V, score_ptr, final_ptr,
-                                      n, cu_ptr, width, state_ptr, grammar_ptr, words, states, norm, token.data_ptr(),
-                                      parent.data_ptr(), out.data_ptr(), ws.data_ptr()))
+    beams = _BEAMS_PACK(logits.data_ptr(), _pitch(logits, V), it, R, V, n, width, norm, cu_ptr, score_ptr, final_ptr, state_ptr, grammar_ptr,
+                        words, states, token.data_ptr(), parent.data_ptr(), out.data_ptr())
+    _check(lib.atspeed_op_beam_select(_raw_stream(stream, dev), beams, ws.data_ptr()))
     return BeamChoice(token, parent, out)
 
 
@@ -764,12 +780,12 @@ def op_fork_pages(table: torch.Tensor, kv_len: torch.Tensor, ref: torch.Tensor, 
     if table.dim() != 2 or table.shape[0] != n or n < 1 or pages < 1 or (parent is None and length is not None and length.numel() != n):
         _refuse(f"{n} rows, table {tuple(table.shape)}, {pages} pages, {'no parents' if parent is None else parent.numel()}")
     m, width = n if parent is None else parent.numel(), table.shape[1]
-    ins = (_given(table, i32, n, "table", gpu), width, page_size, _given(kv_len, i32, n, "kv_len", gpu), _tensor(q_len, i32, n, "q_len", gpu),
-           _tensor(state, i32, n, "state", gpu), _tensor(parent, i32, 1, "parent", gpu), _tensor(length, i32, m, "length", gpu), pages,
-           _given(ref, i32, pages, "ref", gpu))
     n_free_ptr = _given(n_free, i32, 1, "n_free", gpu)
-    free_ptr = _given(free, i32, 0, "free", gpu) if free.numel() else n_free_ptr   # (n_free is 0: nothing is read of it)
-    used_ptr = _tensor(used, i32, 1, "used", gpu)
+    ins = (_given(table, i32, n, "table", gpu), _given(kv_len, i32, n, "kv_len", gpu), _tensor(q_len, i32, n, "q_len", gpu) or 0,
+           _tensor(state, i32, n, "state", gpu) or 0, _tensor(parent, i32, 1, "parent", gpu) or 0, _tensor(length, i32, m, "length", gpu) or 0,
+           _given(ref, i32, pages, "ref", gpu),
+           _given(free, i32, 0, "free", gpu) if free.numel() else n_free_ptr,   # (n_free is 0: nothing is read of it)
+           n_free_ptr, _tensor(used, i32, 1, "used", gpu) or 0)
     if out is None:   # (one tensor and views of it, the counts at its start: eight tensors take longer)
         cells = m * width
         whole, = _outputs(dev, stream, ((2 * pages + cells + 4 * m + 1,), i32))
@@ -782,7 +798,7 @@ def op_fork_pages(table: torch.Tensor, kv_len: torch.Tensor, ref: torch.Tensor, 
             _refuse(f"out.table: [{m}][{width}], not {tuple(out.table.shape)}")
         sizes = (m * width, m, m, m, m, pages, pages, 1)
         outs = [_given(getattr(out, k), i32, size, "out." + k, gpu) for k, size in zip(PageFork.__slots__, sizes)]
-    _check(load().atspeed_op_fork_pages(_raw_stream(stream, dev), n, m, *ins, free_ptr, n_free_ptr, used_ptr, *outs))
+    _check(load().atspeed_op_fork_pages(_raw_stream(stream, dev), _FORK_PACK(n, m, width, page_size, pages, *ins, *outs)))
     return out
 
 

@@ -900,33 +900,31 @@ extern "C" size_t atspeed_op_beam_select_workspace(int R, int vocab, int width) 
   return R > 0 && vocab > 0 && width > 0 ? layout_of(R, vocab, std::min(width, kMaxWidth)).bytes : 0;
 }
 
-extern "C" atspeed_status atspeed_op_beam_select(atspeed_stream stream, const void* d_logits, atspeed_dtype type, int64_t ld, int R,
-                                                 int vocab, const float* d_score, const int32_t* d_final, int n_req,
-                                                 const int32_t* d_cu_beam, int width, const int32_t* d_state,
-                                                 const uint32_t* d_grammar, int64_t grammar_stride, int n_states,
-                                                 atspeed_norm_mode norm, int32_t* d_token, int32_t* d_parent,
-                                                 float* d_out_score, void* d_ws) {
-  if (!d_logits || !d_cu_beam || !d_token || !d_parent || !d_out_score || !d_ws || R <= 0 || vocab <= 0 || n_req <= 0 || width <= 0 ||
-      ld < vocab || !dtype_size(type) || reinterpret_cast<uintptr_t>(d_logits) % dtype_size(type) || !aligned16(d_ws) ||
-      (norm != ATSPEED_NORM_MASKED && norm != ATSPEED_NORM_FULL) ||
-      (d_state && (!d_grammar || n_states <= 0 || grammar_stride < (vocab + 31LL) / 32)))
+extern "C" atspeed_status atspeed_op_beam_select(atspeed_stream stream, const atspeed_beams* beams, void* d_ws) {
+  if (!beams) return ATSPEED_E_ARG;
+  const atspeed_beams& s = *beams;
+  const int R = s.R, vocab = s.vocab, width = s.width;
+  if (!s.d_logits || !s.d_cu_beam || !s.d_token || !s.d_parent || !s.d_out_score || !d_ws || R <= 0 || vocab <= 0 || s.n_req <= 0 ||
+      width <= 0 || s.ld < vocab || !dtype_size(s.type) || reinterpret_cast<uintptr_t>(s.d_logits) % dtype_size(s.type) ||
+      !aligned16(d_ws) || (s.norm != ATSPEED_NORM_MASKED && s.norm != ATSPEED_NORM_FULL) ||
+      (s.d_state && (!s.d_grammar || s.n_states <= 0 || s.grammar_stride < (vocab + 31LL) / 32)))
     return ATSPEED_E_ARG;
   const Layout l = layout_of(R, vocab, std::min(width, kMaxWidth));
   if (width > kMaxWidth || vocab > 1 << 30 || (long long)R * l.pieces > 0x7fffffffLL) return ATSPEED_E_SHAPE;
   SelectArgs a = {};
-  a.logits = d_logits, a.ld = ld, a.R = R, a.V = vocab, a.n_req = n_req, a.W = width, a.pieces = l.pieces, a.cap = cap_of(width);
+  a.logits = s.d_logits, a.ld = s.ld, a.R = R, a.V = vocab, a.n_req = s.n_req, a.W = width, a.pieces = l.pieces, a.cap = cap_of(width);
   a.span = (int)(((vocab + (long long)l.pieces - 1) / l.pieces + kTile - 1) / kTile * kTile);
-  a.score = d_score, a.final = d_final, a.cu = d_cu_beam, a.state = d_state, a.grammar = d_grammar;
-  a.grammar_stride = grammar_stride, a.n_states = d_state ? n_states : 0, a.full = norm == ATSPEED_NORM_FULL;
+  a.score = s.d_score, a.final = s.d_final, a.cu = s.d_cu_beam, a.state = s.d_state, a.grammar = s.d_grammar;
+  a.grammar_stride = s.grammar_stride, a.n_states = s.d_state ? s.n_states : 0, a.full = s.norm == ATSPEED_NORM_FULL;
   a.per_piece = l.pieces > 1 ? (uint32_t)((0x100000000ll + l.pieces - 1) / l.pieces) : 0u;
-  a.token = d_token, a.parent = d_parent, a.out_score = d_out_score;
+  a.token = s.d_token, a.parent = s.d_parent, a.out_score = s.d_out_score;
   char* ws = static_cast<char*>(d_ws);
   a.head = reinterpret_cast<Header*>(ws), a.cand = reinterpret_cast<uint2*>(ws + l.cand);
   a.rows = reinterpret_cast<Row*>(ws + l.rows), a.quick = reinterpret_cast<Quick*>(ws + l.quick);
   static std::atomic<unsigned long long> done{0};
   if (smem_attr_once(done, beam_rank_kernel, (int)sizeof(RankShared)) != cudaSuccess) return ATSPEED_E_CUDA;
   const int grid = R * l.pieces;
-  const bool aligned = aligned16(d_logits) && ld * dtype_size(type) % 16 == 0;
+  const bool aligned = aligned16(s.d_logits) && s.ld * dtype_size(s.type) % 16 == 0;
   static std::atomic<unsigned long long> ready[6];
   const auto go = [&](auto kernel, int i) {
     if (smem_attr_once(ready[i], kernel, (int)sizeof(PieceShared)) != cudaSuccess) return ATSPEED_E_CUDA;
@@ -934,14 +932,14 @@ extern "C" atspeed_status atspeed_op_beam_select(atspeed_stream stream, const vo
     return launch_status();
   };
   const atspeed_status launched =
-      type == ATSPEED_F32    ? aligned ? go(beam_pieces_kernel<ATSPEED_F32, true>, 0) : go(beam_pieces_kernel<ATSPEED_F32, false>, 1)
-      : type == ATSPEED_BF16 ? aligned ? go(beam_pieces_kernel<ATSPEED_BF16, true>, 2) : go(beam_pieces_kernel<ATSPEED_BF16, false>, 3)
-      : aligned              ? go(beam_pieces_kernel<ATSPEED_F16, true>, 4)
-                             : go(beam_pieces_kernel<ATSPEED_F16, false>, 5);
+      s.type == ATSPEED_F32    ? aligned ? go(beam_pieces_kernel<ATSPEED_F32, true>, 0) : go(beam_pieces_kernel<ATSPEED_F32, false>, 1)
+      : s.type == ATSPEED_BF16 ? aligned ? go(beam_pieces_kernel<ATSPEED_BF16, true>, 2) : go(beam_pieces_kernel<ATSPEED_BF16, false>, 3)
+      : aligned                ? go(beam_pieces_kernel<ATSPEED_F16, true>, 4)
+                               : go(beam_pieces_kernel<ATSPEED_F16, false>, 5);
   if (launched != ATSPEED_OK) return launched;
   // (it may start while the last of the pieces are read, and waits for them)
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n_req), cfg.blockDim = dim3(kRankThreads), cfg.dynamicSmemBytes = sizeof(RankShared), cfg.stream = (cudaStream_t)stream;
+  cfg.gridDim = dim3(s.n_req), cfg.blockDim = dim3(kRankThreads), cfg.dynamicSmemBytes = sizeof(RankShared), cfg.stream = (cudaStream_t)stream;
   cudaLaunchAttribute attr = {};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;

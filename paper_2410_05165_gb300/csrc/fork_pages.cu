@@ -273,21 +273,20 @@ __global__ void __launch_bounds__(kThreads, 1) fork_pages_kernel(const __grid_co
 
 using namespace atspeed;
 
-extern "C" atspeed_status atspeed_op_fork_pages(atspeed_stream stream, int n_old, int n_new, const int32_t* d_table, int table_width,
-                                                int page_size, const int32_t* d_kv_len, const int32_t* d_q_len,
-                                                const int32_t* d_old_state, const int32_t* d_parent, const int32_t* d_length,
-                                                int n_pages, const int32_t* d_ref, const int32_t* d_free,
-                                                const int32_t* d_n_free, const int32_t* d_used, int32_t* d_new_table,
-                                                int32_t* d_new_len, int32_t* d_new_state, int32_t* d_src, int32_t* d_dst,
-                                                int32_t* d_new_ref, int32_t* d_new_free, int32_t* d_new_n_free) {
-  if (!d_table || !d_kv_len || !d_ref || !d_free || !d_n_free || !d_new_table || !d_new_len || !d_new_state || !d_src || !d_dst ||
-      !d_new_ref || !d_new_free || !d_new_n_free || n_old <= 0 || n_new <= 0 || table_width <= 0 || page_size <= 0 || n_pages <= 0)
+extern "C" atspeed_status atspeed_op_fork_pages(atspeed_stream stream, const atspeed_page_fork* fork) {
+  if (!fork) return ATSPEED_E_ARG;
+  const atspeed_page_fork& f = *fork;
+  const int n_old = f.n_old, n_new = f.n_new, n_pages = f.n_pages, table_width = f.table_width;
+  if (!f.d_table || !f.d_kv_len || !f.d_ref || !f.d_free || !f.d_n_free || !f.d_new_table || !f.d_new_len || !f.d_new_state || !f.d_src ||
+      !f.d_dst || !f.d_new_ref || !f.d_new_free || !f.d_new_n_free || n_old <= 0 || n_new <= 0 || table_width <= 0 || f.page_size <= 0 ||
+      n_pages <= 0)
     return ATSPEED_E_ARG;
-  if ((!d_parent && n_old != n_new) || d_new_table == d_table || d_new_ref == d_ref || d_new_free == d_free) return ATSPEED_E_ARG;
+  if ((!f.d_parent && n_old != n_new) || f.d_new_table == f.d_table || f.d_new_ref == f.d_ref || f.d_new_free == f.d_free) return ATSPEED_E_ARG;
   if (n_old > kMaxRequests || n_new > kMaxRequests || n_pages > kMaxPages) return ATSPEED_E_SHAPE;
-  const ForkArgs a = {n_old,  n_new,  table_width, page_size,   n_pages,   aligned16(d_ref) && aligned16(d_new_ref), d_table,   d_kv_len, d_q_len, d_old_state, d_parent,  d_length,
-                      d_ref,  d_free, d_n_free,    d_used,      d_new_table, d_new_len, d_new_state, d_src, d_dst, d_new_ref, d_new_free,
-                      d_new_n_free};
+  const ForkArgs a = {n_old,     n_new,        table_width, f.page_size,   n_pages,       aligned16(f.d_ref) && aligned16(f.d_new_ref),
+                      f.d_table, f.d_kv_len,   f.d_q_len,   f.d_old_state, f.d_parent,    f.d_length, f.d_ref,
+                      f.d_free,  f.d_n_free,   f.d_used,    f.d_new_table, f.d_new_len,   f.d_new_state, f.d_src,
+                      f.d_dst,   f.d_new_ref,  f.d_new_free, f.d_new_n_free};
   const int smem = n_old * (int)sizeof(unsigned long long) + n_new * (int)sizeof(int);
   // Rows by as many CTAs as there is work for, up to the SMs that are left.  One CTA makes the counts of few pages and rows.
   const long long warps = (long long)n_new * ((table_width + kPiece - 1) / kPiece);

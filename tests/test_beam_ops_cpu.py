@@ -20,10 +20,13 @@ def lib():
 
 
 def _select(lib, **kw):
-    d = dict(stream=None, logits=P, type=0, ld=100, R=3, V=100, score=P, final=None, n=2, cu=P, width=10, state=None, grammar=None,
-             stride=0, n_states=0, norm=0, token=P, parent=P, out=P, ws=P)
-    d.update(kw)
-    return lib.atspeed_op_beam_select(*d.values())
+    from paper_2410_05165_gb300.binding import BeamsDesc
+    d = dict(d_logits=P, ld=100, type=0, R=3, vocab=100, n_req=2, width=10, norm=0, d_cu_beam=P, d_score=P, d_token=P, d_parent=P, d_out_score=P)
+    names = dict(logits="d_logits", V="vocab", n="n_req", cu="d_cu_beam", state="d_state", grammar="d_grammar", stride="grammar_stride",
+                 token="d_token", parent="d_parent", out="d_out_score")
+    ws = kw.pop("ws", P)
+    d.update((names.get(k, k), v) for k, v in kw.items())
+    return lib.atspeed_op_beam_select(None, bytes(BeamsDesc(**d)), ws)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -36,6 +39,10 @@ def test_beam_select_refuses(lib, kw, status):
     assert _select(lib, **kw) == status
 
 
+def test_null_descriptions_are_refused(lib):
+    assert lib.atspeed_op_beam_select(None, None, P) == E_ARG and lib.atspeed_op_fork_pages(None, None) == E_ARG
+
+
 def test_beam_select_workspace(lib):
     assert lib.atspeed_op_beam_select_workspace(0, 5, 5) == 0 and lib.atspeed_op_beam_select_workspace(5, 5, -1) == 0
     small, large = lib.atspeed_op_beam_select_workspace(1, 1, 1), lib.atspeed_op_beam_select_workspace(1 << 14, 1 << 17, 256)
@@ -43,11 +50,12 @@ def test_beam_select_workspace(lib):
 
 
 def _fork(lib, **kw):
-    d = dict(stream=None, n_old=4, n_new=4, table=P, width=3, page=16, kv=P, q=None, state=None, parent=None, length=None, n_pages=9,
-             ref=P, free=P, n_free=P, used=None, new_table=2 * P, new_len=P, new_state=P, src=P, dst=P, new_ref=2 * P, new_free=2 * P,
-             new_n_free=P)
-    d.update(kw)
-    return lib.atspeed_op_fork_pages(*d.values())
+    from paper_2410_05165_gb300.binding import PageForkDesc
+    d = dict(n_old=4, n_new=4, table_width=3, page_size=16, n_pages=9, d_table=P, d_kv_len=P, d_ref=P, d_free=P, d_n_free=P, d_new_table=2 * P,
+             d_new_len=P, d_new_state=P, d_src=P, d_dst=P, d_new_ref=2 * P, d_new_free=2 * P, d_new_n_free=P)
+    names = dict(width="table_width", page="page_size", kv="d_kv_len")
+    d.update((names.get(k, k if k.startswith("n_") and k != "n_free" else "d_" + k), v) for k, v in kw.items())
+    return lib.atspeed_op_fork_pages(None, bytes(PageForkDesc(**d)))
 
 
 @pytest.mark.parametrize("kw,status", [(dict([(k, None)]), E_ARG) for k in (
