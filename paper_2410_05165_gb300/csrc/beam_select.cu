@@ -1,7 +1,7 @@
 // Beam search's selection over beams and vocabulary (atspeed_op_beam_select).
 //   score(r, v) = cum_r + ((x_rv - m_r) - log s_r),  m_r = max x_r,  s_r = sum_v exp(x_rv - m_r);  the best W of a request's rows
 // Bound: HBM (each logit read once).  3840 rows of 33024 (32 bits, W = 80) take 99 us, 5.1 TB/s: 75 of them the logits alone (a copy's rate), 3
-// the bounds, 10 the second reads, 10 the ranking.  732 rows of 100003 (bf16, at odd addresses, W = 32) 38 us, 3.9 TB/s, where
+// the bounds, 10 the second reads, 10 the ranking.  738 rows of 100003 (bf16, at odd addresses, W = 32) 38 us, 3.9 TB/s, where
 // unpacking and exponentials take as long as the bytes.  Ten rows of 33024 11 us: latency, half of it the ranking's.
 //
 // Two launches.  The first reads the logits, a CTA a piece of a row: the piece's maximum, its sum of exponentials and the

@@ -281,7 +281,9 @@ extern "C" atspeed_status atspeed_op_fork_pages(atspeed_stream stream, const ats
       !f.d_dst || !f.d_new_ref || !f.d_new_free || !f.d_new_n_free || n_old <= 0 || n_new <= 0 || table_width <= 0 || f.page_size <= 0 ||
       n_pages <= 0)
     return ATSPEED_E_ARG;
-  if ((!f.d_parent && n_old != n_new) || f.d_new_table == f.d_table || f.d_new_ref == f.d_ref || f.d_new_free == f.d_free) return ATSPEED_E_ARG;
+  if ((!f.d_parent && n_old != n_new) || f.d_new_table == f.d_table || f.d_new_ref == f.d_ref || f.d_new_free == f.d_free ||
+      f.d_new_len == f.d_kv_len || f.d_new_len == f.d_length || f.d_new_state == f.d_old_state || f.d_new_n_free == f.d_n_free)
+    return ATSPEED_E_ARG;
   if (n_old > kMaxRequests || n_new > kMaxRequests || n_pages > kMaxPages) return ATSPEED_E_SHAPE;
   const ForkArgs a = {n_old,     n_new,        table_width, f.page_size,   n_pages,       aligned16(f.d_ref) && aligned16(f.d_new_ref),
                       f.d_table, f.d_kv_len,   f.d_q_len,   f.d_old_state, f.d_parent,    f.d_length, f.d_ref,

@@ -52,7 +52,7 @@ def test_beam_select_workspace(lib):
 def _fork(lib, **kw):
     from paper_2410_05165_gb300.binding import PageForkDesc
     d = dict(n_old=4, n_new=4, table_width=3, page_size=16, n_pages=9, d_table=P, d_kv_len=P, d_ref=P, d_free=P, d_n_free=P, d_new_table=2 * P,
-             d_new_len=P, d_new_state=P, d_src=P, d_dst=P, d_new_ref=2 * P, d_new_free=2 * P, d_new_n_free=P)
+             d_new_len=2 * P, d_new_state=2 * P, d_src=P, d_dst=P, d_new_ref=2 * P, d_new_free=2 * P, d_new_n_free=2 * P)
     names = dict(width="table_width", page="page_size", kv="d_kv_len")
     d.update((names.get(k, k if k.startswith("n_") and k != "n_free" else "d_" + k), v) for k, v in kw.items())
     return lib.atspeed_op_fork_pages(None, bytes(PageForkDesc(**d)))
@@ -61,7 +61,8 @@ def _fork(lib, **kw):
 @pytest.mark.parametrize("kw,status", [(dict([(k, None)]), E_ARG) for k in (
     "table", "kv", "ref", "free", "n_free", "new_table", "new_len", "new_state", "src", "dst", "new_ref", "new_free", "new_n_free")] + [
     (dict(n_old=0), E_ARG), (dict(n_new=0), E_ARG), (dict(width=0), E_ARG), (dict(page=0), E_ARG), (dict(n_pages=0), E_ARG),
-    (dict(n_new=5), E_ARG), (dict(new_table=P), E_ARG), (dict(new_ref=P), E_ARG), (dict(new_free=P), E_ARG),
+    (dict(n_new=5), E_ARG), (dict(new_table=P), E_ARG), (dict(new_ref=P), E_ARG), (dict(new_free=P), E_ARG), (dict(new_len=P), E_ARG),
+    (dict(new_n_free=P), E_ARG), (dict(old_state=2 * P), E_ARG), (dict(length=2 * P), E_ARG),
     (dict(n_old=16385, parent=P), E_SHAPE), (dict(n_new=16385, parent=P), E_SHAPE), (dict(n_pages=(1 << 26) + 1), E_SHAPE)])
 def test_fork_pages_refuses(lib, kw, status):
     assert _fork(lib, **kw) == status

@@ -288,6 +288,28 @@ def test_select_leaves_other_rows(ats):
     _check_select(ats, logits, [3, 3], 7, first=2)
 
 
+def test_select_past_2_31_logits(ats):
+    """66 000 rows of 33 001: two requests of 33 000 beams, whose best continuations lie in the last rows."""
+    R, V = 66000, 33001
+    logits = torch.zeros(R, V, dtype=torch.bfloat16, device="cuda")
+    assert logits.numel() > 2 ** 31
+    score = np.full(R, -100.0, np.float32)
+    want = [[], []]
+    for b, (first, step) in enumerate(((32990, 1), (65999, -1))):
+        for i in range(10):
+            r, v = first + i * step, V - 1 - 7 * i
+            logits[r, v] = 8.0
+            score[r] = -1.0 - i
+            # (the rows' log-sums are the same; a row's other tokens, the first ten of them, have equal scores)
+            want[b] += [(-1.0 - i + 8.0, r, v, 8.0)] + [(-1.0 - i, r, t, 0.0) for t in range(10)]
+    got = ats.op_beam_select(logits, _dev([0, 33000, 66000]), 10, score=_dev(score, torch.float32))
+    lse = np.log(V - 1 + np.exp(8.0))
+    for b in range(2):
+        best = sorted(want[b], key=lambda c: (-c[0], c[1], -c[3], c[2]))[:10]
+        assert list(zip(got.parent[b].tolist(), got.token[b].tolist())) == [c[1:3] for c in best]
+        assert np.abs(got.score[b].double().cpu().numpy() - [c[0] - lse for c in best]).max() <= _tolerance(V) + 16 * 2.0 ** -24
+
+
 def test_select_on_streams_and_in_graphs(ats):
     a, b = _logits(1, 20, 33024, torch.float32), _logits(2, 20, 33024, torch.float32)
     cu = _dev([0, 10, 20])
@@ -468,6 +490,14 @@ def test_fork_free_list_of_any_pool(ats, n_pages):
     _check_fork(ats, np.array([[-1]], np.int32), np.array([0]), ref, free, len(free), 16)
 
 
+def test_fork_of_more_pages_handed_out_than_there_are(ats):
+    """A count of pages taken that is past the free list's end or below 0."""
+    table, ref, free = _dev([[0, 1]]), _dev([1, 1, 0, 0, 0]), _dev([2, 3, 4])
+    for used, left in ((-7, [2, 3, 4]), (99, [])):
+        f = ats.op_fork_pages(table, _dev([20]), ref, free, _dev([3]), 16, used=_dev([used]))
+        assert f.ref.tolist() == [1, 1] + [0 if left else 1] * 3 and f.free.tolist()[:int(f.n_free)] == left
+
+
 def test_fork_without_a_free_page(ats):
     table, ref = np.array([[0, 1]], np.int32), np.array([1, 1], np.int32)
     _check_fork(ats, table, np.array([20]), ref, np.zeros(0, np.int32), 0, 16, parent=np.array([0, 0]))
@@ -506,7 +536,6 @@ def test_plan_and_fork_keep_the_pages(ats, page):
     cache = torch.full((n_pages * page,), -1, dtype=torch.int64, device="cuda")   # a token's number in its cache row
     said = [[] for _ in range(n)]
     number = 0
-    layers = None
     for step in range(25):
         q = rng.integers(5, 20, size=n) if step == 0 else rng.integers(0, 3, size=n)
         if step == 0:
@@ -546,7 +575,6 @@ def test_plan_and_fork_keep_the_pages(ats, page):
         np.testing.assert_array_equal(ref.cpu().numpy(), holds)
         assert int(n_free) == (holds == 0).sum()
         np.testing.assert_array_equal(free.cpu().numpy()[:int(n_free)], np.nonzero(holds == 0)[0])
-    assert layers is None
 
 
 # ---------------------------------------------------------------------------------------------------
@@ -605,6 +633,23 @@ def test_copy_pages(ats, layout, layers, page, heads, hd, types):
         for p, q in zip(mine, want):
             for x, y in zip(p, q):
                 assert torch.equal(_whole(x).view(torch.int16), _whole(y).view(torch.int16))
+
+
+@pytest.mark.parametrize("n", [255, 256, 257, 1000])
+def test_copy_many_pages(ats, n):
+    """More pairs than a CTA lists at a time, most of them none."""
+    rng = np.random.default_rng(n)
+    order = rng.permutation(2 * n)
+    src, dst = order[:n].copy(), order[n:].copy()
+    src[rng.random(n) < 0.6] = -1
+    length = rng.integers(0, 50, size=n)
+    mine = _layers(4, 2, 2 * n, 7, 2, 16, MIXED, "token")
+    want = [tuple(t.clone() for t in p) for p in mine]
+    _copied(want, src, dst, np.where(length > 0, (length - 1) % 7 + 1, 0), 2 * n)
+    ats.op_copy_pages(ats.CacheLayers(mine), _dev(src), _dev(dst), length=_dev(length))
+    for p, q in zip(mine, want):
+        for x, y in zip(p, q):
+            assert torch.equal(x.view(torch.int16), y.view(torch.int16))
 
 
 def _compacted(caches, slot, cu, keep, n_keep, ok, page, rows):
