@@ -47,6 +47,8 @@ def _select_reference(x, dtype, cu, width, score, final, allowed, full):
         c = np.concatenate(got, axis=1) if got else np.zeros((4, 0))
         with np.errstate(over="ignore"):
             c = c[:, c[0].astype(np.float32) > NEG]   # (NaN is not)
+        if c.shape[1] > 4 * width:   # (what is well below the last one chosen is not sorted)
+            c = c[:, c[0] >= np.partition(c[0], -width)[-width] - 1e-3]
         order = np.lexsort((c[3], -c[2], c[1], -c[0]))
         out.append(c[:, order])
     return out
@@ -151,6 +153,26 @@ def test_select_grammar(ats, norm, dtype):
     table[4, [0, V - 1]] = True   # (3: nothing)
     state = np.array([-1, 0, 1, 2, 3, 4, 5, 99, 0, 4, 3, 3])
     _check_select(ats, _logits(5, R, V, dtype), [5, 5, 2], 25, score=-rng.exponential(1.0, R), table=table, state=state, norm=norm)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("R,V", [(761, 12289), (1500, 8193), (900, 16385), (2000, 12290)])
+def test_select_more_rows_than_run_at_once(ats, dtype, R, V):
+    """Rows of four tiles and more that CTAs take one after the other: ended beams, states of every kind and rows of no request among
+    them, at the beginning too."""
+    rng = np.random.default_rng(R)
+    logits = _logits(R, R, V, dtype, pitch=R % 3)
+    final = np.where(rng.random(R) < 0.3, rng.integers(0, V, size=R), -1)
+    final[:5] = 3
+    table = rng.random((4, V)) < np.array([0.5, 0.001, 0.0, 1.0])[:, None]
+    state = rng.integers(-1, 6, size=R)
+    first, last = 7, 11
+    counts = [R // 3, 0, 1, R - first - last - R // 3 - 1]
+    logits[:first] = float("nan")
+    logits[R - last:] = float("nan")
+    for kw in (dict(), dict(final=final), dict(final=final, table=table, state=state, norm="full"), dict(table=table, state=state)):
+        _check_select(ats, logits, counts, 15, score=-rng.exponential(2.0, R), first=first, **kw)
+    _check_select(ats, logits, counts, 15, score=-rng.exponential(2.0, R), first=first, final=np.zeros(R, int))   # (every one of them)
 
 
 def test_select_ended_beams(ats):
