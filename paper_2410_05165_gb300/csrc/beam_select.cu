@@ -32,7 +32,6 @@ constexpr int kVec = 4;                     // 16-byte vectors of a thread in a 
 constexpr int kList = 1024;                 // candidates that a piece's list holds
 constexpr int kGroups = kThreads * kVec;
 constexpr int kMaxWidth = 256;
-constexpr int kRankThreads = 1024, kRankList = 2048;
 constexpr uint32_t kNone = 0x007fffffu;     // the key of -infinity
 
 struct Header {   // of a piece
@@ -662,11 +661,15 @@ struct Quick {
 };
 
 constexpr int kMostCtas = 304, kManyPieces = kMostCtas / 3 + 1;   // of the first launch where rows are in pieces; rows of three pieces or more
+// Few candidates (places of a request's lists) are ranked by a CTA of 256, whose barriers and instructions are fewer: ten rows of 33024, W = 10,
+// 11.3 -> 10.8 us, 320 rows 16.5 -> 15.5; 10240 places of 80 beams need the 1024 threads.
+constexpr int kFewPlaces = 4096;
 constexpr int kRows = 256;   // that shared memory holds (of more: device memory)
-struct RankShared {
-  unsigned long long score[kRankList], rest[kRankList];
-  uint32_t tok[kRankList];
-  uint32_t scratch[3 * kRankThreads / 32];
+template <int T>
+struct RankShared {   // of T threads
+  unsigned long long score[2 * T], rest[2 * T];
+  uint32_t tok[2 * T];
+  uint32_t scratch[3 * T / 32];
   float top[kManyPieces];   // rows' maxima, on the way to their logarithms
   Row row[kRows];
   Quick quick[kRows];
@@ -676,11 +679,11 @@ struct RankShared {
 
 // Ranks the list's n entries and hands each that is among the W best to put(rank, entry).  Every thread of the CTA; several threads
 // an entry, neighbours in a warp.
-template <class Put>
-__device__ __forceinline__ void rank_list(const RankShared& sh, int n, int W, Put&& put) {
+template <int T, class Put>
+__device__ __forceinline__ void rank_list(const RankShared<T>& sh, int n, int W, Put&& put) {
   int share = 32;   // threads an entry
-  while (share > 1 && share * n > kRankThreads) share >>= 1;
-  const int per = kRankThreads / share, sub = threadIdx.x & (share - 1), mine = threadIdx.x / share;
+  while (share > 1 && share * n > T) share >>= 1;
+  const int per = T / share, sub = threadIdx.x & (share - 1), mine = threadIdx.x / share;
   for (int j0 = 0; j0 < n; j0 += per) {
     if (j0 + (threadIdx.x & ~31) / share >= n) break;   // (the warp has none)
     const int j = j0 + mine;
@@ -697,9 +700,10 @@ __device__ __forceinline__ void rank_list(const RankShared& sh, int n, int W, Pu
   }
 }
 
-__global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid_constant__ SelectArgs a) {
+template <int T>
+__global__ void __launch_bounds__(T, 1) beam_rank_kernel(const __grid_constant__ SelectArgs a) {
   extern __shared__ __align__(16) unsigned char raw[];
-  RankShared& sh = *reinterpret_cast<RankShared*>(raw);
+  RankShared<T>& sh = *reinterpret_cast<RankShared<T>*>(raw);
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int r0 = max(max(0, __ldg(a.cu)), __ldg(a.cu + b));
   const int r1 = min(min(a.R, __ldg(a.cu + a.n_req)), __ldg(a.cu + b + 1));
@@ -711,7 +715,7 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
   pdl_wait();
   // Candidates: a thread has place `at` of list my_list and of every at_once-th list from there; kHold of them in a round, the
   // first of which are under way while the rows' sums are made.
-  const int at_once = kRankThreads / a.cap, at = tid & (a.cap - 1), my_list = tid / a.cap;
+  const int at_once = T / a.cap, at = tid & (a.cap - 1), my_list = tid / a.cap;
   constexpr int kHold = 16, kBatch = 8;
   const auto fetch = [&](int l) { return l < lists ? a.cand[((long long)r0 * a.pieces + l) * a.cap + at] : make_uint2(0xff800000u, 0u); };
   uint2 c[kBatch];
@@ -724,7 +728,7 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
   // (Sums as multiples of 2^-32, whole numbers: a row's is at least 0.7 and at most 1.5 times its length.)
   const auto whole = [&](float s) { return (unsigned long long)(s * 0x1p32f); };
   const auto set_row = [&](int r, float M, unsigned long long s) {   // r: r0 + tid and every thousandth from there
-    const bool first = r - r0 < kRankThreads, near = fabsf(M) < kFar;
+    const bool first = r - r0 < T, near = fabsf(M) < kFar;
     Row w = {};
     w.cum = first ? my_cum : a.score ? __ldg(a.score + r) : 0.f;
     w.final = first ? my_final : a.final ? __ldg(a.final + r) : -1;
@@ -737,7 +741,7 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
     quick_at(r) = w.final >= 0 ? Quick{w.cum, -1.f} : Quick{w.cum - w.off.hi - w.more.hi, fabsf(w.cum) + fabsf(w.off.hi) + fabsf(w.more.hi)};
   };
   if (a.pieces <= 2) {
-    for (int r = r0 + tid; r < r1; r += kRankThreads) {
+    for (int r = r0 + tid; r < r1; r += T) {
       const Header* h = a.head + (long long)r * a.pieces;
       const float m0 = h[0].m, s0 = h[0].s, m1 = a.pieces > 1 ? h[1].m : -INFINITY, s1 = a.pieces > 1 ? h[1].s : 0.f;
       const float M = fmaxf(m0, m1);
@@ -745,7 +749,7 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
     }
   } else {
     // (rows of three pieces or more are fewer than kManyPieces; their sums wait in the list's place)
-    for (int r = r0 + warp; r < r1; r += kRankThreads / 32) {
+    for (int r = r0 + warp; r < r1; r += T / 32) {
       const Header* h = a.head + (long long)r * a.pieces;
       const float m0 = lane < a.pieces ? h[lane].m : -INFINITY, s0 = lane < a.pieces ? h[lane].s : 0.f;
       float M = m0;
@@ -795,7 +799,7 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
   const int per_round = kHold * at_once;
   for (int l0 = 0; l0 < lists; l0 += per_round) round(l0);
   // what is below `from` is not among the W best: the W-th of the threads' best
-  const uint32_t group[1] = {key_of(g)}, bound = threshold_of<1, kRankThreads / 32>(group, a.W, a.W + a.W / 8, sh.scratch);
+  const uint32_t group[1] = {key_of(g)}, bound = threshold_of<1, T / 32>(group, a.W, a.W + a.W / 8, sh.scratch);
   float from = bound ? value_of(bound) : -INFINITY;
   const auto put = [&](int l) {
     uint2 x = fetch(l);
@@ -823,7 +827,7 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
     __syncthreads();
     const int all = sh.hits[turn], had = sh.n;
     if (tid == 0) sh.hits[turn ^ 1] = 0;
-    if (had + all <= kRankList) {
+    if (had + all <= 2 * T) {
       __syncthreads();   // (everyone knows `had`)
 #pragma unroll 1
       for (; hits; hits &= hits - 1) put(l0 + (__ffs(hits) - 1) * at_once + my_list);
@@ -834,11 +838,11 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
         if (hits >> q & 1) put(l0 + q * at_once + my_list);
         __syncthreads();
         const int n = sh.n;
-        if (n <= kRankList - kRankThreads) continue;
+        if (n <= T) continue;
         rank_list(sh, n, a.W, [&](int r, const Entry& e) { sh.best[r] = e; });
         __syncthreads();
         const int left = min(n, a.W);
-        for (int j = tid; j < left; j += kRankThreads) sh.score[j] = sh.best[j].score, sh.rest[j] = sh.best[j].rest, sh.tok[j] = sh.best[j].tok;
+        for (int j = tid; j < left; j += T) sh.score[j] = sh.best[j].score, sh.rest[j] = sh.best[j].rest, sh.tok[j] = sh.best[j].tok;
         if (tid == 0) sh.n = left;
         if (n >= a.W) from = fmaxf(from, value_of((uint32_t)(sh.best[a.W - 1].score >> 32)));
       }
@@ -853,7 +857,7 @@ __global__ void __launch_bounds__(kRankThreads, 1) beam_rank_kernel(const __grid
     a.parent[o + r] = (int)~(uint32_t)(e.rest >> 32);
     a.out_score[o + r] = value_of((uint32_t)(e.score >> 32));
   });
-  for (int j = n + tid; j < a.W; j += kRankThreads) {
+  for (int j = n + tid; j < a.W; j += T) {
     a.token[o + j] = -1;
     a.parent[o + j] = -1;
     a.out_score[o + j] = -INFINITY;
@@ -864,7 +868,7 @@ constexpr int kTile = In<ATSPEED_F32>::TILE;
 // Pieces of a row: up to two CTAs an SM, none shorter than four tiles (of 32-bit logits, whatever the type).  Each costs a bound and more
 // candidates to rank.  us for 1 / 2 / 4 / 9 / 17 pieces of 33024 logits: 10 rows 12.4 / 11.1 / 10.6 / 10.3 / 11.2, 16 rows 13.2 / 11.5 /
 // 11.4 / 12.1 / 12.5, 320 rows 15.9 / 16.0 / 20.2 / 25.6 / 43, 3840 rows 100 / 112 / 155 / 357 / 580.
-static_assert(kManyPieces <= kRankThreads, "a thread a row of several pieces");
+static_assert(kManyPieces <= 256, "a thread a row of several pieces");
 int pieces_of(int R, int V) {
   const long long tiles = (V + kTile - 1LL) / kTile, most = std::max(1LL, std::min((tiles + 3) / 4, (long long)kMostCtas / R));
   const long long span = (tiles + most - 1) / most;
@@ -921,8 +925,6 @@ extern "C" atspeed_status atspeed_op_beam_select(atspeed_stream stream, const at
   char* ws = static_cast<char*>(d_ws);
   a.head = reinterpret_cast<Header*>(ws), a.cand = reinterpret_cast<uint2*>(ws + l.cand);
   a.rows = reinterpret_cast<Row*>(ws + l.rows), a.quick = reinterpret_cast<Quick*>(ws + l.quick);
-  static std::atomic<unsigned long long> done{0};
-  if (smem_attr_once(done, beam_rank_kernel, (int)sizeof(RankShared)) != cudaSuccess) return ATSPEED_E_CUDA;
   const int grid = R * l.pieces;
   const bool aligned = aligned16(s.d_logits) && s.ld * dtype_size(s.type) % 16 == 0;
   static std::atomic<unsigned long long> ready[6];
@@ -937,12 +939,19 @@ extern "C" atspeed_status atspeed_op_beam_select(atspeed_stream stream, const at
       : aligned                ? go(beam_pieces_kernel<ATSPEED_F16, true>, 4)
                                : go(beam_pieces_kernel<ATSPEED_F16, false>, 5);
   if (launched != ATSPEED_OK) return launched;
-  // (it may start while the last of the pieces are read, and waits for them)
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(s.n_req), cfg.blockDim = dim3(kRankThreads), cfg.dynamicSmemBytes = sizeof(RankShared), cfg.stream = (cudaStream_t)stream;
-  cudaLaunchAttribute attr = {};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr, cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, beam_rank_kernel, a) == cudaSuccess ? ATSPEED_OK : ATSPEED_E_CUDA;
+  // The ranking may start while the last of the pieces are read, and waits for them.
+  const auto rank = [&](auto kernel, int threads, size_t shared, std::atomic<unsigned long long>& done) {
+    if (smem_attr_once(done, kernel, (int)shared) != cudaSuccess) return ATSPEED_E_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(s.n_req), cfg.blockDim = dim3(threads), cfg.dynamicSmemBytes = shared, cfg.stream = (cudaStream_t)stream;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr, cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess ? ATSPEED_OK : ATSPEED_E_CUDA;
+  };
+  static std::atomic<unsigned long long> done[2];
+  const long long places = (long long)grid * a.cap / s.n_req;   // of candidates, a request's on average
+  return width <= 64 && places <= kFewPlaces ? rank(beam_rank_kernel<256>, 256, sizeof(RankShared<256>), done[0])
+                                             : rank(beam_rank_kernel<1024>, 1024, sizeof(RankShared<1024>), done[1]);
 }

@@ -293,14 +293,15 @@ def test_select_orders_that_meet_one_group(ats, order, width):
     _check_select(ats, logits, [1, 1], width, exact=True)
 
 
-def test_select_many_equal_beams(ats):
+@pytest.mark.parametrize("width", [8, 20, 64, 256])
+def test_select_many_equal_beams(ats, width):
     """More candidates of one score than the ranking holds at a time."""
     logits = torch.zeros(90, 700, device="cuda")
-    _check_select(ats, logits, [90], 256, exact=True)
+    _check_select(ats, logits, [90], width, exact=True)
     logits = _logits(1, 1, 700, torch.float32).expand(90, 700).contiguous()
-    _check_select(ats, logits, [90], 256, exact=True)
+    _check_select(ats, logits, [90], width, exact=True)
     # (better and better beams)
-    _check_select(ats, logits, [90], 256, score=np.linspace(-90, 0, 90), exact=True)
+    _check_select(ats, logits, [90], width, score=np.linspace(-90, 0, 90), exact=True)
 
 
 def test_select_leaves_other_rows(ats):
