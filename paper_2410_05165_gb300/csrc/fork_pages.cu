@@ -2,7 +2,9 @@
 //   kept_j = ceil(len_j / page) entries of the parent's row; a partial last one: the parent's heir (the child with the largest
 //   (len, -j)) goes on in it if its count is at most 1, the others copy it to the next free page
 //   count' = count + handed out - old rows that hold the page + new rows that hold it;  free' = {page : count' <= 0}
-// Bound: latency, for large tables HBM (the old entries in, the new ones out).
+// Bound: latency, for large tables HBM (the old entries in, the new ones out).  us in a graph: 10 rows of 9 pages 8, 320 rows of up to 64
+// 12, 1021 rows of up to 2000 pages of a pool of 300 000 21
+// (4 for the old counts, 4 for the new ones' zeros, by the eight CTAs that share them).
 //
 // One launch.  Every CTA works out for itself which children are heirs and which page a copy gets (a few bytes a row, from L2, and
 // one sum over the rows) instead of waiting for another launch.  The first CTA, or for many pages a cluster of eight, then makes the counts
@@ -97,7 +99,7 @@ __global__ void __launch_bounds__(kThreads, 1) fork_pages_kernel(const __grid_co
 
   if (blockIdx.x < kCluster) {   // the old counts, under way meanwhile
     const int step = kCluster * kThreads, first = rank * kThreads + tid, n4 = a.wide ? a.n_pages / 4 : 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int p = first; p < n4; p += step) reinterpret_cast<int4*>(a.new_ref)[p] = __ldg(reinterpret_cast<const int4*>(a.ref) + p);
 #pragma unroll 4
     for (int p = 4 * n4 + first; p < a.n_pages; p += step) a.new_ref[p] = __ldg(a.ref + p);
@@ -228,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, 1) fork_pages_kernel(const __grid_co
   };
   unsigned long long held = 0;
   int zeros = 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int t = 0; t < steps; ++t) {
     const uint32_t bits = free_of(t);
     if (t < kHeld) held |= (unsigned long long)bits << 4 * t;
@@ -249,21 +251,27 @@ __global__ void __launch_bounds__(kThreads, 1) fork_pages_kernel(const __grid_co
   }
   for (int t = 0; t < steps; ++t) {
     const uint32_t bits = t < kHeld ? (uint32_t)(held >> 4 * t) & 15u : free_of(t);
-    const int mine = __popc(bits);
-    int x = mine;
+    if (!__any_sync(0xffffffffu, bits)) continue;
+    // (the lanes' pages in order: those of the lanes before, then the lane's own)
+    const unsigned before = (1u << lane) - 1u;
+    int to = at;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
+    for (int i = 0; i < 4; ++i) {
+      const unsigned same = __ballot_sync(0xffffffffu, bits >> i & 1);
+      to += __popc(same & before);
+      at += __popc(same);
     }
-    int to = at + x - mine;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (bits >> i & 1) a.new_free[to++] = (int)(p0 + 128ll * t + i);
-    at += __shfl_sync(0xffffffffu, x, 31);
   }
-#pragma unroll 4
-  for (int i = total + rank * kThreads + tid; i < a.n_pages; i += kCluster * kThreads) a.new_free[i] = -1;
+  // -1 behind the free pages: up to a multiple of 16 bytes one by one, then by vectors
+  int* rest = a.new_free + total;
+  const int left = a.n_pages - total, me = rank * kThreads + tid;
+  const int head = min(left, (int)((16 - (reinterpret_cast<uintptr_t>(rest) & 15)) & 15) / 4), vectors = (left - head) / 4;
+  if (me < head) rest[me] = -1;
+  for (int i = me; i < vectors; i += kCluster * kThreads) reinterpret_cast<int4*>(rest + head)[i] = make_int4(-1, -1, -1, -1);
+  if (me < left - head - 4 * vectors) rest[head + 4 * vectors + me] = -1;
   if (rank == 0 && tid == 0) *a.new_n_free = total;
   if constexpr (kCluster > 1) cluster_sync();   // (no CTA leaves while others may write to its counts)
 }
