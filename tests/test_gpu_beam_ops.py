@@ -141,6 +141,13 @@ def test_select_one_piece_and_many(ats, R, V, width):
     _check_select(ats, _logits(R, R, V, torch.float32), counts, width, score=-np.random.default_rng(R).exponential(2.0, R))
 
 
+@pytest.mark.parametrize("width", [10, 70])
+def test_select_one_request_of_many_beams_among_small_ones(ats, width):
+    counts = [1] * 99 + [3000] + [0, 2]
+    _check_select(ats, _logits(6, 3101, 300, torch.float32), counts, width, score=-np.random.default_rng(6).exponential(2.0, 3101),
+                  final=np.where(np.arange(3101) % 7 == 3, 5, -1))
+
+
 @pytest.mark.parametrize("norm", ["masked", "full"])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_select_grammar(ats, norm, dtype):
