@@ -123,6 +123,8 @@ def binding(stand_library, monkeypatch):  # noqa: F811
             return (lambda *a: 64) if name == "atspeed_op_beam_select_workspace" else super().__getattr__(name)
 
     monkeypatch.setattr(b, "load", Lib)
+    monkeypatch.setattr(b, "_raw_alloc", lambda n, stream: 1 << 20)
+    monkeypatch.setattr(b, "_raw_delete", lambda p: None)
     monkeypatch.setattr(Stand, "split_with_sizes", lambda self, sizes: [Stand((n,), self.dtype, self.device) for n in sizes], raising=False)
     monkeypatch.setattr(Stand, "view", lambda self, *shape: Stand(shape, self.dtype, self.device), raising=False)
     return b

@@ -362,6 +362,39 @@ def test_select_on_streams_and_in_graphs(ats):
         assert torch.equal(got.token, w.token) and torch.equal(got.score, w.score)
 
 
+def test_select_workspaces_are_given_back(ats):
+    """A call's workspace is free after it, on every stream and after a refusal; calls that are captured have their graph's memory."""
+    cu, logits = _dev([0, 10, 20]), _logits(1, 20, 33024, torch.float32)
+    side = torch.cuda.Stream()
+    for stream in (None, side):
+        ats.op_beam_select(logits, cu, 10, stream=stream)
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        for _ in range(50):
+            ats.op_beam_select(logits, cu, 10, stream=stream)
+        with pytest.raises(ats.AtSpeedError):
+            ats.op_beam_select(logits, cu, 257, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.cuda.memory_allocated() == before
+    # (two graphs of calls one after the other, replayed beside each other and beside calls of their own)
+    want = ats.op_beam_select(logits, cu, 10)
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got = [ats.op_beam_select(logits, cu, 10) for _ in range(5)]
+        graphs.append((g, got, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for g, _, s in graphs:
+            with torch.cuda.stream(s):
+                g.replay()
+        own = ats.op_beam_select(logits, cu, 10)
+        torch.cuda.synchronize()
+        for r in [own] + [r for _, got, _ in graphs for r in got]:
+            assert torch.equal(r.token, want.token) and torch.equal(r.parent, want.parent) and torch.equal(r.score, want.score)
+
+
 # ---------------------------------------------------------------------------------------------------
 # fork
 # ---------------------------------------------------------------------------------------------------
