@@ -1,7 +1,7 @@
 // Rows of paged caches that change their place, in all layers at once: the filled part of pages to other pages
 // (atspeed_op_copy_pages) and an accepted path's tokens behind the cached ones (atspeed_op_compact_tokens).
 // Bound: HBM (each moved byte read once and written once); few bytes: the launch and the chain lengths -> rows.  Copies of 569 MB take
-// 77 us, 7.4 TB/s (some of the writes stay in L2), of 1 MB 3.8.
+// 73 us, 7.8 TB/s (some of the writes stay in L2), of 1 MB 4.3.
 #include <algorithm>
 
 #include "common.cuh"
@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kLayers = 120;   // of a launch (their addresses are kernel parameters: 4 KB)
-constexpr int kBatch = 8;      // 16-byte loads that a thread has under way
+constexpr int kBatch = 6;      // 16-byte loads that a thread has under way
 
 struct Geometry {   // the same in all layers, in 16-byte vectors
   int n_pages, page, heads, vecs;   // vecs: of a head's row
@@ -38,7 +38,7 @@ struct CompactArgs {
   Layers l;
 };
 
-// Copies from `from` to `to` what a warp has of one layer's K or V: i-th vectors at at(i), i < n, eight under way a lane.
+// Copies from `from` to `to` what a warp has of one layer's K or V: i-th vectors at at(i), i < n, six under way a lane.
 template <class At>
 __device__ __forceinline__ void warp_copy(uint4* to, const uint4* from, int n, At&& at) {
   const int lane = threadIdx.x & 31;
@@ -58,23 +58,31 @@ __device__ __forceinline__ void warp_copy(uint4* to, const uint4* from, int n, A
 }
 
 // A warp takes some rows (512 vectors, a row at least) of a copy in one layer's K or V after some rows.  Copies come and go with the lengths,
-// so every CTA lists 256 of them at a time with the rows that they have, and the grid's warps share those out: with a CTA a (copy,
-// layer, K or V) and pairs of -1 among them, 59 copies of 8 of 16 tokens in 32 layers of 32 heads of 128 took 118 us.
-__global__ void __launch_bounds__(kThreads) copy_pages_kernel(const __grid_constant__ CopyArgs a) {
-  __shared__ int s_upto[kThreads], s_src[kThreads], s_dst[kThreads], s_rows[kThreads], s_warp[kWarps];
+// so every CTA lists 1024 of them at a time with the rows that they have, and the grid's warps share those out: with a CTA a (copy,
+// layer, K or V) and pairs of -1 among them, the 569 MB took 118 us.  (344 pairs in two lists of 256: 18 us, in one 13.  Three or four CTAs an
+// SM: the same for many bytes, 1 to 2 us more for few.)
+constexpr int kPairs = 1024, kEach = kPairs / kThreads, kCopyCtas = 2;   // CTAs an SM
+__global__ void __launch_bounds__(kThreads, kCopyCtas) copy_pages_kernel(const __grid_constant__ CopyArgs a) {
+  __shared__ int s_upto[kPairs], s_src[kPairs], s_dst[kPairs], s_rows[kPairs], s_warp[kWarps];
   const Geometry& g = a.g;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, all_warps = gridDim.x * kWarps;
   const int row = g.heads * g.vecs, some = max(1, 512 / row);   // vectors of a row, rows that a warp takes at once
   long long turn = blockIdx.x * kWarps + warp;                  // this warp's next piece of work
-  for (int j0 = 0; j0 < a.n; j0 += kThreads) {
-    const int j = j0 + tid;
-    int src = -1, dst = -1, rows = 0;
-    if (j < a.n) {
-      src = __ldg(a.src + j), dst = __ldg(a.dst + j);
+  for (int j0 = 0; j0 < a.n; j0 += kPairs) {
+    int src[kEach], dst[kEach], rows[kEach], upto = 0;
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+      const int j = j0 + q * kThreads + tid;   // (the list's order does not matter)
+      src[q] = dst[q] = -1, rows[q] = 0;
+      if (j >= a.n) continue;
+      src[q] = __ldg(a.src + j), dst[q] = __ldg(a.dst + j);
       const int len = a.length ? __ldg(a.length + j) : g.page;
-      if ((unsigned)src < (unsigned)g.n_pages && (unsigned)dst < (unsigned)g.n_pages && src != dst && len > 0) rows = (len - 1) % g.page + 1;
+      if ((unsigned)src[q] < (unsigned)g.n_pages && (unsigned)dst[q] < (unsigned)g.n_pages && src[q] != dst[q] && len > 0)
+        rows[q] = (len - 1) % g.page + 1;
     }
-    int upto = (rows + some - 1) / some;
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) upto += (rows[q] + some - 1) / some;
+    const int mine = upto;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, upto, o);
@@ -83,16 +91,22 @@ __global__ void __launch_bounds__(kThreads) copy_pages_kernel(const __grid_const
     __syncthreads();   // (the list before this one is done with)
     if (lane == 31) s_warp[warp] = upto;
     __syncthreads();
+    upto -= mine;
     for (int w = 0; w < warp; ++w) upto += s_warp[w];
-    s_upto[tid] = upto, s_src[tid] = src, s_dst[tid] = dst, s_rows[tid] = rows;
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+      upto += (rows[q] + some - 1) / some;
+      const int at = tid * kEach + q;
+      s_upto[at] = upto, s_src[at] = src[q], s_dst[at] = dst[q], s_rows[at] = rows[q];
+    }
     __syncthreads();
-    const int units = s_upto[kThreads - 1];
+    const int units = s_upto[kPairs - 1];
     const long long work = (long long)units * 2 * a.layers;
     for (; turn < work; turn += all_warps) {
       const int lv = (int)(turn / units), u = (int)(turn % units);
       int c = 0;   // the first copy whose work ends behind u
 #pragma unroll
-      for (int step = kThreads / 2; step > 0; step >>= 1)
+      for (int step = kPairs / 2; step > 0; step >>= 1)
         if (s_upto[c + step - 1] <= u) c += step;
       const int t0 = (u - (c ? s_upto[c - 1] : 0)) * some, n = min(some, s_rows[c] - t0);
       const bool v = lv & 1;
@@ -207,8 +221,8 @@ extern "C" atspeed_status atspeed_op_copy_pages(atspeed_stream stream, const ats
   a.n = n, a.src = d_src, a.dst = d_dst, a.length = d_length;
   for (int first = 0; first < n_layers; first += kLayers) {
     a.layers = set_layers(a.l, layers, first, n_layers);
-    // (four CTAs an SM; few copies: a warp a row at most)
-    const int grid = (int)std::min(152LL * 4, (2LL * n * a.layers * std::min(64, a.g.page) + kWarps - 1) / kWarps);
+    // (what runs at once; few copies: a warp a row at most)
+    const int grid = (int)std::min(152LL * kCopyCtas, (2LL * n * a.layers * std::min(64, a.g.page) + kWarps - 1) / kWarps);
     copy_pages_kernel<<<grid, kThreads, 0, (cudaStream_t)stream>>>(a);
   }
   return launch_status();

@@ -698,7 +698,7 @@ def test_copy_pages(ats, layout, layers, page, heads, hd, types):
                 assert torch.equal(_whole(x).view(torch.int16), _whole(y).view(torch.int16))
 
 
-@pytest.mark.parametrize("n", [255, 256, 257, 1000])
+@pytest.mark.parametrize("n", [255, 257, 1024, 1025, 2500])
 def test_copy_many_pages(ats, n):
     """More pairs than a CTA lists at a time, most of them none."""
     rng = np.random.default_rng(n)
