@@ -709,7 +709,7 @@ __global__ void __launch_bounds__(T, 1) beam_rank_kernel(const __grid_constant__
   const int r1 = min(min(a.R, __ldg(a.cu + a.n_req)), __ldg(a.cu + b + 1));
   const int lists = max(0, r1 - r0) * a.pieces;
   if (tid == 0) sh.n = sh.hits[0] = 0;
-  // (the first thousand rows' inputs, before the sums are there)
+  // (the first T rows' inputs, before the sums are there)
   const float my_cum = a.score && r0 + tid < r1 ? __ldg(a.score + r0 + tid) : 0.f;
   const int my_final = a.final && r0 + tid < r1 ? __ldg(a.final + r0 + tid) : -1;
   pdl_wait();
@@ -727,7 +727,7 @@ __global__ void __launch_bounds__(T, 1) beam_rank_kernel(const __grid_constant__
   // A row's maximum and sum from its pieces, many by a warp, few by a thread; then its logarithm.
   // (Sums as multiples of 2^-32, whole numbers: a row's is at least 0.7 and at most 1.5 times its length.)
   const auto whole = [&](float s) { return (unsigned long long)(s * 0x1p32f); };
-  const auto set_row = [&](int r, float M, unsigned long long s) {   // r: r0 + tid and every thousandth from there
+  const auto set_row = [&](int r, float M, unsigned long long s) {   // r: r0 + tid and every T-th from there
     const bool first = r - r0 < T, near = fabsf(M) < kFar;
     Row w = {};
     w.cum = first ? my_cum : a.score ? __ldg(a.score + r) : 0.f;
@@ -748,7 +748,7 @@ __global__ void __launch_bounds__(T, 1) beam_rank_kernel(const __grid_constant__
       set_row(r, M, M > -INFINITY ? whole(s0 * rescale(m0, M)) + whole(s1 * rescale(m1, M)) : 0ull);
     }
   } else {
-    // (rows of three pieces or more are fewer than kManyPieces; their sums wait in the list's place)
+    // (there are fewer than kManyPieces rows of three pieces or more; their sums wait in the list's place)
     for (int r = r0 + warp; r < r1; r += T / 32) {
       const Header* h = a.head + (long long)r * a.pieces;
       const float m0 = lane < a.pieces ? h[lane].m : -INFINITY, s0 = lane < a.pieces ? h[lane].s : 0.f;
@@ -874,7 +874,7 @@ int pieces_of(int R, int V) {
   const long long span = (tiles + most - 1) / most;
   return (int)((tiles + span - 1) / span);
 }
-int cap_of(int W) {   
+int cap_of(int W) {   // candidates that a piece hands on at most: a power of two
   int cap = 32;
   while (cap < W + W / 2 + 8) cap *= 2;
   return cap;
