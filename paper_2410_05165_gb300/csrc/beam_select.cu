@@ -153,20 +153,9 @@ struct Shared {
   int tok[kList];
   uint32_t scratch[3 * kWarps];
   int read[kGroups];         // vectors to be read again: from the front by their first tokens, from the back in every tile
-  int n, n_reads, count[kWarps];   // n_reads: those at the front, and 65536 times those at the back
+  int n, n_reads, count[kWarps], same[kWarps];   // n_reads: those at the front, and 65536 times those at the back
   float m[kWarps], s[kWarps];
 };
-
-__device__ __forceinline__ int block_count(int v, Shared& sh) {   // the sum over the CTA
-  v = __reduce_add_sync(0xffffffffu, v);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh.count[threadIdx.x >> 5] = v;
-  __syncthreads();
-  int t = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) t += sh.count[w];
-  return t;
-}
 
 // A sum of exponentials below a maximum m: for |m| < kFar in units of the whole power of two 2^unit_of(m), its terms 2^(x l - unit)
 // by one multiply-add (l = log2 e in 32 bits), so that another maximum rescales it exactly, whatever their order; from
@@ -218,51 +207,67 @@ __device__ __forceinline__ uint32_t key_at(const char* in, const uint32_t* allow
 }
 
 // The W best of the tokens [begin, end), of which more than W are at or above `from`, exactly (equal ones in the tokens' order), into the
-// list.  Every thread of the CTA.
+// list.  Every thread of the CTA; a warp has a share of the tokens, in order.  A pass over them halves the keys that the W-th best may have
+// and goes on to the next one that there is, so that few different logits need few passes: 3840 rows of 33024 take 888 us where they are
+// whole numbers (6015 with the halving alone), 1124 where all are equal (3083 with barriers for every 128 tokens and the ranking by
+// a thousand threads at a time); 109 where no row needs this.  `most`: no key is above it.
 template <int TYPE>
-__device__ __noinline__ void put_exactly(const char* in, const uint32_t* allowed, int begin, int end, uint32_t from, int W, Shared& sh) {
-  const int tid = threadIdx.x;
-  const auto count = [&](uint32_t least) {
-    int c = 0;
-    for (int t = begin + tid; t < end; t += kThreads) c += key_at<TYPE>(in, allowed, t, least) != 0;
-    return block_count(c, sh);
-  };
-  uint32_t lo = from, hi = 0xffffffffu;
-  int above = count(lo + 1);
-  if (above >= W) {   // at least W at lo + 1, fewer above hi
-    ++lo;
-    while (lo < hi) {
-      const uint32_t mid = lo + (hi - lo) / 2 + 1;
-      if (count(mid) >= W) lo = mid;
-      else hi = mid - 1;
+__device__ __noinline__ void put_exactly(const char* in, const uint32_t* allowed, int begin, int end, uint32_t from, uint32_t most, int W, Shared& sh) {
+  constexpr int kAtOnce = 8;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int share = (end - begin + 32 * kWarps - 1) / (32 * kWarps) * 32, t0 = begin + warp * share, t1 = min(end, t0 + share);
+  const auto each = [&](uint32_t least, auto&& go) {   // go(token, key at or above `least` or 0), 32 tokens after 32
+    for (int t = t0; t < t1; t += 32 * kAtOnce) {
+      uint32_t k[kAtOnce];
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) k[q] = t + 32 * q + lane < t1 ? key_at<TYPE>(in, allowed, t + 32 * q + lane, least) : 0u;
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) go(t + 32 * q + lane, k[q]);
     }
-    above = count(lo + 1);
+  };
+  int above, before, same;     // of all tokens above lo; at lo, of the warps before this one and of this one
+  uint32_t lo = from, hi = most;   // at least W are at or above lo, fewer above hi
+  while (true) {
+    const uint32_t mid = lo + (hi - lo) / 2 + 1;
+    int up = 0, at = 0, mids = 0;    // above lo, at it, at or above mid
+    uint32_t next = ~0u, mid_next = ~0u;   // the smallest of them
+    each(lo, [&](int, uint32_t k) {
+      at += k == lo;
+      if (k > lo) ++up, next = min(next, k);
+      if (k >= mid) ++mids, mid_next = min(mid_next, k);
+    });
+    up = __reduce_add_sync(0xffffffffu, up), same = __reduce_add_sync(0xffffffffu, at), mids = __reduce_add_sync(0xffffffffu, mids);
+    next = __reduce_min_sync(0xffffffffu, next), mid_next = __reduce_min_sync(0xffffffffu, mid_next);
+    __syncthreads();
+    if (lane == 0) {
+      sh.count[warp] = up, sh.same[warp] = same;
+      sh.scratch[warp] = (uint32_t)mids, sh.scratch[kWarps + warp] = next, sh.scratch[2 * kWarps + warp] = mid_next;
+    }
+    __syncthreads();
+    above = before = mids = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      above += sh.count[w], before += w < warp ? sh.same[w] : 0;
+      mids += (int)sh.scratch[w], next = min(next, sh.scratch[kWarps + w]), mid_next = min(mid_next, sh.scratch[2 * kWarps + w]);
+    }
+    if (above < W) break;
+    if (mids >= W) lo = mid_next;
+    else lo = next, hi = mid - 1;
   }
   if (tid == 0) sh.n = 0;
   __syncthreads();
-  int at = above, room = W - above;   // of the equal ones
-  for (int t0 = begin; t0 < end; t0 += kThreads) {
-    const int t = t0 + tid;
-    const uint32_t k = t < end ? key_at<TYPE>(in, allowed, t, lo) : 0u;
-    const unsigned same = __ballot_sync(0xffffffffu, k == lo);
-    const int all = room > 0 ? block_count((tid & 31) == 0 ? __popc(same) : 0, sh) : 0;   // (sh.count: the warps')
-    int place = -1;
-    if (k > lo) {
-      place = atomicAdd(&sh.n, 1);
-    } else if (k == lo && room > 0) {
-      int nth = __popc(same & ((1u << (tid & 31)) - 1u));
-      for (int w = 0; w < tid >> 5; ++w) nth += sh.count[w];
-      if (nth < room) place = at + nth;
-    }
-    if (place >= 0) {
+  int at = above + before;
+  each(lo, [&](int t, uint32_t k) {
+    const unsigned equal = __ballot_sync(0xffffffffu, k == lo);
+    int place = k > lo ? atomicAdd(&sh.n, 1) : k == lo ? at + __popc(equal & ((1u << lane) - 1u)) : W;
+    at += __popc(equal);
+    if (place < W) {
       sh.key[place] = k;
       sh.tok[place] = t;
     }
-    at += min(room, all);
-    room -= min(room, all);
-  }
+  });
   __syncthreads();
-  if (tid == 0) sh.n = at;
+  if (tid == 0) sh.n = W;
   __syncthreads();
 }
 
@@ -548,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
   }
   __syncthreads();
   const int n_one = sh.n_reads & 0xffff, n_every = sh.n_reads >> 16, reads = n_one + n_every * tiles;
-  for (int i0 = tid; i0 < reads; i0 += kVec * kThreads) {
+  for (int i0 = tid; i0 < reads && *(volatile int*)&sh.n <= kList; i0 += kVec * kThreads) {   // (beyond kList it stays so)
     uint32_t w[kVec][4], ok[kVec];
     int t[kVec];
 #pragma unroll
@@ -594,7 +599,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
   if (n <= a.cap || n > kList || !hand_on_best()) {
     if (n > a.cap) {
       __syncthreads();
-      put_exactly<TYPE>(in, allowed, begin, end, from, a.W, sh);
+      put_exactly<TYPE>(in, allowed, begin, end, from, key_of(M), a.W, sh);
       n = sh.n;
     }
     for (int i = tid; i < n; i += kThreads) hand_on(i, i);
@@ -613,6 +618,9 @@ struct Entry {
   unsigned long long rest;    // ~row, logit's key
   uint32_t tok;
 };
+__device__ __forceinline__ bool before(const Entry& a, const Entry& b) {
+  return a.score > b.score || (a.score == b.score && (a.rest > b.rest || (a.rest == b.rest && a.tok < b.tok)));
+}
 
 // n log 2 + log(s 2^-32) + more to 2^-29, s > 0.  With s = 2^e f, f in [2/3, 4/3): log f = 2 atanh z = 2 (z + z^3 / 3 + ..),
 // z = (f - 1) / (f + 1), |z| <= 1/5; z in two parts (its quotient and what that leaves, times the derivative 1 / (1 - z^2)), the rest of the
@@ -801,17 +809,19 @@ __global__ void __launch_bounds__(T, 1) beam_rank_kernel(const __grid_constant__
   // what is below `from` is not among the W best: the W-th of the threads' best
   const uint32_t group[1] = {key_of(g)}, bound = threshold_of<1, T / 32>(group, a.W, a.W + a.W / 8, sh.scratch);
   float from = bound ? value_of(bound) : -INFINITY;
+  Entry worst = {0, 0, 0};   // what comes after it is not among the W best: the W-th of those known, once there are many
   const auto put = [&](int l) {
     uint2 x = fetch(l);
     const int r = row_of(l);
     const Row& w = row_at(r);
     if (w.final >= 0) x = make_uint2(0u, (uint32_t)w.final);
     const Two y = w.score(__uint_as_float(x.x));
-    if (!(y.hi > -INFINITY)) return;
+    const Entry e = {key_of(y), (unsigned long long)~(uint32_t)r << 32 | key_of(__uint_as_float(x.x)), x.y};
+    if (!(y.hi > -INFINITY) || !before(e, worst)) return;
     const int to = atomicAdd(&sh.n, 1);
-    sh.score[to] = key_of(y);
-    sh.rest[to] = (unsigned long long)~(uint32_t)r << 32 | key_of(__uint_as_float(x.x));
-    sh.tok[to] = x.y;
+    sh.score[to] = e.score;
+    sh.rest[to] = e.rest;
+    sh.tok[to] = e.tok;
   };
   for (int l0 = 0, turn = 0; l0 < lists; l0 += per_round, turn ^= 1) {
     if (lists > per_round) {
@@ -831,20 +841,22 @@ __global__ void __launch_bounds__(T, 1) beam_rank_kernel(const __grid_constant__
       __syncthreads();   // (everyone knows `had`)
 #pragma unroll 1
       for (; hits; hits &= hits - 1) put(l0 + (__ffs(hits) - 1) * at_once + my_list);
-    } else {   // a step at a time, of which the W best stay
+    } else {
+      // Too many, most of them equal: a quarter of the threads at a time, of which the W best stay, and what comes after those is left
+      // out (later rows come after equal ones): an order of fewer, of a quarter of the work.
 #pragma unroll 1
-      for (int q = 0; q < kHold; ++q) {
+      for (int q = 0; q < 4 * kHold; ++q) {
         __syncthreads();
-        if (hits >> q & 1) put(l0 + q * at_once + my_list);
+        if (hits >> q / 4 & 1 && tid / (T / 4) == q % 4) put(l0 + q / 4 * at_once + my_list);
         __syncthreads();
         const int n = sh.n;
-        if (n <= T) continue;
+        if (n < a.W + T / 4) continue;
         rank_list(sh, n, a.W, [&](int r, const Entry& e) { sh.best[r] = e; });
         __syncthreads();
-        const int left = min(n, a.W);
-        for (int j = tid; j < left; j += T) sh.score[j] = sh.best[j].score, sh.rest[j] = sh.best[j].rest, sh.tok[j] = sh.best[j].tok;
-        if (tid == 0) sh.n = left;
-        if (n >= a.W) from = fmaxf(from, value_of((uint32_t)(sh.best[a.W - 1].score >> 32)));
+        for (int j = tid; j < a.W; j += T) sh.score[j] = sh.best[j].score, sh.rest[j] = sh.best[j].rest, sh.tok[j] = sh.best[j].tok;
+        if (tid == 0) sh.n = a.W;
+        worst = sh.best[a.W - 1];
+        from = fmaxf(from, value_of((uint32_t)(worst.score >> 32)));
       }
     }
     __syncthreads();

@@ -311,6 +311,25 @@ def test_select_many_equal_beams(ats, width):
     _check_select(ats, logits, [90], width, score=np.linspace(-90, 0, 90), exact=True)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [20, 80, 256])
+@pytest.mark.parametrize("rules", [False, True])
+def test_select_whole_numbers(ats, dtype, width, rules):
+    """A few different logits, each of them many times, in beams that come in turn from the worst to the best."""
+    V, R, tokens = 12500, 90, 9000
+    rng = np.random.default_rng(width)
+    x = np.round(rng.normal(0, 1.2, V))
+    x[rng.permutation(V)[:30]] = np.arange(30) // 6 + 5
+    logits = torch.from_numpy(np.tile(x, (R, 1)).astype(np.float32)).to("cuda", dtype)
+    score = np.arange(R) // 3 % 4 * 0.25 - 1   # (a sum of whole and quarter steps tells which it is of)
+    kw = {}
+    if rules:
+        kw = dict(table=np.arange(V)[None, :] % 25 < 18, state=np.zeros(R, int))
+        assert kw["table"].sum() == tokens
+    _check_select(ats, logits, [R], width, score=score, exact=True, **kw)
+    _check_select(ats, logits, [1, R - 1], width, score=score, exact=True, **kw)
+
+
 def test_select_leaves_other_rows(ats):
     logits = _logits(8, 10, 3000, torch.float32)
     logits[:2] = float("nan")
