@@ -843,11 +843,13 @@ __global__ void __launch_bounds__(T, 1) beam_rank_kernel(const __grid_constant__
       for (; hits; hits &= hits - 1) put(l0 + (__ffs(hits) - 1) * at_once + my_list);
     } else {
       // Too many, most of them equal: a quarter of the threads at a time, of which the W best stay, and what comes after those is left
-      // out (later rows come after equal ones): an order of fewer, of a quarter of the work.
+      // out (later rows come after equal ones): an order of fewer, of a quarter of the work.  What the rounds before left may fill the list
+      // to its end, so it is ranked before the first share (q = -1): fewer than W + T / 4 are there whenever one is put in.
+      static_assert(kMaxWidth + T / 2 <= 2 * T, "a share more than the list was ranked at");
 #pragma unroll 1
-      for (int q = 0; q < 4 * kHold; ++q) {
+      for (int q = -1; q < 4 * kHold; ++q) {
         __syncthreads();
-        if (hits >> q / 4 & 1 && tid / (T / 4) == q % 4) put(l0 + q / 4 * at_once + my_list);
+        if (q >= 0 && hits >> q / 4 & 1 && tid / (T / 4) == q % 4) put(l0 + q / 4 * at_once + my_list);
         __syncthreads();
         const int n = sh.n;
         if (n < a.W + T / 4) continue;

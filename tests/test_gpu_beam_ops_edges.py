@@ -1,0 +1,60 @@
+"""Beam selection, page fork and moves at the edges of what they allow: lists that fill to their last place, scores near a type's largest
+number, and forks, copies and moves whose counts, lists and buffers are at their limits."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_beam_ops import NEG, _check_select, _dev, ats  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------------------------------
+# selection: a ranking in several rounds whose list fills up
+# ---------------------------------------------------------------------------------------------------
+def _equal_logits(V, hot, dtype, alone):
+    """A row with `hot` equal best logits, the others 25 and more below them (alone: -infinity), and where those are."""
+    rng = np.random.default_rng(hot)
+    row = np.full(V, NEG) if alone else np.floor(rng.uniform(-30, -20, size=V))
+    at = np.sort(rng.choice(V, size=hot, replace=False))
+    row[at] = 5.0
+    return torch.from_numpy(row.astype(np.float32)).to("cuda", dtype), at
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("better", [False, True])
+@pytest.mark.parametrize("over", [-2, -1, 0, 1, 2])
+# width, threads that rank, rows whose candidates are looked at in a round, more rows, other requests
+@pytest.mark.parametrize("width,threads,round_rows,more,others", [
+    (16, 1024, 512, 8, []), (16, 1024, 512, 600, []), (64, 256, 32, 8, [2]), (64, 256, 32, 90, [1, 1, 0, 3]), (30, 256, 64, 80, [3, 1, 2]),
+    (10, 256, 128, 72, [1, 2, 1]), (80, 1024, 128, 12, []), (80, 1024, 128, 300, []), (120, 1024, 64, 20, []), (256, 1024, 32, 8, [])])
+def test_select_fills_the_list_and_goes_on(ats, width, threads, round_rows, more, others, over, better, dtype):  # noqa: F811
+    """Equal scores whose first round fills the list of 2 * threads places, but for a quarter of the threads or one, just so, or one or many too
+    far, before more of them come.  Rows are the same, so that their sums are; what a state allows (of a sum over all) says how many are equal."""
+    V, hot = 1000, 100
+    total = 2 * threads + {-2: -threads // 4, -1: -1, 0: 0, 1: 1, 2: threads // 4 + 3}[over]
+    allow = np.full(round_rows, total // round_rows)
+    allow[:total % round_rows] += 1
+    assert allow.max() <= hot and allow.sum() == total
+    beams = round_rows + more
+    state = np.concatenate([allow, np.full(more + sum(others), total // round_rows)])
+    # (a bound at the equal ones needs `width` threads that meet one: an eighth of them do at least; without others there is no other bound)
+    row, at = _equal_logits(V, hot, dtype, alone=width > threads // 8)
+    table = np.ones((hot + 1, V), bool)
+    for s in range(hot + 1):
+        table[s, at[s:]] = False
+    score = np.zeros(state.size)
+    if better:   # (fewer than `width` of them: the bound stays)
+        score[[round_rows // 2, beams - 1]] = 1.0
+        state[[round_rows // 2, beams - 1]] = 3
+    logits = row.expand(state.size, V).contiguous()
+    _check_select(ats, logits, [beams] + others, width, score=score, table=table, state=state, norm="full", exact=True)
+
+
+@pytest.mark.parametrize("width,beams,tied,others", [(80, 140, [*range(24), *range(128, 140)], []),
+                                                     (10, 200, [*range(51), *range(128, 200)], [1] * 9)])
+def test_select_equal_beams_among_far_ones(ats, width, beams, tied, others):  # noqa: F811
+    """Rows of equal logits, some of them beams of one score, the others far below: nearly a full list, then more."""
+    score = np.full(beams + sum(others), -50.0)
+    score[tied] = 0.0
+    _check_select(ats, torch.zeros(score.size, 700, device="cuda"), [beams] + others, width, score=score, exact=True)
