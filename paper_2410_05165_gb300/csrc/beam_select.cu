@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) beam_pieces_kernel(const __gr
         const char* stop = in + (long long)end * SIZE;
         const auto some = [&](uint4* to, const char* from) {
           const long long left = stop - from;
-          copy16(to, left > 0 ? from : in, left > 0 ? (int)min(16ll, left) : 0);
+          copy16(to, left > 0 ? from : in - lead, left > 0 ? (int)min(16ll, left) : 0);   // (a multiple of 16, if nothing is read there too)
         };
 #pragma unroll
         for (int v = 0; v < kVec; ++v) some(&to[v][lane], from + v * kThreads * 16);

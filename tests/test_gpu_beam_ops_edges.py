@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_beam_ops import NEG, _check_select, _dev, ats  # noqa: F401
+from test_gpu_beam_ops import NEG, TYPES, _check_select, _dev, _logits, ats  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +58,11 @@ def test_select_equal_beams_among_far_ones(ats, width, beams, tied, others):  # 
     score = np.full(beams + sum(others), -50.0)
     score[tied] = 0.0
     _check_select(ats, torch.zeros(score.size, 700, device="cuda"), [beams] + others, width, score=score, exact=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [1, 3, 9, 513, 2049, 4095, 4101, 8193])
+def test_select_rows_that_end_early_in_a_tile(ats, dtype, V):  # noqa: F811
+    """Rows that begin at every place of a 16-byte word and leave most of their last tile's lanes nothing to read."""
+    _check_select(ats, _logits(V, 9, V, dtype, pitch=(1 - V) % 16), [4, 5], 12, score=np.linspace(-1, -2, 9))
+    _check_select(ats, _logits(V, 1, V, dtype, lead=1), [1], 12)
