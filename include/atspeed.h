@@ -484,7 +484,8 @@ atspeed_status atspeed_op_beam_select(atspeed_stream stream, const atspeed_beams
  *     held = d_kv_len[p] + (d_q_len and served ? d_q_len[p] : 0), served: d_old_state NULL or d_old_state[p] = ATSPEED_PLAN_OK
  *     (d_kv_len, d_q_len, d_old_state: the plan's inputs and its output);
  *   d_free [*d_n_free], of which the first *d_used (NULL: 0) have been handed out since d_ref was made (the plan's d_pages):
- *     each of those counts one holder more;
+ *     each of those counts one holder more;  free_size: the entries that d_free has room for, a larger *d_n_free counts as
+ *     that many (0: not known, *d_n_free is taken as it is; negative: none, nothing of d_free is read);
  *   d_parent [n_new]: each new row's old row, negative: an empty row (NULL: row j goes on from row j, n_new = n_old);
  *   d_length [n_new]: the tokens it keeps (NULL: all that its parent holds).
  * A new row keeps its parent's first ceil(length / page_size) pages.  Full ones are shared.  The last one, if not full, will be
@@ -498,7 +499,7 @@ atspeed_status atspeed_op_beam_select(atspeed_stream stream, const atspeed_beams
  * whose new count is 0 or less, ascending, -1 behind them.
  * Entries outside [0, n_pages) are handed on, not counted, not copied.  n_old, n_new <= 16384, n_pages <= 2^26 (ATSPEED_E_SHAPE). */
 typedef struct {
-  int n_old, n_new, table_width, page_size, n_pages;
+  int n_old, n_new, table_width, page_size, n_pages, free_size;
   const int32_t *d_table, *d_kv_len, *d_q_len, *d_old_state, *d_parent, *d_length, *d_ref, *d_free, *d_n_free, *d_used;
   int32_t *d_new_table, *d_new_len, *d_new_state, *d_src, *d_dst, *d_new_ref, *d_new_free, *d_new_n_free;
 } atspeed_page_fork;

@@ -93,14 +93,14 @@ class BeamsDesc(ctypes.Structure):
 
 
 class PageForkDesc(ctypes.Structure):
-    _fields_ = [(f, ctypes.c_int) for f in ("n_old", "n_new", "table_width", "page_size", "n_pages")] + [(f, ctypes.c_void_p) for f in (
+    _fields_ = [(f, ctypes.c_int) for f in ("n_old", "n_new", "table_width", "page_size", "n_pages", "free_size")] + [(f, ctypes.c_void_p) for f in (
         "d_table", "d_kv_len", "d_q_len", "d_old_state", "d_parent", "d_length", "d_ref", "d_free", "d_n_free", "d_used", "d_new_table",
         "d_new_len", "d_new_state", "d_src", "d_dst", "d_new_ref", "d_new_free", "d_new_n_free")]
 
 
 # (packed whole and passed by address: as arguments of their own the fields of a fork take 2 us more)
-_BEAMS_PACK, _FORK_PACK = struct.Struct("@PqiiiiiiPPPPPqiPPP").pack, struct.Struct("@iiiii18P").pack
-assert struct.calcsize("@PqiiiiiiPPPPPqiPPP") == ctypes.sizeof(BeamsDesc) and struct.calcsize("@iiiii18P") == ctypes.sizeof(PageForkDesc)
+_BEAMS_PACK, _FORK_PACK = struct.Struct("@PqiiiiiiPPPPPqiPPP").pack, struct.Struct("@iiiiii18P").pack
+assert struct.calcsize("@PqiiiiiiPPPPPqiPPP") == ctypes.sizeof(BeamsDesc) and struct.calcsize("@iiiiii18P") == ctypes.sizeof(PageForkDesc)
 
 _lib: Optional[ctypes.CDLL] = None
 
@@ -789,12 +789,12 @@ def op_fork_pages(table: torch.Tensor, kv_len: torch.Tensor, ref: torch.Tensor, 
     n, pages = kv_len.numel(), ref.numel()
     if table.dim() != 2 or table.shape[0] != n or n < 1 or pages < 1 or (parent is None and length is not None and length.numel() != n):
         _refuse(f"{n} rows, table {tuple(table.shape)}, {pages} pages, {'no parents' if parent is None else parent.numel()}")
-    m, width = n if parent is None else parent.numel(), table.shape[1]
+    m, width, room = n if parent is None else parent.numel(), table.shape[1], free.numel() or -1
     n_free_ptr = _given(n_free, i32, 1, "n_free", gpu)
     ins = (_given(table, i32, n, "table", gpu), _given(kv_len, i32, n, "kv_len", gpu), _tensor(q_len, i32, n, "q_len", gpu) or 0,
            _tensor(state, i32, n, "state", gpu) or 0, _tensor(parent, i32, 1, "parent", gpu) or 0, _tensor(length, i32, m, "length", gpu) or 0,
            _given(ref, i32, pages, "ref", gpu),
-           _given(free, i32, 0, "free", gpu) if free.numel() else n_free_ptr,   # (n_free is 0: nothing is read of it)
+           _given(free, i32, 0, "free", gpu) if room > 0 else n_free_ptr,   # (of an empty list nothing is read, whatever n_free is)
            n_free_ptr, _tensor(used, i32, 1, "used", gpu) or 0)
     if out is None:   # (one tensor and views of it, the counts at its start: eight tensors take longer)
         cells = m * width
@@ -808,7 +808,7 @@ def op_fork_pages(table: torch.Tensor, kv_len: torch.Tensor, ref: torch.Tensor, 
             _refuse(f"out.table: [{m}][{width}], not {tuple(out.table.shape)}")
         sizes = (m * width, m, m, m, m, pages, pages, 1)
         outs = [_given(getattr(out, k), i32, size, "out." + k, gpu) for k, size in zip(PageFork.__slots__, sizes)]
-    _check(load().atspeed_op_fork_pages(_raw_stream(stream, dev), _FORK_PACK(n, m, width, page_size, pages, *ins, *outs)))
+    _check(load().atspeed_op_fork_pages(_raw_stream(stream, dev), _FORK_PACK(n, m, width, page_size, pages, room, *ins, *outs)))
     return out
 
 

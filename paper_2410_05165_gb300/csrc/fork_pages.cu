@@ -23,7 +23,7 @@ constexpr int kPiece = 512;   // entries of a row that a warp writes
 constexpr int kMaxPages = 1 << 26;
 
 struct ForkArgs {
-  int n_old, n_new, width, page, n_pages;
+  int n_old, n_new, width, page, n_pages, most_free;   // most_free: what the free list has room for
   bool wide;   // counts at multiples of 16 bytes
   const int *table, *kv_len, *q_len, *old_state, *parent, *length, *ref, *free, *n_free, *used;
   int *new_table, *new_len, *new_state, *src, *dst, *new_ref, *new_free, *new_n_free;
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kThreads, 1) fork_pages_kernel(const __grid_co
     return x - v + (warp ? s_sum[warp - 1] : 0);
   };
   const auto in_pool = [&](int e) { return (unsigned)e < (unsigned)a.n_pages; };
-  const int n_free = max(0, __ldg(a.n_free)), used = a.used ? min(n_free, max(0, __ldg(a.used))) : 0;
+  const int n_free = min(a.most_free, max(0, __ldg(a.n_free))), used = a.used ? min(n_free, max(0, __ldg(a.used))) : 0;
 
   if (blockIdx.x < kCluster) {   // the old counts, under way meanwhile
     const int step = kCluster * kThreads, first = rank * kThreads + tid, n4 = a.wide ? a.n_pages / 4 : 0;
@@ -293,7 +293,8 @@ extern "C" atspeed_status atspeed_op_fork_pages(atspeed_stream stream, const ats
       f.d_new_len == f.d_kv_len || f.d_new_len == f.d_length || f.d_new_state == f.d_old_state || f.d_new_n_free == f.d_n_free)
     return ATSPEED_E_ARG;
   if (n_old > kMaxRequests || n_new > kMaxRequests || n_pages > kMaxPages) return ATSPEED_E_SHAPE;
-  const ForkArgs a = {n_old,     n_new,        table_width, f.page_size,   n_pages,       aligned16(f.d_ref) && aligned16(f.d_new_ref),
+  const int most_free = f.free_size ? std::max(0, f.free_size) : 0x7fffffff;
+  const ForkArgs a = {n_old,     n_new,        table_width, f.page_size,   n_pages,       most_free,  aligned16(f.d_ref) && aligned16(f.d_new_ref),
                       f.d_table, f.d_kv_len,   f.d_q_len,   f.d_old_state, f.d_parent,    f.d_length, f.d_ref,
                       f.d_free,  f.d_n_free,   f.d_used,    f.d_new_table, f.d_new_len,   f.d_new_state, f.d_src,
                       f.d_dst,   f.d_new_ref,  f.d_new_free, f.d_new_n_free};

@@ -66,3 +66,29 @@ def test_select_rows_that_end_early_in_a_tile(ats, dtype, V):  # noqa: F811
     """Rows that begin at every place of a 16-byte word and leave most of their last tile's lanes nothing to read."""
     _check_select(ats, _logits(V, 9, V, dtype, pitch=(1 - V) % 16), [4, 5], 12, score=np.linspace(-1, -2, 9))
     _check_select(ats, _logits(V, 1, V, dtype, lead=1), [1], 12)
+
+
+# ---------------------------------------------------------------------------------------------------
+# fork
+# ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n_pages", [8, 20000])   # counts by one CTA, by several
+@pytest.mark.parametrize("entries", [0, 1, 3])
+@pytest.mark.parametrize("used", [None, 1, 6])
+def test_fork_with_a_count_past_the_free_lists_end(ats, n_pages, entries, used):  # noqa: F811
+    """Five children of one partial page, four of which want a copy; n_free says 7, the list has fewer entries."""
+    memory = _dev([2, 3, 4, 5, 6, 7, 5, 5])   # (what lies behind the list is not its)
+    ref = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    ref[:2] = 1
+    f = ats.op_fork_pages(_dev([[0, 1, -1]]), _dev([20]), ref, memory[:entries], _dev([7]), 16, parent=_dev([0] * 5),
+                          used=None if used is None else _dev([used]))
+    taken = min(entries, used or 0)
+    copies = min(4, entries - taken)
+    fresh = memory.tolist()[taken:taken + copies]
+    assert f.state.tolist() == [0] * (1 + copies) + [1] * (4 - copies)
+    assert f.dst.tolist() == [-1] + fresh + [-1] * (4 - copies) and f.src.tolist() == [-1] + [1] * copies + [-1] * (4 - copies)
+    assert f.table.tolist() == [[0, 1, -1]] + [[0, e, -1] for e in fresh] + [[-1] * 3] * (4 - copies)
+    held = [1 + copies, 1] + [0] * (n_pages - 2)
+    for e in memory.tolist()[:taken] + fresh:
+        held[e] = 1
+    free = [e for e, h in enumerate(held) if h == 0]
+    assert f.ref.tolist() == held and int(f.n_free) == len(free) and f.free.tolist() == free + [-1] * (n_pages - len(free))
