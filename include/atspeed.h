@@ -492,8 +492,8 @@ atspeed_status atspeed_op_beam_select(atspeed_stream stream, const atspeed_beams
  * written to: the child of its parent that keeps the most tokens (the first of those) goes on in it if nothing else held it
  * (d_ref at most 1); any other child gets the next page of d_free, from the used ones on, in the order of the rows, and has to
  * be given a copy of it.
- * Outputs (overlapping no input): d_new_table [n_new][table_width], -1 behind the kept pages;  d_new_len [n_new] tokens kept, -1 if not
- * served;  d_new_state [n_new] an atspeed_plan_state (NO_PAGES: no page was left for its copy; LIMIT: a parent of n_old or above,
+ * Outputs (overlapping no input and no other output; ATSPEED_E_ARG): d_new_table [n_new][table_width], -1 behind the kept pages;
+ * d_new_len [n_new] tokens kept, -1 if not served;  d_new_state [n_new] an atspeed_plan_state (NO_PAGES: no page was left for its copy; LIMIT: a parent of n_old or above,
  * a length below 0 or above what the parent holds, or more pages than table_width), a row that is not served holds nothing;  d_src,
  * d_dst [n_new] pages to copy from and to, -1: none;  d_new_ref [n_pages];  d_new_free [n_pages], *d_new_n_free: the pages
  * whose new count is 0 or less, ascending, -1 behind them.

@@ -11,6 +11,7 @@
 // and the free list, in phases with its barrier between them; the others write the rows, a warp some hundred entries.
 // An old row and the child that counts for it cancel: only the entries that a row gains or loses touch a count.
 #include <algorithm>
+#include <iterator>
 
 #include "common.cuh"
 #include "step_ops.cuh"
@@ -276,6 +277,31 @@ __global__ void __launch_bounds__(kThreads, 1) fork_pages_kernel(const __grid_co
   if constexpr (kCluster > 1) cluster_sync();   // (no CTA leaves while others may write to its counts)
 }
 
+// Whether an output shares memory with an input or with another output (CTAs read inputs while others write).
+bool overlapping(const atspeed_page_fork& f) {
+  struct Range {
+    const int* at;
+    long long n;   // entries; of a free list of unknown length the first
+  };
+  const long long o = f.n_old, m = f.n_new, w = f.table_width;
+  const Range in[] = {{f.d_table, o * w}, {f.d_kv_len, o}, {f.d_q_len, o},       {f.d_old_state, o},
+                      {f.d_parent, m},    {f.d_length, m}, {f.d_ref, f.n_pages}, {f.d_free, f.free_size < 0 ? 0 : std::max(1, f.free_size)},
+                      {f.d_n_free, 1},    {f.d_used, 1}};
+  const Range out[] = {{f.d_new_table, m * w}, {f.d_new_len, m},         {f.d_new_state, m},          {f.d_src, m},
+                       {f.d_dst, m},           {f.d_new_ref, f.n_pages}, {f.d_new_free, f.n_pages}, {f.d_new_n_free, 1}};
+  const auto meet = [](const Range& a, const Range& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return x && y && x < y + 4 * b.n && y < x + 4 * a.n;
+  };
+  for (const Range& a : out) {
+    for (const Range& b : in)
+      if (meet(a, b)) return true;
+    for (const Range* b = &a + 1; b != std::end(out); ++b)
+      if (meet(a, *b)) return true;
+  }
+  return false;
+}
+
 }  // namespace
 }  // namespace atspeed
 
@@ -289,10 +315,9 @@ extern "C" atspeed_status atspeed_op_fork_pages(atspeed_stream stream, const ats
       !f.d_dst || !f.d_new_ref || !f.d_new_free || !f.d_new_n_free || n_old <= 0 || n_new <= 0 || table_width <= 0 || f.page_size <= 0 ||
       n_pages <= 0)
     return ATSPEED_E_ARG;
-  if ((!f.d_parent && n_old != n_new) || f.d_new_table == f.d_table || f.d_new_ref == f.d_ref || f.d_new_free == f.d_free ||
-      f.d_new_len == f.d_kv_len || f.d_new_len == f.d_length || f.d_new_state == f.d_old_state || f.d_new_n_free == f.d_n_free)
-    return ATSPEED_E_ARG;
+  if (!f.d_parent && n_old != n_new) return ATSPEED_E_ARG;
   if (n_old > kMaxRequests || n_new > kMaxRequests || n_pages > kMaxPages) return ATSPEED_E_SHAPE;
+  if (overlapping(f)) return ATSPEED_E_ARG;
   const int most_free = f.free_size ? std::max(0, f.free_size) : 0x7fffffff;
   const ForkArgs a = {n_old,     n_new,        table_width, f.page_size,   n_pages,       most_free,  aligned16(f.d_ref) && aligned16(f.d_new_ref),
                       f.d_table, f.d_kv_len,   f.d_q_len,   f.d_old_state, f.d_parent,    f.d_length, f.d_ref,

@@ -92,3 +92,34 @@ def test_fork_with_a_count_past_the_free_lists_end(ats, n_pages, entries, used):
         held[e] = 1
     free = [e for e, h in enumerate(held) if h == 0]
     assert f.ref.tolist() == held and int(f.n_free) == len(free) and f.free.tolist() == free + [-1] * (n_pages - len(free))
+
+
+def test_fork_writes_side_by_side_but_not_over(ats):  # noqa: F811
+    """Inputs and outputs in one buffer, each next to the other: right.  With an output one entry into its neighbour: refused."""
+    n, m, width, pages = 2, 3, 3, 8
+    given = dict(table=[0, 1, -1, 2, -1, -1], kv_len=[20, 3], ref=[1, 1, 1, 0, 0, 0, 0, 0], free=[3, 4, 5, 6, 7], n_free=[5], parent=[0, 0, 1])
+    sizes = dict(table=m * width, kv_len=m, state=m, src=m, dst=m, ref=pages, free=pages, n_free=1)
+    for shifted in (None, *sizes):
+        buffer = torch.full((200,), -7, dtype=torch.int32, device="cuda")
+        at, ins, outs = 50, {}, {}
+        for k, v in given.items():
+            ins[k] = buffer[at:at + len(v)]
+            ins[k].copy_(_dev(v))
+            at += len(v)
+        for k, size in sizes.items():
+            outs[k] = buffer[at - (k == shifted):at - (k == shifted) + size]
+            at += size
+        outs["table"] = outs["table"].view(m, width)
+        ins["table"] = ins["table"].view(n, width)
+        before = buffer.clone()
+        call = lambda: ats.op_fork_pages(**ins, page_size=16, out=ats.PageFork(**outs))  # noqa: E731
+        if shifted:
+            with pytest.raises(ats.AtSpeedError):
+                call()
+            assert torch.equal(buffer, before)
+            continue
+        f, want = call(), ats.op_fork_pages(**ins, page_size=16)
+        for k in sizes:
+            assert torch.equal(getattr(f, k), getattr(want, k)), k
+        assert f.table.tolist() == [[0, 1, -1], [0, 3, -1], [2, -1, -1]] and f.free.tolist() == [4, 5, 6, 7, -1, -1, -1, -1]
+        assert (buffer[:50] == -7).all() and (buffer[at:] == -7).all() and torch.equal(buffer[50:50 + 25], before[50:50 + 25])
