@@ -47,14 +47,25 @@ class Beams:
         self.kv_len, self.ref = _i32([0] * n), _i32([0] * pages)
         self.free, self.n_free = _i32(range(pages)), _i32([pages])
         self.token, self.final = _i32([-1] * td.MAX_TOKENS), _i32([-1] * n)
-        self.score = torch.zeros(n, device="cuda")
+        self.score, self.lost = torch.zeros(n, device="cuda"), torch.zeros((), dtype=torch.bool, device="cuda")
         self.said, self.steps = _i32([[-1] * say] * n), torch.zeros((), dtype=torch.int64, device="cuda")
         self.one, self.every, self.graph = _i32([1] * n), _i32(range(0, n + 1, width)), None
         self._prefill()
 
     def _forward(self, q_len: torch.Tensor):
         plan = ats.op_batch_plan(q_len, self.kv_len, self.table, self.free, self.n_free, td.PAGE, td.MAX_TOKENS)
+        self._drop(plan.state)
         return plan, self.model.logits(self.token, plan, self.table, self.caches)
+
+    def _drop(self, state: torch.Tensor) -> None:
+        """A row for which there were no pages has no history: it is not chosen again, and run() says so."""
+        out = state != ats.PLAN_OK
+        self.lost.logical_or_((out & (self.score > -torch.inf)).any())
+        self.score.masked_fill_(out, -torch.inf)
+
+    def _check(self) -> None:
+        if bool(self.lost):
+            raise RuntimeError("not all beams could go on: too few pages, or rows of the table that are too short")
 
     def _fork(self, plan, q_len, parent=None) -> None:
         """The rows' pages after a step, and from their parents."""
@@ -63,6 +74,7 @@ class Beams:
         ats.op_copy_pages(self.layers, f.src, f.dst, length=f.kv_len)
         for name in ("table", "kv_len", "ref", "free", "n_free"):
             getattr(self, name).copy_(getattr(f, name))
+        self._drop(f.state)
 
     def _prefill(self) -> None:
         """The prompts, but for their last tokens, in each user's first row; then all of its rows share their pages."""
@@ -86,6 +98,7 @@ class Beams:
         # (a row of the logits is a user here, a beam's parent the user's first row)
         self._choose(best, (best.parent * self.width).view(-1))
         self._fork(plan, q_len, best.parent.view(-1) * self.width)
+        self._check()
 
     def _choose(self, best, parent: torch.Tensor) -> None:
         token, rows = best.token.view(-1), parent.long()
@@ -105,7 +118,8 @@ class Beams:
         self._fork(plan, self.one, parent)
 
     def run(self) -> None:
-        """Until `say` tokens are said: one step as it is, the others as replays of a graph of one."""
+        """Until `say` tokens are said: one step as it is, the others as replays of a graph of one.  An error if pages ran out; the
+        beams that are left (those with a score) are right all the same."""
         left = self.say - int(self.steps)
         if left > 0:
             self.step()
@@ -116,6 +130,7 @@ class Beams:
                 self.step()
         for _ in range(left - 1):
             self.graph.replay()
+        self._check()
 
     def lists(self) -> List[List[List[int]]]:
         """Every user's sequences, best first."""

@@ -178,3 +178,40 @@ def test_accepted_paths_are_kept(ex, prompts):
     held = sorted(e for row, k in zip(d.table.tolist(), d.kv_len) for e in row[:-(-k // td.PAGE)])
     assert held == [i for i, r in enumerate(d.ref.tolist()) if r] and max(d.ref.tolist()) == 1
     assert d.pages.tolist()[:int(d.n_free)] == [i for i, r in enumerate(d.ref.tolist()) if r == 0]
+
+
+def _small_pool(ex, pages):
+    """One user's 17 prompt tokens, five beams: one full page that all share, a second one of each, and up to four copies a step."""
+    g = torch.Generator().manual_seed(7)
+    prompt = torch.randint(0, ex.td.VOCAB, (ex.td.PAGE + 1,), generator=g).tolist()
+    return prompt, ex.Beams(ex.td.Model(3), [prompt], width=5, say=SAY, pages=pages)
+
+
+def test_a_pool_that_is_just_large_enough(ex):
+    (_, a), (_, b) = _small_pool(ex, 10), _small_pool(ex, 256)
+    a.run()
+    b.run()
+    assert torch.equal(a.said, b.said) and torch.equal(a.score, b.score)
+
+
+def test_beams_that_get_no_page_are_dropped(ex):
+    """With six pages nothing is left for a beam that goes on twice: an error at the end, and what has a score then is the model's."""
+    prompt, b = _small_pool(ex, 6)
+    with pytest.raises(RuntimeError, match="not all beams"):
+        b.run()
+    assert int(b.steps) == SAY
+    left = [r for r, s in enumerate(b.score.tolist()) if s > float("-inf")]
+    assert 0 < len(left) < 5
+    for r in left:
+        said = b.said[r].tolist()
+        tokens = prompt + said[:-1]
+        assert int(b.kv_len[r]) == len(tokens)
+        _check_keys(ex, b.model, b.caches[0][0], b.table[r, :-(-len(tokens) // ex.td.PAGE)].tolist(), tokens)
+        lp = _log_probs(ex, b.model, tokens)[len(prompt) - 1:]
+        want = float(lp.gather(1, torch.tensor(said, device="cuda")[:, None]).sum())
+        assert abs(float(b.score[r]) - want) <= 2 * LOGIT * SAY
+
+
+def test_a_prompt_that_gets_no_page(ex):
+    with pytest.raises(RuntimeError, match="not all beams"):
+        _small_pool(ex, 1)
