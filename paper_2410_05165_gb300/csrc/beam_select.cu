@@ -746,7 +746,10 @@ __global__ void __launch_bounds__(T, 1) beam_rank_kernel(const __grid_constant__
       else w.off = {M, 0.f}, w.more = l;
     }
     row_at(r) = w;
-    quick_at(r) = w.final >= 0 ? Quick{w.cum, -1.f} : Quick{w.cum - w.off.hi - w.more.hi, fabsf(w.cum) + fabsf(w.off.hi) + fabsf(w.more.hi)};
+    Quick q = {w.cum - w.off.hi - w.more.hi, fabsf(w.cum) + fabsf(w.off.hi) + fabsf(w.more.hi)};
+    // (score and maximum near the largest number: their difference may pass it, a candidate's score need not)
+    if (fabsf(w.cum) < INFINITY && !(fabsf(q.bias) < INFINITY)) q = {0.f, INFINITY};
+    quick_at(r) = w.final >= 0 ? Quick{w.cum, -1.f} : q;
   };
   if (a.pieces <= 2) {
     for (int r = r0 + tid; r < r1; r += T) {

@@ -68,6 +68,25 @@ def test_select_rows_that_end_early_in_a_tile(ats, dtype, V):  # noqa: F811
     _check_select(ats, _logits(V, 1, V, dtype, lead=1), [1], 12)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("down", [float(np.finfo(np.float32).min), -1e38])
+@pytest.mark.parametrize("V", [3, 5000])
+def test_select_scores_and_logits_near_the_largest_number(ats, dtype, down, V):  # noqa: F811
+    """Beams marked as empty by a score far down, whose logits have an infinity or a number near the largest: the one continuation whose
+    score is finite fills a place that nothing better takes."""
+    logits = torch.full((4, V), -1e6, device="cuda")
+    logits[0, :2] = torch.tensor([0.5, -3.0])
+    logits[1, 1] = float("inf")
+    logits[2, 2] = 3e38
+    logits[3, 0] = -2.0
+    logits = logits.to(dtype)
+    got = _check_select(ats, logits, [4], 9, score=[0.0, down, down, NEG])
+    pairs = list(zip(got.parent[0].tolist(), got.token[0].tolist()))
+    assert pairs[:2] == [(0, 0), (0, 1)] and (V > 3 or pairs[3:] == [(1, 1), (2, 2)] + [(-1, -1)] * 4)
+    got = _check_select(ats, logits, [1, 2, 1], 3, score=[0.0, down, down, NEG])
+    assert list(zip(got.parent[1].tolist(), got.token[1].tolist())) == [(1, 1), (2, 2), (-1, -1)]
+
+
 # ---------------------------------------------------------------------------------------------------
 # fork
 # ---------------------------------------------------------------------------------------------------
