@@ -497,7 +497,8 @@ atspeed_status atspeed_op_beam_select(atspeed_stream stream, const atspeed_beams
  * a length below 0 or above what the parent holds, or more pages than table_width), a row that is not served holds nothing;  d_src,
  * d_dst [n_new] pages to copy from and to, -1: none;  d_new_ref [n_pages];  d_new_free [n_pages], *d_new_n_free: the pages
  * whose new count is 0 or less, ascending, -1 behind them.
- * Entries outside [0, n_pages) are handed on, not counted, not copied.  n_old, n_new <= 16384, n_pages <= 2^26 (ATSPEED_E_SHAPE). */
+ * Entries outside [0, n_pages) are handed on, not counted, not copied.  n_old, n_new <= 16384, n_pages <= 2^26, table_width < 2^31 - 512
+ * (ATSPEED_E_SHAPE). */
 typedef struct {
   int n_old, n_new, table_width, page_size, n_pages, free_size;
   const int32_t *d_table, *d_kv_len, *d_q_len, *d_old_state, *d_parent, *d_length, *d_ref, *d_free, *d_n_free, *d_used;
@@ -509,7 +510,7 @@ atspeed_status atspeed_op_fork_pages(atspeed_stream stream, const atspeed_page_f
  * j < n with d_src[j], d_dst[j] both pages of the cache, the first ((d_length[j] - 1) mod page_size) + 1 tokens (d_length NULL:
  * the whole page; a length below 1: none) of page d_src[j] to page d_dst[j], keys and values of all heads.  A page is written by one
  * copy at most and read by none that is written in the same call (fork_pages' pairs are such; others leave either content).
- * head_dim a multiple of 8 (ATSPEED_E_SHAPE). */
+ * head_dim a multiple of 8, n < 2^31 - 1024 (ATSPEED_E_SHAPE). */
 atspeed_status atspeed_op_copy_pages(atspeed_stream stream, const atspeed_kv_pages *layers, int n_layers, int n, const int32_t *d_src,
                                      const int32_t *d_dst, const int32_t *d_length);
 
@@ -519,7 +520,8 @@ atspeed_status atspeed_op_copy_pages(atspeed_stream stream, const atspeed_kv_pag
  * Keys and values of token d_keep[b][i] go from cache row d_slot[d_cu_q[b] + d_keep[b][i]] to d_slot[d_cu_q[b] + i] (the plan's; moves
  * from or to a row outside the cache are left out).  d_new_len [n_req] = d_kv_len[b] + the tokens kept; requests
  * with d_state[b] other than ATSPEED_PLAN_OK (d_state NULL: none) keep nothing, d_kv_len [n_req] are the plan's.
- * T: rows of d_slot (entries of d_cu_q are taken within 0 .. T).  head_dim a multiple of 8 (ATSPEED_E_SHAPE). */
+ * T: rows of d_slot (entries of d_cu_q are taken within 0 .. T).  head_dim a multiple of 8, n_req <= 16384, keep_width < 2^31 - 256
+ * (ATSPEED_E_SHAPE). */
 atspeed_status atspeed_op_compact_tokens(atspeed_stream stream, const atspeed_kv_pages *layers, int n_layers, int n_req, int T,
                                          const int64_t *d_slot, const int32_t *d_cu_q, const int32_t *d_kv_len,
                                          const int32_t *d_state, const int32_t *d_keep, int keep_width, const int32_t *d_n_keep,

@@ -837,8 +837,8 @@ def op_copy_pages(layers: CacheLayers, src: torch.Tensor, dst: torch.Tensor, len
                   stream=None) -> None:
     """The first ((length - 1) mod page size) + 1 tokens (None: all) of pages src to pages dst, K and V of all layers; -1: none."""
     gpu, n, i32 = layers._on(stream), src.numel(), torch.int32
-    if n < 1:
-        _refuse("no pages")
+    if not 0 < n < 1 << 31:
+        _refuse(f"{n} pages")
     _check(load().atspeed_op_copy_pages(_raw_stream(stream, layers.device), layers.desc, layers.n, n, _given(src, i32, n, "src", gpu),
                                         _given(dst, i32, n, "dst", gpu), _tensor(length, i32, n, "length", gpu)))
 
@@ -848,9 +848,9 @@ def op_compact_tokens(layers: CacheLayers, slot: torch.Tensor, cu_q: torch.Tenso
     """Moves the kept ones keep [n][..] (n_keep [n] of them, ascending) of each request's new tokens behind the cached ones, K and V of
     all layers; slot, cu_q, state: the plan's.  Returns the cached tokens of each request [n]."""
     gpu, n, i32 = layers._on(stream), kv_len.numel(), torch.int32
-    if n < 1 or keep.dim() != 2 or keep.shape[0] != n or keep.shape[1] < 1 or slot.numel() < 1:
+    if not 0 < n < 1 << 31 or keep.dim() != 2 or keep.shape[0] != n or not 0 < keep.shape[1] < 1 << 31 or slot.numel() < 1:
         _refuse(f"{n} requests, {slot.numel()} slots, keep {tuple(keep.shape)}")
-    ins = (slot.numel(), _given(slot, torch.int64, 1, "slot", gpu), _given(cu_q, i32, n + 1, "cu_q", gpu), _given(kv_len, i32, n, "kv_len", gpu),
+    ins = (min(slot.numel(), (1 << 31) - 1), _given(slot, torch.int64, 1, "slot", gpu), _given(cu_q, i32, n + 1, "cu_q", gpu), _given(kv_len, i32, n, "kv_len", gpu),
            _tensor(state, i32, n, "state", gpu), _given(keep, i32, n, "keep", gpu), keep.shape[1], _given(n_keep, i32, n, "n_keep", gpu))
     new_len, = _outputs(layers.device, stream, ((n,), i32))
     _check(load().atspeed_op_compact_tokens(_raw_stream(stream, layers.device), layers.desc, layers.n, n, *ins, new_len.data_ptr()))

@@ -316,7 +316,7 @@ extern "C" atspeed_status atspeed_op_fork_pages(atspeed_stream stream, const ats
       n_pages <= 0)
     return ATSPEED_E_ARG;
   if (!f.d_parent && n_old != n_new) return ATSPEED_E_ARG;
-  if (n_old > kMaxRequests || n_new > kMaxRequests || n_pages > kMaxPages) return ATSPEED_E_SHAPE;
+  if (n_old > kMaxRequests || n_new > kMaxRequests || n_pages > kMaxPages || table_width > 0x7fffffff - kPiece) return ATSPEED_E_SHAPE;
   if (overlapping(f)) return ATSPEED_E_ARG;
   const int most_free = f.free_size ? std::max(0, f.free_size) : 0x7fffffff;
   const ForkArgs a = {n_old,     n_new,        table_width, f.page_size,   n_pages,       most_free,  aligned16(f.d_ref) && aligned16(f.d_new_ref),

@@ -218,6 +218,7 @@ extern "C" atspeed_status atspeed_op_copy_pages(atspeed_stream stream, const ats
   if (!d_src || !d_dst || n <= 0) return ATSPEED_E_ARG;
   CopyArgs a = {};
   if (const atspeed_status s = geometry_of(layers, n_layers, a.g)) return s;
+  if (n > 0x7fffffff - kPairs) return ATSPEED_E_SHAPE;   // (a list past the last pair begins below 2^31)
   a.n = n, a.src = d_src, a.dst = d_dst, a.length = d_length;
   for (int first = 0; first < n_layers; first += kLayers) {
     a.layers = set_layers(a.l, layers, first, n_layers);
@@ -236,7 +237,7 @@ extern "C" atspeed_status atspeed_op_compact_tokens(atspeed_stream stream, const
     return ATSPEED_E_ARG;
   CompactArgs a = {};
   if (const atspeed_status s = geometry_of(layers, n_layers, a.g)) return s;
-  if (n_req > kMaxRequests) return ATSPEED_E_SHAPE;
+  if (n_req > kMaxRequests || keep_width > 0x7fffffff - kThreads) return ATSPEED_E_SHAPE;   // (indices past the last entry stay below 2^31)
   a.n = n_req, a.T = T, a.keep_width = keep_width, a.slot = reinterpret_cast<const long long*>(d_slot), a.cu_q = d_cu_q;
   a.kv_len = d_kv_len, a.state = d_state, a.keep = d_keep, a.n_keep = d_n_keep;
   for (int first = 0; first < n_layers; first += kLayers) {

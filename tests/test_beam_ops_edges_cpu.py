@@ -2,7 +2,8 @@
 import pytest
 import torch
 
-from test_beam_ops_cpu import E_ARG, P, _b_fork, binding, lib, stand_library  # noqa: F401
+from test_beam_ops_cpu import (E_ARG, E_SHAPE, P, _array, _b_compact, _b_copy, _b_fork, _compact, _copy, _fork, _pages, binding, lib,  # noqa: F401
+                               stand_library)
 from test_step_ops_devices_cpu import I32, Launched, Stand
 
 
@@ -37,3 +38,33 @@ def test_fork_refuses_outputs_that_overlap(lib, out):  # noqa: F811
                 fork = PageForkDesc(n_old=4, n_new=5, table_width=3, page_size=16, n_pages=9, free_size=6,
                                     **{"d_" + k: p for k, p in {**at, out: place}.items()})
                 assert lib.atspeed_op_fork_pages(None, bytes(fork)) == E_ARG, (other, place)
+
+
+def test_lists_that_end_near_2_31(lib):  # noqa: F811
+    """A kernel's indices go on behind a list's end by less than a CTA's step."""
+    assert _copy(lib, _array(_pages()), n=2 ** 31 - 1) == E_SHAPE and _copy(lib, _array(_pages()), n=2 ** 31 - 1024) == E_SHAPE
+    assert _compact(lib, _array(_pages()), width=2 ** 31 - 256) == E_SHAPE
+    assert _fork(lib, width=2 ** 31 - 512) == E_SHAPE
+
+
+def test_counts_past_2_31_are_not_cut(binding, monkeypatch):  # noqa: F811
+    """2^32 + 3 of anything are not 3."""
+    many = 2 ** 32 + 3
+    for src in (many, 2 ** 31):
+        with pytest.raises(binding.AtSpeedError):
+            _b_copy(binding, src=Stand((src,), I32), dst=Stand((src,), I32), length=Stand((src,), I32))
+    with pytest.raises(binding.AtSpeedError):
+        _b_compact(binding, keep=Stand((2, many), I32))
+    with pytest.raises(binding.AtSpeedError):
+        _b_compact(binding, cu_q=Stand((many + 1,), I32), kv_len=Stand((many,), I32), keep=Stand((many, 3), I32), n_keep=Stand((many,), I32), state=None)
+    seen = []
+
+    class Lib:
+        def atspeed_op_compact_tokens(self, *args):
+            seen.append(args)
+            raise Launched
+
+    monkeypatch.setattr(binding, "load", Lib)
+    with pytest.raises(Launched):   # (offsets among them have 32 bits)
+        _b_compact(binding, slot=Stand((many,), torch.int64))
+    assert seen[0][4] == 2 ** 31 - 1
