@@ -719,7 +719,7 @@ def op_adjust_logits(logits: torch.Tensor, req: torch.Tensor, rules: LogitRules,
 # what follows a step's logits: beam selection, fork of block tables, copies of pages, compaction of an accepted path
 # ---------------------------------------------------------------------------------------------------
 # Memory of the stream that a call is on (or of the graph that captures it), given back after the call: what comes there next comes
-# after it.  (As a tensor it takes 1.4 us more.)
+# after it.  (As a tensor, as a torch without these two has it, it takes 1.4 us more.)
 _raw_alloc = getattr(torch._C, "_cuda_cudaCachingAllocator_raw_alloc", None)
 _raw_delete = getattr(torch._C, "_cuda_cudaCachingAllocator_raw_delete", None)
 
@@ -755,8 +755,12 @@ def op_beam_select(logits: torch.Tensor, cu_beam: torch.Tensor, width: int, scor
     token, parent, out = _outputs(dev, stream, ((n, width), i32), ((n, width), i32), ((n, width), f32))
     beams = _BEAMS_PACK(logits.data_ptr(), _pitch(logits, V), it, R, V, n, width, norm, cu_ptr, score_ptr, final_ptr, state_ptr, grammar_ptr,
                         words, states, token.data_ptr(), parent.data_ptr(), out.data_ptr())
-    st = _raw_stream(stream, dev)
-    ws = _raw_alloc(lib.atspeed_op_beam_select_workspace(R, V, width), st)
+    st, size = _raw_stream(stream, dev), lib.atspeed_op_beam_select_workspace(R, V, width)
+    if _raw_alloc is None or _raw_delete is None:
+        whole, = _outputs(dev, stream, ((size,), torch.uint8))
+        _check(lib.atspeed_op_beam_select(st, beams, whole.data_ptr()))
+        return BeamChoice(token, parent, out)
+    ws = _raw_alloc(size, st)
     try:
         _check(lib.atspeed_op_beam_select(st, beams, ws))
     finally:

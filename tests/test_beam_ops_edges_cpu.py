@@ -2,8 +2,8 @@
 import pytest
 import torch
 
-from test_beam_ops_cpu import (E_ARG, E_SHAPE, P, _array, _b_compact, _b_copy, _b_fork, _compact, _copy, _fork, _pages, binding, lib,  # noqa: F401
-                               stand_library)
+from test_beam_ops_cpu import (E_ARG, E_SHAPE, P, _array, _b_compact, _b_copy, _b_fork, _b_select, _compact, _copy, _fork, _pages,  # noqa: F401
+                               binding, lib, stand_library)
 from test_step_ops_devices_cpu import I32, Launched, Stand
 
 
@@ -68,3 +68,11 @@ def test_counts_past_2_31_are_not_cut(binding, monkeypatch):  # noqa: F811
     with pytest.raises(Launched):   # (offsets among them have 32 bits)
         _b_compact(binding, slot=Stand((many,), torch.int64))
     assert seen[0][4] == 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("missing", ["_raw_alloc", "_raw_delete"])
+def test_select_without_raw_allocations(binding, monkeypatch, missing):  # noqa: F811
+    """A torch that lacks them: the workspace is a tensor."""
+    monkeypatch.setattr(binding, missing, None)
+    with pytest.raises(Launched):
+        _b_select(binding)

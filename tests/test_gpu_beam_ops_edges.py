@@ -87,6 +87,24 @@ def test_select_scores_and_logits_near_the_largest_number(ats, dtype, down, V): 
     assert list(zip(got.parent[1].tolist(), got.token[1].tolist())) == [(1, 1), (2, 2), (-1, -1)]
 
 
+def test_select_with_a_tensor_as_workspace(ats, monkeypatch):  # noqa: F811
+    """As in a torch without raw allocations: the same results, on another stream and in a graph too."""
+    from paper_2410_05165_gb300 import binding
+    logits, cu = _logits(1, 20, 33024, torch.float32), _dev([0, 10, 20])
+    want = ats.op_beam_select(logits, cu, 10)
+    monkeypatch.setattr(binding, "_raw_alloc", None)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        captured = ats.op_beam_select(logits, cu, 10)
+    for _ in range(20):
+        graph.replay()
+        calls = [captured, ats.op_beam_select(logits, cu, 10), ats.op_beam_select(logits, cu, 10, stream=side)]
+        torch.cuda.synchronize()
+        for got in calls:
+            assert torch.equal(got.token, want.token) and torch.equal(got.parent, want.parent) and torch.equal(got.score, want.score)
+
+
 # ---------------------------------------------------------------------------------------------------
 # fork
 # ---------------------------------------------------------------------------------------------------
