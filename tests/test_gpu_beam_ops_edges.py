@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_beam_ops import NEG, TYPES, _check_select, _dev, _logits, ats  # noqa: F401
+from test_gpu_beam_ops import NEG, TYPES, _bits, _check_select, _dev, _logits, ats  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -103,6 +103,70 @@ def test_select_with_a_tensor_as_workspace(ats, monkeypatch):  # noqa: F811
         torch.cuda.synchronize()
         for got in calls:
             assert torch.equal(got.token, want.token) and torch.equal(got.parent, want.parent) and torch.equal(got.score, want.score)
+
+
+# ---------------------------------------------------------------------------------------------------
+# selection: what scores are worth
+# ---------------------------------------------------------------------------------------------------
+# Of a logarithm in two 32-bit parts: 2^-29 (the rest of its series is below 2^-7 and rounded in 32 bits, some operations of 2^-31 each).
+# Twice that for the sums with it, which are exact but for their lower parts' roundings.
+LOG = 2.0 ** -28
+
+
+def _counted(V, counts):
+    """Rows of n zeros among -infinities: their sums are n, without a rounding."""
+    logits = torch.full((len(counts), V), NEG, device="cuda")
+    for r, n in enumerate(counts):
+        logits[r, torch.randperm(V, generator=torch.Generator().manual_seed(r))[:n].cuda()] = 0.0
+    return logits
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [1, 100, 33024, 100003])   # one piece a row, many
+@pytest.mark.parametrize("cum", [0.0, -3.7, 11.0, -1e4])
+def test_select_scores_of_sums_without_a_rounding(ats, dtype, V, cum):  # noqa: F811
+    """cum - log n, off by its own rounding and what the logarithm is off."""
+    counts = [n for n in (1, 2, 3, 5, 7, 100, 1023, 4097, 16384, 33023, 65521, 99991) if n <= V]
+    cum = float(np.float32(cum))
+    got = ats.op_beam_select(_counted(V, counts).to(dtype), _dev(range(len(counts) + 1)), 1, score=_dev(np.full(len(counts), cum), torch.float32))
+    want = cum - np.log(np.array(counts, np.float64))
+    assert (np.abs(got.score[:, 0].double().cpu().numpy() - want) <= np.abs(want) * 2.0 ** -24 + LOG).all()
+
+
+@pytest.mark.parametrize("beams", [17, 64])   # as many in a request
+def test_select_tells_scores_apart_that_32_bits_do_not(ats, beams):  # noqa: F811
+    """Beams whose scores take back all of their sums' logarithms but what 32 bits leave of those, some 2^-22: the order and what is left."""
+    V, R = 20011, 3 * beams
+    rng = np.random.default_rng(beams)
+    counts = rng.choice(np.arange(2000, V), size=R, replace=False)
+    logits, table = _counted(V, counts), np.zeros((R, V), bool)
+    table[np.arange(R), torch.argmax(logits, dim=1).cpu().numpy()] = True   # (one of its tokens may follow a beam)
+    score = np.log(counts.astype(np.float64)).astype(np.float32)
+    exact = score.astype(np.float64) - np.log(counts.astype(np.float64))
+    assert np.abs(exact).max() > 2.0 ** -24
+    got = ats.op_beam_select(logits, _dev([0, beams, 2 * beams, R]), beams, score=_dev(score, torch.float32), grammar=_bits(table),
+                             state=_dev(np.arange(R)), norm=ats.NORM_FULL)
+    for b in range(3):
+        rows = got.parent[b].cpu().numpy()
+        assert sorted(rows) == list(range(b * beams, (b + 1) * beams))
+        assert (np.abs(got.score[b].double().cpu().numpy() - exact[rows]) <= np.abs(exact[rows]) * 2.0 ** -24 + LOG).all()
+        assert (np.diff(exact[rows]) <= 2 * LOG).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("R,V,std", [(10, 33024, 3.0), (320, 33024, 0.5), (200, 100003, 3.0), (300, 33024, 1.5)])
+def test_select_scores_of_random_rows(ats, dtype, R, V, std):  # noqa: F811
+    """In steps of 2^-24 a sum is off by 4 for the exponential (2^-22 at most, of one sign at the worst) and by what roundings of either sign leave:
+    2.3 |d| for a term e^d, |d| 9 on average of a sum that a few terms make (9 / sqrt 3 / 2: 2.7), some 50 additions of a thread's (sqrt 50 / sqrt 3
+    / 2: 2) and ten of the threads' sums (1.8): 3.8 in the mean square, seven times that for the worst row.  32 together."""
+    logits = _logits(R, R, V, dtype, std=std)
+    score = (-np.random.default_rng(V).exponential(2.0, R)).astype(np.float32)
+    got = ats.op_beam_select(logits, _dev(range(R + 1)), 8, score=_dev(score, torch.float32))
+    lp = torch.log_softmax(logits.double(), dim=1) + _dev(score, torch.float64)[:, None]
+    want, token = torch.sort(lp, dim=1, descending=True, stable=True)
+    assert torch.equal(got.token, token[:, :8].int())   # (within a row the order is the logits')
+    off = (got.score.double() - want[:, :8]).abs()
+    assert bool((off <= want[:, :8].abs() * 2.0 ** -24 + 32 * 2.0 ** -24).all()), float(off.max())
 
 
 # ---------------------------------------------------------------------------------------------------
