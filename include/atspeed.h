@@ -454,8 +454,8 @@ atspeed_status atspeed_op_adjust_logits(atspeed_stream stream, const void *d_log
  *   d_final[r] >= 0 (d_final NULL: none): the beam has ended, its one continuation is that token with the score d_score[r].
  * Higher scores come first, compared in two 32-bit parts (48 bits; the terms of a row's sum have 22); of equal ones the lower row, then
  * the larger logit, then the lower token.  A score of -infinity (in 32 bits) or NaN is never chosen.
- * Outputs [n_req][width], best first: d_token, d_parent (the row), d_out_score (rounded to 32 bits); places without a
- * continuation hold -1, -1, -infinity.  Rows of no request do not count.
+ * Outputs [n_req][width] (overlapping no input and no other output; ATSPEED_E_ARG), best first: d_token, d_parent (the row), d_out_score
+ * (rounded to 32 bits); places without a continuation hold -1, -1, -infinity.  Rows of no request do not count.
  * width 1 .. 256, vocab up to 2^30 (ATSPEED_E_SHAPE). */
 typedef struct {
   const void *d_logits;
@@ -493,10 +493,10 @@ atspeed_status atspeed_op_beam_select(atspeed_stream stream, const atspeed_beams
  * (d_ref at most 1); any other child gets the next page of d_free, from the used ones on, in the order of the rows, and has to
  * be given a copy of it.
  * Outputs (overlapping no input and no other output; ATSPEED_E_ARG): d_new_table [n_new][table_width], -1 behind the kept pages;
- * d_new_len [n_new] tokens kept, -1 if not served;  d_new_state [n_new] an atspeed_plan_state (NO_PAGES: no page was left for its copy; LIMIT: a parent of n_old or above,
- * a length below 0 or above what the parent holds, or more pages than table_width), a row that is not served holds nothing;  d_src,
- * d_dst [n_new] pages to copy from and to, -1: none;  d_new_ref [n_pages];  d_new_free [n_pages], *d_new_n_free: the pages
- * whose new count is 0 or less, ascending, -1 behind them.
+ * d_new_len [n_new] tokens kept, -1 if not served;  d_new_state [n_new] an atspeed_plan_state (NO_PAGES: no page was left for its
+ * copy; LIMIT: a parent of n_old or above, a length below 0 or above what the parent holds, or more pages than table_width), a row
+ * that is not served holds nothing;  d_src, d_dst [n_new] pages to copy from and to, -1: none;  d_new_ref [n_pages];
+ * d_new_free [n_pages], *d_new_n_free: the pages whose new count is 0 or less, ascending, -1 behind them.
  * Entries outside [0, n_pages) are handed on, not counted, not copied.  n_old, n_new <= 16384, n_pages <= 2^26, table_width < 2^31 - 512
  * (ATSPEED_E_SHAPE). */
 typedef struct {
@@ -519,7 +519,8 @@ atspeed_status atspeed_op_copy_pages(atspeed_stream stream, const atspeed_kv_pag
  * before their children); the list ends at the first entry that is not below the request's tokens or not above the one before it.
  * Keys and values of token d_keep[b][i] go from cache row d_slot[d_cu_q[b] + d_keep[b][i]] to d_slot[d_cu_q[b] + i] (the plan's; moves
  * from or to a row outside the cache are left out).  d_new_len [n_req] = d_kv_len[b] + the tokens kept; requests
- * with d_state[b] other than ATSPEED_PLAN_OK (d_state NULL: none) keep nothing, d_kv_len [n_req] are the plan's.
+ * with d_state[b] other than ATSPEED_PLAN_OK (d_state NULL: none) keep nothing, d_kv_len [n_req] are the plan's.  d_new_len may be
+ * d_kv_len; it overlaps no other input (ATSPEED_E_ARG).
  * T: rows of d_slot (entries of d_cu_q are taken within 0 .. T).  head_dim a multiple of 8, n_req <= 16384, keep_width < 2^31 - 256
  * (ATSPEED_E_SHAPE). */
 atspeed_status atspeed_op_compact_tokens(atspeed_stream stream, const atspeed_kv_pages *layers, int n_layers, int n_req, int T,

@@ -932,6 +932,12 @@ extern "C" atspeed_status atspeed_op_beam_select(atspeed_stream stream, const at
     return ATSPEED_E_ARG;
   const Layout l = layout_of(R, vocab, std::min(width, kMaxWidth));
   if (width > kMaxWidth || vocab > 1 << 30 || (long long)R * l.pieces > 0x7fffffffLL) return ATSPEED_E_SHAPE;
+  const long long rows = 4ll * R, places = 4ll * s.n_req * width;   // bytes
+  const Span in[] = {{s.d_logits, ((R - 1) * s.ld + vocab) * dtype_size(s.type)}, {s.d_cu_beam, 4ll * s.n_req + 4}, {s.d_score, rows},
+                     {s.d_final, rows}, {s.d_state, rows},
+                     {s.d_state ? s.d_grammar : nullptr, 4 * ((s.n_states - 1ll) * s.grammar_stride + (vocab + 31ll) / 32)}};
+  const Span out[] = {{s.d_token, places}, {s.d_parent, places}, {s.d_out_score, places}};
+  if (outputs_overlap(out, in)) return ATSPEED_E_ARG;   // (a request's places are written while another's rows are read)
   SelectArgs a = {};
   a.logits = s.d_logits, a.ld = s.ld, a.R = R, a.V = vocab, a.n_req = s.n_req, a.W = width, a.pieces = l.pieces, a.cap = cap_of(width);
   a.span = (int)(((vocab + (long long)l.pieces - 1) / l.pieces + kTile - 1) / kTile * kTile);
@@ -968,7 +974,7 @@ extern "C" atspeed_status atspeed_op_beam_select(atspeed_stream stream, const at
     return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess ? ATSPEED_OK : ATSPEED_E_CUDA;
   };
   static std::atomic<unsigned long long> done[2];
-  const long long places = (long long)grid * a.cap / s.n_req;   // of candidates, a request's on average
-  return width <= 64 && places <= kFewPlaces ? rank(beam_rank_kernel<256>, 256, sizeof(RankShared<256>), done[0])
+  const long long looked_at = (long long)grid * a.cap / s.n_req;   // candidates' places, a request's on average
+  return width <= 64 && looked_at <= kFewPlaces ? rank(beam_rank_kernel<256>, 256, sizeof(RankShared<256>), done[0])
                                              : rank(beam_rank_kernel<1024>, 1024, sizeof(RankShared<1024>), done[1]);
 }

@@ -11,7 +11,6 @@
 // and the free list, in phases with its barrier between them; the others write the rows, a warp some hundred entries.
 // An old row and the child that counts for it cancel: only the entries that a row gains or loses touch a count.
 #include <algorithm>
-#include <iterator>
 
 #include "common.cuh"
 #include "step_ops.cuh"
@@ -279,27 +278,12 @@ __global__ void __launch_bounds__(kThreads, 1) fork_pages_kernel(const __grid_co
 
 // Whether an output shares memory with an input or with another output (CTAs read inputs while others write).
 bool overlapping(const atspeed_page_fork& f) {
-  struct Range {
-    const int* at;
-    long long n;   // entries; of a free list of unknown length the first
-  };
-  const long long o = f.n_old, m = f.n_new, w = f.table_width;
-  const Range in[] = {{f.d_table, o * w}, {f.d_kv_len, o}, {f.d_q_len, o},       {f.d_old_state, o},
-                      {f.d_parent, m},    {f.d_length, m}, {f.d_ref, f.n_pages}, {f.d_free, f.free_size < 0 ? 0 : std::max(1, f.free_size)},
-                      {f.d_n_free, 1},    {f.d_used, 1}};
-  const Range out[] = {{f.d_new_table, m * w}, {f.d_new_len, m},         {f.d_new_state, m},          {f.d_src, m},
-                       {f.d_dst, m},           {f.d_new_ref, f.n_pages}, {f.d_new_free, f.n_pages}, {f.d_new_n_free, 1}};
-  const auto meet = [](const Range& a, const Range& b) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
-    return x && y && x < y + 4 * b.n && y < x + 4 * a.n;
-  };
-  for (const Range& a : out) {
-    for (const Range& b : in)
-      if (meet(a, b)) return true;
-    for (const Range* b = &a + 1; b != std::end(out); ++b)
-      if (meet(a, *b)) return true;
-  }
-  return false;
+  const long long o = 4ll * f.n_old, m = 4ll * f.n_new, pages = 4ll * f.n_pages;   // bytes; of a free list of unknown length its first entry's
+  const Span in[] = {{f.d_table, o * f.table_width}, {f.d_kv_len, o}, {f.d_q_len, o}, {f.d_old_state, o}, {f.d_parent, m}, {f.d_length, m},
+                     {f.d_ref, pages}, {f.d_free, f.free_size < 0 ? 0 : 4ll * std::max(1, f.free_size)}, {f.d_n_free, 4}, {f.d_used, 4}};
+  const Span out[] = {{f.d_new_table, m * f.table_width}, {f.d_new_len, m}, {f.d_new_state, m}, {f.d_src, m}, {f.d_dst, m}, {f.d_new_ref, pages},
+                      {f.d_new_free, pages}, {f.d_new_n_free, 4}};
+  return outputs_overlap(out, in);
 }
 
 }  // namespace

@@ -238,6 +238,11 @@ extern "C" atspeed_status atspeed_op_compact_tokens(atspeed_stream stream, const
   CompactArgs a = {};
   if (const atspeed_status s = geometry_of(layers, n_layers, a.g)) return s;
   if (n_req > kMaxRequests || keep_width > 0x7fffffff - kThreads) return ATSPEED_E_SHAPE;   // (indices past the last entry stay below 2^31)
+  // (a request's kept tokens are read by other CTAs than the one that writes its new length)
+  const Span in[] = {{d_slot, 8ll * T}, {d_cu_q, 4ll * n_req + 4}, {d_kv_len == d_new_len ? nullptr : d_kv_len, 4ll * n_req}, {d_state, 4ll * n_req},
+                     {d_keep, 4ll * n_req * keep_width}, {d_n_keep, 4ll * n_req}};
+  const Span out[] = {{d_new_len, 4ll * n_req}};
+  if (outputs_overlap(out, in)) return ATSPEED_E_ARG;
   a.n = n_req, a.T = T, a.keep_width = keep_width, a.slot = reinterpret_cast<const long long*>(d_slot), a.cu_q = d_cu_q;
   a.kv_len = d_kv_len, a.state = d_state, a.keep = d_keep, a.n_keep = d_n_keep;
   for (int first = 0; first < n_layers; first += kLayers) {

@@ -14,6 +14,27 @@ constexpr int kMaxRequests = 16384;   // two 32-bit words of shared memory a req
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 inline int dtype_size(int t) { return t == ATSPEED_F32 ? 4 : t == ATSPEED_BF16 || t == ATSPEED_F16 ? 2 : 0; }
 
+// Memory that a call reads or writes (null: none).
+struct Span {
+  const void* at;
+  long long bytes;
+  bool meets(const Span& b) const {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(at), y = reinterpret_cast<uintptr_t>(b.at);
+    return x && y && x < y + b.bytes && y < x + bytes;
+  }
+};
+// Whether an output shares memory with an input or with another output.
+template <size_t OUT, size_t IN>
+inline bool outputs_overlap(const Span (&out)[OUT], const Span (&in)[IN]) {
+  for (size_t i = 0; i < OUT; ++i) {
+    for (const Span& s : in)
+      if (out[i].meets(s)) return true;
+    for (size_t j = 0; j < i; ++j)
+      if (out[i].meets(out[j])) return true;
+  }
+  return false;
+}
+
 // Pointers, types and strides of a paged cache (what the operators that read or write it need of it alike).
 inline atspeed_status check_pages(const atspeed_kv_pages* c) {
   if (!c || !c->d_k || !c->d_v || c->n_pages <= 0 || c->page_size <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0)

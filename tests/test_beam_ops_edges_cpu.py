@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_beam_ops_cpu import (E_ARG, E_SHAPE, P, _array, _b_compact, _b_copy, _b_fork, _b_select, _compact, _copy, _fork, _pages,  # noqa: F401
+from test_beam_ops_cpu import (E_ARG, E_SHAPE, P, _array, _b_compact, _b_copy, _b_fork, _b_select, _compact, _copy, _fork, _pages, _select,  # noqa: F401
                                binding, lib, stand_library)
 from test_step_ops_devices_cpu import I32, Launched, Stand
 
@@ -76,3 +76,24 @@ def test_select_without_raw_allocations(binding, monkeypatch, missing):  # noqa:
     monkeypatch.setattr(binding, missing, None)
     with pytest.raises(Launched):
         _b_select(binding)
+
+
+def test_select_refuses_outputs_that_overlap(lib):  # noqa: F811
+    """Places [2][10] of a request are written while another's rows are read."""
+    ins = dict(logits=1200, cu=12, d_score=12, d_final=12, state=12, grammar=32)   # bytes: 3 rows of 100, two states
+    outs = dict(token=80, parent=80, out=80)
+    at = {k: P + 4096 * i for i, k in enumerate((*ins, *outs))}
+    for out in outs:
+        for other, size in (*ins.items(), *outs.items()):
+            for place in (at[other], at[other] + size - 4, at[other] - 76):
+                if other != out:
+                    assert _select(lib, n_states=2, stride=4, ws=2 * P, **{**at, out: place}) == E_ARG, (out, other, place)
+
+
+def test_compact_refuses_a_new_length_over_an_input(lib):  # noqa: F811
+    ins = dict(slot=64, cu_q=12, kv=8, state=8, keep=24, n_keep=8)   # bytes: 2 requests, 8 tokens, 3 kept at most
+    at = {k: P + 4096 * i for i, k in enumerate(ins)}
+    for other, size in ins.items():
+        for place in (at[other], at[other] + size - 4, at[other] - 4):
+            if (other, place) != ("kv", at["kv"]):   # (that one is right)
+                assert _compact(lib, _array(_pages(d_k=2 * P, d_v=3 * P)), **at, new_len=place) == E_ARG, (other, place)
