@@ -208,9 +208,9 @@ __device__ __forceinline__ uint32_t key_at(const char* in, const uint32_t* allow
 
 // The W best of the tokens [begin, end), of which more than W are at or above `from`, exactly (equal ones in the tokens' order), into the
 // list.  Every thread of the CTA; a warp has a share of the tokens, in order.  A pass over them halves the keys that the W-th best may have
-// and goes on to the next one that there is, so that few different logits need few passes: 3840 rows of 33024 take 888 us where they are
-// whole numbers (6015 with the halving alone), 1124 where all are equal (3083 with barriers for every 128 tokens and the ranking by
-// a thousand threads at a time); 109 where no row needs this.  `most`: no key is above it.
+// and goes on to the next one that there is, so that few different logits need few passes: 3840 rows of 33024 take 867 us where they are
+// whole numbers in bf16 (6015 with the halving alone; 75 where no row needs this), 1121 where all are equal in 32 bits (3083 with barriers
+// for every 128 tokens and the ranking by a thousand threads at a time; 100 where no row needs this).  `most`: no key is above it.
 template <int TYPE>
 __device__ __noinline__ void put_exactly(const char* in, const uint32_t* allowed, int begin, int end, uint32_t from, uint32_t most, int W, Shared& sh) {
   constexpr int kAtOnce = 8;
@@ -670,7 +670,8 @@ struct Quick {
 
 constexpr int kMostCtas = 304, kManyPieces = kMostCtas / 3 + 1;   // of the first launch where rows are in pieces; rows of three pieces or more
 // Few candidates (places of a request's lists) are ranked by a CTA of 256, whose barriers and instructions are fewer: ten rows of 33024, W = 10,
-// 11.3 -> 10.8 us, 320 rows 16.5 -> 15.5; 10240 places of 80 beams need the 1024 threads.
+// 11.3 -> 10.8 us, 320 rows 16.5 -> 15.5; 10240 places of 80 beams need the 1024 threads.  The requests' average decides: one of 3001 beams
+// among 99 of one takes twice as long as alone (V = 300, W = 10: 224 and 93 us).
 constexpr int kFewPlaces = 4096;
 constexpr int kRows = 256;   // that shared memory holds (of more: device memory)
 template <int T>

@@ -1,4 +1,5 @@
-// Shared by the operators of a batched serving step (plan, cache append, tree attention, logit rules).
+// Shared by the operators of a batched serving step (plan, cache append, tree attention, logit rules) and those after its logits
+// (beam selection, page fork, page copies, token compaction).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
